@@ -451,6 +451,72 @@ int resnet_eval(rn50_plan* plan, const void* state, const void* images, const in
                 const float* master, const void* model, float* logits_out, int32_t* pred_out,
                 int32_t* correct_out, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------- products in 8-bit integers
+ * For models that only answer: rows of activations (tokens, pixels, images) and rows of weights
+ * (output channels) are held as 8-bit integers with one float scale each.  Here and in the distillation
+ * functions below only 8-bit matrices and workspaces have to be 16-byte aligned: rows of x, y, logits and
+ * gradients may start at any element, vectors as well.
+ *
+ * An 8-bit matrix of rows of K numbers has rows of quant_i8_row_bytes(K) bytes, K rounded up to a
+ * multiple of 64; the bytes past K are zero (a product reads them).  0 for K < 1 or K > 131071, the
+ * longest sum of 8-bit products that a 32-bit integer holds. */
+size_t quant_i8_row_bytes(int K);
+/* Per row m of x:  a = max(max_k |x[m,k]|, 2^-100), scale[m] = a / 127,
+ * q[m,k] = rint(x[m,k] * (127 / a)), each operation rounded to float, so |q| <= 127.
+ * A row that holds an infinity or a NaN gets scale NaN and q 0: what is computed from it is NaN.
+ * x: device dtype, rows of K elements ldx >= K elements apart; q: device [M, quant_i8_row_bytes(K)],
+ * written whole; scale: device float[M]. */
+int quant_rows_i8(int M, int K, int dtype, const void* x, int64_t ldx, int8_t* q, float* scale, void* stream);
+/* y[m,n] = float(sum_k q[m,k]*w[n,k]) * q_scale[m] * w_scale[n] + bias[n], the sum exact in 32-bit
+ * integers, the rest in float, rounded once more to y's type.  q [M,row bytes], w [N,row bytes]: device;
+ * q_scale float[M], w_scale float[N], bias float[N] or NULL; y: device y_dtype, rows of N elements
+ * ldy >= N elements apart. */
+int matmul_i8(int M, int N, int K, const int8_t* q, const float* q_scale, const int8_t* w, const float* w_scale,
+              const float* bias, int y_dtype, void* y, int64_t ldy, void* stream);
+/* Both of the above in one call: the rows of x are quantized (into the workspace), then multiplied. */
+size_t fc_i8_workspace_bytes(int M, int K);
+int fc_i8_fwd(int M, int N, int K, int x_dtype, const void* x, int64_t ldx, const int8_t* w, const float* w_scale,
+              const float* bias, int y_dtype, void* y, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------ distillation
+ * The k largest logits of every row, in descending order; equal ones in the order of their classes, a NaN
+ * above every number.  values: device float [N,k]; indices: device int32 [N,k]; where a row has fewer
+ * than k classes the rest is (-infinity, -1).  tail_lse (or NULL): device float[N], the logarithm of the
+ * sum of exp(logit / temperature) over the classes that are not among them (-infinity if there are none).
+ * logits: device dtype, rows of C elements ld >= C elements apart.  1 <= k <= 256. */
+size_t topk_rows_workspace_bytes(int N, int C, int k);
+int topk_rows(int N, int C, int k, int dtype, const void* logits, int64_t ld, float temperature, float* values,
+              int32_t* indices, float* tail_lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Loss of student logits z against a teacher's largest logits, mixed with the cross-entropy of labels, and its
+ * gradient.  Per row, with T = temperature, u = z / T:  the teacher's entries (class i_j, logit t_j) and its
+ * tail (the log-sum-exp of its other logits at T, as topk_rows leaves it; NULL: -infinity) are cells of
+ * probability p_j = exp(t_j / T) / S, p_r = exp(tail) / S, S their sum; the student's are q_j = softmax(u)[i_j]
+ * and q_r, what all other classes have together:
+ *   KL = sum_j p_j log(p_j / q_j) + p_r log(p_r / q_r)
+ *   CE = (1-ls) * -log softmax(z)[label] + ls * mean_i -log softmax(z)_i        (label smoothing ls)
+ *   row_loss = alpha T^2 KL + (1-alpha) CE,   loss = sum_n row_weight[n] row_loss[n]  (NULL: 1/N each)
+ *   dlogits = grad_scale row_weight[n] d row_loss / dz, at class i
+ *     alpha T (softmax(u)_i - p_j) for i = i_j,  alpha T softmax(u)_i (1 - p_r / q_r) for the others,
+ *     + (1-alpha) (softmax(z)_i - (1-ls) [i == label] - ls / C)
+ * An entry whose class is outside [0,C) is absent, and so is one whose class an entry in front of it has.  A row
+ * without entries and tail has KL = 0; a label outside [0,C) (or labels NULL) leaves CE out.  A row of weight 0 is
+ * not read, a row whose logits are all -infinity has no distribution: loss and gradient 0 for both.
+ * logits, dlogits: device dtype, rows of C elements ld >= C apart, grad_ld for the gradient; dlogits may be NULL (the
+ * loss alone) or the logits' own memory (with grad_ld == ld), and must not overlap them otherwise.  t_values float
+ * [N,k], t_indices int32 [N,k], t_tail float[N] or NULL; labels int32[N] or NULL; row_weight float[N] or NULL;
+ * loss_out float[1]; row_loss_out float[N].  0 <= k <= 256 (k = 0: no entries), 0 <= alpha, ls <= 1, T > 0. */
+typedef struct {
+  int N, C, k;
+  int dtype;
+  int64_t ld, grad_ld;
+  float temperature, alpha, label_smoothing, grad_scale;
+} rn50_distill_desc;
+size_t distill_workspace_bytes(const rn50_distill_desc* d);
+int distill_fwd_bwd(const rn50_distill_desc* d, const void* logits, const float* t_values, const int32_t* t_indices,
+                    const float* t_tail, const int32_t* labels, const float* row_weight, float* loss_out,
+                    float* row_loss_out, void* dlogits, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

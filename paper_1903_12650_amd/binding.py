@@ -18,7 +18,9 @@ __all__ = ["F32", "BF16", "Rn50Error", "lib_path", "conv_fwd", "conv_dgrad", "co
            "bn_relu_fwd_workspace_bytes", "bn_relu_bwd_workspace_bytes", "raw", "conv_bn_sums_bytes",
            "conv_fwd_bn_sums", "conv_fwd_bn_in", "conv_wgrad_bn_in", "bn_relu_fwd_from_sums", "relu_mask_like", "conv_dgrad_bn_sums", "bn_relu_bwd_from_sums",
            "LrSchedule", "TrainState", "resnet_train_step", "DECAY_NONE", "DECAY_STEP", "DECAY_POLY", "DECAY_LINEAR",
-           "DECAY_TABLE", "resnet_init_params", "bn_relu_infer", "top1_accuracy", "resnet_eval"]
+           "DECAY_TABLE", "resnet_init_params", "bn_relu_infer", "top1_accuracy", "resnet_eval",
+           "quant_i8_row_bytes", "quant_rows_i8", "matmul_i8", "fc_i8_workspace_bytes", "fc_i8_fwd", "DistillDesc",
+           "topk_rows_workspace_bytes", "topk_rows", "distill_workspace_bytes", "distill_fwd_bwd"]
 
 F32, BF16 = 0, 1
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -60,6 +62,11 @@ class LarsDesc(ctypes.Structure):
                 ("lr", ctypes.c_float), ("eps", ctypes.c_float), ("grad_dtype", ctypes.c_int)]
 
 
+class DistillDesc(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int) for n in ("N", "C", "k", "dtype")] + [(n, ctypes.c_int64) for n in ("ld", "grad_ld")] +
+                [(n, ctypes.c_float) for n in ("temperature", "alpha", "label_smoothing", "grad_scale")])
+
+
 class StepConfig(ctypes.Structure):
     _fields_ = [("N", ctypes.c_int), ("image_hw", ctypes.c_int), ("classes", ctypes.c_int), ("dtype", ctypes.c_int),
                 ("widths", ctypes.c_int * 4), ("blocks", ctypes.c_int * 4), ("stem", ctypes.c_int),
@@ -73,7 +80,8 @@ raw.rn50_profile_tag.restype = ctypes.c_char_p
 for _n in ("conv_fwd_workspace_bytes", "conv_dgrad_workspace_bytes", "conv_wgrad_workspace_bytes",
            "bn_relu_fwd_workspace_bytes", "bn_relu_bwd_workspace_bytes", "lars_update_workspace_bytes",
            "resnet_plan_workspace_bytes", "conv_bn_sums_bytes", "resnet_train_state_bytes",
-           "bn_relu_infer_workspace_bytes"):
+           "bn_relu_infer_workspace_bytes", "quant_i8_row_bytes", "fc_i8_workspace_bytes", "topk_rows_workspace_bytes",
+           "distill_workspace_bytes"):
     if hasattr(raw, _n):
         getattr(raw, _n).restype = ctypes.c_size_t
 for _n in ("resnet_plan_tensor_shape", "resnet_plan_tensor_offset", "resnet_plan_arena_elems", "resnet_plan_bn_channels",
@@ -349,6 +357,52 @@ def xent_fwd_bwd(logits, labels, label_smoothing=0.0, grad_scale=1.0):
     _check(raw.xent_fwd_bwd(N, K, _ptr(logits), _ptr(labels), ctypes.c_float(label_smoothing),
                             ctypes.c_float(grad_scale), _ptr(loss), _ptr(row), _ptr(dl), _stream()))
     return loss, row, dl
+
+
+# ----------------------------------------------------- products in 8-bit integers
+def quant_i8_row_bytes(K):
+    return raw.quant_i8_row_bytes(K)
+
+
+def quant_rows_i8(x):
+    """Returns q [M, quant_i8_row_bytes(K)] int8 and scale [M] of the rows of x [M, K] (float or bfloat16, rows contiguous)."""
+    return _ops.quant_rows_i8(x)
+
+
+def matmul_i8(K, q, q_scale, w, w_scale, bias=None, dtype=torch.float32, y=None):
+    """y [M, N] = (q w^T) * q_scale * w_scale + bias of rows of K numbers, as quant_rows_i8 leaves them."""
+    return _ops.matmul_i8(K, q, q_scale, w, w_scale, bias, dtype, y)
+
+
+def fc_i8_workspace_bytes(M, K):
+    return raw.fc_i8_workspace_bytes(M, K)
+
+
+def fc_i8_fwd(x, w, w_scale, bias=None, dtype=torch.float32, y=None, workspace=None):
+    """y [M, N] = x w^T + bias in 8-bit integers: x [M, K] is quantized by rows, w and w_scale are quant_rows_i8's of the weights."""
+    return _ops.fc_i8_fwd(x, w, w_scale, bias, dtype, y, workspace)
+
+
+# --------------------------------------------------------------- distillation
+def topk_rows_workspace_bytes(N, C, k):
+    return raw.topk_rows_workspace_bytes(N, C, k)
+
+
+def topk_rows(logits, k, temperature=1.0, tail=True, workspace=None):
+    """Returns values [N, k], indices [N, k] int32 and (tail) the log-sum-exp [N] of all other logits at the temperature, else None."""
+    return _ops.topk_rows(logits, k, temperature, tail, workspace)
+
+
+def distill_workspace_bytes(desc):
+    return raw.distill_workspace_bytes(ctypes.byref(desc))
+
+
+def distill_fwd_bwd(logits, t_values, t_indices, t_tail=None, labels=None, temperature=1.0, alpha=1.0, label_smoothing=0.0,
+                    row_weight=None, grad_scale=1.0, grad=True, dlogits=None, workspace=None):
+    """Returns loss (device float[1]), row_loss [N] and dlogits [N, C] (None without grad).  dlogits: optional tensor to fill, which
+    may be the logits themselves."""
+    return _ops.distill_fwd_bwd(logits, t_values, t_indices, t_tail, labels, temperature, alpha, label_smoothing, row_weight, grad_scale,
+                                grad, dlogits, workspace)
 
 
 # ----------------------------------------------------------------------- LARS

@@ -14,6 +14,7 @@ namespace rn50 {
 // ---------------------------------------------------------------- host: errors
 int fail(int code, const char* fmt, ...);
 void clear_error();
+inline bool aligned_to(const void* p, uintptr_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 #define RN50_REQUIRE(cond, code, ...) \

@@ -9,11 +9,13 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <algorithm>
 #include <exception>
 #include <string>
 #include <vector>
 
 #include <ATen/ATen.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -242,6 +244,180 @@ PyObject* bn_relu_bwd_py(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return Py_BuildValue("NNNN", wrap(dx), res, wrap(dgamma), wrap(dbeta));
   });
 }
+// ------------------------------------------- 8-bit products and distillation
+// A matrix whose rows are contiguous, on the current device; `ld`: elements from one row to the next.
+struct Rows {
+  void* p;
+  int64_t n, c, ld;
+};
+void on_current_device(const at::Tensor& t) {
+  PyObject* dev = PyObject_CallNoArgs(g_device);
+  if (!dev) throw PyError();
+  const long i = PyLong_AsLong(dev);
+  Py_DECREF(dev);
+  if (i == -1 && PyErr_Occurred()) throw PyError();
+  if (t.device().index() != i) raise(PyExc_ValueError, "tensors of the current device are expected");
+}
+Rows rows_of(const at::Tensor& t) {
+  if (t.dim() != 2) raise(PyExc_ValueError, "a matrix is expected");
+  const int64_t n = t.size(0), c = t.size(1);
+  if (n > INT32_MAX || c > INT32_MAX) raise(PyExc_ValueError, "a matrix of at most 2^31 - 1 rows and columns is expected");
+  if (!t.is_cuda() || (c > 1 && t.stride(1) != 1)) raise(PyExc_AssertionError, "device tensors with contiguous rows only");
+  return {t.data_ptr(), n, c, n > 1 ? t.stride(0) : std::max<int64_t>(t.stride(0), c)};
+}
+// A contiguous tensor of one type and size (None: null, where that is allowed).
+template <typename T>
+T* vec(PyObject* o, at::ScalarType type, at::IntArrayRef size, const char* what, const at::Tensor& like, bool optional = false) {
+  if (optional && o == Py_None) return nullptr;
+  const at::Tensor& t = required(o);
+  if (t.scalar_type() != type) raise(PyExc_TypeError, (std::string(what) + ": " + c10::toString(type) + " is expected, got " + c10::toString(t.scalar_type())).c_str());
+  if (t.sizes() != size) raise(PyExc_ValueError, (std::string(what) + ": the size does not fit").c_str());
+  T* p = addr<T>(t);
+  if (t.device() != like.device()) raise(PyExc_ValueError, (std::string(what) + ": on another device").c_str());
+  return p;
+}
+at::ScalarType float_type(PyObject* o) {
+  if (!THPDtype_Check(o)) raise(PyExc_TypeError, "a torch.dtype is expected");
+  const at::ScalarType t = reinterpret_cast<THPDtype*>(o)->scalar_type;
+  if (t != at::kFloat && t != at::kBFloat16) raise(PyExc_TypeError, (std::string("unsupported dtype ") + c10::toString(t)).c_str());
+  return t;
+}
+// quant_rows_i8(x)
+PyObject* quant_rows_i8_py(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 1, [&]() -> PyObject* {
+    const at::Tensor& x = required(a[0]);
+    const int dt = dtype_of(x);
+    const Rows r = rows_of(x);
+    on_current_device(x);
+    const at::Tensor q = empty({r.n, static_cast<int64_t>(quant_i8_row_bytes(static_cast<int>(r.c)))}, at::kChar, x), scale = empty({r.n}, at::kFloat, x);
+    int8_t* const pq = addr<int8_t>(q);
+    float* const ps = addr<float>(scale);
+    void* const s = current_stream();
+    call([&] { return quant_rows_i8(static_cast<int>(r.n), static_cast<int>(r.c), dt, r.p, r.ld, pq, ps, s); });
+    return Py_BuildValue("NN", wrap(q), wrap(scale));
+  });
+}
+// The output of a product: a matrix of `rows` x `cols`, given or made.
+at::Tensor product_out(PyObject* given, PyObject* dtype, int64_t rows, int64_t cols, const at::Tensor& like) {
+  const at::Tensor* t = tensor(given);
+  if (!t) return empty({rows, cols}, float_type(dtype), like);
+  if (t->dim() != 2 || t->size(0) != rows || t->size(1) != cols) raise(PyExc_ValueError, "y: the size does not fit");
+  if (t->device() != like.device()) raise(PyExc_ValueError, "y: on another device");
+  return *t;
+}
+// matmul_i8(K, q, q_scale, w, w_scale, bias, dtype, y)
+PyObject* matmul_i8_py(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 8, [&]() -> PyObject* {
+    const int K = to_int(a[0]);
+    const at::Tensor &q = required(a[1]), &w = required(a[3]);
+    if (q.dim() != 2 || w.dim() != 2) raise(PyExc_ValueError, "a matrix is expected");
+    const int64_t row = static_cast<int64_t>(quant_i8_row_bytes(K)), M = q.size(0), N = w.size(0);
+    if (M > INT32_MAX || N > INT32_MAX) raise(PyExc_ValueError, "a matrix of at most 2^31 - 1 rows is expected");
+    const int8_t *pq = vec<int8_t>(a[1], at::kChar, {M, row}, "q", q), *pw = vec<int8_t>(a[3], at::kChar, {N, row}, "w", q);
+    const float *qs = vec<float>(a[2], at::kFloat, {M}, "q_scale", q), *ws = vec<float>(a[4], at::kFloat, {N}, "w_scale", q);
+    const float* bias = vec<float>(a[5], at::kFloat, {N}, "bias", q, true);
+    on_current_device(q);
+    const at::Tensor y = product_out(a[7], a[6], M, N, q);
+    const Rows r = rows_of(y);
+    const int dt = dtype_of(y);
+    void* const s = current_stream();
+    call([&] { return matmul_i8(static_cast<int>(M), static_cast<int>(N), K, pq, qs, pw, ws, bias, dt, r.p, r.ld, s); });
+    return wrap(y);
+  });
+}
+// fc_i8_fwd(x, w, w_scale, bias, dtype, y, workspace)
+PyObject* fc_i8_fwd_py(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 7, [&]() -> PyObject* {
+    const at::Tensor &x = required(a[0]), &w = required(a[1]);
+    const int xt = dtype_of(x);
+    const Rows rx = rows_of(x);
+    if (w.dim() != 2) raise(PyExc_ValueError, "a matrix is expected");
+    const int M = static_cast<int>(rx.n), K = static_cast<int>(rx.c);
+    const int64_t N = w.size(0);
+    if (N > INT32_MAX) raise(PyExc_ValueError, "a matrix of at most 2^31 - 1 rows is expected");
+    const int8_t* pw = vec<int8_t>(a[1], at::kChar, {N, static_cast<int64_t>(quant_i8_row_bytes(K))}, "w", x);
+    const float *ws = vec<float>(a[2], at::kFloat, {N}, "w_scale", x), *bias = vec<float>(a[3], at::kFloat, {N}, "bias", x, true);
+    on_current_device(x);
+    const at::Tensor y = product_out(a[5], a[4], M, N, x);
+    const Rows ry = rows_of(y);
+    const int yt = dtype_of(y);
+    const Workspace work(a[6], a[6] == Py_None ? fc_i8_workspace_bytes(M, K) : 0, x);
+    void* const s = current_stream();
+    call([&] { return fc_i8_fwd(M, static_cast<int>(N), K, xt, rx.p, rx.ld, pw, ws, bias, yt, ry.p, ry.ld, work.p, work.bytes, s); });
+    return wrap(y);
+  });
+}
+// topk_rows(logits, k, temperature, tail, workspace)
+PyObject* topk_rows_py(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 5, [&]() -> PyObject* {
+    const at::Tensor& z = required(a[0]);
+    const int dt = dtype_of(z), k = to_int(a[1]);
+    const Rows r = rows_of(z);
+    const int N = static_cast<int>(r.n), C = static_cast<int>(r.c);
+    const float temperature = static_cast<float>(to_double(a[2]));
+    const int want = PyObject_IsTrue(a[3]);
+    if (want < 0) throw PyError();
+    if (k < 0) raise(PyExc_ValueError, "k is negative");
+    on_current_device(z);
+    const at::Tensor values = empty({r.n, k}, at::kFloat, z), indices = empty({r.n, k}, at::kInt, z);
+    at::Tensor tail;
+    if (want) tail = empty({r.n}, at::kFloat, z);
+    const Workspace ws(a[4], a[4] == Py_None ? topk_rows_workspace_bytes(N, C, k) : 0, z);
+    float *const pv = addr<float>(values), *const pt = want ? addr<float>(tail) : nullptr;
+    int32_t* const pi = addr<int32_t>(indices);
+    void* const s = current_stream();
+    call([&] { return topk_rows(N, C, k, dt, r.p, r.ld, temperature, pv, pi, pt, ws.p, ws.bytes, s); });
+    PyObject* t = Py_None;
+    if (want) t = wrap(tail); else Py_INCREF(Py_None);
+    return Py_BuildValue("NNN", wrap(values), wrap(indices), t);
+  });
+}
+// distill_fwd_bwd(logits, t_values, t_indices, t_tail, labels, temperature, alpha, label_smoothing, row_weight, grad_scale, grad, dlogits, workspace)
+PyObject* distill_fwd_bwd_py(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 13, [&]() -> PyObject* {
+    const at::Tensor& z = required(a[0]);
+    rn50_distill_desc d{};
+    d.dtype = dtype_of(z);
+    const Rows r = rows_of(z);
+    d.N = static_cast<int>(r.n);
+    d.C = static_cast<int>(r.c);
+    d.ld = r.ld;
+    const at::Tensor* entries = tensor(a[1]);
+    if (entries && (entries->dim() != 2 || entries->size(1) > INT32_MAX)) raise(PyExc_ValueError, "t_values: a matrix is expected");
+    d.k = entries ? static_cast<int>(entries->size(1)) : 0;
+    const float* tv = vec<float>(a[1], at::kFloat, {r.n, d.k}, "t_values", z, true);
+    const int32_t* ti = vec<int32_t>(a[2], at::kInt, {r.n, d.k}, "t_indices", z, entries == nullptr);
+    const float* tt = vec<float>(a[3], at::kFloat, {r.n}, "t_tail", z, true);
+    const int32_t* labels = vec<int32_t>(a[4], at::kInt, {r.n}, "labels", z, true);
+    d.temperature = static_cast<float>(to_double(a[5]));
+    d.alpha = static_cast<float>(to_double(a[6]));
+    d.label_smoothing = static_cast<float>(to_double(a[7]));
+    const float* weight = vec<float>(a[8], at::kFloat, {r.n}, "row_weight", z, true);
+    d.grad_scale = static_cast<float>(to_double(a[9]));
+    const int grad = PyObject_IsTrue(a[10]);
+    if (grad < 0) throw PyError();
+    on_current_device(z);
+    at::Tensor dz;
+    Rows g{nullptr, 0, 0, d.C};
+    if (grad) {
+      const at::Tensor* given = tensor(a[11]);
+      dz = given ? *given : empty({r.n, r.c}, z.scalar_type(), z);
+      if (dz.scalar_type() != z.scalar_type()) raise(PyExc_TypeError, "dlogits: the logits' type is expected");
+      if (dz.sizes() != z.sizes()) raise(PyExc_ValueError, "dlogits: the size does not fit");
+      if (dz.device() != z.device()) raise(PyExc_ValueError, "dlogits: on another device");
+      g = rows_of(dz);
+    }
+    d.grad_ld = g.ld;
+    const at::Tensor loss = empty({1}, at::kFloat, z), row = empty({r.n}, at::kFloat, z);
+    const Workspace ws(a[12], a[12] == Py_None ? distill_workspace_bytes(&d) : 0, z);
+    float *const pl = addr<float>(loss), *const pr = addr<float>(row);
+    void* const s = current_stream();
+    call([&] { return distill_fwd_bwd(&d, r.p, tv, ti, tt, labels, weight, pl, pr, g.p, ws.p, ws.bytes, s); });
+    PyObject* out = Py_None;
+    if (grad) out = wrap(dz); else Py_INCREF(Py_None);
+    return Py_BuildValue("NNN", wrap(loss), wrap(row), out);
+  });
+}
 // setup(Rn50Error, current raw stream of a device, current device)
 PyObject* setup_py(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 3, [&]() -> PyObject* {
@@ -257,6 +433,8 @@ PyObject* setup_py(PyObject*, PyObject* const* a, Py_ssize_t n) {
 #define FAST(name, f) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {FAST("conv_fwd", conv_fwd_py), FAST("conv_dgrad", conv_dgrad_py), FAST("conv_wgrad", conv_wgrad_py),
                           FAST("bn_relu_fwd", bn_relu_fwd_py), FAST("bn_relu_bwd", bn_relu_bwd_py),
+                          FAST("quant_rows_i8", quant_rows_i8_py), FAST("matmul_i8", matmul_i8_py), FAST("fc_i8_fwd", fc_i8_fwd_py),
+                          FAST("topk_rows", topk_rows_py), FAST("distill_fwd_bwd", distill_fwd_bwd_py),
                           FAST("setup", setup_py), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_ops", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,558 @@
+"""Quantized rows and products, largest logits, and the distillation loss with its gradient, against their 64-bit forms.
+
+Where the bounds come from (eps = 2^-24, half a unit in the last place of a float):
+ - quantized rows: the definition's roundings are part of it: bit for bit;
+ - products: the sum is exact, then one rounding of the sum to float, two products and an addition: 5 eps of the terms' size; one
+   more rounding (2^-8 of the result) in bfloat16;
+ - sums of exponentials: every term's argument has three roundings, each eps of the argument's own size, on average at most ln C of
+   it (the mean of max - u under the softmax is at most its entropy); the exponential itself 2 eps; an addition or a rescaling of
+   the running sum 4 eps, and no kernel adds more than C / 64 + 64 terms one after another: `sum_error`;
+ - log-sum-exp: that, and one rounding of the result;  losses: four log-probabilities, weighted by at most one each;
+ - gradients: sum_error, and the element's own exponentials, whose arguments have three roundings: of the size of its terms;
+   one more rounding in bfloat16."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import distill as od
+
+pytestmark = pytest.mark.gpu
+EPS = 2.0 ** -24
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module")
+def rn():
+    import paper_1903_12650_amd as rn
+    return rn
+
+
+def sum_error(C):
+    return EPS * (4 * (C / 64 + 64) + 5 * np.log(C + 1) + 16)
+
+
+def spread(t, extra):
+    """The same matrix with rows `extra` elements further apart."""
+    wide = torch.full((t.shape[0], t.shape[1] + extra), float("nan") if t.is_floating_point() else -7, dtype=t.dtype, device=t.device)
+    wide[:, :t.shape[1]] = t
+    return wide[:, :t.shape[1]]
+
+
+def f64(t):
+    return t.detach().double().cpu().numpy()
+
+
+# ----------------------------------------------------------- quantized rows
+QUANT = [(1, 1), (1, 2048), (3, 7), (5, 64), (40, 2048), (2, 65), (300, 255), (9, 1000), (7, 8192), (4, 8200), (2, 20011), (1, 131071), (2049, 130)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("M, K", QUANT)
+def test_quantized_rows(rn, M, K, dtype):
+    g = torch.Generator().manual_seed(M * 131 + K)
+    x = (torch.randn(M, K, generator=g) * torch.exp(2 * torch.randn(M, 1, generator=g))).to(dtype)
+    if M > 2:
+        x[1] = 0
+    for src in (x.cuda(), spread(x.cuda(), 1), spread(x.cuda(), 8)):
+        q, s = rn.quant_rows_i8(src)
+        want_q, want_s = od.quant_rows(x.float().numpy())
+        assert q.shape == (M, rn.quant_i8_row_bytes(K))
+        assert np.array_equal(s.cpu().numpy(), want_s) and np.array_equal(q.cpu().numpy(), want_q)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_quantized_rows_of_extreme_values(rn, dtype):
+    big = torch.finfo(dtype).max
+    tiny = 1e-40 if dtype == F32 else 2.0 ** -133
+    x = torch.randn(12, 517)
+    x[0, 516] = float("inf")
+    x[1, 0] = float("-inf")
+    x[2, 300] = float("nan")
+    x[3] = torch.sign(x[3]) * big
+    x[4] *= tiny
+    x[5] = 0
+    x[5, 100] = -big
+    x[6] = -0.0
+    x[7, 511] = 2.0 ** -101
+    x[7, :511] = 0
+    x[7, 512:] = 0
+    x = x.to(dtype)
+    q, s = rn.quant_rows_i8(x.cuda())
+    want_q, want_s = od.quant_rows(x.float().numpy())
+    np.testing.assert_array_equal(s.cpu().numpy(), want_s)
+    np.testing.assert_array_equal(q.cpu().numpy(), want_q)
+    assert np.isnan(want_s[:3]).all() and np.isfinite(want_s[3:]).all()
+    w = torch.randn(33, 517).cuda()
+    y = rn.fc_i8_fwd(x.cuda(), *rn.quant_rows_i8(w))  # the rows with such values are NaN, whole; no other is (3 and 5 may pass the largest float)
+    assert torch.isnan(y[:3]).all() and not torch.isnan(y[3:]).any() and torch.isfinite(y[4]).all() and torch.isfinite(y[6:]).all()
+
+
+# ----------------------------------------------------------------- products
+PRODUCTS = [(1, 1, 1), (1, 1000, 2048), (1, 17, 64), (2, 33, 100), (3, 5, 4099), (7, 256, 512), (16, 129, 1000), (17, 1000, 2048), (40, 1000, 2048),
+            (33, 96, 640), (64, 64, 64), (65, 130, 128), (127, 255, 192), (129, 257, 320), (256, 256, 256), (257, 300, 65), (300, 513, 1025),
+            (515, 258, 2047), (1001, 777, 448)]
+
+
+def product_bound(size, want, out):
+    return 5 * EPS * size + (2.0 ** -8 * 1.01 * np.abs(want) if out == BF16 else 0) + 1e-44
+
+
+@pytest.mark.parametrize("x_type, y_type, bias", [(BF16, F32, True), (F32, F32, False), (BF16, BF16, True), (F32, BF16, False)])
+@pytest.mark.parametrize("M, N, K", PRODUCTS)
+def test_products(rn, M, N, K, x_type, y_type, bias):
+    g = torch.Generator().manual_seed(M + 1000 * N + K)
+    x = (torch.randn(M, K, generator=g) * torch.exp(torch.randn(M, 1, generator=g))).to(x_type)
+    w = torch.randn(N, K, generator=g)
+    b = torch.randn(N, generator=g).cuda() if bias else None
+    wq, ws = rn.quant_rows_i8(w.cuda())
+    want, size = od.matmul_i8(*od.quant_rows(x.float().numpy()), wq.cpu().numpy(), ws.cpu().numpy(), None if b is None else f64(b))
+    bound = product_bound(size, want, y_type)
+    y = rn.fc_i8_fwd(x.cuda(), wq, ws, b, dtype=y_type)
+    assert y.dtype == y_type and y.shape == (M, N)
+    assert (np.abs(f64(y) - want) <= bound).all()
+    # in two calls, and into rows that lie further apart, whose gaps stay as they are: the same
+    q, s = rn.quant_rows_i8(spread(x.cuda(), 3))
+    assert torch.equal(rn.matmul_i8(K, q, s, wq, ws, b, y_type), y)
+    for extra in (1, 8):
+        wide = torch.full((M, N + extra), 5.0, dtype=y_type, device="cuda")
+        rn.fc_i8_fwd(spread(x.cuda(), extra), wq, ws, b, y=wide[:, :N])
+        assert torch.equal(wide[:, :N], y) and bool((wide[:, N:] == 5.0).all())
+
+
+@pytest.mark.parametrize("M, N", [(1, 3), (5, 70), (70, 5), (200, 130)])
+def test_longest_sums_do_not_overflow(rn, M, N):
+    K = 131071
+    q = torch.full((M, rn.quant_i8_row_bytes(K)), -128, dtype=torch.int8, device="cuda")
+    q[:, K:] = 0
+    w = torch.full((N, q.shape[1]), -128, dtype=torch.int8, device="cuda")
+    w[:, K:] = 0
+    w[N - 1] = 127
+    one = lambda n: torch.ones(n, device="cuda")
+    y = rn.matmul_i8(K, q, one(M), w, one(N))
+    want = np.full((M, N), np.float32(128 * 128 * K), np.float32)
+    want[:, N - 1] = np.float32(-128 * 127 * K)
+    assert np.array_equal(y.cpu().numpy(), want)
+    with pytest.raises(rn.Rn50Error) as e:
+        rn.quant_rows_i8(torch.zeros(1, K + 1, device="cuda"))
+    assert e.value.code == -2
+
+
+def test_nan_scales_stay_in_their_rows_and_columns(rn):
+    x, w = torch.randn(130, 200), torch.randn(140, 200)
+    x[77, 3] = float("nan")
+    w[101, 5] = float("inf")
+    y = rn.fc_i8_fwd(x.cuda(), *rn.quant_rows_i8(w.cuda()))
+    bad = torch.zeros(130, 140, dtype=torch.bool)
+    bad[77], bad[:, 101] = True, True
+    assert torch.equal(torch.isnan(y).cpu(), bad)
+
+
+# ----------------------------------------------------------- largest logits
+def check_topk(rn, x, k, temperature, tail=True):
+    values, indices, t = rn.topk_rows(x, k, temperature, tail)
+    wv, wi, wt = od.topk_rows(f64(x), k, temperature)
+    assert values.dtype == F32 and indices.dtype == torch.int32 and values.shape == indices.shape == (x.shape[0], k)
+    np.testing.assert_array_equal(indices.cpu().numpy(), wi)
+    np.testing.assert_array_equal(values.cpu().numpy(), wv.astype(np.float32))
+    if not tail:
+        assert t is None
+        return
+    t = f64(t)
+    same = np.isnan(wt) == np.isnan(t)
+    assert same.all() and (np.isinf(wt) == np.isinf(t)).all() and (t[np.isinf(wt)] == wt[np.isinf(wt)]).all()
+    fine = np.isfinite(wt)
+    assert (np.abs(t[fine] - wt[fine]) <= sum_error(x.shape[1]) + 2 * EPS * np.abs(wt[fine])).all()
+
+
+TOPK = [(1, 1, 1), (3, 5, 8), (40, 1000, 8), (2, 256, 256), (5, 257, 256), (9, 255, 1), (4, 1024, 100), (33, 4096, 32), (3, 8195, 64), (1, 50001, 100),
+        (2, 65537, 17), (6, 40000, 256), (1, 131072, 64), (3, 300001, 128), (200, 2500, 10), (130, 33000, 50)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("N, C, k", TOPK)
+def test_largest_logits(rn, N, C, k, dtype):
+    g = torch.Generator().manual_seed(N * 7 + C + k)
+    x = (torch.randn(N, C, generator=g) * 2).to(dtype).cuda()
+    check_topk(rn, x, k, 2.0)
+    check_topk(rn, spread(x, 1), k, 0.5)
+    check_topk(rn, spread(x, 8), k, 1.0, tail=False)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("C, k", [(1000, 7), (5000, 64), (70000, 100), (70000, 256)])
+def test_largest_logits_of_awkward_rows(rn, C, k, dtype):
+    g = torch.Generator().manual_seed(C + k)
+    low = torch.finfo(dtype).min
+    x = torch.randn(16, C, generator=g)
+    x[0] = float("-inf")                                   # nothing is left
+    x[1] = float("-inf")
+    x[1, C - 3] = 1.0                                      # one class is left
+    x[2] = low
+    x[2, ::C // 5] = 2.0
+    x[3] = 0.25                                            # all equal
+    x[4] = torch.round(x[4])                               # a handful of values
+    x[5] = torch.arange(C) / C                             # ascending
+    x[6] = -torch.arange(C) / C
+    x[7, 5] = float("nan")
+    x[7, C - 1] = float("nan")
+    x[8, 11] = float("inf")
+    x[9, C // 2:C // 2 + k] += 50                          # all in one place
+    x[10, ::2], x[10, 1::2] = 0.0, -0.0
+    x[11] = float("nan")
+    x[12, :k + 40] = 9.0                                   # more ties at the top than places
+    x[13, 64:] = float("-inf")
+    x[14] = x[14] * 1e-38
+    x[15] = x[15].sign() * torch.finfo(dtype).max
+    check_topk(rn, x.to(dtype).cuda(), k, 1.0)
+    one = x.to(dtype).cuda()
+    for n in (0, 3, 9, 12):
+        check_topk(rn, one[n:n + 1], k, 1.0)               # the forms for few rows
+
+
+# ------------------------------------------------------- distillation loss
+def teacher(rn, N, C, k, T, seed, tail=True, absent=False):
+    g = torch.Generator().manual_seed(seed)
+    t = torch.randn(N, C, generator=g) * 3
+    v, i, tl = od.topk_rows(t.numpy(), k, T)
+    if absent:
+        i = np.where(np.arange(k)[None] >= 1 + np.arange(N)[:, None] % k, -1, i)
+    z = 0.7 * t + torch.randn(N, C, generator=g)
+    labels = torch.randint(0, C, (N,), generator=g).to(torch.int32)
+    f = lambda a: torch.from_numpy(np.ascontiguousarray(a)).to(F32).cuda()
+    return z, f(v), torch.from_numpy(i).to(torch.int32).cuda(), f(tl) if tail else None, labels.cuda()
+
+
+def check_distill(rn, z, v, i, tl, labels, T=1.0, alpha=1.0, ls=0.0, w=None, scale=1.0, **more):
+    a = dict(temperature=T, alpha=alpha, label_smoothing=ls, row_weight=w, grad_scale=scale)
+    keep = z.clone()
+    loss, rows, grad = rn.distill_fwd_bwd(z, v, i, tl, labels, **a, **more)
+    n64 = lambda t: None if t is None else f64(t)
+    host = lambda t: None if t is None else t.cpu().numpy()
+    a["row_weight"] = n64(w)
+    want_loss, want_rows, want, size = od.distill(f64(keep), n64(v), host(i), n64(tl), host(labels), **a)
+    N, C = z.shape
+    e = sum_error(C)
+    zz = f64(keep)
+    finite = np.where(np.isfinite(zz), zz, 0)
+    reach = np.abs(finite).max(1) + (np.abs(f64(v)).max(1, initial=0, where=np.isfinite(f64(v))) if v is not None else 0)
+    row_bound = alpha * T * T * (4 * e + 8 * EPS * (reach / T + np.log(C + 1))) + (1 - alpha) * (4 * e + 8 * EPS * (reach + np.log(C + 1))) \
+        + 2 * EPS * np.abs(np.where(np.isfinite(want_rows), want_rows, 0))
+    got_rows = f64(rows)
+    assert (np.isfinite(got_rows) == np.isfinite(want_rows)).all(), (got_rows, want_rows)
+    ok = np.isfinite(want_rows)
+    assert (np.abs(got_rows[ok] - want_rows[ok]) <= row_bound[ok]).all()
+    ww = np.full(N, 1.0 / N) if w is None else f64(w)
+    if ok.all():
+        assert abs(float(loss) - want_loss) <= float((np.abs(ww) * row_bound).sum()) + 2 * EPS * abs(want_loss)
+    if grad is None:
+        return None
+    # an element's exponentials: three roundings of (z - m) / T, of z - m
+    away = np.abs(finite.max(1)[:, None] - finite) * max(1.0, 1.0 / T)
+    bound = size * (2 * e + EPS * (5 * np.minimum(away, 90) + 16)) + 1e-36
+    if z.dtype == BF16:
+        bound += 2.0 ** -8 * 1.01 * (np.abs(want) + bound) + 1e-38
+    got = f64(grad)
+    assert grad.dtype == z.dtype and np.isfinite(got).all()
+    off = np.abs(got - want) - bound
+    assert (off <= 0).all(), (np.unravel_index(off.argmax(), off.shape), off.max(), got.flat[off.argmax()], want.flat[off.argmax()])
+    return loss, rows, grad
+
+
+SHAPES = [(1, 1, 1), (2, 3, 2), (40, 1000, 8), (5, 257, 256), (3, 1023, 33), (6, 4100, 64), (1, 50001, 100), (2, 70000, 16), (7, 131072, 32), (64, 8192, 50),
+          (300, 515, 5), (3, 200003, 20)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("tail, alpha, ls, T, absent", [(True, 0.5, 0.1, 4.0, False), (False, 1.0, 0.0, 1.0, True), (True, 0.7, 0.0, 2.0, True),
+                                                       (True, 1.0, 0.0, 0.5, False), (True, 0.0, 0.1, 1.0, False)])
+@pytest.mark.parametrize("N, C, k", SHAPES)
+def test_distillation(rn, N, C, k, dtype, tail, alpha, ls, T, absent):
+    z, v, i, tl, labels = teacher(rn, N, C, k, T, N + C + k, tail, absent)
+    z = z.to(dtype).cuda()
+    w = torch.linspace(0.5, 1.5, N).cuda() / N
+    if N > 2:
+        w[1] = 0
+    loss, rows, grad = check_distill(rn, z, v, i, tl, labels, T, alpha, ls, w, 3.0)
+    # the loss alone; rows that lie apart; in place
+    only = rn.distill_fwd_bwd(z, v, i, tl, labels, T, alpha, ls, w, 3.0, grad=False)
+    assert only[2] is None and torch.equal(only[0], loss) and torch.equal(only[1], rows)
+    for extra in (1, 8):
+        zz = spread(z, extra)
+        out = torch.full((N, C + 2 * extra), 5.0, dtype=dtype, device="cuda")
+        l2, r2, _ = rn.distill_fwd_bwd(zz, v, i, tl, labels, T, alpha, ls, w, 3.0, dlogits=out[:, :C])
+        assert torch.equal(l2, loss) and torch.equal(r2, rows) and torch.equal(out[:, :C], grad) and bool((out[:, C:] == 5.0).all())
+        l2, r2, _ = rn.distill_fwd_bwd(zz, v, i, tl, labels, T, alpha, ls, w, 3.0, dlogits=zz)
+        assert torch.equal(l2, loss) and torch.equal(r2, rows) and torch.equal(zz, grad)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_without_a_teacher_it_is_the_cross_entropy(rn, dtype):
+    z = torch.randn(40, 1000).to(dtype).cuda()
+    labels = torch.randint(0, 1000, (40,), dtype=torch.int32).cuda()
+    loss, rows, grad = check_distill(rn, z, None, None, None, labels, alpha=0.0, ls=0.1, scale=2.0)
+    want = rn.xent_fwd_bwd(z.float(), labels, 0.1, 2.0)
+    assert torch.allclose(loss, want[0], rtol=1e-5) and torch.allclose(rows, want[1], rtol=1e-5)
+    assert float((grad.float() - want[2]).norm() / want[2].norm()) < (4e-3 if dtype == BF16 else 1e-5)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("C", [700, 60000])
+def test_rows_where_something_is_missing(rn, C, dtype):
+    N, k, T = 14, 6, 2.0
+    low = torch.finfo(dtype).min
+    z, v, i, tl, labels = teacher(rn, N, C, k, T, C)
+    w = torch.full((N,), 1.0 / N)
+    z[0] = float("-inf")                                  # no distribution
+    i[1], tl[1] = -1, float("-inf")                       # no teacher
+    i[2] = -1                                             # only the teacher's tail
+    z[3], w[3] = float("nan"), 0.0                        # padding
+    labels[4] = -100                                      # no label
+    i[5, 3] = i[5, 0]                                     # an entry twice
+    i[6, 2], i[6, 4] = C, 2 ** 31 - 1                     # classes that do not exist
+    keep = torch.zeros(C, dtype=torch.bool)
+    keep[i[7].cpu().long()] = True
+    keep[labels[7].item()] = True
+    keep[C // 2] = True
+    z[7, ~keep] = float("-inf")                           # the student's mask leaves the entries, the label and one more
+    z[8, ~keep] = low                                     # ... and the lowest value as a mask
+    z[8, i[8].cpu().long()] = 1.0
+    z[8, labels[8].item()] = 0.5
+    z[9] = low                                            # all masked alike: a uniform distribution
+    v[10] = float("-inf")                                 # entries of no mass: the tail alone
+    tl[11] = float("-inf")
+    z[12, C // 2:] = float("-inf")
+    z[12, i[12].cpu().long()] = 3.0
+    z[12, labels[12].item()] = 0.0
+    z[13] *= 20                                           # far apart
+    check_distill(rn, z.to(dtype).cuda(), v, i, tl, labels, T, 0.6, 0.0, w.cuda())
+    for n in (0, 2, 5, 7, 9, 13):                         # the forms for few rows
+        s = slice(n, n + 1)
+        check_distill(rn, z[s].to(dtype).cuda(), v[s].contiguous(), i[s].contiguous(), tl[s].contiguous(), labels[s].contiguous(), T, 1.0)
+
+
+@pytest.mark.parametrize("C", [700, 60000])
+def test_losses_that_have_no_end(rn, C):
+    """A class that the teacher holds possible and the student does not: infinite loss, a gradient without NaN; NaN and +infinity in a
+    row make its loss NaN and leave the other rows alone."""
+    z, v, i, tl, labels = teacher(rn, 4, C, 5, 1.0, 3)
+    z[0, i[0, 2].item()] = float("-inf")
+    z[1, C // 3] = float("nan")
+    z[2, C // 3] = float("inf")
+    loss, rows, grad = rn.distill_fwd_bwd(z.cuda(), v, i, tl)
+    rows = rows.cpu()
+    assert torch.isposinf(rows[0]) and torch.isnan(rows[1]) and torch.isnan(rows[2]) and torch.isfinite(rows[3])
+    assert torch.isfinite(grad[0]).all() and torch.isfinite(grad[3]).all() and torch.isnan(grad[1]).any() and torch.isnan(grad[2]).any()
+    _, _, want, _ = od.distill(f64(z), f64(v), i.cpu().numpy(), f64(tl))
+    assert np.abs(f64(grad[0]) - want[0]).max() < 1e-5
+    # every class of the student's tail is masked while the teacher's tail has mass
+    z, v, i, tl, labels = teacher(rn, 2, C, 5, 1.0, 4)
+    inside = torch.full((C,), float("-inf"))
+    inside[i[0].cpu().long()] = 1.0
+    z[0] = inside
+    _, rows, grad = rn.distill_fwd_bwd(z.cuda(), v, i, tl)
+    assert torch.isposinf(rows[0]) and torch.isfinite(rows[1]) and torch.isfinite(grad).all()
+
+
+def test_gradient_against_differences_of_the_loss(rn):
+    """In float, along directions: the loss of the row's own kernel, two-sided.  Bound: the third derivative's part (h^2) and the loss's
+    rounding over 2h."""
+    N, C, k, T = 4, 900, 12, 2.0
+    z, v, i, tl, labels = teacher(rn, N, C, k, T, 5)
+    z = z.cuda()
+    a = dict(temperature=T, alpha=0.6, label_smoothing=0.1)
+    _, rows, grad = rn.distill_fwd_bwd(z, v, i, tl, labels, **a)
+    g = torch.Generator().manual_seed(9)
+    h = 2.0 ** -6
+    for _ in range(4):
+        d = torch.randn(N, C, generator=g).cuda()
+        d /= d.abs().max()
+        up, down = (rn.distill_fwd_bwd(z + s * h * d, v, i, tl, labels, grad=False, **a)[1] for s in (1, -1))
+        want = f64((up.double() - down.double()) / (2 * h))
+        got = (f64(grad) * f64(d)).sum(1) * N
+        noise = 8 * EPS * np.abs(f64(rows)).max() / h + sum_error(C) / h
+        assert (np.abs(got - want) <= noise + h * h * 4).all()
+
+
+# -------------------------------------------------------- how they are called
+@pytest.mark.parametrize("N, ld, used", [(3, 2 ** 30, 5003), (40, 2 ** 26 + 8, 1000)])
+def test_rows_past_32_bits(rn, N, ld, used):
+    """The last rows start past 2^31 elements and 4 GB."""
+    base = torch.empty(N * ld, dtype=BF16, device="cuda")
+    x = base.view(N, ld)[:, :used]
+    z, v, i, tl, labels = teacher(rn, N, used, 9, 1.0, 1)
+    x.copy_(z.to(BF16))
+    z = x.contiguous()
+    for got, want in zip(rn.topk_rows(x, 9), rn.topk_rows(z, 9)):
+        assert torch.equal(got, want)
+    for got, want in zip(rn.quant_rows_i8(x), rn.quant_rows_i8(z)):
+        assert torch.equal(got, want)
+    want = rn.distill_fwd_bwd(z, v, i, tl, labels, alpha=0.5)
+    got = rn.distill_fwd_bwd(x, v, i, tl, labels, alpha=0.5, dlogits=x)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and torch.equal(x, want[2])
+    w = rn.quant_rows_i8(torch.randn(used, 64, device="cuda"))
+    a = torch.randn(N, 64, device="cuda")
+    rn.fc_i8_fwd(a, *w, y=x)
+    assert torch.equal(x, rn.fc_i8_fwd(a, *w, dtype=BF16))
+
+
+def test_one_long_row(rn):
+    """More classes than 2^25, one row: the forms that share a row among workgroups."""
+    C = 2 ** 25 + 37
+    x = torch.randn(1, C, device="cuda")
+    values, indices, tail = rn.topk_rows(x, 50, 1.0)
+    want, at = torch.sort(x[0], descending=True, stable=True)
+    assert torch.equal(values[0], want[:50]) and torch.equal(indices[0].long(), at[:50])
+    rest = torch.logsumexp(want[50:].double(), 0)
+    assert abs(float(tail) - float(rest)) < 1e-4
+    loss, row, grad = rn.distill_fwd_bwd(x, values, indices, tail)  # its own teacher
+    assert abs(float(loss)) < 1e-4 and float(grad.abs().max()) < 1e-5
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_rows_that_start_anywhere(rn, dtype):
+    z, v, i, tl, labels = teacher(rn, 9, 1001, 7, 2.0, 8)
+    z = z.to(dtype).cuda()
+    wide = spread(z, 5)
+    for r, c in ((1, 0), (2, 1), (3, 2), (0, 3), (5, 997)):
+        part = wide[r:, c:1001]
+        whole = part.contiguous()
+        for got, want in zip((*rn.topk_rows(part, 7), *rn.quant_rows_i8(part)), (*rn.topk_rows(whole, 7), *rn.quant_rows_i8(whole))):
+            assert torch.equal(got, want)
+        a = (v[r:], (i[r:] - c), tl[r:], labels[r:] - c, 2.0, 0.5, 0.1)  # (entries and labels in front of the part are absent)
+        for got, want in zip(rn.distill_fwd_bwd(part, *a), rn.distill_fwd_bwd(whole, *(t.clone() if torch.is_tensor(t) else t for t in a))):
+            assert torch.equal(got, want)
+        w = rn.quant_rows_i8(torch.randn(1001 - c, 70, device="cuda"))
+        x = torch.randn(9 - r, 70, device="cuda")
+        out = torch.full_like(wide, 5.0)
+        rn.fc_i8_fwd(x, *w, y=out[r:, c:1001])
+        assert torch.equal(out[r:, c:1001], rn.fc_i8_fwd(x, *w, dtype=dtype))
+        out[r:, c:1001] = 5.0
+        assert bool((out == 5.0).all())
+
+
+@pytest.mark.parametrize("N, C", [(3, 70000), (200, 3000)])
+def test_on_another_stream_and_twice(rn, N, C):
+    z, v, i, tl, labels = teacher(rn, N, C, 20, 2.0, 8)
+    z = z.to(BF16).cuda()
+    x, w = torch.randn(N, 520).cuda(), torch.randn(130, 520).cuda()
+
+    def everything():
+        wq, ws = rn.quant_rows_i8(w)
+        return [*rn.topk_rows(z, 20, 2.0), *rn.distill_fwd_bwd(z, v, i, tl, labels, 2.0, 0.5, 0.1), wq, ws, rn.fc_i8_fwd(x, wq, ws)]
+
+    want = everything()
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        got = everything()
+    stream.synchronize()
+    for a, b in zip(want, got):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("N, C", [(3, 70000), (40, 1000)])
+def test_captured_in_a_graph(rn, N, C):
+    z, v, i, tl, labels = teacher(rn, N, C, 20, 2.0, 8)
+    z, x, w = z.cuda(), torch.randn(N, 520).cuda(), torch.randn(130, 520).cuda()
+    wq, ws = rn.quant_rows_i8(w)
+
+    def everything():
+        return [*rn.topk_rows(z, 20, 2.0), *rn.distill_fwd_bwd(z, v, i, tl, labels, 2.0, 0.5, 0.1), rn.fc_i8_fwd(x, wq, ws)]
+
+    everything()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = everything()
+    for seed in range(4):
+        z.copy_(torch.randn(N, C, generator=torch.Generator().manual_seed(seed)))
+        x.copy_(torch.randn(N, 520, generator=torch.Generator().manual_seed(seed)))
+        want = everything()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(want, got):
+            assert torch.equal(a, b)
+
+
+def test_a_workspace_of_the_callers(rn):
+    z, v, i, tl, labels = teacher(rn, 3, 70000, 20, 2.0, 8)
+    z = z.cuda()
+    d = rn.DistillDesc(3, 70000, 20, rn.F32, 70000, 70000, 2.0, 1.0, 0.0, 1.0)
+    ws = torch.full((max(256, rn.distill_workspace_bytes(d), rn.topk_rows_workspace_bytes(3, 70000, 20)),), 255, dtype=torch.uint8, device="cuda")
+    for a, b in ((rn.topk_rows(z, 20, workspace=ws), rn.topk_rows(z, 20)),
+                 (rn.distill_fwd_bwd(z, v, i, tl, temperature=2.0, workspace=ws), rn.distill_fwd_bwd(z, v, i, tl, temperature=2.0))):
+        for s, t in zip(a, b):
+            assert torch.equal(s, t)
+    need = rn.fc_i8_workspace_bytes(3, 70000)
+    w = rn.quant_rows_i8(z)
+    with pytest.raises(rn.Rn50Error) as e:
+        rn.fc_i8_fwd(z, *w, workspace=torch.empty(need - 1, dtype=torch.uint8, device="cuda"))
+    assert e.value.code == -3
+
+
+@pytest.mark.parametrize("call, error", [
+    (lambda rn, z, i: rn.topk_rows(z, 0), "rn50"),
+    (lambda rn, z, i: rn.topk_rows(z, 257), "rn50"),
+    (lambda rn, z, i: rn.topk_rows(z, 3, 0.0), "rn50"),
+    (lambda rn, z, i: rn.topk_rows(z, 3, float("nan")), "rn50"),
+    (lambda rn, z, i: rn.topk_rows(z[:0], 3), "rn50"),
+    (lambda rn, z, i: rn.topk_rows(z.t(), 3), AssertionError),
+    (lambda rn, z, i: rn.topk_rows(z[:1].expand(5, 64), 3), "rn50"),         # rows on top of each other
+    (lambda rn, z, i: rn.topk_rows(z.half(), 3), TypeError),
+    (lambda rn, z, i: rn.topk_rows(z[0], 3), ValueError),
+    (lambda rn, z, i: rn.quant_rows_i8(i), TypeError),
+    (lambda rn, z, i: rn.quant_rows_i8(z[:, :0]), "rn50"),
+    (lambda rn, z, i: rn.distill_fwd_bwd(z, z[:, :3], i), AssertionError),   # entries that are not contiguous
+    (lambda rn, z, i: rn.distill_fwd_bwd(z, z[:, :3].contiguous(), i.long()), TypeError),
+    (lambda rn, z, i: rn.distill_fwd_bwd(z, z[:, :3].contiguous(), i[:, :2].contiguous()), ValueError),
+    (lambda rn, z, i: rn.distill_fwd_bwd(z, z[:, :3].contiguous(), None), TypeError),
+    (lambda rn, z, i: rn.distill_fwd_bwd(z, z[:, :3].contiguous(), i, alpha=1.5), "rn50"),
+    (lambda rn, z, i: rn.distill_fwd_bwd(z, z[:, :3].contiguous(), i, alpha=float("nan")), "rn50"),
+    (lambda rn, z, i: rn.distill_fwd_bwd(z, z[:, :3].contiguous(), i, temperature=-1.0), "rn50"),
+    (lambda rn, z, i: rn.distill_fwd_bwd(z, z[:, :3].contiguous(), i, label_smoothing=2.0), "rn50"),
+    (lambda rn, z, i: rn.distill_fwd_bwd(z, z[:, :3].contiguous(), i, dlogits=z.bfloat16()), TypeError),
+    (lambda rn, z, i: rn.distill_fwd_bwd(z, z[:, :3].contiguous(), i, dlogits=z[:3]), ValueError),
+    (lambda rn, z, i: rn.matmul_i8(64, *rn.quant_rows_i8(z), *rn.quant_rows_i8(z[:, :32])), None),   # both are rows of 64 bytes
+    (lambda rn, z, i: rn.matmul_i8(65, *rn.quant_rows_i8(z), *rn.quant_rows_i8(z)), ValueError),
+    (lambda rn, z, i: rn.fc_i8_fwd(z, z, z[0]), TypeError),
+    (lambda rn, z, i: rn.fc_i8_fwd(z, *rn.quant_rows_i8(z), dtype=torch.float16), TypeError),
+    (lambda rn, z, i: rn.fc_i8_fwd(z, *rn.quant_rows_i8(z), y=z), ValueError),
+    (lambda rn, z, i: rn.fc_i8_fwd(z, *rn.quant_rows_i8(z), bias=z[0, :3].contiguous()), ValueError),
+])
+def test_what_is_refused(rn, call, error):
+    z = torch.randn(5, 64, device="cuda")
+    i = torch.zeros(5, 3, dtype=torch.int32, device="cuda")
+    if error is None:
+        call(rn, z, i)
+        return
+    with pytest.raises(rn.Rn50Error if error == "rn50" else error):
+        call(rn, z, i)
+    torch.cuda.synchronize()
+
+
+def test_the_interface_refuses_before_it_launches(rn):
+    """C ABI: every error has its code, and nothing is written."""
+    raw, p = rn.raw, ctypes.c_void_p
+    out = torch.full((4096,), 3.0, device="cuda")
+    o, f, ld = p(out.data_ptr()), ctypes.c_float, ctypes.c_int64
+    odd = p(out.data_ptr() + 2)
+    z = ctypes.c_size_t(0)
+    assert raw.topk_rows(2, 8, 3, 7, o, ld(8), f(1), o, o, None, None, z, None) == -1
+    assert raw.topk_rows(2, 8, 3, 0, o, ld(7), f(1), o, o, None, None, z, None) == -1
+    assert raw.topk_rows(2, 8, 3, 0, odd, ld(8), f(1), o, o, None, None, z, None) == -4
+    assert raw.topk_rows(2, 8, 3, 0, None, ld(8), f(1), o, o, None, None, z, None) == -1
+    assert raw.quant_rows_i8(2, 8, 0, o, ld(8), None, o, None) == -1
+    assert raw.quant_rows_i8(2, 200000, 0, o, ld(200000), o, o, None) == -2
+    assert raw.matmul_i8(2, 2, 8, o, o, o, None, None, 0, o, ld(2), None) == -1
+    assert raw.matmul_i8(2, 2, 8, o, o, o, o, None, 0, o, ld(1), None) == -1
+    assert raw.fc_i8_fwd(2, 2, 8, 0, o, ld(8), o, o, None, 0, o, ld(2), None, z, None) == -3
+    d = rn.DistillDesc(2, 8, 3, 0, 8, 9, 1.0, 1.0, 0.0, 1.0)
+    assert raw.distill_fwd_bwd(ctypes.byref(d), o, o, o, None, None, None, o, o, o, None, z, None) == -1   # in place, other rows
+    assert raw.distill_fwd_bwd(None, o, o, o, None, None, None, o, o, o, None, z, None) == -1
+    assert raw.distill_fwd_bwd(ctypes.byref(d), o, None, o, None, None, None, o, o, None, None, z, None) == -1
+    torch.cuda.synchronize()
+    assert bool((out == 3.0).all())
