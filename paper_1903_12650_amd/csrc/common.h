@@ -153,6 +153,19 @@ __device__ __forceinline__ Vec16 load16(const T* p) {
   v.u = *reinterpret_cast<const uint4*>(p);
   return v;
 }
+// The same from and to any element's address (global memory takes 16 bytes at any of them).
+template <typename T>
+__device__ __forceinline__ Vec16 load16_any(const T* p) {
+  typedef unsigned int v4 __attribute__((ext_vector_type(4)));
+  typedef v4 v4_any __attribute__((aligned(2)));
+  return __builtin_bit_cast(Vec16, static_cast<v4>(*reinterpret_cast<const v4_any*>(p)));
+}
+template <typename T>
+__device__ __forceinline__ void store16_any(T* p, const Vec16& v) {
+  typedef unsigned int v4 __attribute__((ext_vector_type(4)));
+  typedef v4 v4_any __attribute__((aligned(2)));
+  *reinterpret_cast<v4_any*>(p) = __builtin_bit_cast(v4, v.u);
+}
 // The same past the caches: for what nobody reads again soon.
 typedef int i32x4_nt __attribute__((ext_vector_type(4)));
 template <typename T>

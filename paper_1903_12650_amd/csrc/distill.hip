@@ -148,176 +148,390 @@ struct DistillArgs {
   float temperature, alpha, smoothing, grad_scale;
 };
 
-constexpr int kChunk = 65536;  // classes whose membership bits are in LDS at a time
+// What a row's kernel has to know of the sums' exponentials.  The loss needs those of (z - m) / T and, with labels, of z - m.
+// EXPS = 1: one of the two (T = 1, or alpha = 0 or 1); 2, 4: T = 2 or 4, whose second exponential is a power of the first (a
+// multiplication or two in place of an exponential's four issue slots); 0: both.
+struct Scales {
+  float t, one;  // log2(e) / T and log2(e) (EXPS = 1: the one that is needed, twice)
+  float slack;   // the reference stays while logits pass it by less than this: 2^20 in either sum
+};
+__device__ __forceinline__ Scales scales_of(const DistillArgs& a, int exps) {
+  Scales s;
+  s.t = exps == 1 && a.alpha == 0.f ? kLog2e : kLog2e / a.temperature;
+  s.one = exps == 1 ? s.t : kLog2e;
+  s.slack = 20.f / fmaxf(s.t, s.one);
+  return s;
+}
 
-// The row's numbers that the gradient pass needs.
-struct RowGrad {
-  float m;       // reference of the exponentials
-  float coef_t;  // of exp((z - m) / T): alpha T w (q_r - p_r) / s
-  float coef_1;  // of exp(z - m): (1 - alpha) w / S
-  float offset;  // (1 - alpha) w ls / C
+// A running sum of exponentials.  Its reference is a logit that has been seen, not the largest one: the sums lose nothing by a
+// reference that is too low by less than `slack`, and moving it with every new maximum would cost two exponentials a vector.
+template <int EXPS>
+struct Sums {
+  float ref = -FLT_MAX, lim = -FLT_MAX, st = 0.f, s1 = 0.f;
+  __device__ __forceinline__ void one(float x, const Scales& sc) {
+    const float d = x - ref, y = __builtin_amdgcn_exp2f(d * sc.t);
+    st += y;
+    if constexpr (EXPS == 2) s1 = fmaf(y, y, s1);
+    if constexpr (EXPS == 4) {
+      const float y2 = y * y;
+      s1 = fmaf(y2, y2, s1);
+    }
+    if constexpr (EXPS == 0) s1 += __builtin_amdgcn_exp2f(d * sc.one);
+  }
+  template <int V>
+  __device__ __forceinline__ void add(const float* x, const Scales& sc) {
+    float top = x[0];
+#pragma unroll
+    for (int j = 1; j < V; ++j) top = fmaxf(top, x[j]);
+    if (top > lim) {
+      const float f = __builtin_amdgcn_exp2f((ref - top) * sc.t);
+      st *= f;
+      if constexpr (EXPS == 0) s1 *= __builtin_amdgcn_exp2f((ref - top) * sc.one);
+      if constexpr (EXPS == 2) s1 *= f * f;
+      if constexpr (EXPS == 4) s1 *= (f * f) * (f * f);
+      ref = top;
+      lim = top + sc.slack;
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j) one(x[j], sc);
+  }
 };
 
-// One workgroup per row.
+// The sums of a row (or of a slice of one), complete: s_t * exp((.) / T) and s_1 * exp(.) about `ref`, and the sum of the logits.
+struct RowSums {
+  float ref, st, s1;
+  double sz;
+};
+// Sums of a workgroup's threads, in a fixed order; complete in every thread.  `red`: a RowSums for each wave.
+template <int EXPS, int NT>
+__device__ __forceinline__ RowSums block_sums(const Sums<EXPS>& a, double sz, bool want_sz, const Scales& sc, RowSums* red) {
+  const int wave = threadIdx.x >> 6;
+  RowSums r;
+  r.ref = wave_max(a.ref);
+  const float f = __builtin_amdgcn_exp2f((a.ref - r.ref) * sc.t);
+  r.st = wave_sum(a.st * f);
+  if constexpr (EXPS == 1) r.s1 = r.st;
+  if constexpr (EXPS == 2) r.s1 = wave_sum(a.s1 * (f * f));
+  if constexpr (EXPS == 4) r.s1 = wave_sum(a.s1 * ((f * f) * (f * f)));
+  if constexpr (EXPS == 0) r.s1 = wave_sum(a.s1 * __builtin_amdgcn_exp2f((a.ref - r.ref) * sc.one));
+  r.sz = want_sz ? wave_sum(sz) : 0.0;
+  if constexpr (NT == 64) return r;
+  if ((threadIdx.x & 63) == 0) red[wave] = r;
+  __syncthreads();
+  RowSums t = red[0];
+  for (int w = 1; w < NT / 64; ++w) t.ref = fmaxf(t.ref, red[w].ref);
+  t.st = t.s1 = 0.f;
+  t.sz = 0.0;
+  for (int w = 0; w < NT / 64; ++w) {
+    const float d = red[w].ref - t.ref;
+    t.st += red[w].st * __builtin_amdgcn_exp2f(d * sc.t);
+    t.s1 += red[w].s1 * __builtin_amdgcn_exp2f(d * sc.one);
+    t.sz += red[w].sz;
+  }
+  return t;
+}
+
+// What the gradient pass needs of its row: d = coef_t * exp((z - ref) / T) + coef_1 * exp(z - ref) - offset (EXPS = 1: both
+// coefficients in coef_t) for every class; the classes at[0..special) get value[] instead.
+struct RowGrad {
+  float ref, coef_t, coef_1, offset;
+};
+struct RowShared {
+  int at[kTopMax + 1];      // classes of the entries (-1: absent), then the label's if it is none of theirs
+  float z[kTopMax + 1];     // their logits; z[kTopMax]: the label's
+  float value[kTopMax + 1];
+  RowGrad g;
+};
+
+// A row's loss and the coefficients of its gradient, by one wave.  Everything is relative to the largest logit and the largest
+// cell, in double: the logarithms are those of sums of exponentials, and differences of them are small beside the logits.
+// (Loops that are not unrolled: this is done once a row, and its registers are the kernel's.)
+template <int EXPS>
+__device__ __forceinline__ void row_finish(const DistillArgs& a, const Scales& sc, const RowSums& r, int n, float w, int label, RowShared& sh) {
+  const int lane = threadIdx.x & 63;
+  const bool kl_on = a.alpha > 0.f, ce_on = label >= 0;
+  const int k = kl_on ? a.k : 0;
+  const double t_inv = 1.0 / static_cast<double>(a.temperature), log2e = static_cast<double>(kLog2e);
+  const float* tv = a.t_values + static_cast<int64_t>(n) * a.k;
+  float M = r.ref;
+  float vt = -INFINITY;  // (of the teacher's logits; its largest cell follows)
+#pragma unroll 1
+  for (int j = lane; j < k; j += 64)
+    if (sh.at[j] >= 0) {
+      M = fmaxf(M, sh.z[j]);
+      vt = fmaxf(vt, tv[j]);
+    }
+  M = wave_max(M);
+  vt = wave_max(vt);
+  const float tail = kl_on && a.t_tail ? a.t_tail[n] : -INFINITY;
+  const double Mt = fmax(static_cast<double>(tail), vt * t_inv);
+  const bool empty = Mt == -INFINITY;
+  const double tau = empty ? -INFINITY : static_cast<double>(tail) - Mt;
+  // sums: the student's at T and at 1, the teacher's
+  float eT = 0.f, e1 = 0.f, eS = 0.f;
+#pragma unroll 1
+  for (int j = lane; j < k; j += 64)
+    if (sh.at[j] >= 0) {
+      const float d = sh.z[j] - M, e = __builtin_amdgcn_exp2f(d * sc.t);
+      eT += e;
+      e1 += EXPS == 1 ? e : __builtin_amdgcn_exp2f(d * sc.one);
+      eS += empty ? 0.f : __builtin_amdgcn_exp2f(static_cast<float>((tv[j] * t_inv - Mt) * log2e));
+    }
+  const float down = r.ref - M, pt = empty ? 0.f : __builtin_amdgcn_exp2f(static_cast<float>(tau * log2e));
+  const double AT = static_cast<double>(wave_sum(eT)) + static_cast<double>(r.st) * __builtin_amdgcn_exp2f(down * sc.t);
+  const double A1 = static_cast<double>(wave_sum(e1)) + static_cast<double>(r.s1) * __builtin_amdgcn_exp2f(down * sc.one);
+  const double S = static_cast<double>(wave_sum(eS)) + pt;
+  const bool none = AT == 0;  // every logit is -infinity
+  // four logarithms at once (log 0 = -infinity)
+  const double lg = log(lane == 0 ? AT : lane == 1 ? A1 : lane == 2 ? S : static_cast<double>(r.st));
+  const double Z = __shfl(lg, 0, 64), Z1 = __shfl(lg, 1, 64), L = __shfl(lg, 2, 64);
+  const double to_t = static_cast<double>(sc.t) / log2e, to_1 = static_cast<double>(sc.one) / log2e;  // the scales as the exponentials have them
+  const double lam = static_cast<double>(down) * to_t + __shfl(lg, 3, 64);
+  const double pr = pt / S, qr = static_cast<double>(r.st) * __builtin_amdgcn_exp2f(down * sc.t) / AT;
+  const double g = none ? 0.0 : static_cast<double>(a.grad_scale) * w;
+  const double gt = empty ? 0.0 : g * a.alpha * a.temperature, g1 = ce_on ? g * (1.0 - a.alpha) : 0.0;
+  RowGrad c;
+  c.ref = r.ref;
+  c.coef_t = r.st == 0.f || gt == 0 ? 0.f : static_cast<float>(gt * (qr - pr) / r.st);
+  c.coef_1 = g1 == 0 ? 0.f : static_cast<float>(g1 * __builtin_amdgcn_exp2f(down * sc.one) / A1);
+  c.offset = static_cast<float>(g1 * a.smoothing / a.C);
+  if constexpr (EXPS == 1) c.coef_t += c.coef_1;  // (the same exponential)
+  double kl = 0;
+  bool label_is_entry = false;
+#pragma unroll 1
+  for (int j = lane; j < k; j += 64)
+    if (sh.at[j] >= 0) {
+      const float d = sh.z[j] - M;
+      float p = 0.f;
+      if (!empty) {
+        const double logp = tv[j] * t_inv - Mt - L;
+        p = __builtin_amdgcn_exp2f(static_cast<float>(logp * log2e));
+        if (p != 0.f) kl += p * (logp - ((static_cast<double>(sh.z[j]) - M) * to_t - Z));
+      }
+      double v = -static_cast<double>(c.offset);
+      const float e = __builtin_amdgcn_exp2f(d * sc.t);
+      if (gt != 0) v += gt * (e / AT - p);
+      if (g1 != 0) v += g1 * (EXPS == 1 ? e : __builtin_amdgcn_exp2f(d * sc.one)) / A1;
+      if (ce_on && sh.at[j] == label) v -= g1 * (1.0 - a.smoothing), label_is_entry = true;
+      sh.value[j] = static_cast<float>(v);
+    }
+  kl = wave_sum(kl);
+  if (pr != 0) kl += pr * ((tau - L) - (lam - Z));
+  const float z_label = ce_on ? sh.z[kTopMax] : 0.f;
+  const bool known = __any(label_is_entry);
+  if (lane == 0) {
+    double loss = 0;
+    if (!none) {
+      if (!empty) loss += static_cast<double>(a.alpha) * a.temperature * a.temperature * kl;
+      if (ce_on) {
+        double ce = -(1.0 - a.smoothing) * ((static_cast<double>(z_label) - M) * to_1 - Z1);
+        if (a.smoothing > 0.f) ce -= static_cast<double>(a.smoothing) / a.C * ((r.sz - static_cast<double>(a.C) * M) - a.C * Z1);
+        loss += (1.0 - a.alpha) * ce;
+      }
+    }
+    a.row_loss[n] = static_cast<float>(loss);
+    sh.at[kTopMax] = ce_on && !known ? label : -1;
+    if (ce_on && !known) {
+      const float d = z_label - c.ref, y = __builtin_amdgcn_exp2f(d * sc.t);
+      float v = fmaf(c.coef_t, y, -c.offset);
+      if constexpr (EXPS != 1) v += c.coef_1 * __builtin_amdgcn_exp2f(d * sc.one);
+      sh.value[kTopMax] = v - static_cast<float>(g1 * (1.0 - a.smoothing));
+    }
+    sh.g = c;
+  }
+}
+
 template <typename T>
-__global__ __launch_bounds__(256) void distill_rows_kernel(const DistillArgs a) {
-  __shared__ uint32_t member[kChunk / 32];
-  __shared__ int at_s[kTopMax];
-  __shared__ float z_s[kTopMax];
-  __shared__ double v_s[kTopMax];
-  __shared__ float red[4][4];
-  __shared__ double red_z[4];
-  __shared__ double shared_d[8];
-  __shared__ RowGrad rg_s;
-  __shared__ int state_s;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const float scale = kLog2e / a.temperature;
-  const double beta = 1.0 / static_cast<double>(a.temperature);
-  const bool kl_on = a.alpha > 0.f;
-  for (int n = blockIdx.x; n < a.N; n += gridDim.x) {
-    const T* row = static_cast<const T*>(a.logits) + n * a.ld;
+struct RowOf {  // a row as vectors of V elements: whole ones, then what is left of the last, the rest of it -infinity
+  static constexpr int V = Elem<T>::VEC;
+  const T* p;
+  int C;
+  __device__ __forceinline__ Vec16 load(int v) const {
+    const int i = v * V;
+    Vec16 x;
+    if (i + V <= C) {
+      x = load16_any(p + i);
+    } else {
+      float f[V];
+#pragma unroll
+      for (int j = 0; j < V; ++j) f[j] = i + j < C ? Elem<T>::load(p + i + j) : -INFINITY;
+      Elem<T>::pack(f, x);
+    }
+    return x;
+  }
+};
+template <typename T>
+__device__ __forceinline__ void store_vector(T* p, int C, int v, const float* f) {
+  constexpr int V = Elem<T>::VEC;
+  const int i = v * V;
+  if (i + V <= C) {
+    Vec16 x;
+    Elem<T>::pack(f, x);
+    store16_any(p + i, x);
+  } else {
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+      if (i + j < C) Elem<T>::store(p + i + j, f[j]);
+  }
+}
+template <typename T, int EXPS>
+__device__ __forceinline__ void gradient_of(const Vec16& x, const RowGrad& g, const Scales& sc, float* d) {
+  constexpr int V = Elem<T>::VEC;
+  float z[V];
+  Elem<T>::unpack(x, z);
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const float u = z[j] - g.ref, y = __builtin_amdgcn_exp2f(u * sc.t);
+    d[j] = fmaf(g.coef_t, y, -g.offset);
+    if constexpr (EXPS == 2) d[j] = fmaf(g.coef_1, y * y, d[j]);
+    if constexpr (EXPS == 4) {
+      const float y2 = y * y;
+      d[j] = fmaf(g.coef_1, y2 * y2, d[j]);
+    }
+    if constexpr (EXPS == 0) d[j] = fmaf(g.coef_1, __builtin_amdgcn_exp2f(u * sc.one), d[j]);
+  }
+}
+
+// Reads a row's entries, those of classes that exist and appear for the first time: sh.at, sh.z.  Every thread of the workgroup calls it.
+// (Which of two equal classes comes first is found by comparison with those in front, but only where the bits say that there are two.)
+template <typename T, int NT>
+__device__ __forceinline__ void read_entries(const DistillArgs& a, const T* row, int n, int k, int label, RowShared& sh) {
+  const int tid = threadIdx.x;
+  static_assert(NT >= 64, "waves");
+  for (int j = tid; j < k; j += NT) {
+    const int c = a.t_indices[static_cast<int64_t>(n) * a.k + j];
+    sh.at[j] = c >= 0 && c < a.C ? c : -1;
+  }
+  if (tid == 0 && label >= 0) sh.z[kTopMax] = Elem<T>::load(row + label);
+  __syncthreads();
+}
+template <typename T, int NT>
+__device__ __forceinline__ void drop_repeated(const T* row, int k, bool repeated, RowShared& sh) {
+  const int tid = threadIdx.x;
+  if (__syncthreads_or(repeated)) {
+    bool drop[(kTopMax + NT - 1) / NT];
+#pragma unroll
+    for (int i = 0; i < (kTopMax + NT - 1) / NT; ++i) {
+      const int j = tid + NT * i, c = j < k ? sh.at[j] : -1;
+      drop[i] = false;
+      for (int h = 0; h < j && c >= 0; ++h) drop[i] |= sh.at[h] == c;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < (kTopMax + NT - 1) / NT; ++i)
+      if (drop[i]) sh.at[tid + NT * i] = -1;
+  }
+  for (int j = tid; j < k; j += NT)  // (each thread its own entries)
+    if (sh.at[j] >= 0) sh.z[j] = Elem<T>::load(row + sh.at[j]);
+  __syncthreads();
+}
+
+// One workgroup per row, NT threads.
+// U > 0: the row is U vectors a thread at most and stays in registers between the sums and the gradient: it is read once.  U = 0: it is
+// read twice, in chunks of classes whose membership bits fit LDS.
+template <typename T, int EXPS, int NT, int U>
+__global__ __launch_bounds__(NT) void distill_rows_kernel(const DistillArgs a) {
+  constexpr int V = Elem<T>::VEC;
+  constexpr int CHUNK = U > 0 ? U * NT * V : 65536;  // classes whose membership bits are in LDS at a time
+  __shared__ uint32_t member[CHUNK / 32];
+  __shared__ RowShared sh;
+  __shared__ RowSums red[NT / 64];
+  const int tid = threadIdx.x;
+  const Scales sc = scales_of(a, EXPS);
+  const int k = a.alpha > 0.f ? a.k : 0;
+  // (a grid of rows, not a loop over them: what the end of a row needs in constants would stay in registers through its sums)
+  const int n = blockIdx.y * gridDim.x + blockIdx.x;
+  if (n >= a.N) return;
+  {
+    const RowOf<T> row{static_cast<const T*>(a.logits) + n * a.ld, a.C};
     T* grad = a.grad ? static_cast<T*>(a.grad) + n * a.grad_ld : nullptr;
+    const int vecs = (a.C + V - 1) / V;
     const float w = a.row_weight ? a.row_weight[n] : 1.f / static_cast<float>(a.N);
     if (w == 0.f) {
-      for (int i = tid; grad && i < a.C; i += 256) Elem<T>::store(grad + i, 0.f);
+      float zero[V] = {};
+      for (int v = tid; grad && v < vecs; v += NT) store_vector(grad, a.C, v, zero);
       if (tid == 0) a.row_loss[n] = 0.f;
-      continue;
+      return;
     }
-    const int label = a.labels && a.alpha < 1.f ? a.labels[n] : -1;
-    const bool ce_on = label >= 0 && label < a.C;
-    // entries: absent ones have class -1
-    const int k = kl_on ? a.k : 0;
-    if (tid < k) at_s[tid] = a.t_indices[static_cast<int64_t>(n) * a.k + tid];
-    __syncthreads();
-    int at = -1;
-    if (tid < k) {
-      at = at_s[tid];
-      if (at < 0 || at >= a.C) at = -1;
-      for (int j = 0; j < tid && at >= 0; ++j)
-        if (at_s[j] == at) at = -1;
+    int label = a.labels && a.alpha < 1.f ? a.labels[n] : -1;
+    if (label >= a.C) label = -1;
+    const bool want_sz = label >= 0 && a.smoothing > 0.f;
+    Vec16 held[U > 0 ? U : 1];
+    if constexpr (U > 0) {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (u * NT + tid < vecs) held[u] = row.load(u * NT + tid);
     }
-    __syncthreads();
-    if (tid < k) {
-      at_s[tid] = at;
-      z_s[tid] = at >= 0 ? Elem<T>::load(row + at) : -INFINITY;
-      v_s[tid] = at >= 0 ? a.t_values[static_cast<int64_t>(n) * a.k + tid] * beta : -INFINITY;
-    }
-    const float z_label = ce_on ? Elem<T>::load(row + label) : 0.f;
-    // the classes that are no entry: maximum, sum at T, sum at 1, sum of the logits
-    float m = -FLT_MAX, st = 0.f, s1 = 0.f;
-    double sz = 0;  // (in double: of masked classes at the lowest float it still leaves what the others add)
-    for (int c0 = 0; c0 < a.C; c0 += kChunk) {
+    read_entries<T, NT>(a, row.p, n, k, label, sh);
+    Sums<EXPS> sums;
+    double sz = 0;  // (in double: beside classes masked with the lowest float it still holds what the others add)
+    auto add = [&](const Vec16& x, int v, int first) __attribute__((always_inline)) {
+      float z[V];
+      Elem<T>::unpack(x, z);
+      if (want_sz) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) sz += v * V + j < a.C ? static_cast<double>(z[j]) : 0.0;
+      }
+      const int at = (v - first) * V;
+      const uint32_t bits = member[at >> 5] >> (at & 31) & ((1u << V) - 1);
+      if (bits) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) z[j] = bits >> j & 1 ? -INFINITY : z[j];
+      }
+      sums.template add<V>(z, sc);
+    };
+    bool repeated = false;
+    for (int c0 = 0; c0 < a.C; c0 += CHUNK) {
+      const int chunk = min(a.C - c0, CHUNK);
+      if (c0) __syncthreads();
+      for (int i = tid; i < (chunk + 31) / 32; i += NT) member[i] = 0;
       __syncthreads();
-      for (int i = tid; i < kChunk / 32; i += 256) member[i] = 0;
+      for (int j = tid; j < k; j += NT) {
+        const int at = sh.at[j] - c0;
+        if (sh.at[j] >= c0 && at < chunk) repeated |= atomicOr(&member[at >> 5], 1u << (at & 31)) >> (at & 31) & 1;
+      }
       __syncthreads();
-      if (tid < k && at >= c0 && at - c0 < kChunk) atomicOr(&member[(at - c0) >> 5], 1u << ((at - c0) & 31));
-      __syncthreads();
-      for (int i = c0 + tid; i < min(a.C, c0 + kChunk); i += 256) {
-        const float z = Elem<T>::load(row + i);
-        if (a.smoothing > 0.f) sz += z;
-        if ((member[(i - c0) >> 5] >> ((i - c0) & 31)) & 1) continue;
-        const float top = fmaxf(m, z);
-        st = st * exp_scaled(m - top, scale) + exp_scaled(z - top, scale);
-        s1 = s1 * exp_scaled(m - top, kLog2e) + exp_scaled(z - top, kLog2e);
-        m = top;
+      if constexpr (U > 0) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (u * NT + tid < vecs) {
+            add(held[u], u * NT + tid, 0);
+            // the gradient unpacks them again: floats kept from here would be twice the registers
+            asm volatile("" : "+v"(held[u].u.x), "+v"(held[u].u.y), "+v"(held[u].u.z), "+v"(held[u].u.w));
+            __builtin_amdgcn_sched_barrier(0);
+          }
+      } else {
+        const int first = c0 / V, last = (c0 + chunk + V - 1) / V;
+        for (int v = first + tid; v < last; v += NT) add(row.load(v), v, first);
       }
     }
-    {
-      const float wm = wave_max(m);
-      const float wt = wave_sum(st * exp_scaled(m - wm, scale)), w1 = wave_sum(s1 * exp_scaled(m - wm, kLog2e));
-      const double wz = wave_sum(sz);
-      if (lane == 0) red[wave][0] = wm, red[wave][1] = wt, red[wave][2] = w1, red_z[wave] = wz;
-    }
-    __syncthreads();
-    if (tid == 0) {  // (first form: one thread)
-      float top = -FLT_MAX;
-      for (int i = 0; i < 4; ++i) top = fmaxf(top, red[i][0]);
-      double ST = 0, S1 = 0, SZ = 0;
-      for (int i = 0; i < 4; ++i) {
-        ST += red[i][1] * exp_scaled(red[i][0] - top, scale);
-        S1 += red[i][2] * exp_scaled(red[i][0] - top, kLog2e);
-        SZ += red_z[i];
-      }
-      const double rest = ST;
-      float M = top;
-      for (int j = 0; j < k; ++j) M = fmaxf(M, z_s[j]);
-      double AT = rest * exp_scaled(top - M, scale), A1 = S1 * exp_scaled(top - M, kLog2e);
-      for (int j = 0; j < k; ++j) {
-        AT += exp_scaled(z_s[j] - M, scale);
-        A1 += exp_scaled(z_s[j] - M, kLog2e);
-      }
-      const bool none = AT == 0;  // every logit is -infinity
-      // relative to M and Mt, so that nothing is lost beside large ones: log sums of exponentials (log 0 = -infinity)
-      const double Z = log(AT), Z1 = log(A1), lam = (static_cast<double>(top) - M) * beta + log(rest);
-      const double tau = kl_on && a.t_tail ? static_cast<double>(a.t_tail[n]) : -INFINITY;
-      double Mt = tau, kl = 0, pr = 0, L = 0;
-      for (int j = 0; j < k; ++j) Mt = fmax(Mt, v_s[j]);
-      const bool empty = Mt == -INFINITY;
-      if (!empty) {
-        double S = exp(tau - Mt);
-        for (int j = 0; j < k; ++j) S += exp(v_s[j] - Mt);
-        L = log(S);
-        for (int j = 0; j < k; ++j) {
-          const double p = exp(v_s[j] - Mt - L);
-          if (p != 0) kl += p * ((v_s[j] - Mt - L) - ((static_cast<double>(z_s[j]) - M) * beta - Z));
-        }
-        pr = exp(tau - Mt - L);
-        if (pr != 0) kl += pr * ((tau - Mt - L) - (lam - Z));
-      }
-      double loss = 0;
-      if (!none) {
-        if (!empty) loss += static_cast<double>(a.alpha) * a.temperature * a.temperature * kl;
-        if (ce_on) {
-          double ce = -(1.0 - a.smoothing) * (static_cast<double>(z_label) - M - Z1);
-          if (a.smoothing > 0.f) ce -= static_cast<double>(a.smoothing) / a.C * ((SZ - static_cast<double>(a.C) * M) - a.C * Z1);
-          loss += (1.0 - a.alpha) * ce;
-        }
-      }
-      a.row_loss[n] = static_cast<float>(loss);
-      const double g = none ? 0.0 : static_cast<double>(a.grad_scale) * w;
-      const double gt = empty ? 0.0 : g * a.alpha * a.temperature, g1 = ce_on ? g * (1.0 - a.alpha) : 0.0;
-      RowGrad r;
-      r.m = top;
-      r.coef_t = rest == 0 || gt == 0 ? 0.f : static_cast<float>(gt * (exp(lam - Z) - pr) / rest);
-      r.coef_1 = g1 == 0 ? 0.f : static_cast<float>(g1 * exp_scaled(top - M, kLog2e) / A1);
-      r.offset = static_cast<float>(g1 * a.smoothing / a.C);
-      rg_s = r;
-      state_s = none;
-      shared_d[0] = Z; shared_d[1] = L; shared_d[2] = gt; shared_d[3] = g1; shared_d[4] = Z1; shared_d[5] = M; shared_d[6] = Mt;
-    }
+    drop_repeated<T, NT>(row.p, k, repeated, sh);
+    const RowSums r = block_sums<EXPS, NT>(sums, sz, want_sz, sc, red);
+    if (tid < 64) row_finish<EXPS>(a, sc, r, n, w, label, sh);
     __syncthreads();
     if (grad) {
-      const RowGrad r = rg_s;
-      const double Z = shared_d[0], L = shared_d[1], gt = shared_d[2], g1 = shared_d[3], Z1 = shared_d[4], M = shared_d[5], Mt = shared_d[6];
-      const bool none = state_s;
-      for (int i = tid; i < a.C; i += 256) {
-        const float z = Elem<T>::load(row + i);
-        float d = none ? 0.f : -r.offset;
-        if (r.coef_t != 0.f) d += r.coef_t * exp_scaled(z - r.m, scale);
-        if (r.coef_1 != 0.f) d += r.coef_1 * exp_scaled(z - r.m, kLog2e);
-        Elem<T>::store(grad + i, d);
+      const RowGrad g = sh.g;
+      float d[V];
+      if constexpr (U > 0) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (u * NT + tid < vecs) {
+            gradient_of<T, EXPS>(held[u], g, sc, d);
+            store_vector(grad, a.C, u * NT + tid, d);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+      } else {
+        for (int v = tid; v < vecs; v += NT) {
+          gradient_of<T, EXPS>(row.load(v), g, sc, d);
+          store_vector(grad, a.C, v, d);
+        }
       }
       __syncthreads();
-      // the entries' classes and the label's: written once more, whole
-      if (!none) {
-        const double off = g1 * a.smoothing / a.C;
-        bool label_is_entry = false;
-        for (int j = 0; j < k; ++j) label_is_entry |= at_s[j] == label;
-        if (tid < k && at >= 0) {
-          double d = -off;
-          if (gt != 0) d += gt * (exp((z_s[tid] - M) * beta - Z) - exp(v_s[tid] - Mt - L));
-          if (g1 != 0) d += g1 * exp(z_s[tid] - M - Z1);
-          if (at == label) d -= g1 * (1.0 - a.smoothing);
-          Elem<T>::store(grad + at, static_cast<float>(d));
-        }
-        if (tid == 0 && ce_on && !label_is_entry) {
-          float d = -r.offset + r.coef_t * exp_scaled(z_label - r.m, scale) + r.coef_1 * exp_scaled(z_label - r.m, kLog2e);
-          d -= static_cast<float>(g1 * (1.0 - a.smoothing));
-          Elem<T>::store(grad + label, d);
-        }
-      }
+      // the entries' classes and the label's: written once more (behind the barrier: the same memory)
+      for (int j = tid; j < k; j += NT)
+        if (sh.at[j] >= 0) Elem<T>::store(grad + sh.at[j], sh.value[j]);
+      if (tid == 0 && sh.at[kTopMax] >= 0) Elem<T>::store(grad + sh.at[kTopMax], sh.value[kTopMax]);
     }
-    __syncthreads();
   }
 }
 
@@ -347,6 +561,25 @@ static int check_rows(const char* who, int N, int C, int dtype, const void* logi
   RN50_REQUIRE(ld >= C, RN50_ERR_INVALID, "%s: rows of %d elements %lld apart", who, C, static_cast<long long>(ld));
   RN50_REQUIRE(aligned_to(logits, dtype == RN50_BF16 ? 2 : 4), RN50_ERR_ALIGN, "%s: pointer not aligned to an element", who);
   return RN50_OK;
+}
+template <typename T, int EXPS>
+static void distill_rows(const DistillArgs& a, dim3 grid, hipStream_t s) {
+  constexpr int V = Elem<T>::VEC;
+  const int64_t vecs = ceil_div(a.C, V);
+  if (vecs <= 256) RN50_LAUNCH("distill", (distill_rows_kernel<T, EXPS, 256, 1>), grid, dim3(256), 0, s, a);
+  else if (vecs <= 256 * 4) RN50_LAUNCH("distill", (distill_rows_kernel<T, EXPS, 256, 4>), grid, dim3(256), 0, s, a);
+  else if (vecs <= 512 * 8) RN50_LAUNCH("distill", (distill_rows_kernel<T, EXPS, 512, 8>), grid, dim3(512), 0, s, a);
+  else if (vecs <= 1024 * 8) RN50_LAUNCH("distill", (distill_rows_kernel<T, EXPS, 1024, 8>), grid, dim3(1024), 0, s, a);
+  else if (vecs <= 1024 * 16) RN50_LAUNCH("distill", (distill_rows_kernel<T, EXPS, 1024, 16>), grid, dim3(1024), 0, s, a);
+  else RN50_LAUNCH("distill", (distill_rows_kernel<T, EXPS, 256, 0>), grid, dim3(256), 0, s, a);
+}
+template <typename T>
+static void distill_run(const DistillArgs& a, dim3 grid, hipStream_t s) {
+  const bool both = a.alpha > 0.f && a.alpha < 1.f && a.labels;
+  if (!both || a.temperature == 1.f) distill_rows<T, 1>(a, grid, s);
+  else if (a.temperature == 2.f) distill_rows<T, 2>(a, grid, s);
+  else if (a.temperature == 4.f) distill_rows<T, 4>(a, grid, s);
+  else distill_rows<T, 0>(a, grid, s);
 }
 constexpr int kRowGrid = 1 << 20;  // workgroups of a launch over rows, at most: they take the rows in turn
 
@@ -410,8 +643,8 @@ extern "C" int distill_fwd_bwd(const rn50_distill_desc* d, const void* logits, c
   DistillArgs a{logits, dlogits, t_values, t_indices, t_tail, row_weight, labels, row_loss_out, d->ld, d->grad_ld, d->N, d->C, d->k,
                 d->temperature, d->alpha, d->label_smoothing, d->grad_scale};
   const dim3 grid(std::min(d->N, kRowGrid));
-  if (d->dtype == RN50_BF16) RN50_LAUNCH("distill", distill_rows_kernel<uint16_t>, grid, dim3(256), 0, s, a);
-  else RN50_LAUNCH("distill", distill_rows_kernel<float>, grid, dim3(256), 0, s, a);
+  if (d->dtype == RN50_BF16) distill_run<uint16_t>(a, grid, s);
+  else distill_run<float>(a, grid, s);
   RN50_LAUNCH("distill_loss", distill_loss_kernel, dim3(1), dim3(256), 0, s, row_loss_out, row_weight, d->N, loss_out);
   return launch_status(who);
 }
