@@ -157,14 +157,20 @@ __device__ __forceinline__ Vec16 load16(const T* p) {
 template <typename T>
 __device__ __forceinline__ Vec16 load16_any(const T* p) {
   typedef unsigned int v4 __attribute__((ext_vector_type(4)));
-  typedef v4 v4_any __attribute__((aligned(2)));
+  typedef v4 v4_any __attribute__((aligned(2), may_alias));
   return __builtin_bit_cast(Vec16, static_cast<v4>(*reinterpret_cast<const v4_any*>(p)));
 }
 template <typename T>
 __device__ __forceinline__ void store16_any(T* p, const Vec16& v) {
   typedef unsigned int v4 __attribute__((ext_vector_type(4)));
-  typedef v4 v4_any __attribute__((aligned(2)));
+  typedef v4 v4_any __attribute__((aligned(2), may_alias));
   *reinterpret_cast<v4_any*>(p) = __builtin_bit_cast(v4, v.u);
+}
+template <typename T>
+__device__ __forceinline__ void store16_any_stream(T* p, const Vec16& v) {
+  typedef unsigned int v4 __attribute__((ext_vector_type(4)));
+  typedef v4 v4_any __attribute__((aligned(2), may_alias));
+  __builtin_nontemporal_store(__builtin_bit_cast(v4, v.u), reinterpret_cast<v4_any*>(p));
 }
 // The same past the caches: for what nobody reads again soon.
 typedef int i32x4_nt __attribute__((ext_vector_type(4)));

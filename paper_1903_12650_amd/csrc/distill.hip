@@ -5,6 +5,7 @@
 // nothing is ever subtracted from an infinity of its own sign: a logit of -infinity adds exp(-infinity) = 0, a row of nothing else
 // leaves s = 0, a logit of +infinity or NaN makes s NaN.
 #include <float.h>
+#include <stdlib.h>
 
 #include <algorithm>
 
@@ -20,8 +21,32 @@ __device__ __forceinline__ double wave_sum(double v) {
   for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
   return v;
 }
+// Sum and maximum of a wave's floats, the same in every lane: four exchanges inside rows of 16 lanes (moves between lanes in the ALU; through
+// LDS, as wave_sum has them, each is some hundred cycles that a row's end waits for), then the four rows' values from scalar registers.
+template <int CTRL>
+__device__ __forceinline__ float lane_move(float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float from_lane(float x, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), lane)); }
+__device__ __forceinline__ float quick_sum(float x) {
+  x += lane_move<0xB1>(x);   // lanes 1 apart
+  x += lane_move<0x4E>(x);   // 2 apart
+  x += lane_move<0x141>(x);  // the other half of 8, mirrored
+  x += lane_move<0x140>(x);  // the other half of 16, mirrored
+  return (from_lane(x, 0) + from_lane(x, 16)) + (from_lane(x, 32) + from_lane(x, 48));
+}
+__device__ __forceinline__ float quick_max(float x) {
+  x = fmaxf(x, lane_move<0xB1>(x));
+  x = fmaxf(x, lane_move<0x4E>(x));
+  x = fmaxf(x, lane_move<0x141>(x));
+  x = fmaxf(x, lane_move<0x140>(x));
+  return fmaxf(fmaxf(from_lane(x, 0), from_lane(x, 16)), fmaxf(from_lane(x, 32), from_lane(x, 48)));
+}
 // exp(x) for x <= 0 with the hardware's exponential; `scale` = log2(e) / T.
 __device__ __forceinline__ float exp_scaled(float x, float scale) { return __builtin_amdgcn_exp2f(x * scale); }
+
+// A workgroup for each of N rows, row blockIdx.y * gridDim.x + blockIdx.x.
+static dim3 row_grid(int N) { return N <= 65536 ? dim3(N) : dim3(65536, static_cast<unsigned>(ceil_div(N, 65536))); }
 
 // ------------------------------------------------------------- largest logits
 // The order of the logits as unsigned integers: -0 and +0 are one, a NaN is above everything.
@@ -45,7 +70,9 @@ __global__ __launch_bounds__(256) void topk_rows_kernel(const T* __restrict__ lo
   __shared__ int taken[5];
   __shared__ float red_m[4], red_s[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  for (int n = blockIdx.x; n < N; n += gridDim.x) {
+  const int n = blockIdx.y * gridDim.x + blockIdx.x;
+  if (n >= N) return;
+  {
     const T* row = logits + n * ld;
     const int kk = min(k, C);
     uint32_t prefix = 0;
@@ -202,355 +229,525 @@ struct RowSums {
   float ref, st, s1;
   double sz;
 };
+// The sums of `n` parts, in their order.
+__device__ __forceinline__ RowSums joined(const RowSums* part, int n, const Scales& sc) {
+  RowSums t = part[0];
+  for (int w = 1; w < n; ++w) t.ref = fmaxf(t.ref, part[w].ref);
+  t.st = t.s1 = 0.f;
+  t.sz = 0.0;
+  for (int w = 0; w < n; ++w) {
+    const float d = part[w].ref - t.ref;
+    t.st += part[w].st * __builtin_amdgcn_exp2f(d * sc.t);
+    t.s1 += part[w].s1 * __builtin_amdgcn_exp2f(d * sc.one);
+    t.sz += part[w].sz;
+  }
+  return t;
+}
 // Sums of a workgroup's threads, in a fixed order; complete in every thread.  `red`: a RowSums for each wave.
 template <int EXPS, int NT>
 __device__ __forceinline__ RowSums block_sums(const Sums<EXPS>& a, double sz, bool want_sz, const Scales& sc, RowSums* red) {
   const int wave = threadIdx.x >> 6;
   RowSums r;
-  r.ref = wave_max(a.ref);
+  r.ref = quick_max(a.ref);
   const float f = __builtin_amdgcn_exp2f((a.ref - r.ref) * sc.t);
-  r.st = wave_sum(a.st * f);
+  r.st = quick_sum(a.st * f);
   if constexpr (EXPS == 1) r.s1 = r.st;
-  if constexpr (EXPS == 2) r.s1 = wave_sum(a.s1 * (f * f));
-  if constexpr (EXPS == 4) r.s1 = wave_sum(a.s1 * ((f * f) * (f * f)));
-  if constexpr (EXPS == 0) r.s1 = wave_sum(a.s1 * __builtin_amdgcn_exp2f((a.ref - r.ref) * sc.one));
+  if constexpr (EXPS == 2) r.s1 = quick_sum(a.s1 * (f * f));
+  if constexpr (EXPS == 4) r.s1 = quick_sum(a.s1 * ((f * f) * (f * f)));
+  if constexpr (EXPS == 0) r.s1 = quick_sum(a.s1 * __builtin_amdgcn_exp2f((a.ref - r.ref) * sc.one));
   r.sz = want_sz ? wave_sum(sz) : 0.0;
   if constexpr (NT == 64) return r;
   if ((threadIdx.x & 63) == 0) red[wave] = r;
   __syncthreads();
-  RowSums t = red[0];
-  for (int w = 1; w < NT / 64; ++w) t.ref = fmaxf(t.ref, red[w].ref);
-  t.st = t.s1 = 0.f;
-  t.sz = 0.0;
-  for (int w = 0; w < NT / 64; ++w) {
-    const float d = red[w].ref - t.ref;
-    t.st += red[w].st * __builtin_amdgcn_exp2f(d * sc.t);
-    t.s1 += red[w].s1 * __builtin_amdgcn_exp2f(d * sc.one);
-    t.sz += red[w].sz;
-  }
-  return t;
+  return joined(red, NT / 64, sc);
 }
 
 // What the gradient pass needs of its row: d = coef_t * exp((z - ref) / T) + coef_1 * exp(z - ref) - offset (EXPS = 1: both
-// coefficients in coef_t) for every class; the classes at[0..special) get value[] instead.
+// coefficients in coef_t) for every class; the classes at[0..k] get value[] instead.
 struct RowGrad {
   float ref, coef_t, coef_1, offset;
 };
 struct RowShared {
   int at[kTopMax + 1];      // classes of the entries (-1: absent), then the label's if it is none of theirs
   float z[kTopMax + 1];     // their logits; z[kTopMax]: the label's
+  float t[kTopMax];         // the teacher's
   float value[kTopMax + 1];
+  int first[1024], next[kTopMax + 1];  // the entries of every thread, as lists
   RowGrad g;
 };
+// Hands entry j, of class c, to the thread that writes class c's gradient: of whole vectors of V classes in turn, of the classes behind
+// them one each.  (c and C: from the first class of the workgroup's slice, and the slice's classes; a class outside is nobody's here.)
+template <int V, int NT>
+__device__ __forceinline__ void hand_over(RowShared& sh, int C, int j, int c) {
+  const int whole = C / V * V;
+  if (c >= 0 && c < C) sh.next[j] = atomicExch(&sh.first[c < whole ? c / V % NT : c - whole], j);
+}
 
-// A row's loss and the coefficients of its gradient, by one wave.  Everything is relative to the largest logit and the largest
-// cell, in double: the logarithms are those of sums of exponentials, and differences of them are small beside the logits.
-// (Loops that are not unrolled: this is done once a row, and its registers are the kernel's.)
-template <int EXPS>
-__device__ __forceinline__ void row_finish(const DistillArgs& a, const Scales& sc, const RowSums& r, int n, float w, int label, RowShared& sh) {
-  const int lane = threadIdx.x & 63;
-  const bool kl_on = a.alpha > 0.f, ce_on = label >= 0;
-  const int k = kl_on ? a.k : 0;
-  const double t_inv = 1.0 / static_cast<double>(a.temperature), log2e = static_cast<double>(kLog2e);
-  const float* tv = a.t_values + static_cast<int64_t>(n) * a.k;
-  float M = r.ref;
-  float vt = -INFINITY;  // (of the teacher's logits; its largest cell follows)
+// A row's gradient coefficients and loss, by one wave.  Everything is relative to the largest logit and the largest cell; the logarithms
+// are those of sums of exponentials, and differences of them are small beside the logits: in double.  The coefficients first (the
+// other waves wait for them), the loss when they are gone.  (Loops that are not unrolled: their registers are the kernel's.)
+template <int EXPS, int V, int NT>
+struct RowEnd {
+  const DistillArgs& a;
+  const Scales& sc;
+  const RowSums& r;
+  RowShared& sh;
+  int label, k, first, classes;  // (the workgroup's slice of the row)
+  float M, tau, AT, A1, S, pt;
+  double Mt;
+  bool empty, none;
+
+  __device__ __forceinline__ RowEnd(const DistillArgs& a_, const Scales& sc_, const RowSums& r_, RowShared& sh_, int label_, int k_, int first_, int classes_)
+      : a(a_), sc(sc_), r(r_), sh(sh_), label(label_), k(k_), first(first_), classes(classes_) {}
+  __device__ __forceinline__ float cell(double over) const { return __builtin_amdgcn_exp2f(static_cast<float>(over * static_cast<double>(kLog2e))); }
+  __device__ __forceinline__ double teacher(int j) const { return sh.t[j] * (1.0 / static_cast<double>(a.temperature)) - Mt; }
+
+  __device__ __forceinline__ void gradient(float w, float tail) {
+    const int lane = threadIdx.x & 63;
+    M = r.ref;
+    float vt = -INFINITY;
 #pragma unroll 1
-  for (int j = lane; j < k; j += 64)
-    if (sh.at[j] >= 0) {
-      M = fmaxf(M, sh.z[j]);
-      vt = fmaxf(vt, tv[j]);
+    for (int j = lane; j < k; j += 64)
+      if (sh.at[j] >= 0) {
+        M = fmaxf(M, sh.z[j]);
+        vt = fmaxf(vt, sh.t[j]);
+      }
+    M = quick_max(M);
+    vt = quick_max(vt);
+    Mt = fmax(static_cast<double>(tail), vt * (1.0 / static_cast<double>(a.temperature)));
+    empty = Mt == -INFINITY;
+    tau = empty ? -INFINITY : static_cast<float>(tail - Mt);
+    // sums: the student's at T and at 1, the teacher's
+    float eT = 0.f, e1 = 0.f, eS = 0.f;
+#pragma unroll 1
+    for (int j = lane; j < k; j += 64)
+      if (sh.at[j] >= 0) {
+        const float d = sh.z[j] - M, e = __builtin_amdgcn_exp2f(d * sc.t);
+        eT += e;
+        if constexpr (EXPS != 1) e1 += __builtin_amdgcn_exp2f(d * sc.one);
+        if (!empty) eS += cell(teacher(j));
+      }
+    const float down = r.ref - M, rest = r.st * __builtin_amdgcn_exp2f(down * sc.t), from_1 = __builtin_amdgcn_exp2f(down * sc.one);
+    pt = empty ? 0.f : __builtin_amdgcn_exp2f(tau * kLog2e);
+    AT = quick_sum(eT) + rest;
+    A1 = EXPS == 1 ? AT : fmaf(r.s1, from_1, quick_sum(e1));
+    S = quick_sum(eS) + pt;
+    none = AT == 0.f;  // every logit is -infinity
+    if (!a.grad) return;
+    const bool ce_on = label >= 0;
+    const float g = none ? 0.f : a.grad_scale * w;
+    const float gt = empty ? 0.f : g * a.alpha * a.temperature, g1 = ce_on ? g * (1.f - a.alpha) : 0.f;
+    const float by_t = 1.f / AT, by_1 = EXPS == 1 ? by_t : 1.f / A1, by_s = empty ? 0.f : 1.f / S;
+    RowGrad c;
+    c.ref = r.ref;
+    c.coef_t = r.st == 0.f || gt == 0.f ? 0.f : gt * (rest * by_t - pt * by_s) / r.st;
+    c.coef_1 = g1 == 0.f ? 0.f : g1 * from_1 * by_1;
+    c.offset = g1 * a.smoothing / static_cast<float>(a.C);
+    if constexpr (EXPS == 1) c.coef_t += c.coef_1;  // (the same exponential)
+    bool label_is_entry = false;
+#pragma unroll 1
+    for (int j = lane; j < k; j += 64)
+      if (sh.at[j] >= 0) {
+        const float d = sh.z[j] - M, e = __builtin_amdgcn_exp2f(d * sc.t);
+        float v = -c.offset;
+        if (gt != 0.f) v += gt * (e * by_t - cell(teacher(j)) * by_s);
+        if (g1 != 0.f) v += g1 * (EXPS == 1 ? e : __builtin_amdgcn_exp2f(d * sc.one)) * by_1;
+        if (ce_on && sh.at[j] == label) v -= g1 * (1.f - a.smoothing), label_is_entry = true;
+        sh.value[j] = v;
+      }
+    const bool known = __any(label_is_entry);
+    if (lane == 0) {
+      sh.at[kTopMax] = label;
+      if (ce_on && !known) {
+        const float d = sh.z[kTopMax] - c.ref, y = __builtin_amdgcn_exp2f(d * sc.t);
+        float v = fmaf(c.coef_t, y, -c.offset);
+        if constexpr (EXPS != 1) v += c.coef_1 * __builtin_amdgcn_exp2f(d * sc.one);
+        sh.value[kTopMax] = v - g1 * (1.f - a.smoothing);
+        hand_over<V, NT>(sh, classes, kTopMax, label - first);
+      }
+      sh.g = c;
     }
-  M = wave_max(M);
-  vt = wave_max(vt);
-  const float tail = kl_on && a.t_tail ? a.t_tail[n] : -INFINITY;
-  const double Mt = fmax(static_cast<double>(tail), vt * t_inv);
-  const bool empty = Mt == -INFINITY;
-  const double tau = empty ? -INFINITY : static_cast<double>(tail) - Mt;
-  // sums: the student's at T and at 1, the teacher's
-  float eT = 0.f, e1 = 0.f, eS = 0.f;
+  }
+
+  __device__ __forceinline__ float loss() const {  // (valid in lane 0)
+    const int lane = threadIdx.x & 63;
+    // four logarithms at once (log 0 = -infinity)
+    const double lg = log(static_cast<double>(lane == 0 ? AT : lane == 1 ? A1 : lane == 2 ? S : r.st));
+    const double Z = __shfl(lg, 0, 64), Z1 = __shfl(lg, 1, 64), L = __shfl(lg, 2, 64);
+    const double ln2 = 0.69314718055994530942;
+    const double to_t = static_cast<double>(sc.t) * ln2, to_1 = static_cast<double>(sc.one) * ln2;  // the scales as the exponentials have them
+    const double lam = (static_cast<double>(r.ref) - M) * to_t + __shfl(lg, 3, 64);
+    double kl = 0;
 #pragma unroll 1
-  for (int j = lane; j < k; j += 64)
-    if (sh.at[j] >= 0) {
-      const float d = sh.z[j] - M, e = __builtin_amdgcn_exp2f(d * sc.t);
-      eT += e;
-      e1 += EXPS == 1 ? e : __builtin_amdgcn_exp2f(d * sc.one);
-      eS += empty ? 0.f : __builtin_amdgcn_exp2f(static_cast<float>((tv[j] * t_inv - Mt) * log2e));
-    }
-  const float down = r.ref - M, pt = empty ? 0.f : __builtin_amdgcn_exp2f(static_cast<float>(tau * log2e));
-  const double AT = static_cast<double>(wave_sum(eT)) + static_cast<double>(r.st) * __builtin_amdgcn_exp2f(down * sc.t);
-  const double A1 = static_cast<double>(wave_sum(e1)) + static_cast<double>(r.s1) * __builtin_amdgcn_exp2f(down * sc.one);
-  const double S = static_cast<double>(wave_sum(eS)) + pt;
-  const bool none = AT == 0;  // every logit is -infinity
-  // four logarithms at once (log 0 = -infinity)
-  const double lg = log(lane == 0 ? AT : lane == 1 ? A1 : lane == 2 ? S : static_cast<double>(r.st));
-  const double Z = __shfl(lg, 0, 64), Z1 = __shfl(lg, 1, 64), L = __shfl(lg, 2, 64);
-  const double to_t = static_cast<double>(sc.t) / log2e, to_1 = static_cast<double>(sc.one) / log2e;  // the scales as the exponentials have them
-  const double lam = static_cast<double>(down) * to_t + __shfl(lg, 3, 64);
-  const double pr = pt / S, qr = static_cast<double>(r.st) * __builtin_amdgcn_exp2f(down * sc.t) / AT;
-  const double g = none ? 0.0 : static_cast<double>(a.grad_scale) * w;
-  const double gt = empty ? 0.0 : g * a.alpha * a.temperature, g1 = ce_on ? g * (1.0 - a.alpha) : 0.0;
-  RowGrad c;
-  c.ref = r.ref;
-  c.coef_t = r.st == 0.f || gt == 0 ? 0.f : static_cast<float>(gt * (qr - pr) / r.st);
-  c.coef_1 = g1 == 0 ? 0.f : static_cast<float>(g1 * __builtin_amdgcn_exp2f(down * sc.one) / A1);
-  c.offset = static_cast<float>(g1 * a.smoothing / a.C);
-  if constexpr (EXPS == 1) c.coef_t += c.coef_1;  // (the same exponential)
-  double kl = 0;
-  bool label_is_entry = false;
-#pragma unroll 1
-  for (int j = lane; j < k; j += 64)
-    if (sh.at[j] >= 0) {
-      const float d = sh.z[j] - M;
-      float p = 0.f;
-      if (!empty) {
-        const double logp = tv[j] * t_inv - Mt - L;
-        p = __builtin_amdgcn_exp2f(static_cast<float>(logp * log2e));
+    for (int j = lane; j < k; j += 64)
+      if (sh.at[j] >= 0 && !empty) {
+        const double logp = teacher(j) - L;
+        const float p = cell(logp);
         if (p != 0.f) kl += p * (logp - ((static_cast<double>(sh.z[j]) - M) * to_t - Z));
       }
-      double v = -static_cast<double>(c.offset);
-      const float e = __builtin_amdgcn_exp2f(d * sc.t);
-      if (gt != 0) v += gt * (e / AT - p);
-      if (g1 != 0) v += g1 * (EXPS == 1 ? e : __builtin_amdgcn_exp2f(d * sc.one)) / A1;
-      if (ce_on && sh.at[j] == label) v -= g1 * (1.0 - a.smoothing), label_is_entry = true;
-      sh.value[j] = static_cast<float>(v);
-    }
-  kl = wave_sum(kl);
-  if (pr != 0) kl += pr * ((tau - L) - (lam - Z));
-  const float z_label = ce_on ? sh.z[kTopMax] : 0.f;
-  const bool known = __any(label_is_entry);
-  if (lane == 0) {
+    kl = wave_sum(kl);
+    if (pt != 0.f) kl += cell(tau - L) * ((tau - L) - (lam - Z));
     double loss = 0;
     if (!none) {
       if (!empty) loss += static_cast<double>(a.alpha) * a.temperature * a.temperature * kl;
-      if (ce_on) {
-        double ce = -(1.0 - a.smoothing) * ((static_cast<double>(z_label) - M) * to_1 - Z1);
+      if (label >= 0) {
+        double ce = -(1.0 - a.smoothing) * ((static_cast<double>(sh.z[kTopMax]) - M) * to_1 - Z1);
         if (a.smoothing > 0.f) ce -= static_cast<double>(a.smoothing) / a.C * ((r.sz - static_cast<double>(a.C) * M) - a.C * Z1);
         loss += (1.0 - a.alpha) * ce;
       }
     }
-    a.row_loss[n] = static_cast<float>(loss);
-    sh.at[kTopMax] = ce_on && !known ? label : -1;
-    if (ce_on && !known) {
-      const float d = z_label - c.ref, y = __builtin_amdgcn_exp2f(d * sc.t);
-      float v = fmaf(c.coef_t, y, -c.offset);
-      if constexpr (EXPS != 1) v += c.coef_1 * __builtin_amdgcn_exp2f(d * sc.one);
-      sh.value[kTopMax] = v - static_cast<float>(g1 * (1.0 - a.smoothing));
-    }
-    sh.g = c;
-  }
-}
-
-template <typename T>
-struct RowOf {  // a row as vectors of V elements: whole ones, then what is left of the last, the rest of it -infinity
-  static constexpr int V = Elem<T>::VEC;
-  const T* p;
-  int C;
-  __device__ __forceinline__ Vec16 load(int v) const {
-    const int i = v * V;
-    Vec16 x;
-    if (i + V <= C) {
-      x = load16_any(p + i);
-    } else {
-      float f[V];
-#pragma unroll
-      for (int j = 0; j < V; ++j) f[j] = i + j < C ? Elem<T>::load(p + i + j) : -INFINITY;
-      Elem<T>::pack(f, x);
-    }
-    return x;
+    return static_cast<float>(loss);
   }
 };
-template <typename T>
-__device__ __forceinline__ void store_vector(T* p, int C, int v, const float* f) {
-  constexpr int V = Elem<T>::VEC;
-  const int i = v * V;
-  if (i + V <= C) {
-    Vec16 x;
-    Elem<T>::pack(f, x);
-    store16_any(p + i, x);
-  } else {
-#pragma unroll
-    for (int j = 0; j < V; ++j)
-      if (i + j < C) Elem<T>::store(p + i + j, f[j]);
+
+template <int EXPS>
+__device__ __forceinline__ float gradient_of(float z, const RowGrad& g, const Scales& sc) {
+  const float u = z - g.ref, y = __builtin_amdgcn_exp2f(u * sc.t);
+  float d = fmaf(g.coef_t, y, -g.offset);
+  if constexpr (EXPS == 2) d = fmaf(g.coef_1, y * y, d);
+  if constexpr (EXPS == 4) {
+    const float y2 = y * y;
+    d = fmaf(g.coef_1, y2 * y2, d);
   }
+  if constexpr (EXPS == 0) d = fmaf(g.coef_1, __builtin_amdgcn_exp2f(u * sc.one), d);
+  return d;
 }
-template <typename T, int EXPS>
-__device__ __forceinline__ void gradient_of(const Vec16& x, const RowGrad& g, const Scales& sc, float* d) {
+template <typename T, int EXPS, bool STREAM>
+__device__ __forceinline__ void store_gradient(T* to, const Vec16& x, const RowGrad& g, const Scales& sc) {
   constexpr int V = Elem<T>::VEC;
   float z[V];
   Elem<T>::unpack(x, z);
 #pragma unroll
-  for (int j = 0; j < V; ++j) {
-    const float u = z[j] - g.ref, y = __builtin_amdgcn_exp2f(u * sc.t);
-    d[j] = fmaf(g.coef_t, y, -g.offset);
-    if constexpr (EXPS == 2) d[j] = fmaf(g.coef_1, y * y, d[j]);
-    if constexpr (EXPS == 4) {
-      const float y2 = y * y;
-      d[j] = fmaf(g.coef_1, y2 * y2, d[j]);
-    }
-    if constexpr (EXPS == 0) d[j] = fmaf(g.coef_1, __builtin_amdgcn_exp2f(u * sc.one), d[j]);
-  }
+  for (int j = 0; j < V; ++j) z[j] = gradient_of<EXPS>(z[j], g, sc);
+  Vec16 d;
+  Elem<T>::pack(z, d);
+  if constexpr (STREAM) store16_any_stream(to, d);
+  else store16_any(to, d);
 }
 
-// Reads a row's entries, those of classes that exist and appear for the first time: sh.at, sh.z.  Every thread of the workgroup calls it.
-// (Which of two equal classes comes first is found by comparison with those in front, but only where the bits say that there are two.)
-template <typename T, int NT>
-__device__ __forceinline__ void read_entries(const DistillArgs& a, const T* row, int n, int k, int label, RowShared& sh) {
-  const int tid = threadIdx.x;
-  static_assert(NT >= 64, "waves");
-  for (int j = tid; j < k; j += NT) {
-    const int c = a.t_indices[static_cast<int64_t>(n) * a.k + j];
-    sh.at[j] = c >= 0 && c < a.C ? c : -1;
-  }
-  if (tid == 0 && label >= 0) sh.z[kTopMax] = Elem<T>::load(row + label);
-  __syncthreads();
-}
-template <typename T, int NT>
-__device__ __forceinline__ void drop_repeated(const T* row, int k, bool repeated, RowShared& sh) {
-  const int tid = threadIdx.x;
-  if (__syncthreads_or(repeated)) {
-    bool drop[(kTopMax + NT - 1) / NT];
-#pragma unroll
-    for (int i = 0; i < (kTopMax + NT - 1) / NT; ++i) {
-      const int j = tid + NT * i, c = j < k ? sh.at[j] : -1;
-      drop[i] = false;
-      for (int h = 0; h < j && c >= 0; ++h) drop[i] |= sh.at[h] == c;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < (kTopMax + NT - 1) / NT; ++i)
-      if (drop[i]) sh.at[tid + NT * i] = -1;
-  }
-  for (int j = tid; j < k; j += NT)  // (each thread its own entries)
-    if (sh.at[j] >= 0) sh.z[j] = Elem<T>::load(row + sh.at[j]);
-  __syncthreads();
-}
-
-// One workgroup per row, NT threads.
+// One workgroup per row, NT threads, at least as many as a row has entries: a thread has one at most.  Whole vectors of V classes go round the
+// threads, the C % V classes behind the last of them are one thread's each.
 // U > 0: the row is U vectors a thread at most and stays in registers between the sums and the gradient: it is read once.  U = 0: it is
-// read twice, in chunks of classes whose membership bits fit LDS.
+// read for the sums and again for the gradient, in chunks of classes whose membership bits fit LDS; the gradient is stored past the
+// caches, which keep the rows for their second reading (2048 x 131072 bf16 272 -> 246 us, float 500 -> 476).  A thread adds the same vectors in
+// the same order in both.
 template <typename T, int EXPS, int NT, int U>
 __global__ __launch_bounds__(NT) void distill_rows_kernel(const DistillArgs a) {
   constexpr int V = Elem<T>::VEC;
-  constexpr int CHUNK = U > 0 ? U * NT * V : 65536;  // classes whose membership bits are in LDS at a time
+  constexpr int CHUNK = U > 0 ? U * NT * V + 32 : 65536;  // classes whose membership bits are in LDS at a time
+  constexpr int G = 4;                                    // vectors whose loads go out together (U = 0)
   __shared__ uint32_t member[CHUNK / 32];
   __shared__ RowShared sh;
   __shared__ RowSums red[NT / 64];
   const int tid = threadIdx.x;
-  const Scales sc = scales_of(a, EXPS);
-  const int k = a.alpha > 0.f ? a.k : 0;
   // (a grid of rows, not a loop over them: what the end of a row needs in constants would stay in registers through its sums)
   const int n = blockIdx.y * gridDim.x + blockIdx.x;
   if (n >= a.N) return;
-  {
-    const RowOf<T> row{static_cast<const T*>(a.logits) + n * a.ld, a.C};
-    T* grad = a.grad ? static_cast<T*>(a.grad) + n * a.grad_ld : nullptr;
-    const int vecs = (a.C + V - 1) / V;
-    const float w = a.row_weight ? a.row_weight[n] : 1.f / static_cast<float>(a.N);
-    if (w == 0.f) {
-      float zero[V] = {};
-      for (int v = tid; grad && v < vecs; v += NT) store_vector(grad, a.C, v, zero);
-      if (tid == 0) a.row_loss[n] = 0.f;
-      return;
+  const Scales sc = scales_of(a, EXPS);
+  const int k = a.alpha > 0.f ? a.k : 0, whole = a.C / V, left = a.C - whole * V;
+  const T* row = static_cast<const T*>(a.logits) + n * a.ld;
+  T* grad = a.grad ? static_cast<T*>(a.grad) + n * a.grad_ld : nullptr;
+  // what the row's end needs goes out first: it is a chain of loads (entry, its logit)
+  int at = -1;
+  if (tid < k) {
+    at = a.t_indices[static_cast<int64_t>(n) * a.k + tid];
+    sh.t[tid] = a.t_values[static_cast<int64_t>(n) * a.k + tid];
+  }
+  const float w = a.row_weight ? a.row_weight[n] : 1.f / static_cast<float>(a.N);
+  const float tail = a.alpha > 0.f && a.t_tail ? a.t_tail[n] : -INFINITY;
+  int label = a.labels && a.alpha < 1.f ? a.labels[n] : -1;
+  if (label >= a.C) label = -1;
+  Vec16 held[U > 0 ? U : 1];
+  if constexpr (U > 0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (u * NT + tid < whole) held[u] = load16_any(row + (u * NT + tid) * V);
+  }
+  const int mine = whole * V + tid;  // (tid < left)
+  const float z_left = tid < left ? Elem<T>::load(row + mine) : -INFINITY;
+  if (w == 0.f) {  // (behind the loads: the weight is a load as well)
+    for (int i = tid; grad && i < a.C; i += NT) Elem<T>::store(grad + i, 0.f);
+    if (tid == 0) a.row_loss[n] = 0.f;
+    return;
+  }
+  if (at >= a.C || at < 0) at = -1;
+  const float z_at = at >= 0 ? Elem<T>::load(row + at) : -INFINITY;
+  if (tid == 0 && label >= 0) sh.z[kTopMax] = Elem<T>::load(row + label);
+
+  const bool want_sz = label >= 0 && a.smoothing > 0.f;
+  Sums<EXPS> sums;
+  double sz = 0;  // (in double: beside classes masked with the lowest float it still holds what the others add)
+  auto add = [&](const Vec16& x, int e) __attribute__((always_inline)) {  // e: the vector's first class, from the chunk's first
+    float z[V];
+    Elem<T>::unpack(x, z);
+    if (want_sz) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) sz += static_cast<double>(z[j]);
     }
-    int label = a.labels && a.alpha < 1.f ? a.labels[n] : -1;
-    if (label >= a.C) label = -1;
-    const bool want_sz = label >= 0 && a.smoothing > 0.f;
-    Vec16 held[U > 0 ? U : 1];
+    const uint32_t bits = member[e >> 5] >> (e & 31) & ((1u << V) - 1);
+    if (bits) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) z[j] = bits >> j & 1 ? -INFINITY : z[j];
+    }
+    sums.template add<V>(z, sc);
+  };
+  bool repeated = false;
+  for (int c0 = 0; c0 < a.C; c0 += CHUNK) {
+    const int chunk = min(a.C - c0, CHUNK);
+    if (c0) __syncthreads();
+    for (int i = tid; i < (chunk + 31) / 32; i += NT) member[i] = 0;
+    __syncthreads();
+    if (at >= c0 && at - c0 < chunk) repeated = atomicOr(&member[(at - c0) >> 5], 1u << ((at - c0) & 31)) >> ((at - c0) & 31) & 1;
+    __syncthreads();
     if constexpr (U > 0) {
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        if (u * NT + tid < vecs) held[u] = row.load(u * NT + tid);
+        if (u * NT + tid < whole) {
+          add(held[u], (u * NT + tid) * V);
+          // the gradient unpacks them again: floats kept from here would be twice the registers
+          asm volatile("" : "+v"(held[u].u.x), "+v"(held[u].u.y), "+v"(held[u].u.z), "+v"(held[u].u.w));
+          __builtin_amdgcn_sched_barrier(0);
+        }
+    } else {
+      const T* from = row + c0;
+      const int vecs = chunk / V;
+      int v = tid;
+      for (; v + (G - 1) * NT < vecs; v += G * NT) {
+        Vec16 x[G];
+#pragma unroll
+        for (int g = 0; g < G; ++g) x[g] = load16_any(from + (v + g * NT) * V);
+#pragma unroll
+        for (int g = 0; g < G; ++g) add(x[g], (v + g * NT) * V);
+      }
+      for (; v < vecs; v += NT) add(load16_any(from + v * V), v * V);
     }
-    read_entries<T, NT>(a, row.p, n, k, label, sh);
-    Sums<EXPS> sums;
-    double sz = 0;  // (in double: beside classes masked with the lowest float it still holds what the others add)
-    auto add = [&](const Vec16& x, int v, int first) __attribute__((always_inline)) {
-      float z[V];
-      Elem<T>::unpack(x, z);
-      if (want_sz) {
-#pragma unroll
-        for (int j = 0; j < V; ++j) sz += v * V + j < a.C ? static_cast<double>(z[j]) : 0.0;
-      }
-      const int at = (v - first) * V;
-      const uint32_t bits = member[at >> 5] >> (at & 31) & ((1u << V) - 1);
-      if (bits) {
-#pragma unroll
-        for (int j = 0; j < V; ++j) z[j] = bits >> j & 1 ? -INFINITY : z[j];
-      }
-      sums.template add<V>(z, sc);
-    };
-    bool repeated = false;
-    for (int c0 = 0; c0 < a.C; c0 += CHUNK) {
-      const int chunk = min(a.C - c0, CHUNK);
-      if (c0) __syncthreads();
-      for (int i = tid; i < (chunk + 31) / 32; i += NT) member[i] = 0;
-      __syncthreads();
-      for (int j = tid; j < k; j += NT) {
-        const int at = sh.at[j] - c0;
-        if (sh.at[j] >= c0 && at < chunk) repeated |= atomicOr(&member[at >> 5], 1u << (at & 31)) >> (at & 31) & 1;
-      }
-      __syncthreads();
-      if constexpr (U > 0) {
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-          if (u * NT + tid < vecs) {
-            add(held[u], u * NT + tid, 0);
-            // the gradient unpacks them again: floats kept from here would be twice the registers
-            asm volatile("" : "+v"(held[u].u.x), "+v"(held[u].u.y), "+v"(held[u].u.z), "+v"(held[u].u.w));
-            __builtin_amdgcn_sched_barrier(0);
-          }
-      } else {
-        const int first = c0 / V, last = (c0 + chunk + V - 1) / V;
-        for (int v = first + tid; v < last; v += NT) add(row.load(v), v, first);
-      }
+    if (tid < left && mine - c0 < chunk) {
+      if (want_sz) sz += static_cast<double>(z_left);
+      if (!(member[(mine - c0) >> 5] >> ((mine - c0) & 31) & 1)) sums.template add<1>(&z_left, sc);
     }
-    drop_repeated<T, NT>(row.p, k, repeated, sh);
-    const RowSums r = block_sums<EXPS, NT>(sums, sz, want_sz, sc, red);
-    if (tid < 64) row_finish<EXPS>(a, sc, r, n, w, label, sh);
+  }
+  if (tid < k) {
+    sh.at[tid] = at;
+    sh.z[tid] = z_at;
+  }
+  sh.first[tid] = -1;
+  if (__syncthreads_or(repeated)) {  // of entries with the same class the first stands
+    bool drop = false;
+    for (int h = 0; h < tid && at >= 0 && tid < k; ++h) drop |= sh.at[h] == at;
     __syncthreads();
+    if (drop) sh.at[tid] = at = -1;
+  }
+  if (at >= 0) hand_over<V, NT>(sh, a.C, tid, at);
+  const RowSums r = block_sums<EXPS, NT>(sums, sz, want_sz, sc, red);
+  RowEnd<EXPS, V, NT> end(a, sc, r, sh, label, k, 0, a.C);
+  if (tid < 64) end.gradient(w, tail);
+  __syncthreads();
+  if (tid < 64) {
+    const float loss = end.loss();
+    if (tid == 0) a.row_loss[n] = loss;
+  }
+  if (!grad) return;
+  const RowGrad g = sh.g;
+  if constexpr (U > 0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (u * NT + tid < whole) {
+        store_gradient<T, EXPS, false>(grad + (u * NT + tid) * V, held[u], g, sc);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+  } else {
+    // from the end, where the caches still have the row
+    int v = (whole - 1 - tid) / NT * NT + tid;  // (whole <= tid: below tid)
+    if (whole <= tid) v = -1;
+    for (; v >= (G - 1) * NT; v -= G * NT) {
+      Vec16 x[G];
+#pragma unroll
+      for (int i = 0; i < G; ++i) x[i] = load16_any(row + (v - i * NT) * V);
+#pragma unroll
+      for (int i = 0; i < G; ++i) store_gradient<T, EXPS, true>(grad + (v - i * NT) * V, x[i], g, sc);
+    }
+    for (; v >= 0; v -= NT) store_gradient<T, EXPS, true>(grad + v * V, load16_any(row + v * V), g, sc);
+  }
+  if (tid < left) Elem<T>::store(grad + mine, gradient_of<EXPS>(z_left, g, sc));
+  // The entries' classes and the label's: written once more, each by the thread that wrote it first (whose stores to one address stay in
+  // order: no barrier, which would wait for every store of the row).
+  for (int j = sh.first[tid]; j >= 0; j = sh.next[j]) Elem<T>::store(grad + sh.at[j], sh.value[j]);
+}
+
+// Few rows: slices of a row by workgroups of their own, in two launches.  The first leaves the sums of every slice and, from the slice that
+// has it, every entry's class and logit (a gradient in the logits' place overwrites them in the second); the second joins the
+// sums, every slice for itself, and writes the slice's gradient.
+struct SliceArgs {
+  RowSums* sums;  // [N][slices]
+  int* at;        // [N][kTopMax]
+  float* z;       // [N][kTopMax + 1], the last the label's
+  float* loss;
+  int slices, width;  // (width: a multiple of 32 classes)
+};
+constexpr int kSliceThreads = 256;
+template <typename T, int EXPS>
+__global__ __launch_bounds__(kSliceThreads) void distill_slice_sums_kernel(const DistillArgs a, const SliceArgs p) {
+  constexpr int V = Elem<T>::VEC, NT = kSliceThreads, CHUNK = 16384, G = 2;
+  __shared__ uint32_t member[CHUNK / 32];
+  __shared__ RowSums red[NT / 64];
+  __shared__ int at_s[kTopMax];
+  const int tid = threadIdx.x, slice = blockIdx.x, n = blockIdx.y;
+  const int first = slice * p.width, classes = min(p.width, a.C - first);
+  const Scales sc = scales_of(a, EXPS);
+  const int k = a.alpha > 0.f ? a.k : 0;
+  const T* row = static_cast<const T*>(a.logits) + n * a.ld + first;
+  int at = tid < k ? a.t_indices[static_cast<int64_t>(n) * a.k + tid] : -1;
+  if (a.row_weight && a.row_weight[n] == 0.f) return;
+  int label = a.labels && a.alpha < 1.f ? a.labels[n] : -1;
+  if (label >= a.C) label = -1;
+  if (at >= a.C || at < 0) at = -1;
+  const bool mine = at >= first && at - first < classes;
+  const float z_at = mine ? Elem<T>::load(row + (at - first)) : -INFINITY;
+  if (tid == 0 && label >= first && label - first < classes) p.z[static_cast<int64_t>(n) * (kTopMax + 1) + kTopMax] = Elem<T>::load(row + (label - first));
+  if (tid < k) at_s[tid] = at;
+  const bool want_sz = label >= 0 && a.smoothing > 0.f;
+  Sums<EXPS> sums;
+  double sz = 0;
+  auto add = [&](const Vec16& x, int e) __attribute__((always_inline)) {
+    float z[V];
+    Elem<T>::unpack(x, z);
+    if (want_sz) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) sz += static_cast<double>(z[j]);
+    }
+    const uint32_t bits = member[e >> 5] >> (e & 31) & ((1u << V) - 1);
+    if (bits) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) z[j] = bits >> j & 1 ? -INFINITY : z[j];
+    }
+    sums.template add<V>(z, sc);
+  };
+  bool repeated = false;
+  for (int c0 = 0; c0 < classes; c0 += CHUNK) {
+    const int chunk = min(classes - c0, CHUNK), vecs = chunk / V, e_at = at - first - c0;
+    if (c0) __syncthreads();
+    for (int i = tid; i < (chunk + 31) / 32; i += NT) member[i] = 0;
+    __syncthreads();
+    if (mine && e_at >= 0 && e_at < chunk) repeated = atomicOr(&member[e_at >> 5], 1u << (e_at & 31)) >> (e_at & 31) & 1;
+    __syncthreads();
+    const T* from = row + c0;
+    int v = tid;
+    for (; v + (G - 1) * NT < vecs; v += G * NT) {
+      Vec16 x[G];
+#pragma unroll
+      for (int g = 0; g < G; ++g) x[g] = load16_any(from + (v + g * NT) * V);
+#pragma unroll
+      for (int g = 0; g < G; ++g) add(x[g], (v + g * NT) * V);
+    }
+    for (; v < vecs; v += NT) add(load16_any(from + v * V), v * V);
+    const int e = vecs * V + tid;
+    if (e < chunk) {
+      const float z = Elem<T>::load(from + e);
+      if (want_sz) sz += static_cast<double>(z);
+      if (!(member[e >> 5] >> (e & 31) & 1)) sums.template add<1>(&z, sc);
+    }
+  }
+  if (__syncthreads_or(repeated)) {  // of entries with the same class, all of them in this slice, the first stands
+    bool drop = false;
+    for (int h = 0; h < tid && mine; ++h) drop |= at_s[h] == at;
+    if (drop) at = -1;
+  }
+  if (mine || (tid < k && at < 0 && slice == 0)) {  // (an entry of no class: the first slice's)
+    p.at[static_cast<int64_t>(n) * kTopMax + tid] = at;
+    p.z[static_cast<int64_t>(n) * (kTopMax + 1) + tid] = z_at;
+  }
+  const RowSums r = block_sums<EXPS, NT>(sums, sz, want_sz, sc, red);
+  if (tid == 0) p.sums[static_cast<int64_t>(n) * p.slices + slice] = r;
+}
+template <typename T, int EXPS>
+__global__ __launch_bounds__(kSliceThreads) void distill_slice_end_kernel(const DistillArgs a, const SliceArgs p) {
+  constexpr int V = Elem<T>::VEC, NT = kSliceThreads, G = 2;
+  __shared__ RowShared sh;
+  __shared__ RowSums red[NT / 64];
+  const int tid = threadIdx.x, slice = blockIdx.x, n = blockIdx.y;
+  const int first = slice * p.width, classes = min(p.width, a.C - first), whole = classes / V, left = classes - whole * V;
+  const Scales sc = scales_of(a, EXPS);
+  const int k = a.alpha > 0.f ? a.k : 0;
+  const float w = a.row_weight ? a.row_weight[n] : 1.f / static_cast<float>(a.N);
+  const T* row = static_cast<const T*>(a.logits) + n * a.ld + first;
+  T* grad = a.grad ? static_cast<T*>(a.grad) + n * a.grad_ld + first : nullptr;
+  if (w != 0.f) {
+    const float tail = a.alpha > 0.f && a.t_tail ? a.t_tail[n] : -INFINITY;
+    int label = a.labels && a.alpha < 1.f ? a.labels[n] : -1;
+    if (label >= a.C) label = -1;
+    int at = -1;
+    if (tid < k) {
+      at = p.at[static_cast<int64_t>(n) * kTopMax + tid];
+      sh.at[tid] = at;
+      sh.z[tid] = p.z[static_cast<int64_t>(n) * (kTopMax + 1) + tid];
+      sh.t[tid] = a.t_values[static_cast<int64_t>(n) * a.k + tid];
+    }
+    if (tid == 0 && label >= 0) sh.z[kTopMax] = p.z[static_cast<int64_t>(n) * (kTopMax + 1) + kTopMax];
+    sh.first[tid] = -1;
+    Sums<EXPS> sums;  // a slice's a thread
+    double sz = 0;
+    if (tid < p.slices) {
+      const RowSums part = p.sums[static_cast<int64_t>(n) * p.slices + tid];
+      sums.ref = part.ref; sums.st = part.st; sums.s1 = part.s1;
+      sz = part.sz;
+    }
+    __syncthreads();
+    if (at >= 0) hand_over<V, NT>(sh, classes, tid, at - first);
+    const RowSums r = block_sums<EXPS, NT>(sums, sz, label >= 0 && a.smoothing > 0.f, sc, red);
+    RowEnd<EXPS, V, NT> end(a, sc, r, sh, label, k, first, classes);
+    if (tid < 64) end.gradient(w, tail);
+    __syncthreads();
+    if (slice == 0 && tid < 64) {
+      const float loss = end.loss();
+      if (tid == 0) a.row_loss[n] = loss;
+      if (tid == 0 && a.N == 1) *p.loss = w * loss;
+    }
     if (grad) {
       const RowGrad g = sh.g;
-      float d[V];
-      if constexpr (U > 0) {
+      int v = tid;
+      for (; v + (G - 1) * NT < whole; v += G * NT) {
+        Vec16 x[G];
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-          if (u * NT + tid < vecs) {
-            gradient_of<T, EXPS>(held[u], g, sc, d);
-            store_vector(grad, a.C, u * NT + tid, d);
-            __builtin_amdgcn_sched_barrier(0);
-          }
-      } else {
-        for (int v = tid; v < vecs; v += NT) {
-          gradient_of<T, EXPS>(row.load(v), g, sc, d);
-          store_vector(grad, a.C, v, d);
-        }
+        for (int i = 0; i < G; ++i) x[i] = load16_any(row + (v + i * NT) * V);
+#pragma unroll
+        for (int i = 0; i < G; ++i) store_gradient<T, EXPS, false>(grad + (v + i * NT) * V, x[i], g, sc);
       }
-      __syncthreads();
-      // the entries' classes and the label's: written once more (behind the barrier: the same memory)
-      for (int j = tid; j < k; j += NT)
-        if (sh.at[j] >= 0) Elem<T>::store(grad + sh.at[j], sh.value[j]);
-      if (tid == 0 && sh.at[kTopMax] >= 0) Elem<T>::store(grad + sh.at[kTopMax], sh.value[kTopMax]);
+      for (; v < whole; v += NT) store_gradient<T, EXPS, false>(grad + v * V, load16_any(row + v * V), g, sc);
+      if (tid < left) Elem<T>::store(grad + whole * V + tid, gradient_of<EXPS>(Elem<T>::load(row + whole * V + tid), g, sc));
+      for (int j = sh.first[tid]; j >= 0; j = sh.next[j]) Elem<T>::store(grad + (sh.at[j] - first), sh.value[j]);
     }
+  } else {
+    for (int i = tid; grad && i < classes; i += NT) Elem<T>::store(grad + i, 0.f);
+    if (slice == 0 && tid == 0) a.row_loss[n] = 0.f;
+    if (slice == 0 && tid == 0 && a.N == 1) *p.loss = 0.f;
   }
 }
 
-// loss = sum_n w_n row_loss_n, in double, in a fixed order.
-__global__ __launch_bounds__(256) void distill_loss_kernel(const float* __restrict__ row_loss, const float* __restrict__ row_weight, int N,
-                                                           float* __restrict__ loss) {
-  __shared__ double red[256];
+// loss = sum_n w_n row_loss_n, in double, in a fixed order.  One workgroup: a few kilobytes, eight of each thread's loads at a time
+// (one at a time 32768 rows took 77 us).
+__global__ __launch_bounds__(1024) void distill_loss_kernel(const float* __restrict__ row_loss, const float* __restrict__ row_weight, int N,
+                                                            float* __restrict__ loss) {
+  __shared__ double red[16];
+  constexpr int U = 8;
   double s = 0;
-  for (int n = threadIdx.x; n < N; n += 256) {
-    if (row_weight == nullptr) s += row_loss[n];
-    else if (row_weight[n] != 0.f) s += static_cast<double>(row_weight[n]) * row_loss[n];
+  for (int64_t n0 = threadIdx.x; n0 < N; n0 += U * 1024) {
+    float l[U], w[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t n = n0 + u * 1024;
+      l[u] = n < N ? row_loss[n] : 0.f;
+      w[u] = n < N && row_weight ? row_weight[n] : 1.f;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) s += w[u] != 0.f ? static_cast<double>(w[u]) * l[u] : 0.0;
   }
-  red[threadIdx.x] = s;
+  s = wave_sum(s);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
   __syncthreads();
-  for (int step = 128; step > 0; step >>= 1) {
-    if (threadIdx.x < step) red[threadIdx.x] += red[threadIdx.x + step];
-    __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < 16; ++i) s += red[i];
+    loss[0] = static_cast<float>(row_weight ? s : s / N);
   }
-  if (threadIdx.x == 0) loss[0] = static_cast<float>(row_weight ? red[0] : red[0] / N);
 }
 
 static int check_rows(const char* who, int N, int C, int dtype, const void* logits, int64_t ld) {
@@ -566,22 +763,98 @@ template <typename T, int EXPS>
 static void distill_rows(const DistillArgs& a, dim3 grid, hipStream_t s) {
   constexpr int V = Elem<T>::VEC;
   const int64_t vecs = ceil_div(a.C, V);
-  if (vecs <= 256) RN50_LAUNCH("distill", (distill_rows_kernel<T, EXPS, 256, 1>), grid, dim3(256), 0, s, a);
-  else if (vecs <= 256 * 4) RN50_LAUNCH("distill", (distill_rows_kernel<T, EXPS, 256, 4>), grid, dim3(256), 0, s, a);
-  else if (vecs <= 512 * 8) RN50_LAUNCH("distill", (distill_rows_kernel<T, EXPS, 512, 8>), grid, dim3(512), 0, s, a);
-  else if (vecs <= 1024 * 8) RN50_LAUNCH("distill", (distill_rows_kernel<T, EXPS, 1024, 8>), grid, dim3(1024), 0, s, a);
-  else if (vecs <= 1024 * 16) RN50_LAUNCH("distill", (distill_rows_kernel<T, EXPS, 1024, 16>), grid, dim3(1024), 0, s, a);
-  else RN50_LAUNCH("distill", (distill_rows_kernel<T, EXPS, 256, 0>), grid, dim3(256), 0, s, a);
+#define ROWS(NT, U) RN50_LAUNCH("distill", (distill_rows_kernel<T, EXPS, NT, U>), grid, dim3(NT), 0, s, a)
+#ifdef RN50_TUNING  // tuning builds only: RN50_DISTILL=threads,vectors held by a thread
+  if constexpr (EXPS == 2) {
+    int nt, u;
+    if (const char* e = getenv("RN50_DISTILL"); e && sscanf(e, "%d,%d", &nt, &u) == 2) {
+#define FORCED(NT, U) if (nt == NT && u == U) { ROWS(NT, U); return; }
+      FORCED(64, 4) FORCED(64, 8) FORCED(128, 2) FORCED(128, 4) FORCED(256, 0) FORCED(512, 0) FORCED(1024, 0) FORCED(256, 1) FORCED(256, 2) FORCED(256, 4) FORCED(256, 8) FORCED(512, 4) FORCED(512, 8) FORCED(512, 16) FORCED(1024, 8)
+#undef FORCED
+    }
+  }
+#endif
+  // Small workgroups for short rows: a row is mostly its own end, which few waves share and barriers of few waves part (32768 rows of 1000
+  // bf16 106 us with 256 threads, 71 with 128; of 4096 164 -> 127; of 8192 134 streamed, 127 held).  From 1024 vectors on the row is
+  // streamed: held in registers it leaves too few workgroups to cover one another (4096 x 50001 bf16 228 us, held by 512 threads 309).
+  // 256 threads against 512: 8192 x 16384 bf16 120 us, 136; 4096 x 50001 239, 228; 2048 x 131072 284, 246; of 512 KB rows and more the rows in
+  // flight pass the last-level cache: 2048 x 131072 float 532 us with 512, 476 with 1024.
+  const bool few = a.k <= 128;  // (an entry a thread)
+  if (vecs <= 256) {
+    if (few) ROWS(128, 2);
+    else ROWS(256, 1);
+  } else if (vecs <= 512) {
+    if (few) ROWS(128, 4);
+    else ROWS(256, 2);
+  } else if (vecs <= 1024) {
+    ROWS(256, 4);
+  } else if (vecs <= 4096) {
+    ROWS(256, 0);
+  } else if (vecs <= 24576) {
+    ROWS(512, 0);
+  } else {
+    ROWS(1024, 0);
+  }
+#undef ROWS
+}
+template <typename T, int EXPS>
+static void distill_slices(const DistillArgs& a, const SliceArgs& p, hipStream_t s) {
+  RN50_LAUNCH("distill", (distill_slice_sums_kernel<T, EXPS>), dim3(p.slices, a.N), dim3(kSliceThreads), 0, s, a, p);
+  RN50_LAUNCH("distill", (distill_slice_end_kernel<T, EXPS>), dim3(a.grad ? p.slices : 1, a.N), dim3(kSliceThreads), 0, s, a, p);
+}
+template <typename T, int EXPS>
+static void distill_exps(const DistillArgs& a, const SliceArgs& p, hipStream_t s) {
+  if (p.slices > 1) distill_slices<T, EXPS>(a, p, s);
+  else distill_rows<T, EXPS>(a, row_grid(a.N), s);
+  if (p.slices == 1 || a.N > 1) {  // (the slices of a single row leave its loss)
+    RN50_LAUNCH("distill_loss", distill_loss_kernel, dim3(1), dim3(1024), 0, s, a.row_loss, a.row_weight, a.N, p.loss);
+  }
 }
 template <typename T>
-static void distill_run(const DistillArgs& a, dim3 grid, hipStream_t s) {
+static void distill_run(const DistillArgs& a, const SliceArgs& p, hipStream_t s) {
   const bool both = a.alpha > 0.f && a.alpha < 1.f && a.labels;
-  if (!both || a.temperature == 1.f) distill_rows<T, 1>(a, grid, s);
-  else if (a.temperature == 2.f) distill_rows<T, 2>(a, grid, s);
-  else if (a.temperature == 4.f) distill_rows<T, 4>(a, grid, s);
-  else distill_rows<T, 0>(a, grid, s);
+  if (!both || a.temperature == 1.f) distill_exps<T, 1>(a, p, s);
+  else if (a.temperature == 2.f) distill_exps<T, 2>(a, p, s);
+  else if (a.temperature == 4.f) distill_exps<T, 4>(a, p, s);
+  else distill_exps<T, 0>(a, p, s);
 }
-constexpr int kRowGrid = 1 << 20;  // workgroups of a launch over rows, at most: they take the rows in turn
+
+// Slices of a row (1: a workgroup does the row) and their width.  Loss and gradient, 64 entries, a workgroup a row -> slices: 1 x 131072 bf16
+// 27.1 -> 9.8 us, 7 x 131072 27.6 -> 11.7, 64 x 32768 15.3 -> 13.4, 128 x 131072 29.2 -> 24.9; 200 x 131072 32.2 -> 35.7, 7 x 20000 float 11.5 -> 12.1,
+// 16 x 8192 float 10.2 -> 11.9: up to 128 rows of 4096 vectors and more.
+static int distill_slicing(int N, int C, int dtype, int* width) {
+  const int V = dtype == RN50_BF16 ? 8 : 4;
+  *width = C;
+  int least = 4096 * V, target = 1024, most_rows = 128;
+#ifdef RN50_TUNING  // tuning builds only: RN50_DISTILL_SLICES=least vectors of a row,workgroups,rows
+  if (const char* e = getenv("RN50_DISTILL_SLICES")) {
+    sscanf(e, "%d,%d,%d", &least, &target, &most_rows);
+    least *= V;
+  }
+#endif
+  if (N > most_rows || C < least) return 1;
+  const int64_t want = std::min<int64_t>({ceil_div(target, N), ceil_div(C, kSliceThreads * V), kSliceThreads});
+  if (want < 2) return 1;
+  *width = static_cast<int>(align_up(static_cast<size_t>(ceil_div(C, want)), 32));
+  return static_cast<int>(ceil_div(C, *width));
+}
+static SliceArgs slice_args(int N, int C, int dtype, void* workspace, size_t* bytes) {
+  SliceArgs p{};
+  p.slices = distill_slicing(N, C, dtype, &p.width);
+  size_t at = 0;
+  auto part = [&](size_t size) {
+    unsigned char* b = static_cast<unsigned char*>(workspace) + at;
+    at += align_up(size, 256);
+    return workspace ? b : nullptr;
+  };
+  if (p.slices > 1) {
+    p.sums = reinterpret_cast<RowSums*>(part(sizeof(RowSums) * N * p.slices));
+    p.at = reinterpret_cast<int*>(part(sizeof(int) * N * kTopMax));
+    p.z = reinterpret_cast<float*>(part(sizeof(float) * N * (kTopMax + 1)));
+  }
+  *bytes = at;
+  return p;
+}
 
 }  // namespace rn50
 
@@ -604,7 +877,7 @@ extern "C" int topk_rows(int N, int C, int k, int dtype, const void* logits, int
   const size_t need = topk_rows_workspace_bytes(N, C, k);
   RN50_REQUIRE(workspace_bytes >= need && (need == 0 || workspace), RN50_ERR_WORKSPACE, "topk_rows: workspace %zu < %zu bytes", workspace_bytes, need);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const dim3 grid(std::min(N, kRowGrid));
+  const dim3 grid = row_grid(N);
   if (dtype == RN50_BF16)
     RN50_LAUNCH("topk_rows", topk_rows_kernel<uint16_t>, grid, dim3(256), 0, s, static_cast<const uint16_t*>(logits), ld, N, C, k, temperature, values, indices, tail_lse);
   else
@@ -613,8 +886,9 @@ extern "C" int topk_rows(int N, int C, int k, int dtype, const void* logits, int
 }
 
 extern "C" size_t distill_workspace_bytes(const rn50_distill_desc* d) {
-  (void)d;
-  return 0;
+  size_t bytes = 0;
+  if (d && d->N > 0 && d->C > 0) slice_args(d->N, d->C, d->dtype, nullptr, &bytes);
+  return bytes;
 }
 
 extern "C" int distill_fwd_bwd(const rn50_distill_desc* d, const void* logits, const float* t_values, const int32_t* t_indices, const float* t_tail,
@@ -642,9 +916,10 @@ extern "C" int distill_fwd_bwd(const rn50_distill_desc* d, const void* logits, c
   hipStream_t s = static_cast<hipStream_t>(stream);
   DistillArgs a{logits, dlogits, t_values, t_indices, t_tail, row_weight, labels, row_loss_out, d->ld, d->grad_ld, d->N, d->C, d->k,
                 d->temperature, d->alpha, d->label_smoothing, d->grad_scale};
-  const dim3 grid(std::min(d->N, kRowGrid));
-  if (d->dtype == RN50_BF16) distill_run<uint16_t>(a, grid, s);
-  else distill_run<float>(a, grid, s);
-  RN50_LAUNCH("distill_loss", distill_loss_kernel, dim3(1), dim3(256), 0, s, row_loss_out, row_weight, d->N, loss_out);
+  size_t bytes;
+  SliceArgs p = slice_args(d->N, d->C, d->dtype, workspace, &bytes);
+  p.loss = loss_out;
+  if (d->dtype == RN50_BF16) distill_run<uint16_t>(a, p, s);
+  else distill_run<float>(a, p, s);
   return launch_status(who);
 }

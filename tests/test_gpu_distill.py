@@ -397,6 +397,23 @@ def test_rows_past_32_bits(rn, N, ld, used):
     assert torch.equal(x, rn.fc_i8_fwd(a, *w, dtype=BF16))
 
 
+def test_more_rows_than_one_line_of_the_grid(rn):
+    N, C, k = 70001, 9, 3
+    z = torch.randn(N, C, device="cuda")
+    v, i, tl = rn.topk_rows(torch.randn(N, C, device="cuda"), k)
+    w = torch.rand(N, device="cuda") / N
+    loss, rows, grad = rn.distill_fwd_bwd(z, v, i, tl, row_weight=w)
+    q, s = rn.quant_rows_i8(z)
+    values, indices, tail = rn.topk_rows(z, k)
+    total = 0.0
+    for a, b in ((0, 30000), (30000, 65536), (65536, 65537), (65537, N)):
+        part = rn.distill_fwd_bwd(z[a:b], v[a:b], i[a:b], tl[a:b], row_weight=w[a:b])
+        assert torch.equal(part[1], rows[a:b]) and torch.equal(part[2], grad[a:b])
+        total += float(part[0])
+        assert all(torch.equal(x, y[a:b]) for x, y in zip((*rn.quant_rows_i8(z[a:b].contiguous()), *rn.topk_rows(z[a:b], k)), (q, s, values, indices, tail)))
+    assert abs(total - float(loss)) < 1e-5 * total
+
+
 def test_one_long_row(rn):
     """More classes than 2^25, one row: the forms that share a row among workgroups."""
     C = 2 ** 25 + 37
