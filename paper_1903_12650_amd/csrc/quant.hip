@@ -1,7 +1,11 @@
 // Products in 8-bit integers: rows quantized with one scale each, and y = (sum_k q w) * q_scale * w_scale + bias on the
 // integer matrix cores (v_mfma_i32_32x32x32_i8).
-#include "common.h"
+#include <stdlib.h>
+
 #include <algorithm>
+
+#include "common.h"
+#include "conv_internal.h"
 
 namespace rn50 {
 
@@ -25,53 +29,212 @@ __device__ __forceinline__ uint32_t i8_of(float x, float inv) {
   return __float_as_uint(t + 12582912.f) & 255u;
 }
 
-// One workgroup per row, which is read twice.
+// Largest magnitude of a 16-byte vector, as bits: magnitudes order like unsigned integers, an infinity and NaN above every number.
 template <typename T>
+__device__ __forceinline__ uint32_t top_of(uint32_t top, const Vec16& x) {
+  if constexpr (sizeof(T) == 4) {
+    return max(max(max(top, x.u.x & 0x7fffffffu), max(x.u.y & 0x7fffffffu, x.u.z & 0x7fffffffu)), x.u.w & 0x7fffffffu);
+  } else {  // two halves side by side, each its own maximum
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    auto half = [](uint32_t v) { return __builtin_bit_cast(u16x2, v & 0x7fff7fffu); };
+    const u16x2 m = __builtin_elementwise_max(__builtin_elementwise_max(half(x.u.x), half(x.u.y)), __builtin_elementwise_max(half(x.u.z), half(x.u.w)));
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, top), m));
+  }
+}
+template <typename T>
+__device__ __forceinline__ uint32_t top_float_bits(uint32_t top) {  // as a float's
+  return sizeof(T) == 4 ? top : max(top & 0xffffu, top >> 16) << 16;
+}
+// Four quantized numbers, the first in the low byte (0 where the row is not finite: inv is 0 then, and the bytes are cleared).
+__device__ __forceinline__ uint32_t i8_four(const float* x, float inv) {
+  const uint32_t a = i8_of(x[0], inv), b = i8_of(x[1], inv), c = i8_of(x[2], inv), d = i8_of(x[3], inv);
+  return (a | b << 8) | (c << 16 | d << 24);
+}
+template <typename T>
+__device__ __forceinline__ void store_quantized(int8_t* to, const Vec16& x, float inv) {  // (to: aligned to the vector's bytes)
+  float f[Elem<T>::VEC];
+  Elem<T>::unpack(x, f);
+  if constexpr (sizeof(T) == 4) *reinterpret_cast<uint32_t*>(to) = inv != 0.f ? i8_four(f, inv) : 0u;
+  else *reinterpret_cast<uint2*>(to) = inv != 0.f ? make_uint2(i8_four(f, inv), i8_four(f + 4, inv)) : make_uint2(0u, 0u);
+}
+
+// NT threads per row (a wave, or the workgroup), the row U vectors a thread at most: it is read once.  U = 0: it is read twice.
+template <typename T, int NT, int U>
 __global__ __launch_bounds__(256) void quant_rows_kernel(const T* __restrict__ x, int64_t ldx, int M, int K, int Kp, int8_t* __restrict__ q,
                                                          float* __restrict__ scale) {
+  constexpr int V = Elem<T>::VEC;
+  static_assert(NT == 64 || NT == 256, "a wave or a workgroup");
   __shared__ uint32_t red[4];
-  for (int m = blockIdx.x; m < M; m += gridDim.x) {
-    const T* row = x + m * ldx;
-    uint32_t top = 0;
-    for (int k = threadIdx.x; k < K; k += 256) top = max(top, __float_as_uint(Elem<T>::load(row + k)) & 0x7fffffffu);
+  const int64_t m = static_cast<int64_t>(blockIdx.x) * (256 / NT) + threadIdx.x / NT;
+  if (m >= M) return;  // (a whole wave, or all of them)
+  const int t = threadIdx.x % NT, whole = K / V, left = K - whole * V;
+  const T* row = x + m * ldx;
+  int8_t* out = q + m * Kp;
+  uint32_t top = 0;
+  Vec16 held[U > 0 ? U : 1];
+  const float z_left = t < left ? Elem<T>::load(row + whole * V + t) : 0.f;
+  if constexpr (U > 0) {
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), off, 64)));
-    __syncthreads();
+    for (int u = 0; u < U; ++u) {
+      held[u].u = make_uint4(0, 0, 0, 0);
+      if (u * NT + t < whole) held[u] = load16_any(row + (u * NT + t) * V);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) top = top_of<T>(top, held[u]);
+  } else {
+#pragma unroll 4
+    for (int v = t; v < whole; v += NT) top = top_of<T>(top, load16_any(row + v * V));
+  }
+  top = max(top_float_bits<T>(top), __float_as_uint(z_left) & 0x7fffffffu);
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), off, 64)));
+  if constexpr (NT == 256) {
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = top;
     __syncthreads();
     top = max(max(red[0], red[1]), max(red[2], red[3]));
-    float inv;
-    const float s = i8_scale(top, &inv);
-    const bool finite = top < 0x7f800000u;
-    int8_t* out = q + static_cast<int64_t>(m) * Kp;
-    for (int k = threadIdx.x; k < Kp; k += 256)
-      out[k] = k < K && finite ? static_cast<int8_t>(i8_of(Elem<T>::load(row + k), inv)) : static_cast<int8_t>(0);
-    if (threadIdx.x == 0) scale[m] = s;
   }
+  float inv;
+  const float s = i8_scale(top, &inv);
+  if constexpr (U > 0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (u * NT + t < whole) store_quantized<T>(out + (u * NT + t) * V, held[u], inv);
+  } else {
+#pragma unroll 4
+    for (int v = t; v < whole; v += NT) store_quantized<T>(out + v * V, load16_any(row + v * V), inv);
+  }
+  // the numbers behind the last whole vector, and the zeros behind them
+  const int rest = Kp - whole * V;
+  for (int i = t; i < rest; i += NT) out[whole * V + i] = static_cast<int8_t>(i < left && inv != 0.f ? i8_of(z_left, inv) : 0u);
+  if (t == 0) scale[m] = s;
 }
 
-// 64x64 outputs per workgroup, 32x32 per wave, operands from memory.  Lane l supplies row l % 32, bytes 16 * (l / 32)..+15 of a k step
-// of 32; it receives column l % 32 (of the second operand), rows (v / 4) * 8 + (l / 32) * 4 + v % 4.
-template <typename T>
-__global__ __launch_bounds__(256) void matmul_i8_kernel(const int8_t* __restrict__ q, const float* __restrict__ qs, const int8_t* __restrict__ w,
-                                                        const float* __restrict__ ws, const float* __restrict__ bias, T* __restrict__ y,
-                                                        int64_t ldy, int M, int N, int Kp) {
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int m0 = blockIdx.y * 64 + (wave & 1) * 32, n0 = blockIdx.x * 64 + (wave >> 1) * 32;
-  const int8_t* pa = q + static_cast<int64_t>(min(m0 + (lane & 31), M - 1)) * Kp + 16 * (lane >> 5);
-  const int8_t* pb = w + static_cast<int64_t>(min(n0 + (lane & 31), N - 1)) * Kp + 16 * (lane >> 5);
-  i32x16 acc;
+// ------------------------------------------------------------------- product
+struct ProductArgs {
+  const int8_t *q, *w;
+  const float *qs, *ws, *bias;
+  void* y;
+  int64_t ldy;
+  int M, N, Kp, tiles_m, tiles_n;
+};
+
+// Tile BM x BN, WM x WN waves of 32x32 blocks (v_mfma_i32_32x32x32_i8).  A chunk is 128 bytes of every row of both operands, brought
+// straight into LDS (16 bytes a lane) into one of two buffers while the other is multiplied: one barrier a chunk.  Piece p (16 bytes) of
+// row r lies in slot p ^ ((r >> 1) & 7), which spreads the fragment reads (32 rows of one piece) over all banks.  Rows past the last and
+// the second half of a last chunk of 64 bytes are zeros.  The weights are the first operand, so that a lane has 4 consecutive columns of one row.
+template <typename T, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) void matmul_i8_kernel(const ProductArgs a) {
+  constexpr int NT = 64 * WM * WN, RPL = NT / 8, RA = BM / RPL, RB = BN / RPL, TM = BM / WM / 32, TN = BN / WN / 32;
+  constexpr int STAGE = (BM + BN) * 128;
+  static_assert(RA * RPL == BM && RB * RPL == BN && TM >= 1 && TN >= 1, "whole passes, whole blocks");
+  extern __shared__ __align__(16) unsigned char smem[];
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const int wm = wave % WM, wn = wave / WM;
+  // Neighbouring tiles run on one XCD: they go down GROUP row tiles before the next column tile, so that the tiles of an XCD's 32 compute
+  // units share rows of both operands in its L2.
+  constexpr int GROUP = 4;
+  const int id = xcd_remap(blockIdx.x, gridDim.x);
+  const int per = GROUP * a.tiles_n, g = id / per, r = id - g * per, high = min(GROUP, a.tiles_m - g * GROUP);
+  const int m0 = (g * GROUP + r % high) * BM, n0 = r / high * BN;
+  const int rows = min(BM, a.M - m0), cols = min(BN, a.N - n0);
+  const rsrc_words rsA = make_rsrc_words(a.q + static_cast<int64_t>(m0) * a.Kp, static_cast<uint32_t>(rows) * a.Kp);
+  const rsrc_words rsB = make_rsrc_words(a.w + static_cast<int64_t>(n0) * a.Kp, static_cast<uint32_t>(cols) * a.Kp);
+  const int slot = tid & 7, lrow = tid >> 3, piece = slot ^ ((lrow >> 1) & 7);
+  uint32_t at_a[RA], at_b[RB];
 #pragma unroll
-  for (int v = 0; v < 16; ++v) acc[v] = 0;
-  for (int k = 0; k < Kp; k += 32)
-    acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(*reinterpret_cast<const i32x4*>(pa + k), *reinterpret_cast<const i32x4*>(pb + k), acc, 0, 0, 0);
-  const int n = n0 + (lane & 31);
-  if (n >= N) return;
-  const float t = ws[n], b = bias ? bias[n] : 0.f;
+  for (int i = 0; i < RA; ++i) at_a[i] = lrow + RPL * i < rows ? static_cast<uint32_t>(lrow + RPL * i) * a.Kp + piece * 16 : kOob;
 #pragma unroll
-  for (int v = 0; v < 16; ++v) {
-    const int m = m0 + (v >> 2) * 8 + (lane >> 5) * 4 + (v & 3);
-    if (m < M) Elem<T>::store(y + m * ldy + n, fmaf(static_cast<float>(acc[v]) * qs[m], t, b));
+  for (int i = 0; i < RB; ++i) at_b[i] = lrow + RPL * i < cols ? static_cast<uint32_t>(lrow + RPL * i) * a.Kp + piece * 16 : kOob;
+  typedef __attribute__((address_space(3))) unsigned char* lds_byte_ptr;
+  const uint32_t dst = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_byte_ptr)smem)) + static_cast<uint32_t>(wave) * 1024u);
+  const int chunks = (a.Kp + 127) >> 7;
+  auto load = [&](int c) __attribute__((always_inline)) {
+    const uint32_t so = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(c) * 128u), to = dst + static_cast<uint32_t>(c & 1) * STAGE;
+    const bool in = c * 128 + piece * 16 < a.Kp;
+#pragma unroll
+    for (int i = 0; i < RA; ++i) buffer_load16_to_lds(rsA, to + i * (RPL * 128), in ? at_a[i] : kOob, so);
+#pragma unroll
+    for (int i = 0; i < RB; ++i) buffer_load16_to_lds(rsB, to + BM * 128 + i * (RPL * 128), in ? at_b[i] : kOob, so);
+  };
+  i32x16 acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[i][j][v] = 0;
+  int frag[4];
+#pragma unroll
+  for (int kk = 0; kk < 4; ++kk) frag[kk] = (lane & 31) * 128 + (((2 * kk + (lane >> 5)) ^ ((lane >> 1) & 7)) << 4);
+  load(0);
+  for (int c = 0; c < chunks; ++c) {
+    wait_loads_then_barrier<0>();  // this chunk is there, and the other buffer has been read
+    if (c + 1 < chunks) load(c + 1);
+    const unsigned char* ta = smem + (c & 1) * STAGE + wm * (BM / WM) * 128;
+    const unsigned char* tb = smem + (c & 1) * STAGE + BM * 128 + wn * (BN / WN) * 128;
+    i32x4 fa[2][TM], fb[2][TN];
+    auto read = [&](int kk) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i) fa[kk & 1][i] = *reinterpret_cast<const i32x4*>(ta + i * 32 * 128 + frag[kk]);
+#pragma unroll
+      for (int j = 0; j < TN; ++j) fb[kk & 1][j] = *reinterpret_cast<const i32x4*>(tb + j * 32 * 128 + frag[kk]);
+    };
+    read(0);
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) {
+      if (kk < 3) read(kk + 1);
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fb[kk & 1][j], fa[kk & 1][i], acc[i][j], 0, 0, 0);
+    }
+  }
+  // Output: a wave's 32 rows at a time through LDS (its own part of it), whole rows of the wave's columns from there.
+  constexpr int WC = BN / WN, PITCH = WC + 4;  // floats (rows 16 bytes further along the banks)
+  static_assert(WM * WN * 32 * PITCH * 4 <= 2 * STAGE, "the output stage fits the ring");
+  lds_reads_then_barrier();
+  float* mine = reinterpret_cast<float*>(smem) + wave * 32 * PITCH;
+  constexpr int V = Elem<T>::VEC, LPR = WC / V, RPP = 64 / LPR;  // lanes a row, rows a pass
+  const int col = n0 + wn * WC + lane % LPR * V;
+  float t[V], b[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    t[j] = col + j < a.N ? a.ws[col + j] : 0.f;
+    b[j] = a.bias && col + j < a.N ? a.bias[col + j] : 0.f;
+  }
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        float4 f = make_float4(acc[i][j][4 * v], acc[i][j][4 * v + 1], acc[i][j][4 * v + 2], acc[i][j][4 * v + 3]);
+        *reinterpret_cast<float4*>(mine + (lane & 31) * PITCH + j * 32 + v * 8 + (lane >> 5) * 4) = f;
+      }
+    __builtin_amdgcn_wave_barrier();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int p = 0; p < 32 / RPP; ++p) {
+      const int row = p * RPP + lane / LPR, m = m0 + wm * (BM / WM) + i * 32 + row;
+      if (m < a.M && col < a.N) {
+        const float s = a.qs[m];
+        float f[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) f[j] = fmaf(mine[row * PITCH + lane % LPR * V + j] * s, t[j], b[j]);
+        T* to = static_cast<T*>(a.y) + m * a.ldy + col;
+        if (col + V <= a.N) {
+          Vec16 o;
+          Elem<T>::pack(f, o);
+          store16_any(to, o);
+        } else {
+#pragma unroll
+          for (int j = 0; j < V; ++j)
+            if (col + j < a.N) Elem<T>::store(to + j, f[j]);
+        }
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   }
 }
 
@@ -89,7 +252,7 @@ static int check_product(const char* who, int M, int N, int K, const void* w, co
   RN50_REQUIRE(y_dtype == RN50_F32 || y_dtype == RN50_BF16, RN50_ERR_INVALID, "%s: dtype %d", who, y_dtype);
   RN50_REQUIRE(M > 0 && N > 0 && K > 0, RN50_ERR_INVALID, "%s: non-positive size", who);
   RN50_REQUIRE(K <= kI8MaxK, RN50_ERR_UNSUPPORTED, "%s: K=%d beyond %d, what a 32-bit sum holds", who, K, kI8MaxK);
-  RN50_REQUIRE(ceil_div(M, 64) <= 65535 && N <= (1 << 28), RN50_ERR_UNSUPPORTED, "%s: M=%d or N=%d beyond the launch grid", who, M, N);
+  RN50_REQUIRE(ceil_div(M, 64) * ceil_div(N, 64) <= (1 << 22), RN50_ERR_UNSUPPORTED, "%s: M=%d by N=%d beyond the launch grid", who, M, N);
   RN50_REQUIRE(w && w_scale && y, RN50_ERR_INVALID, "%s: null pointer", who);
   RN50_REQUIRE(ldy >= N, RN50_ERR_INVALID, "%s: rows of %d elements %lld apart", who, N, static_cast<long long>(ldy));
   RN50_REQUIRE(aligned16(w), RN50_ERR_ALIGN, "%s: 8-bit rows not 16-byte aligned", who);
@@ -98,22 +261,55 @@ static int check_product(const char* who, int M, int N, int K, const void* w, co
   return RN50_OK;
 }
 
-static void quant_run(int M, int K, int dtype, const void* x, int64_t ldx, int8_t* q, float* scale, hipStream_t s) {
+template <typename T>
+static void quant_typed(int M, int K, const T* x, int64_t ldx, int8_t* q, float* scale, hipStream_t s) {
   const int Kp = static_cast<int>(quant_i8_row_bytes(K));
-  const dim3 grid(std::min(M, 1 << 20));
-  if (dtype == RN50_BF16)
-    RN50_LAUNCH("quant_rows_i8", quant_rows_kernel<uint16_t>, grid, dim3(256), 0, s, static_cast<const uint16_t*>(x), ldx, M, K, Kp, q, scale);
-  else
-    RN50_LAUNCH("quant_rows_i8", quant_rows_kernel<float>, grid, dim3(256), 0, s, static_cast<const float*>(x), ldx, M, K, Kp, q, scale);
+  const int64_t vecs = K / Elem<T>::VEC;
+#define QUANT(NT, U) RN50_LAUNCH("quant_rows_i8", (quant_rows_kernel<T, NT, U>), dim3(static_cast<unsigned>(ceil_div(M, 256 / NT))), dim3(256), 0, s, x, ldx, M, K, Kp, q, scale)
+  if (vecs <= 64) QUANT(64, 1);
+  else if (vecs <= 64 * 2) QUANT(64, 2);
+  else if (vecs <= 64 * 4) QUANT(64, 4);
+  else if (vecs <= 64 * 8) QUANT(64, 8);
+  else if (vecs <= 256 * 4) QUANT(256, 4);
+  else if (vecs <= 256 * 8) QUANT(256, 8);
+  else QUANT(256, 0);
+#undef QUANT
+}
+static void quant_run(int M, int K, int dtype, const void* x, int64_t ldx, int8_t* q, float* scale, hipStream_t s) {
+  if (dtype == RN50_BF16) quant_typed(M, K, static_cast<const uint16_t*>(x), ldx, q, scale, s);
+  else quant_typed(M, K, static_cast<const float*>(x), ldx, q, scale, s);
+}
+template <typename T, int BM, int BN, int WM, int WN>
+static void product_tile(ProductArgs a, hipStream_t s) {
+  constexpr int lds = 2 * (BM + BN) * 128;
+  a.tiles_m = static_cast<int>(ceil_div(a.M, BM));
+  a.tiles_n = static_cast<int>(ceil_div(a.N, BN));
+  const auto kernel = matmul_i8_kernel<T, BM, BN, WM, WN>;
+  allow_big_lds(kernel, lds);
+  RN50_LAUNCH("matmul_i8", kernel, dim3(static_cast<unsigned>(a.tiles_m) * a.tiles_n), dim3(64 * WM * WN), lds, s, a);
+}
+template <typename T>
+static void product_typed(const ProductArgs& a, hipStream_t s) {
+#ifdef RN50_TUNING  // tuning builds only: RN50_I8_TILE=rows
+  if (const char* e = getenv("RN50_I8_TILE")) {
+    switch (atoi(e)) {
+      case 256: return product_tile<T, 256, 256, 2, 4>(a, s);
+      case 192: return product_tile<T, 256, 128, 4, 2>(a, s);
+      case 128: return product_tile<T, 128, 128, 2, 2>(a, s);
+      case 64: return product_tile<T, 64, 64, 2, 2>(a, s);
+    }
+  }
+#endif
+  auto tiles = [&](int bm, int bn) { return ceil_div(a.M, bm) * ceil_div(a.N, bn); };
+  if (tiles(256, 256) >= 256) product_tile<T, 256, 256, 2, 4>(a, s);
+  else if (tiles(128, 128) >= 256) product_tile<T, 128, 128, 2, 2>(a, s);
+  else product_tile<T, 64, 64, 2, 2>(a, s);
 }
 static void product_run(int M, int N, int K, const int8_t* q, const float* qs, const int8_t* w, const float* ws, const float* bias, int y_dtype,
                         void* y, int64_t ldy, hipStream_t s) {
-  const int Kp = static_cast<int>(quant_i8_row_bytes(K));
-  const dim3 grid(ceil_div(N, 64), ceil_div(M, 64));
-  if (y_dtype == RN50_BF16)
-    RN50_LAUNCH("matmul_i8", matmul_i8_kernel<uint16_t>, grid, dim3(256), 0, s, q, qs, w, ws, bias, static_cast<uint16_t*>(y), ldy, M, N, Kp);
-  else
-    RN50_LAUNCH("matmul_i8", matmul_i8_kernel<float>, grid, dim3(256), 0, s, q, qs, w, ws, bias, static_cast<float*>(y), ldy, M, N, Kp);
+  const ProductArgs a{q, w, qs, ws, bias, y, ldy, M, N, static_cast<int>(quant_i8_row_bytes(K)), 0, 0};
+  if (y_dtype == RN50_BF16) product_typed<uint16_t>(a, s);
+  else product_typed<float>(a, s);
 }
 
 }  // namespace rn50
