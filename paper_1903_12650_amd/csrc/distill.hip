@@ -48,119 +48,6 @@ __device__ __forceinline__ float exp_scaled(float x, float scale) { return __bui
 // A workgroup for each of N rows, row blockIdx.y * gridDim.x + blockIdx.x.
 static dim3 row_grid(int N) { return N <= 65536 ? dim3(N) : dim3(65536, static_cast<unsigned>(ceil_div(N, 65536))); }
 
-// ------------------------------------------------------------- largest logits
-// The order of the logits as unsigned integers: -0 and +0 are one, a NaN is above everything.
-__device__ __forceinline__ uint32_t order_key(float x) {
-  uint32_t u = __float_as_uint(x);
-  if ((u & 0x7fffffffu) > 0x7f800000u) return 0xffffffffu;
-  if (u == 0x80000000u) u = 0;
-  return u & 0x80000000u ? ~u : u | 0x80000000u;
-}
-
-// One workgroup per row.  The key of the k-th largest logit is found digit by digit (four of 8 bits, a histogram each over the
-// logits that share the digits in front); logits above it are taken as they come, those equal to it in the order of their classes;
-// a rank by counting puts them in order.  The row is read six times: right for every row, fast for none.
-template <typename T>
-__global__ __launch_bounds__(256) void topk_rows_kernel(const T* __restrict__ logits, int64_t ld, int N, int C, int k, float temperature,
-                                                        float* __restrict__ values, int32_t* __restrict__ indices, float* __restrict__ tail) {
-  __shared__ uint32_t hist[256];
-  __shared__ uint32_t found[4];
-  __shared__ uint32_t sel_key[kTopMax];
-  __shared__ int sel_at[kTopMax];
-  __shared__ int taken[5];
-  __shared__ float red_m[4], red_s[4];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int n = blockIdx.y * gridDim.x + blockIdx.x;
-  if (n >= N) return;
-  {
-    const T* row = logits + n * ld;
-    const int kk = min(k, C);
-    uint32_t prefix = 0;
-    int need = kk;  // how many are still to be taken among the logits that share the prefix
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      hist[tid] = 0;
-      __syncthreads();
-      for (int i = tid; i < C; i += 256) {
-        const uint32_t key = order_key(Elem<T>::load(row + i));
-        if (shift == 24 || key >> (shift + 8) == prefix) atomicAdd(&hist[(key >> shift) & 255], 1u);
-      }
-      __syncthreads();
-      if (tid == 0) {
-        int above = 0, d = 255;
-        while (d > 0 && above + static_cast<int>(hist[d]) < need) above += hist[d--];
-        found[0] = d;
-        found[1] = above;
-      }
-      __syncthreads();
-      prefix = prefix << 8 | found[0];
-      need -= found[1];
-      __syncthreads();
-    }
-    if (tid == 0) taken[4] = 0;
-    __syncthreads();
-    // above the k-th key: kk - need of them, in any order; equal to it: the first `need` classes, counted chunk by chunk
-    int equal = 0, last = -1;
-    for (int base = 0; base < C; base += 256) {
-      const int i = base + tid;
-      const uint32_t key = i < C ? order_key(Elem<T>::load(row + i)) : 0;
-      if (i < C && key > prefix) {
-        const int at = atomicAdd(&taken[4], 1);
-        sel_key[at] = key;
-        sel_at[at] = i;
-      }
-      const bool eq = i < C && key == prefix;
-      const uint64_t votes = __ballot(eq);
-      if (lane == 0) taken[wave] = __popcll(votes);
-      __syncthreads();
-      int before = equal;
-      for (int w = 0; w < wave; ++w) before += taken[w];
-      const int pos = before + __popcll(votes & ((1ull << lane) - 1));
-      if (eq && pos < need) {
-        sel_key[kk - need + pos] = key;
-        sel_at[kk - need + pos] = i;
-        if (pos == need - 1) found[2] = i;
-      }
-      equal += taken[0] + taken[1] + taken[2] + taken[3];
-      __syncthreads();
-    }
-    last = found[2];  // the last class that was taken among the equal ones
-    if (tid < kk) {
-      const uint32_t key = sel_key[tid];
-      const int at = sel_at[tid];
-      int rank = 0;
-      for (int j = 0; j < kk; ++j) rank += sel_key[j] > key || (sel_key[j] == key && sel_at[j] < at);
-      values[static_cast<int64_t>(n) * k + rank] = Elem<T>::load(row + at);
-      indices[static_cast<int64_t>(n) * k + rank] = at;
-    } else if (tid < k) {
-      values[static_cast<int64_t>(n) * k + tid] = -INFINITY;
-      indices[static_cast<int64_t>(n) * k + tid] = -1;
-    }
-    if (tail) {
-      const float scale = kLog2e / temperature;
-      float m = -FLT_MAX, s = 0.f;
-      for (int i = tid; i < C; i += 256) {
-        const float x = Elem<T>::load(row + i);
-        const uint32_t key = order_key(x);
-        if (key > prefix || (key == prefix && i <= last)) continue;
-        const float top = fmaxf(m, x);
-        s = s * exp_scaled(m - top, scale) + exp_scaled(x - top, scale);
-        m = top;
-      }
-      const float wm = wave_max(m);
-      const float wsum = wave_sum(s * exp_scaled(m - wm, scale));
-      if (lane == 0) red_m[wave] = wm, red_s[wave] = wsum;
-      __syncthreads();
-      if (tid == 0) {
-        const float top = fmaxf(fmaxf(red_m[0], red_m[1]), fmaxf(red_m[2], red_m[3]));
-        float sum = 0.f;
-        for (int w = 0; w < 4; ++w) sum += red_s[w] * exp_scaled(red_m[w] - top, scale);
-        tail[n] = sum == 0.f ? -INFINITY : static_cast<float>(static_cast<double>(top) / temperature + log(static_cast<double>(sum)));
-      }
-    }
-    __syncthreads();
-  }
-}
-
 // --------------------------------------------------------- distillation loss
 struct DistillArgs {
   const void* logits;
@@ -205,20 +92,28 @@ struct Sums {
     }
     if constexpr (EXPS == 0) s1 += __builtin_amdgcn_exp2f(d * sc.one);
   }
+  __device__ __forceinline__ void move(float to, const Scales& sc) {
+    const float f = __builtin_amdgcn_exp2f((ref - to) * sc.t);
+    st *= f;
+    if constexpr (EXPS == 0) s1 *= __builtin_amdgcn_exp2f((ref - to) * sc.one);
+    if constexpr (EXPS == 2) s1 *= f * f;
+    if constexpr (EXPS == 4) s1 *= (f * f) * (f * f);
+    ref = to;
+    lim = to + sc.slack;
+  }
+  __device__ __forceinline__ void join(Sums other, const Scales& sc) {
+    const float to = fmaxf(ref, other.ref);
+    move(to, sc);
+    other.move(to, sc);
+    st += other.st;
+    s1 += other.s1;
+  }
   template <int V>
   __device__ __forceinline__ void add(const float* x, const Scales& sc) {
     float top = x[0];
 #pragma unroll
     for (int j = 1; j < V; ++j) top = fmaxf(top, x[j]);
-    if (top > lim) {
-      const float f = __builtin_amdgcn_exp2f((ref - top) * sc.t);
-      st *= f;
-      if constexpr (EXPS == 0) s1 *= __builtin_amdgcn_exp2f((ref - top) * sc.one);
-      if constexpr (EXPS == 2) s1 *= f * f;
-      if constexpr (EXPS == 4) s1 *= (f * f) * (f * f);
-      ref = top;
-      lim = top + sc.slack;
-    }
+    if (top > lim) move(top, sc);
 #pragma unroll
     for (int j = 0; j < V; ++j) one(x[j], sc);
   }
@@ -260,6 +155,339 @@ __device__ __forceinline__ RowSums block_sums(const Sums<EXPS>& a, double sz, bo
   if ((threadIdx.x & 63) == 0) red[wave] = r;
   __syncthreads();
   return joined(red, NT / 64, sc);
+}
+
+// ------------------------------------------------------------- largest logits
+// The order of the logits as unsigned integers: -0 and +0 are one, a NaN is above everything.
+__device__ __forceinline__ uint32_t order_key(float x) {
+  uint32_t u = __float_as_uint(x);
+  if ((u & 0x7fffffffu) > 0x7f800000u) return 0xffffffffu;
+  if (u == 0x80000000u) u = 0;
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+constexpr uint32_t kKeyOfNothing = 0x007fffffu;  // order_key(-infinity)
+
+struct TopkArgs {
+  const void* logits;
+  int64_t ld;
+  int N, C, k;
+  float temperature;
+  float* values;
+  int32_t* indices;
+  float* tail;  // (or null)
+  // slices of rows: each one's largest logits, their classes, and the sum of its others
+  int slices, width;
+  float* part_values;
+  int32_t* part_at;
+  RowSums* part_sums;
+};
+enum { kTopkRows, kTopkSlices, kTopkJoin };  // whole rows; slices of rows; the slices' largest logits as rows of their own
+constexpr int kTopkThreads = 256, kTopkCand = 1024;
+
+struct TopkShared {
+  unsigned long long cand[kTopkCand];  // (key, ~class) of the logits that may be among the largest: larger is in front
+  float value[kTopkCand], spare[kTopkCand];
+  uint16_t owner[kTopkThreads * 4];
+  int count[2][16];
+  int taken;
+  int last;
+  uint32_t hist[256], found[2];
+  RowSums red[kTopkThreads / 64];
+};
+
+// Where a row's results go.
+template <int MODE>
+struct TopkOut {
+  const TopkArgs& a;
+  int n, slice;
+  __device__ __forceinline__ void put(int rank, float x, int at) const {
+    if (MODE == kTopkSlices) {
+      const int64_t i = (static_cast<int64_t>(n) * a.slices + slice) * a.k + rank;
+      a.part_values[i] = x;
+      a.part_at[i] = at < 0 ? at : at + slice * a.width;
+    } else {
+      const int64_t i = static_cast<int64_t>(n) * a.k + rank;
+      a.values[i] = x;
+      a.indices[i] = MODE == kTopkJoin ? a.part_at[static_cast<int64_t>(n) * a.C + at] : at;
+    }
+  }
+};
+
+// The `need` first classes whose key is `key`, in their order, to the ranks from `rank` on; returns the last of them.  Every thread calls it.
+template <typename T, int MODE>
+__device__ __forceinline__ int take_equal(const T* row, int C, uint32_t key, int need, int rank, const TopkOut<MODE>& out, TopkShared& sh) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int before = 0;
+#pragma unroll 1
+  for (int base = 0; base < C && before < need; base += kTopkThreads) {
+    const int i = base + tid;
+    const float x = i < C ? Elem<T>::load(row + i) : 0.f;
+    const bool eq = i < C && order_key(x) == key;
+    const uint64_t votes = __ballot(eq);
+    __syncthreads();
+    if (lane == 0) sh.count[0][wave] = __popcll(votes);
+    __syncthreads();
+    int pos = before + __popcll(votes & ((1ull << lane) - 1));
+    for (int w = 0; w < wave; ++w) pos += sh.count[0][w];
+    if (eq && pos < need) {
+      out.put(rank + pos, x, i);
+      if (pos == need - 1) sh.last = i;
+    }
+    before += sh.count[0][0] + sh.count[0][1] + sh.count[0][2] + sh.count[0][3];
+  }
+  __syncthreads();
+  return sh.last;
+}
+// The sum over the classes that were not taken: keys below `key`, and equal to it behind class `last`.
+template <typename T>
+__device__ __forceinline__ void add_rest(const T* row, int C, uint32_t key, int last, const Scales& sc, Sums<1>& rest) {
+#pragma unroll 1
+  for (int i = threadIdx.x; i < C; i += kTopkThreads) {
+    const float x = Elem<T>::load(row + i);
+    const uint32_t o = order_key(x);
+    if (o < key || (o == key && i > last)) rest.template add<1>(&x, sc);
+  }
+}
+
+// Any row, NaN and infinities among it: the key of the k-th largest logit digit by digit (four of 8 bits, a histogram each over the logits
+// that share the digits in front).  The row is read seven times; only rows that the way below cannot take come here.
+template <typename T, int MODE>
+__device__ __noinline__ void topk_any(const T* row, int C, int kk, bool want_tail, const Scales& sc, const TopkOut<MODE>& out, TopkShared& sh, Sums<1>& rest) {
+  const int tid = threadIdx.x;
+  uint32_t prefix = 0;
+  int need = kk;  // how many are still to be taken among the logits that share the prefix
+#pragma unroll 1
+  for (int shift = 24; shift >= 0; shift -= 8) {
+    __syncthreads();
+    sh.hist[tid] = 0;
+    __syncthreads();
+    for (int i = tid; i < C; i += kTopkThreads) {
+      const uint32_t key = order_key(Elem<T>::load(row + i));
+      if (shift == 24 || key >> (shift + 8) == prefix) atomicAdd(&sh.hist[(key >> shift) & 255], 1u);
+    }
+    __syncthreads();
+    if (tid == 0) {
+      int above = 0, d = 255;
+      while (d > 0 && above + static_cast<int>(sh.hist[d]) < need) above += sh.hist[d--];
+      sh.found[0] = d;
+      sh.found[1] = above;
+    }
+    __syncthreads();
+    prefix = prefix << 8 | sh.found[0];
+    need -= sh.found[1];
+  }
+  __syncthreads();
+  if (tid == 0) sh.taken = 0;
+  __syncthreads();
+  for (int i = tid; i < C; i += kTopkThreads) {  // (kk - need of them)
+    const float x = Elem<T>::load(row + i);
+    const uint32_t key = order_key(x);
+    if (key > prefix) {
+      const int at = atomicAdd(&sh.taken, 1);
+      sh.cand[at] = static_cast<unsigned long long>(key) << 32 | ~static_cast<uint32_t>(i);
+      sh.value[at] = x;
+    }
+  }
+  __syncthreads();
+  const int above = kk - need;
+  if (tid < above) {
+    const unsigned long long mine = sh.cand[tid];
+    int rank = 0;
+    for (int j = 0; j < above; ++j) rank += sh.cand[j] > mine;
+    out.put(rank, sh.value[tid], static_cast<int>(~static_cast<uint32_t>(mine)));
+  }
+  const int last = take_equal<T, MODE>(row, C, prefix, need, above, out, sh);
+  rest = Sums<1>();
+  if (want_tail) add_rest(row, C, prefix, last, sc, rest);
+}
+
+// One workgroup per row (or slice of one).  The row goes by once in 1024 streams, four a thread, each with its largest logit and its sum of
+// exponentials.  A bound below which no logit of the row's k largest can lie is the k-th largest of the 1024 maxima, or a little less:
+// streams whose maximum reaches it (little more than k) are read again, from the caches, for the logits that reach it (little more
+// than k again), and these are put in order by counting.  Their streams' sums are taken anew without them: nothing is subtracted.
+// Where many maxima are equal (masks, ties), the logits above their value are the candidates and the rest of the k is taken from the
+// equal ones in the order of the classes.
+template <typename T, int MODE>
+__global__ __launch_bounds__(kTopkThreads) void topk_rows_kernel(const TopkArgs a) {
+  constexpr int V = Elem<T>::VEC, NT = kTopkThreads, G = 4;
+  __shared__ TopkShared sh;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int slice = MODE == kTopkSlices ? blockIdx.x : 0, n = MODE == kTopkSlices ? blockIdx.y : blockIdx.y * gridDim.x + blockIdx.x;
+  if (n >= a.N) return;
+  const int C = MODE == kTopkSlices ? min(a.width, a.C - slice * a.width) : a.C;
+  const T* row = static_cast<const T*>(a.logits) + n * a.ld + static_cast<int64_t>(slice) * a.width;
+  const int kk = min(a.k, C), whole = C / V, left = C - whole * V;
+  const TopkOut<MODE> out{a, n, slice};
+  Scales sc;
+  sc.t = sc.one = kLog2e / a.temperature;
+  sc.slack = 20.f / sc.t;
+  float m[G];
+  Sums<1> s[G];
+#pragma unroll
+  for (int g = 0; g < G; ++g) m[g] = -INFINITY;
+  auto take = [&](const Vec16& x, int g) __attribute__((always_inline)) {
+    float z[V];
+    Elem<T>::unpack(x, z);
+    float top = z[0];
+#pragma unroll
+    for (int j = 1; j < V; ++j) top = fmaxf(top, z[j]);
+    m[g] = fmaxf(m[g], top);
+    s[g].template add<V>(z, sc);
+  };
+  int v = tid;
+  for (; v + (G - 1) * NT < whole; v += G * NT) {
+    Vec16 x[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g) x[g] = load16_any(row + (v + g * NT) * V);
+#pragma unroll
+    for (int g = 0; g < G; ++g) take(x[g], g);
+  }
+#pragma unroll
+  for (int g = 0; g < G; ++g)
+    if (v + g * NT < whole) take(load16_any(row + (v + g * NT) * V), g);
+  if (tid < left) {  // (the classes behind the last vector: of the threads' first streams)
+    const float z = Elem<T>::load(row + whole * V + tid);
+    m[0] = fmaxf(m[0], z);
+    s[0].template add<1>(&z, sc);
+  }
+  if (tid == 0) sh.taken = 0;
+  uint32_t key[G];
+#pragma unroll
+  for (int g = 0; g < G; ++g) key[g] = order_key(m[g]);
+  // A sum is NaN where a logit is NaN or +infinity: maxima say nothing then.
+  const float all = (s[0].st + s[1].st) + (s[2].st + s[3].st);
+  const bool odd = __syncthreads_or(!(all == all));
+  Sums<1> rest;
+  bool done = false;
+  if (!odd) {
+    // The bound: at least kk maxima reach lo, hardly more than kk if possible; fewer than kk reach hi.
+    {
+      const float tm = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+      const float most = quick_max(tm), least = -quick_max(tid < kk ? -tm : -INFINITY);
+      if (lane == 0) sh.count[1][wave] = __float_as_int(most), sh.count[1][4 + wave] = __float_as_int(least);
+    }
+    __syncthreads();
+    float most = -INFINITY, least = INFINITY;
+    for (int w = 0; w < 4; ++w) {
+      most = fmaxf(most, __int_as_float(sh.count[1][w]));
+      least = fminf(least, __int_as_float(sh.count[1][4 + w]));
+    }
+    uint32_t lo = order_key(least), hi = order_key(most) + 1;  // (the first kk threads' maxima reach lo)
+    const int enough = kk + kk / 2 + 16;
+    uint32_t mid = lo;
+    int reach = 0, turn = 0;
+    bool tie = false;
+    while (true) {
+      int c = 0;
+#pragma unroll
+      for (int g = 0; g < G; ++g) c += __popcll(__ballot(key[g] >= mid));
+      if (lane == 0) sh.count[turn][8 + wave] = c;
+      __syncthreads();
+      c = (sh.count[turn][8] + sh.count[turn][9]) + (sh.count[turn][10] + sh.count[turn][11]);
+      turn ^= 1;
+      if (c >= kk) lo = mid, reach = c;
+      else hi = mid;
+      if (reach <= enough) break;
+      if (hi - lo <= 1) {
+        tie = true;
+        break;
+      }
+      mid = lo + ((hi - lo) >> 1);
+    }
+    const uint32_t bound = tie ? hi : lo;
+    // the streams that are read again, listed in a fixed order; the others' sums stay
+    int owners = 0;
+    {
+      uint64_t votes[G];
+      __syncthreads();
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        votes[g] = __ballot(key[g] >= bound);
+        if (lane == 0) sh.count[0][g * 4 + wave] = __popcll(votes[g]);
+      }
+      __syncthreads();
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        int at = owners;
+        for (int w = 0; w < wave; ++w) at += sh.count[0][g * 4 + w];
+        if (key[g] >= bound) sh.owner[at + __popcll(votes[g] & ((1ull << lane) - 1))] = static_cast<uint16_t>(tid * G + g);
+        else rest.join(s[g], sc);
+        for (int w = 0; w < 4; ++w) owners += sh.count[0][g * 4 + w];
+      }
+    }
+    __syncthreads();
+    auto candidate = [&](float x, int i) __attribute__((always_inline)) {
+      const int at = atomicAdd(&sh.taken, 1);
+      if (at < kTopkCand) {
+        sh.cand[at] = static_cast<unsigned long long>(order_key(x)) << 32 | ~static_cast<uint32_t>(i);
+        sh.value[at] = x;
+      }
+    };
+    const int rounds = max(1, (whole + G * NT - 1) / (G * NT));
+    for (int i = tid; i < owners * rounds; i += NT) {
+      const int o = i / rounds, r = i - o * rounds, own = sh.owner[o], g = own & (G - 1), t = own / G;
+      const int vec = t + (r * G + g) * NT;
+      if (vec < whole) {
+        float z[V];
+        Elem<T>::unpack(load16_any(row + vec * V), z);
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+          if (order_key(z[j]) >= bound) {
+            candidate(z[j], vec * V + j);
+            z[j] = -INFINITY;
+          }
+        rest.template add<V>(z, sc);
+      }
+      if (g == 0 && r == 0 && t < left) {
+        const float z = Elem<T>::load(row + whole * V + t);
+        if (order_key(z) >= bound) candidate(z, whole * V + t);
+        else rest.template add<1>(&z, sc);
+      }
+    }
+    __syncthreads();
+    const int cands = sh.taken;
+    if (cands <= kTopkCand) {
+      done = true;
+      for (int c = tid; c < cands; c += NT) {
+        const unsigned long long mine = sh.cand[c];
+        int rank = 0;
+        for (int j = 0; j < cands; ++j) rank += sh.cand[j] > mine;
+        if (rank < kk) out.put(rank, sh.value[c], static_cast<int>(~static_cast<uint32_t>(mine)));
+        else sh.spare[rank - kk] = sh.value[c];
+      }
+      __syncthreads();
+      for (int c = tid; c < cands - kk; c += NT) rest.template add<1>(&sh.spare[c], sc);
+      if (cands < kk) {  // (many equal maxima)
+        const int last = take_equal<T, MODE>(row, C, lo, kk - cands, cands, out, sh);
+        if (lo != kKeyOfNothing) {  // (the sums have all of the equal ones, and nothing is subtracted)
+          rest = Sums<1>();
+          add_rest(row, C, lo, last, sc, rest);
+        }
+      }
+    }
+  }
+  if (!done) topk_any<T, MODE>(row, C, kk, true, sc, out, sh, rest);
+  for (int r = kk + tid; r < a.k; r += NT) {
+    if (MODE == kTopkSlices) {
+      out.put(r, -INFINITY, -1);
+    } else {
+      a.values[static_cast<int64_t>(n) * a.k + r] = -INFINITY;
+      a.indices[static_cast<int64_t>(n) * a.k + r] = -1;
+    }
+  }
+  if (MODE != kTopkSlices && a.tail == nullptr) return;
+  if (MODE == kTopkJoin && tid < a.slices) {
+    const RowSums part = a.part_sums[static_cast<int64_t>(n) * a.slices + tid];
+    Sums<1> p;
+    p.ref = part.ref;
+    p.st = part.st;
+    rest.join(p, sc);
+  }
+  __syncthreads();
+  const RowSums sum = block_sums<1, NT>(rest, 0.0, false, sc, sh.red);
+  if (tid != 0) return;
+  if (MODE == kTopkSlices) a.part_sums[static_cast<int64_t>(n) * a.slices + slice] = sum;
+  else a.tail[n] = sum.st == 0.f ? -INFINITY : static_cast<float>(static_cast<double>(sum.ref) / a.temperature + log(static_cast<double>(sum.st)));
 }
 
 // What the gradient pass needs of its row: d = coef_t * exp((z - ref) / T) + coef_1 * exp(z - ref) - offset (EXPS = 1: both
@@ -750,6 +978,41 @@ __global__ __launch_bounds__(1024) void distill_loss_kernel(const float* __restr
   }
 }
 
+// Slices of a row where rows are few (1: a workgroup does the row), every one of at least k classes but the last, and the parts of the
+// workspace that they need.
+static void topk_slicing(int N, int C, int k, TopkArgs* a, void* workspace, size_t* bytes) {
+  int least = 32768, target = 512, most_rows = 128, narrow = 2048;
+#ifdef RN50_TUNING  // tuning builds only: RN50_TOPK_SLICES=least classes of a row,workgroups,rows,least classes of a slice
+  if (const char* e = getenv("RN50_TOPK_SLICES")) sscanf(e, "%d,%d,%d,%d", &least, &target, &most_rows, &narrow);
+#endif
+  *bytes = 0;
+  if (N > most_rows || C < least) return;
+  const int64_t want = std::min<int64_t>({ceil_div(target, N), ceil_div(C, narrow), kTopkThreads, std::max(2, 16384 / k)});
+  if (want < 2) return;
+  const int width = static_cast<int>(align_up(static_cast<size_t>(ceil_div(C, want)), 32)), slices = static_cast<int>(ceil_div(C, width));
+  const size_t list = align_up(static_cast<size_t>(N) * slices * k * 4, 256);
+  *bytes = 2 * list + sizeof(RowSums) * N * slices;
+  if (!a) return;
+  unsigned char* p = static_cast<unsigned char*>(workspace);
+  a->slices = slices;
+  a->width = width;
+  a->part_values = reinterpret_cast<float*>(p);
+  a->part_at = reinterpret_cast<int32_t*>(p + list);
+  a->part_sums = reinterpret_cast<RowSums*>(p + 2 * list);
+}
+template <typename T>
+static void topk_run(TopkArgs a, hipStream_t s) {
+  if (a.slices < 2) {
+    RN50_LAUNCH("topk_rows", (topk_rows_kernel<T, kTopkRows>), row_grid(a.N), dim3(kTopkThreads), 0, s, a);
+    return;
+  }
+  RN50_LAUNCH("topk_rows", (topk_rows_kernel<T, kTopkSlices>), dim3(a.slices, a.N), dim3(kTopkThreads), 0, s, a);
+  a.logits = a.part_values;
+  a.C = a.slices * a.k;
+  a.ld = a.C;
+  RN50_LAUNCH("topk_rows", (topk_rows_kernel<float, kTopkJoin>), row_grid(a.N), dim3(kTopkThreads), 0, s, a);
+}
+
 static int check_rows(const char* who, int N, int C, int dtype, const void* logits, int64_t ld) {
   RN50_REQUIRE(dtype == RN50_F32 || dtype == RN50_BF16, RN50_ERR_INVALID, "%s: dtype %d", who, dtype);
   RN50_REQUIRE(N > 0 && C > 0, RN50_ERR_INVALID, "%s: non-positive size", who);
@@ -861,8 +1124,9 @@ static SliceArgs slice_args(int N, int C, int dtype, void* workspace, size_t* by
 using namespace rn50;
 
 extern "C" size_t topk_rows_workspace_bytes(int N, int C, int k) {
-  (void)N; (void)C; (void)k;
-  return 0;
+  size_t bytes = 0;
+  if (N > 0 && C > 0 && k > 0 && k <= kTopMax) topk_slicing(N, C, k, nullptr, nullptr, &bytes);
+  return bytes;
 }
 
 extern "C" int topk_rows(int N, int C, int k, int dtype, const void* logits, int64_t ld, float temperature, float* values, int32_t* indices,
@@ -877,11 +1141,11 @@ extern "C" int topk_rows(int N, int C, int k, int dtype, const void* logits, int
   const size_t need = topk_rows_workspace_bytes(N, C, k);
   RN50_REQUIRE(workspace_bytes >= need && (need == 0 || workspace), RN50_ERR_WORKSPACE, "topk_rows: workspace %zu < %zu bytes", workspace_bytes, need);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const dim3 grid = row_grid(N);
-  if (dtype == RN50_BF16)
-    RN50_LAUNCH("topk_rows", topk_rows_kernel<uint16_t>, grid, dim3(256), 0, s, static_cast<const uint16_t*>(logits), ld, N, C, k, temperature, values, indices, tail_lse);
-  else
-    RN50_LAUNCH("topk_rows", topk_rows_kernel<float>, grid, dim3(256), 0, s, static_cast<const float*>(logits), ld, N, C, k, temperature, values, indices, tail_lse);
+  TopkArgs a{logits, ld, N, C, k, temperature, values, indices, tail_lse, 1, 0, nullptr, nullptr, nullptr};
+  size_t bytes;
+  topk_slicing(N, C, k, &a, workspace, &bytes);
+  if (dtype == RN50_BF16) topk_run<uint16_t>(a, s);
+  else topk_run<float>(a, s);
   return launch_status("topk_rows");
 }
 
