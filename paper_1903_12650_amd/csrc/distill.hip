@@ -158,10 +158,10 @@ __device__ __forceinline__ RowSums block_sums(const Sums<EXPS>& a, double sz, bo
 }
 
 // ------------------------------------------------------------- largest logits
-// The order of the logits as unsigned integers: -0 and +0 are one, a NaN is above everything.
+// The order of the logits as unsigned integers: -0 and +0 are one, a NaN is above everything (and below the last integer).
 __device__ __forceinline__ uint32_t order_key(float x) {
   uint32_t u = __float_as_uint(x);
-  if ((u & 0x7fffffffu) > 0x7f800000u) return 0xffffffffu;
+  if ((u & 0x7fffffffu) > 0x7f800000u) return 0xfffffffeu;
   if (u == 0x80000000u) u = 0;
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
@@ -181,14 +181,14 @@ struct TopkArgs {
   int32_t* part_at;
   RowSums* part_sums;
 };
-enum { kTopkRows, kTopkSlices, kTopkJoin };  // whole rows; slices of rows; the slices' largest logits as rows of their own
-constexpr int kTopkThreads = 256, kTopkCand = 1024;
+enum { kTopkRows, kTopkSlices, kTopkJoin };  // whole rows; slices of rows; the slices' largest logits
+constexpr int kTopkThreads = 256, kTopkCand = 1024, kTopkStreams = 8;  // threads of a row, candidates, streams of a thread
 
 struct TopkShared {
-  unsigned long long cand[kTopkCand];  // (key, ~class) of the logits that may be among the largest: larger is in front
+  __align__(16) unsigned long long cand[kTopkCand];  // (key, ~class) of the logits that may be among the largest: larger is in front
   float value[kTopkCand], spare[kTopkCand];
-  uint16_t owner[kTopkThreads * 4];
-  int count[2][16];
+  uint16_t owner[kTopkThreads * kTopkStreams];
+  int count[2][4 * 16];
   int taken;
   int last;
   uint32_t hist[256], found[2];
@@ -208,10 +208,58 @@ struct TopkOut {
     } else {
       const int64_t i = static_cast<int64_t>(n) * a.k + rank;
       a.values[i] = x;
-      a.indices[i] = MODE == kTopkJoin ? a.part_at[static_cast<int64_t>(n) * a.C + at] : at;
+      a.indices[i] = MODE == kTopkJoin ? a.part_at[static_cast<int64_t>(n) * a.slices * a.k + at] : at;
     }
   }
 };
+
+// A key that at least kk of the workgroup's keys reach, hardly more if possible; where that takes a key that many have (`tie`), fewer than
+// kk reach the one after it.  lo: kk keys reach it; hi: none does.  Every thread calls it, behind a barrier.
+template <int G>
+__device__ __forceinline__ uint32_t find_bound(const uint32_t* key, uint32_t lo, uint32_t hi, int kk, bool* tie, TopkShared& sh) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int enough = kk + kk / 2 + 16;
+  uint32_t mid = lo;
+  int reach = 0, turn = 0;
+  while (true) {
+    int c = 0;
+#pragma unroll
+    for (int g = 0; g < G; ++g) c += __popcll(__ballot(key[g] >= mid));
+    if (lane == 0) sh.count[turn][8 + wave] = c;
+    __syncthreads();
+    c = (sh.count[turn][8] + sh.count[turn][9]) + (sh.count[turn][10] + sh.count[turn][11]);
+    turn ^= 1;
+    if (c >= kk) lo = mid, reach = c;
+    else hi = mid;
+    *tie = hi - lo <= 1 && reach > enough;
+    if (reach <= enough || *tie) break;
+    mid = lo + ((hi - lo) >> 1);
+  }
+  return lo;
+}
+// Candidates in order: the first kk to the output, the others' values to `spare`.  Every thread calls it, behind a barrier.
+template <int MODE>
+__device__ __forceinline__ void put_ranked(int cands, int kk, const TopkOut<MODE>& out, TopkShared& sh) {
+  typedef unsigned long long u64x2 __attribute__((ext_vector_type(2)));
+  const int padded = (cands + 7) & ~7;  // (cands <= kTopkCand, a multiple of 8)
+  if (static_cast<int>(threadIdx.x) < padded - cands) sh.cand[cands + threadIdx.x] = 0;
+  __syncthreads();
+  for (int c = threadIdx.x; c < cands; c += kTopkThreads) {
+    const unsigned long long mine = sh.cand[c];
+    int rank = 0;
+#pragma unroll 1
+    for (int j = 0; j < padded; j += 8) {
+      u64x2 v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const u64x2*>(&sh.cand[j + 2 * i]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) rank += (v[i].x > mine) + (v[i].y > mine);
+    }
+    if (rank < kk) out.put(rank, sh.value[c], static_cast<int>(~static_cast<uint32_t>(mine)));
+    else sh.spare[rank - kk] = sh.value[c];
+  }
+  __syncthreads();
+}
 
 // The `need` first classes whose key is `key`, in their order, to the ranks from `rank` on; returns the last of them.  Every thread calls it.
 template <typename T, int MODE>
@@ -247,6 +295,10 @@ __device__ __forceinline__ void add_rest(const T* row, int C, uint32_t key, int 
     const uint32_t o = order_key(x);
     if (o < key || (o == key && i > last)) rest.template add<1>(&x, sc);
   }
+}
+
+__device__ __forceinline__ float tail_of(const RowSums& sum, float temperature) {
+  return sum.st == 0.f ? -INFINITY : static_cast<float>(static_cast<double>(sum.ref) / temperature + log(static_cast<double>(sum.st)));
 }
 
 // Any row, NaN and infinities among it: the key of the k-th largest logit digit by digit (four of 8 bits, a histogram each over the logits
@@ -301,15 +353,15 @@ __device__ __noinline__ void topk_any(const T* row, int C, int kk, bool want_tai
   if (want_tail) add_rest(row, C, prefix, last, sc, rest);
 }
 
-// One workgroup per row (or slice of one).  The row goes by once in 1024 streams, four a thread, each with its largest logit and its sum of
-// exponentials.  A bound below which no logit of the row's k largest can lie is the k-th largest of the 1024 maxima, or a little less:
-// streams whose maximum reaches it (little more than k) are read again, from the caches, for the logits that reach it (little more
-// than k again), and these are put in order by counting.  Their streams' sums are taken anew without them: nothing is subtracted.
+// One workgroup per row (or slice of one).  The row goes by once in 2048 streams, eight a thread, each with its largest logit and its sum
+// of exponentials.  A bound below which no logit of the row's k largest can lie is the k-th largest of the streams' maxima, or a little
+// less: streams whose maximum reaches it (little more than k) are read again, from the caches, for the logits that reach it (little
+// more than k again), and these are put in order by counting.  Their streams' sums are taken anew without them: nothing is subtracted.
 // Where many maxima are equal (masks, ties), the logits above their value are the candidates and the rest of the k is taken from the
 // equal ones in the order of the classes.
 template <typename T, int MODE>
 __global__ __launch_bounds__(kTopkThreads) void topk_rows_kernel(const TopkArgs a) {
-  constexpr int V = Elem<T>::VEC, NT = kTopkThreads, G = 4;
+  constexpr int V = Elem<T>::VEC, NT = kTopkThreads, G = kTopkStreams, HALF = G / 2;
   __shared__ TopkShared sh;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int slice = MODE == kTopkSlices ? blockIdx.x : 0, n = MODE == kTopkSlices ? blockIdx.y : blockIdx.y * gridDim.x + blockIdx.x;
@@ -321,10 +373,18 @@ __global__ __launch_bounds__(kTopkThreads) void topk_rows_kernel(const TopkArgs 
   Scales sc;
   sc.t = sc.one = kLog2e / a.temperature;
   sc.slack = 20.f / sc.t;
-  float m[G];
-  Sums<1> s[G];
+  float m[G], st[G], ref = -FLT_MAX, lim = -FLT_MAX;  // (one reference for a thread's streams, as in Sums)
 #pragma unroll
-  for (int g = 0; g < G; ++g) m[g] = -INFINITY;
+  for (int g = 0; g < G; ++g) m[g] = -INFINITY, st[g] = 0.f;
+  auto refer = [&](float top) __attribute__((always_inline)) {
+    if (top > lim) {
+      const float f = __builtin_amdgcn_exp2f((ref - top) * sc.t);
+#pragma unroll
+      for (int g = 0; g < G; ++g) st[g] *= f;
+      ref = top;
+      lim = top + sc.slack;
+    }
+  };
   auto take = [&](const Vec16& x, int g) __attribute__((always_inline)) {
     float z[V];
     Elem<T>::unpack(x, z);
@@ -332,88 +392,84 @@ __global__ __launch_bounds__(kTopkThreads) void topk_rows_kernel(const TopkArgs 
 #pragma unroll
     for (int j = 1; j < V; ++j) top = fmaxf(top, z[j]);
     m[g] = fmaxf(m[g], top);
-    s[g].template add<V>(z, sc);
+    refer(top);
+#pragma unroll
+    for (int j = 0; j < V; ++j) st[g] += __builtin_amdgcn_exp2f((z[j] - ref) * sc.t);
   };
   int v = tid;
   for (; v + (G - 1) * NT < whole; v += G * NT) {
-    Vec16 x[G];
 #pragma unroll
-    for (int g = 0; g < G; ++g) x[g] = load16_any(row + (v + g * NT) * V);
+    for (int h = 0; h < G; h += HALF) {
+      Vec16 x[HALF];
 #pragma unroll
-    for (int g = 0; g < G; ++g) take(x[g], g);
+      for (int g = 0; g < HALF; ++g) x[g] = load16_any(row + (v + (h + g) * NT) * V);
+#pragma unroll
+      for (int g = 0; g < HALF; ++g) take(x[g], h + g);
+    }
   }
 #pragma unroll
-  for (int g = 0; g < G; ++g)
-    if (v + g * NT < whole) take(load16_any(row + (v + g * NT) * V), g);
+  for (int h = 0; h < G; h += HALF) {
+    Vec16 x[HALF];
+#pragma unroll
+    for (int g = 0; g < HALF; ++g)
+      if (v + (h + g) * NT < whole) x[g] = load16_any(row + (v + (h + g) * NT) * V);
+#pragma unroll
+    for (int g = 0; g < HALF; ++g)
+      if (v + (h + g) * NT < whole) take(x[g], h + g);
+  }
   if (tid < left) {  // (the classes behind the last vector: of the threads' first streams)
     const float z = Elem<T>::load(row + whole * V + tid);
     m[0] = fmaxf(m[0], z);
-    s[0].template add<1>(&z, sc);
+    refer(z);
+    st[0] += __builtin_amdgcn_exp2f((z - ref) * sc.t);
   }
   if (tid == 0) sh.taken = 0;
   uint32_t key[G];
+  float all = 0.f, tm = m[0];
 #pragma unroll
-  for (int g = 0; g < G; ++g) key[g] = order_key(m[g]);
+  for (int g = 0; g < G; ++g) {
+    key[g] = order_key(m[g]);
+    all += st[g];
+    tm = fmaxf(tm, m[g]);
+  }
+  {
+    const float most = quick_max(tm), least = -quick_max(tid < kk ? -tm : -INFINITY);
+    if (lane == 0) sh.count[1][wave] = __float_as_int(most), sh.count[1][4 + wave] = __float_as_int(least);
+  }
   // A sum is NaN where a logit is NaN or +infinity: maxima say nothing then.
-  const float all = (s[0].st + s[1].st) + (s[2].st + s[3].st);
   const bool odd = __syncthreads_or(!(all == all));
   Sums<1> rest;
   bool done = false;
   if (!odd) {
-    // The bound: at least kk maxima reach lo, hardly more than kk if possible; fewer than kk reach hi.
-    {
-      const float tm = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
-      const float most = quick_max(tm), least = -quick_max(tid < kk ? -tm : -INFINITY);
-      if (lane == 0) sh.count[1][wave] = __float_as_int(most), sh.count[1][4 + wave] = __float_as_int(least);
-    }
-    __syncthreads();
     float most = -INFINITY, least = INFINITY;
     for (int w = 0; w < 4; ++w) {
       most = fmaxf(most, __int_as_float(sh.count[1][w]));
       least = fminf(least, __int_as_float(sh.count[1][4 + w]));
     }
-    uint32_t lo = order_key(least), hi = order_key(most) + 1;  // (the first kk threads' maxima reach lo)
-    const int enough = kk + kk / 2 + 16;
-    uint32_t mid = lo;
-    int reach = 0, turn = 0;
-    bool tie = false;
-    while (true) {
-      int c = 0;
-#pragma unroll
-      for (int g = 0; g < G; ++g) c += __popcll(__ballot(key[g] >= mid));
-      if (lane == 0) sh.count[turn][8 + wave] = c;
-      __syncthreads();
-      c = (sh.count[turn][8] + sh.count[turn][9]) + (sh.count[turn][10] + sh.count[turn][11]);
-      turn ^= 1;
-      if (c >= kk) lo = mid, reach = c;
-      else hi = mid;
-      if (reach <= enough) break;
-      if (hi - lo <= 1) {
-        tie = true;
-        break;
-      }
-      mid = lo + ((hi - lo) >> 1);
-    }
-    const uint32_t bound = tie ? hi : lo;
+    bool tie;
+    const uint32_t lo = find_bound<G>(key, order_key(least), order_key(most) + 1, kk, &tie, sh);  // (the first kk threads' maxima reach `least`)
+    const uint32_t bound = tie ? lo + 1 : lo;
     // the streams that are read again, listed in a fixed order; the others' sums stay
+    uint64_t votes[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      votes[g] = __ballot(key[g] >= bound);
+      if (lane == 0) sh.count[0][16 + g * 4 + wave] = __popcll(votes[g]);
+    }
+    __syncthreads();
+    rest.ref = ref;
+    rest.lim = lim;
     int owners = 0;
-    {
-      uint64_t votes[G];
-      __syncthreads();
 #pragma unroll
-      for (int g = 0; g < G; ++g) {
-        votes[g] = __ballot(key[g] >= bound);
-        if (lane == 0) sh.count[0][g * 4 + wave] = __popcll(votes[g]);
+    for (int g = 0; g < G; ++g) {
+      int at = owners;
+      for (int w = 0; w < 4; ++w) {
+        const int c = sh.count[0][16 + g * 4 + w];
+        at += w < wave ? c : 0;
+        owners += c;
       }
-      __syncthreads();
-#pragma unroll
-      for (int g = 0; g < G; ++g) {
-        int at = owners;
-        for (int w = 0; w < wave; ++w) at += sh.count[0][g * 4 + w];
-        if (key[g] >= bound) sh.owner[at + __popcll(votes[g] & ((1ull << lane) - 1))] = static_cast<uint16_t>(tid * G + g);
-        else rest.join(s[g], sc);
-        for (int w = 0; w < 4; ++w) owners += sh.count[0][g * 4 + w];
-      }
+      if (key[g] >= bound) sh.owner[at + __popcll(votes[g] & ((1ull << lane) - 1))] = static_cast<uint16_t>(tid * G + g);
+      else rest.st += st[g];
     }
     __syncthreads();
     auto candidate = [&](float x, int i) __attribute__((always_inline)) {
@@ -448,14 +504,7 @@ __global__ __launch_bounds__(kTopkThreads) void topk_rows_kernel(const TopkArgs 
     const int cands = sh.taken;
     if (cands <= kTopkCand) {
       done = true;
-      for (int c = tid; c < cands; c += NT) {
-        const unsigned long long mine = sh.cand[c];
-        int rank = 0;
-        for (int j = 0; j < cands; ++j) rank += sh.cand[j] > mine;
-        if (rank < kk) out.put(rank, sh.value[c], static_cast<int>(~static_cast<uint32_t>(mine)));
-        else sh.spare[rank - kk] = sh.value[c];
-      }
-      __syncthreads();
+      put_ranked(cands, kk, out, sh);
       for (int c = tid; c < cands - kk; c += NT) rest.template add<1>(&sh.spare[c], sc);
       if (cands < kk) {  // (many equal maxima)
         const int last = take_equal<T, MODE>(row, C, lo, kk - cands, cands, out, sh);
@@ -475,19 +524,97 @@ __global__ __launch_bounds__(kTopkThreads) void topk_rows_kernel(const TopkArgs 
       a.indices[static_cast<int64_t>(n) * a.k + r] = -1;
     }
   }
-  if (MODE != kTopkSlices && a.tail == nullptr) return;
-  if (MODE == kTopkJoin && tid < a.slices) {
+  if (MODE == kTopkRows && a.tail == nullptr) return;
+  __syncthreads();
+  const RowSums sum = block_sums<1, NT>(rest, 0.0, false, sc, sh.red);
+  if (tid != 0) return;
+  if (MODE == kTopkSlices) a.part_sums[static_cast<int64_t>(n) * a.slices + slice] = sum;
+  else a.tail[n] = tail_of(sum, a.temperature);
+}
+
+// The largest of a row's slices' largest logits: kJoin of them a thread at most, in registers (slices in their order, each in its own:
+// equal logits lie in the order of their classes).  One workgroup per row.
+constexpr int kJoin = 16;
+__global__ __launch_bounds__(kTopkThreads) void topk_join_kernel(const TopkArgs a) {
+  constexpr int NT = kTopkThreads;
+  __shared__ TopkShared sh;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = blockIdx.x;
+  const int total = a.slices * a.k;  // (at least k of them logits: every slice but the last has k)
+  const float* list = a.part_values + static_cast<int64_t>(n) * total;
+  const TopkOut<kTopkJoin> out{a, n, 0};
+  Scales sc;
+  sc.t = sc.one = kLog2e / a.temperature;
+  sc.slack = 20.f / sc.t;
+  float z[kJoin];
+  uint32_t key[kJoin], most = 0;
+#pragma unroll
+  for (int g = 0; g < kJoin; ++g) {
+    const int i = g * NT + tid;
+    z[g] = i < total ? list[i] : -INFINITY;
+    key[g] = i < total ? order_key(z[g]) : 0;
+    most = max(most, key[g]);
+  }
+  if (tid == 0) sh.taken = 0;
+  // of the first slice's k logits the last is one that k reach
+  const uint32_t least = order_key(list[a.k - 1]);
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), off, 64)));
+  if (lane == 0) sh.count[1][wave] = static_cast<int>(most);
+  __syncthreads();
+  for (int w = 0; w < 4; ++w) most = max(most, static_cast<uint32_t>(sh.count[1][w]));
+  bool tie;
+  const uint32_t lo = find_bound<kJoin>(key, least, most + 1, a.k, &tie, sh);
+  const uint32_t bound = tie ? lo + 1 : lo;
+#pragma unroll
+  for (int g = 0; g < kJoin; ++g)
+    if (key[g] >= bound) {
+      const int at = atomicAdd(&sh.taken, 1);
+      if (at < kTopkCand) {
+        sh.cand[at] = static_cast<unsigned long long>(key[g]) << 32 | ~static_cast<uint32_t>(g * NT + tid);
+        sh.value[at] = z[g];
+      }
+      z[g] = -INFINITY;
+    }
+  __syncthreads();
+  const int cands = min(sh.taken, kTopkCand);
+  put_ranked(cands, a.k, out, sh);
+  if (cands < a.k) {  // the rest from the equal ones, in their order
+    const int need = a.k - cands;
+    uint64_t votes[kJoin];
+#pragma unroll
+    for (int g = 0; g < kJoin; ++g) {
+      votes[g] = __ballot(key[g] == lo);
+      if (lane == 0) sh.count[0][g * 4 + wave] = __popcll(votes[g]);
+    }
+    __syncthreads();
+    int before = 0;
+#pragma unroll
+    for (int g = 0; g < kJoin; ++g) {
+      int pos = before + __popcll(votes[g] & ((1ull << lane) - 1));
+      for (int w = 0; w < 4; ++w) {
+        const int c = sh.count[0][g * 4 + w];
+        pos += w < wave ? c : 0;
+        before += c;
+      }
+      if (key[g] == lo && pos < need) {
+        out.put(cands + pos, z[g], g * NT + tid);
+        z[g] = -INFINITY;
+      }
+    }
+  }
+  if (a.tail == nullptr) return;
+  Sums<1> rest;
+  rest.template add<kJoin>(z, sc);
+  for (int c = tid; c < cands - a.k; c += NT) rest.template add<1>(&sh.spare[c], sc);
+  if (tid < a.slices) {
     const RowSums part = a.part_sums[static_cast<int64_t>(n) * a.slices + tid];
     Sums<1> p;
     p.ref = part.ref;
     p.st = part.st;
     rest.join(p, sc);
   }
-  __syncthreads();
   const RowSums sum = block_sums<1, NT>(rest, 0.0, false, sc, sh.red);
-  if (tid != 0) return;
-  if (MODE == kTopkSlices) a.part_sums[static_cast<int64_t>(n) * a.slices + slice] = sum;
-  else a.tail[n] = sum.st == 0.f ? -INFINITY : static_cast<float>(static_cast<double>(sum.ref) / a.temperature + log(static_cast<double>(sum.st)));
+  if (tid == 0) a.tail[n] = tail_of(sum, a.temperature);
 }
 
 // What the gradient pass needs of its row: d = coef_t * exp((z - ref) / T) + coef_1 * exp(z - ref) - offset (EXPS = 1: both
@@ -987,7 +1114,7 @@ static void topk_slicing(int N, int C, int k, TopkArgs* a, void* workspace, size
 #endif
   *bytes = 0;
   if (N > most_rows || C < least) return;
-  const int64_t want = std::min<int64_t>({ceil_div(target, N), ceil_div(C, narrow), kTopkThreads, std::max(2, 16384 / k)});
+  const int64_t want = std::min<int64_t>({ceil_div(target, N), ceil_div(C, narrow), kTopkThreads, kJoin * kTopkThreads / k});
   if (want < 2) return;
   const int width = static_cast<int>(align_up(static_cast<size_t>(ceil_div(C, want)), 32)), slices = static_cast<int>(ceil_div(C, width));
   const size_t list = align_up(static_cast<size_t>(N) * slices * k * 4, 256);
@@ -1007,10 +1134,7 @@ static void topk_run(TopkArgs a, hipStream_t s) {
     return;
   }
   RN50_LAUNCH("topk_rows", (topk_rows_kernel<T, kTopkSlices>), dim3(a.slices, a.N), dim3(kTopkThreads), 0, s, a);
-  a.logits = a.part_values;
-  a.C = a.slices * a.k;
-  a.ld = a.C;
-  RN50_LAUNCH("topk_rows", (topk_rows_kernel<float, kTopkJoin>), row_grid(a.N), dim3(kTopkThreads), 0, s, a);
+  RN50_LAUNCH("topk_rows", topk_join_kernel, dim3(a.N), dim3(kTopkThreads), 0, s, a);
 }
 
 static int check_rows(const char* who, int N, int C, int dtype, const void* logits, int64_t ld) {
