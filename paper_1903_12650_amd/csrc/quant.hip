@@ -3,6 +3,7 @@
 #include <stdlib.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "common.h"
 #include "conv_internal.h"
@@ -119,10 +120,10 @@ struct ProductArgs {
 };
 
 // Tile BM x BN, WM x WN waves of 32x32 blocks (v_mfma_i32_32x32x32_i8).  A chunk is 128 bytes of every row of both operands, brought
-// straight into LDS (16 bytes a lane) into one of two buffers while the other is multiplied: one barrier a chunk.  Piece p (16 bytes) of
+// straight into LDS (16 bytes a lane) into one of RING buffers while another is multiplied: one barrier a chunk.  Piece p (16 bytes) of
 // row r lies in slot p ^ ((r >> 1) & 7), which spreads the fragment reads (32 rows of one piece) over all banks.  Rows past the last and
 // the second half of a last chunk of 64 bytes are zeros.  The weights are the first operand, so that a lane has 4 consecutive columns of one row.
-template <typename T, int BM, int BN, int WM, int WN>
+template <typename T, int BM, int BN, int WM, int WN, int RING>
 __global__ __launch_bounds__(64 * WM * WN) void matmul_i8_kernel(const ProductArgs a) {
   constexpr int NT = 64 * WM * WN, RPL = NT / 8, RA = BM / RPL, RB = BN / RPL, TM = BM / WM / 32, TN = BN / WN / 32;
   constexpr int STAGE = (BM + BN) * 128;
@@ -148,8 +149,8 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_i8_kernel(const ProductAr
   typedef __attribute__((address_space(3))) unsigned char* lds_byte_ptr;
   const uint32_t dst = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_byte_ptr)smem)) + static_cast<uint32_t>(wave) * 1024u);
   const int chunks = (a.Kp + 127) >> 7;
-  auto load = [&](int c) __attribute__((always_inline)) {
-    const uint32_t so = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(c) * 128u), to = dst + static_cast<uint32_t>(c & 1) * STAGE;
+  auto load = [&](int c, int buffer) __attribute__((always_inline)) {
+    const uint32_t so = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(c) * 128u), to = dst + static_cast<uint32_t>(buffer) * STAGE;
     const bool in = c * 128 + piece * 16 < a.Kp;
 #pragma unroll
     for (int i = 0; i < RA; ++i) buffer_load16_to_lds(rsA, to + i * (RPL * 128), in ? at_a[i] : kOob, so);
@@ -166,12 +167,17 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_i8_kernel(const ProductAr
   int frag[4];
 #pragma unroll
   for (int kk = 0; kk < 4; ++kk) frag[kk] = (lane & 31) * 128 + (((2 * kk + (lane >> 5)) ^ ((lane >> 1) & 7)) << 4);
-  load(0);
+#pragma unroll
+  for (int c = 0; c < RING - 1; ++c)
+    if (c < chunks) load(c, c);
+  int now = 0, next = RING - 1;  // buffers of this chunk and of the one that is requested
   for (int c = 0; c < chunks; ++c) {
-    wait_loads_then_barrier<0>();  // this chunk is there, and the other buffer has been read
-    if (c + 1 < chunks) load(c + 1);
-    const unsigned char* ta = smem + (c & 1) * STAGE + wm * (BM / WM) * 128;
-    const unsigned char* tb = smem + (c & 1) * STAGE + BM * 128 + wn * (BN / WN) * 128;
+    ring_wait<RING, RA + RB>(chunks - 1 - c);  // this chunk is there, and the buffer of the one before it has been read
+    if (c + RING - 1 < chunks) load(c + RING - 1, next);
+    const unsigned char* ta = smem + now * STAGE + wm * (BM / WM) * 128;
+    const unsigned char* tb = smem + now * STAGE + BM * 128 + wn * (BN / WN) * 128;
+    now = now + 1 == RING ? 0 : now + 1;
+    next = next + 1 == RING ? 0 : next + 1;
     i32x4 fa[2][TM], fb[2][TN];
     auto read = [&](int kk) __attribute__((always_inline)) {
 #pragma unroll
@@ -191,7 +197,7 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_i8_kernel(const ProductAr
   }
   // Output: a wave's 32 rows at a time through LDS (its own part of it), whole rows of the wave's columns from there.
   constexpr int WC = BN / WN, PITCH = WC + 4;  // floats (rows 16 bytes further along the banks)
-  static_assert(WM * WN * 32 * PITCH * 4 <= 2 * STAGE, "the output stage fits the ring");
+  static_assert(WM * WN * 32 * PITCH * 4 <= RING * STAGE, "the output stage fits the ring");
   lds_reads_then_barrier();
   float* mine = reinterpret_cast<float*>(smem) + wave * 32 * PITCH;
   constexpr int V = Elem<T>::VEC, LPR = WC / V, RPP = 64 / LPR;  // lanes a row, rows a pass
@@ -238,6 +244,116 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_i8_kernel(const ProductAr
   }
 }
 
+// Few rows (M <= 16 * MB): the weights go by once, bound by memory; a workgroup owns 16 columns, its waves a part of K each.  A wave's lane reads
+// 16 bytes of column lane % 16 at 16 * (lane / 16) of a step of 64, straight into the matrix cores (v_mfma_i32_16x16x64_i8), U steps'
+// loads in flight; the rows of activations are the second operand.  The waves' integer sums are added through LDS.
+// X: the activations are float or bfloat16 and quantized here (up to kFusedRows rows, into LDS), while the first weights are on their way:
+// no second launch; every workgroup does so for itself.
+constexpr int kFewThreads = 512, kFewWaves = kFewThreads / 64, kFusedRows = 4;
+struct FewArgs {
+  ProductArgs p;
+  const void* x;
+  int64_t ldx;
+  int K;
+};
+template <typename T, int MB, typename X>
+__global__ __launch_bounds__(kFewThreads) void matmul_i8_few_kernel(const FewArgs a) {
+  constexpr bool FUSED = !std::is_void<X>::value;
+  constexpr int U = 8;
+  extern __shared__ __align__(16) unsigned char smem[];
+  __shared__ int red[kFewWaves][MB][256];
+  __shared__ float scale_s[16 * MB];
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const int n0 = blockIdx.x * 16, M = a.p.M, N = a.p.N, Kp = a.p.Kp;
+  const int steps = Kp >> 6, from = steps * wave / kFewWaves, to = steps * (wave + 1) / kFewWaves;
+  const int8_t* wp = a.p.w + static_cast<int64_t>(min(n0 + (lane & 15), N - 1)) * Kp + 16 * (lane >> 4);
+  i32x4 fw[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+    if (from + u < to) fw[u] = *reinterpret_cast<const i32x4*>(wp + (from + u) * 64);
+  const int8_t* xq[MB];  // this lane's rows
+  if constexpr (FUSED) {
+    constexpr int V = Elem<X>::VEC;
+    const int whole = a.K / V, left = a.K - whole * V;
+    uint32_t top[kFusedRows];
+    float z_left[kFusedRows];
+#pragma unroll
+    for (int m = 0; m < kFusedRows; ++m) {
+      top[m] = 0;
+      z_left[m] = 0.f;
+      if (m < M) {
+        const X* row = static_cast<const X*>(a.x) + m * a.ldx;
+        for (int v = tid; v < whole; v += kFewThreads) top[m] = top_of<X>(top[m], load16_any(row + v * V));
+        if (tid < left) z_left[m] = Elem<X>::load(row + whole * V + tid);
+      }
+    }
+#pragma unroll
+    for (int m = 0; m < kFusedRows; ++m)
+      if (m < M) {
+        uint32_t t = max(top_float_bits<X>(top[m]), __float_as_uint(z_left[m]) & 0x7fffffffu);
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) t = max(t, static_cast<uint32_t>(__shfl_xor(static_cast<int>(t), off, 64)));
+        if (lane == 0) red[wave][0][m] = static_cast<int>(t);
+      }
+    __syncthreads();
+#pragma unroll
+    for (int m = 0; m < kFusedRows; ++m)
+      if (m < M) {
+        uint32_t t = 0;
+#pragma unroll
+        for (int w = 0; w < kFewWaves; ++w) t = max(t, static_cast<uint32_t>(red[w][0][m]));
+        float inv;
+        const float s = i8_scale(t, &inv);
+        const X* row = static_cast<const X*>(a.x) + m * a.ldx;
+        int8_t* out = reinterpret_cast<int8_t*>(smem) + m * Kp;
+        for (int v = tid; v < whole; v += kFewThreads) store_quantized<X>(out + v * V, load16_any(row + v * V), inv);
+        if (tid < Kp - whole * V) out[whole * V + tid] = static_cast<int8_t>(tid < left && inv != 0.f ? i8_of(z_left[m], inv) : 0u);
+        if (tid == 0) scale_s[m] = s;
+      }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int b = 0; b < MB; ++b) {
+    const int m = min(b * 16 + (lane & 15), M - 1);
+    xq[b] = (FUSED ? reinterpret_cast<const int8_t*>(smem) : a.p.q) + static_cast<int64_t>(m) * Kp + 16 * (lane >> 4);
+  }
+  i32x4 acc[MB];
+#pragma unroll
+  for (int b = 0; b < MB; ++b) acc[b] = i32x4{0, 0, 0, 0};
+  for (int s = from; s < to; s += U) {
+    i32x4 w[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) w[u] = fw[u];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (s + U + u < to) fw[u] = *reinterpret_cast<const i32x4*>(wp + (s + U + u) * 64);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (s + u < to) {
+#pragma unroll
+        for (int b = 0; b < MB; ++b)
+          acc[b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[u], *reinterpret_cast<const i32x4*>(xq[b] + (s + u) * 64), acc[b], 0, 0, 0);
+      }
+  }
+  // column 4 * (lane / 16) + i of the 16, row lane % 16
+#pragma unroll
+  for (int b = 0; b < MB; ++b)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) red[wave][b][(lane & 15) * 16 + 4 * (lane >> 4) + i] = acc[b][i];
+  __syncthreads();
+#pragma unroll
+  for (int e = tid; e < MB * 256; e += kFewThreads) {
+    const int b = e >> 8, m = b * 16 + ((e >> 4) & 15), n = n0 + (e & 15);
+    if (m < M && n < N) {
+      int sum = 0;
+#pragma unroll
+      for (int w = 0; w < kFewWaves; ++w) sum += red[w][b][e & 255];
+      const float s = FUSED ? scale_s[m] : a.p.qs[m];
+      Elem<T>::store(static_cast<T*>(a.p.y) + m * a.p.ldy + n, fmaf(static_cast<float>(sum) * s, a.p.ws[n], a.p.bias ? a.p.bias[n] : 0.f));
+    }
+  }
+}
+
 static int check_quant(const char* who, int M, int K, int dtype, const void* x, int64_t ldx) {
   RN50_REQUIRE(dtype == RN50_F32 || dtype == RN50_BF16, RN50_ERR_INVALID, "%s: dtype %d", who, dtype);
   RN50_REQUIRE(M > 0 && K > 0, RN50_ERR_INVALID, "%s: non-positive size", who);
@@ -279,31 +395,63 @@ static void quant_run(int M, int K, int dtype, const void* x, int64_t ldx, int8_
   if (dtype == RN50_BF16) quant_typed(M, K, static_cast<const uint16_t*>(x), ldx, q, scale, s);
   else quant_typed(M, K, static_cast<const float*>(x), ldx, q, scale, s);
 }
-template <typename T, int BM, int BN, int WM, int WN>
+template <typename T, int BM, int BN, int WM, int WN, int RING>
 static void product_tile(ProductArgs a, hipStream_t s) {
-  constexpr int lds = 2 * (BM + BN) * 128;
+  constexpr int lds = RING * (BM + BN) * 128;
   a.tiles_m = static_cast<int>(ceil_div(a.M, BM));
   a.tiles_n = static_cast<int>(ceil_div(a.N, BN));
-  const auto kernel = matmul_i8_kernel<T, BM, BN, WM, WN>;
+  const auto kernel = matmul_i8_kernel<T, BM, BN, WM, WN, RING>;
   allow_big_lds(kernel, lds);
   RN50_LAUNCH("matmul_i8", kernel, dim3(static_cast<unsigned>(a.tiles_m) * a.tiles_n), dim3(64 * WM * WN), lds, s, a);
+}
+template <typename T, int MB, typename X>
+static void few_rows(const FewArgs& a, hipStream_t s) {
+  const auto kernel = matmul_i8_few_kernel<T, MB, X>;
+  const int lds = std::is_void<X>::value ? 0 : static_cast<int>(align_up(static_cast<size_t>(a.p.M) * a.p.Kp, 16));
+  if (lds) allow_big_lds(kernel, lds);
+  RN50_LAUNCH("matmul_i8", kernel, dim3(static_cast<unsigned>(ceil_div(a.p.N, 16))), dim3(kFewThreads), lds, s, a);
+}
+template <typename T>
+static void few_rows_quantized(const ProductArgs& p, hipStream_t s) {
+  const FewArgs a{p, nullptr, 0, 0};
+  if (p.M <= 16) few_rows<T, 1, void>(a, s);
+  else if (p.M <= 32) few_rows<T, 2, void>(a, s);
+  else few_rows<T, 4, void>(a, s);
+}
+constexpr int kFewRows = 64;
+// Whether fc_i8_fwd takes its rows as they are.
+static bool few_fused(int M, int K) {
+  int64_t most = 16384;
+#ifdef RN50_TUNING  // tuning builds only: RN50_I8_FUSED=numbers
+  if (const char* e = getenv("RN50_I8_FUSED")) most = atoi(e);
+#endif
+  return M <= kFusedRows && static_cast<int64_t>(M) * static_cast<int64_t>(quant_i8_row_bytes(K)) <= most;
 }
 template <typename T>
 static void product_typed(const ProductArgs& a, hipStream_t s) {
 #ifdef RN50_TUNING  // tuning builds only: RN50_I8_TILE=rows
   if (const char* e = getenv("RN50_I8_TILE")) {
     switch (atoi(e)) {
-      case 256: return product_tile<T, 256, 256, 2, 4>(a, s);
-      case 192: return product_tile<T, 256, 128, 4, 2>(a, s);
-      case 128: return product_tile<T, 128, 128, 2, 2>(a, s);
-      case 64: return product_tile<T, 64, 64, 2, 2>(a, s);
+      case 256: return product_tile<T, 256, 256, 2, 4, 2>(a, s);
+      case 128: return product_tile<T, 128, 128, 2, 2, 2>(a, s);
+      case 12864: return product_tile<T, 128, 64, 2, 2, 3>(a, s);
+      case 64: return product_tile<T, 64, 64, 2, 2, 2>(a, s);
+      case 1: return few_rows_quantized<T>(a, s);
     }
   }
 #endif
+  if (a.M <= kFewRows) return few_rows_quantized<T>(a, s);
+  // The largest tile of which there are enough for the 256 compute units (256x256, 128x128, 128x64, 64x64 in us): 4096^3 65, 79, 90, 106;
+  // 5000 x 5000 -> 1000 (80, 320, 640, 1264 tiles) 66, 40, 47, 54; 300 x 8192 -> 8192 (64, 192, 384, 640) 96, 42, 34, 39; 512 x 4096 -> 4096
+  // (32, 128, 256, 512) 50, 23, 17, 18; 1000 x 2048 -> 1000 (16, 64, 128, 256) 29, 13, 9.4, 7.5.  The 256x256 one leaves a unit a single
+  // workgroup, so only where the last round is full enough.  Three or four buffers instead of two cost the workgroups that share a unit:
+  // 4096^3 128x128 79 -> 99, 64x64 106 -> 110, 118.
   auto tiles = [&](int bm, int bn) { return ceil_div(a.M, bm) * ceil_div(a.N, bn); };
-  if (tiles(256, 256) >= 256) product_tile<T, 256, 256, 2, 4>(a, s);
-  else if (tiles(128, 128) >= 256) product_tile<T, 128, 128, 2, 2>(a, s);
-  else product_tile<T, 64, 64, 2, 2>(a, s);
+  const int64_t large = tiles(256, 256);
+  if (large >= 256 && large * 5 >= ceil_div(large, 256) * 256 * 4) product_tile<T, 256, 256, 2, 4, 2>(a, s);
+  else if (tiles(128, 128) >= 256) product_tile<T, 128, 128, 2, 2, 2>(a, s);
+  else if (tiles(128, 64) >= 256) product_tile<T, 128, 64, 2, 2, 3>(a, s);
+  else product_tile<T, 64, 64, 2, 2, 2>(a, s);
 }
 static void product_run(int M, int N, int K, const int8_t* q, const float* qs, const int8_t* w, const float* ws, const float* bias, int y_dtype,
                         void* y, int64_t ldy, hipStream_t s) {
@@ -353,6 +501,14 @@ extern "C" int fc_i8_fwd(int M, int N, int K, int x_dtype, const void* x, int64_
   hipStream_t s = static_cast<hipStream_t>(stream);
   int8_t* q = static_cast<int8_t*>(workspace);
   float* qs = reinterpret_cast<float*>(q + align_up(static_cast<size_t>(M) * quant_i8_row_bytes(K), 256));
+  if (few_fused(M, K)) {
+    const FewArgs a{{nullptr, w, nullptr, w_scale, bias, y, ldy, M, N, static_cast<int>(quant_i8_row_bytes(K)), 0, 0}, x, ldx, K};
+    if (x_dtype == RN50_BF16 && y_dtype == RN50_BF16) few_rows<uint16_t, 1, uint16_t>(a, s);
+    else if (x_dtype == RN50_BF16) few_rows<float, 1, uint16_t>(a, s);
+    else if (y_dtype == RN50_BF16) few_rows<uint16_t, 1, float>(a, s);
+    else few_rows<float, 1, float>(a, s);
+    return launch_status("fc_i8_fwd");
+  }
   quant_run(M, K, x_dtype, x, ldx, q, qs, s);
   product_run(M, N, K, q, qs, w, w_scale, bias, y_dtype, y, ldy, s);
   return launch_status("fc_i8_fwd");
