@@ -215,46 +215,9 @@ struct TopkOut {
   }
 };
 
-// A key that at least kk of the workgroup's keys reach, hardly more if possible; where that takes a key that many have (`tie`), fewer than
-// kk reach the one after it.  lo: kk keys reach it; hi: none does.  Every thread calls it, behind a barrier.
-template <int G>
-__device__ __forceinline__ uint32_t find_bound(const uint32_t* key, uint32_t lo, uint32_t hi, int kk, bool* tie, TopkShared& sh) {
+// Of 256 bins, one a thread, with `mine` in this thread's: how many are in this and all higher ones.  Behind it the waves are past a barrier.
+__device__ __forceinline__ int sum_from_here(int mine, TopkShared& sh) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int enough = kk + kk / 2 + 16;
-  uint32_t mid = lo;
-  int reach = 0, turn = 0;
-  while (true) {
-    int c = 0;
-#pragma unroll
-    for (int g = 0; g < G; ++g) c += __popcll(__ballot(key[g] >= mid));
-    if (lane == 0) sh.count[turn][8 + wave] = c;
-    __syncthreads();
-    c = (sh.count[turn][8] + sh.count[turn][9]) + (sh.count[turn][10] + sh.count[turn][11]);
-    turn ^= 1;
-    if (c >= kk) lo = mid, reach = c;
-    else hi = mid;
-    *tie = hi - lo <= 1 && reach > enough;
-    if (reach <= enough || *tie) break;
-    mid = lo + ((hi - lo) >> 1);
-  }
-  return lo;
-}
-// Candidates in order: the first kk to the output, the others' values to `spare`.  Their keys, lo to hi, fall into 256 bins; a candidate comes
-// behind those of higher bins, and behind the larger ones of its own, which it looks through.  (Looking through all of them took 4 us
-// for 147 candidates, 13 for 365.)  Every thread calls it, behind a barrier; `hist` is zero and `first` -1 then.
-static_assert(kTopkThreads == 256, "a bin a thread");
-template <int MODE>
-__device__ __forceinline__ void put_ranked(int cands, int kk, uint32_t lo, uint32_t hi, const TopkOut<MODE>& out, TopkShared& sh) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int shift = max(0, 24 - __clz(static_cast<int>(hi - lo)));
-  for (int c = tid; c < cands; c += kTopkThreads) {
-    const uint32_t bin = (static_cast<uint32_t>(sh.cand[c] >> 32) - lo) >> shift;
-    atomicAdd(&sh.hist[bin], 1u);
-    sh.next[c] = static_cast<int16_t>(atomicExch(&sh.first[bin], c));
-  }
-  __syncthreads();
-  // of every bin, how many are in higher ones
-  const int mine = static_cast<int>(sh.hist[tid]);
   int sum = mine;
 #pragma unroll
   for (int off = 1; off < 64; off <<= 1) {
@@ -264,6 +227,64 @@ __device__ __forceinline__ void put_ranked(int cands, int kk, uint32_t lo, uint3
   if (lane == 0) sh.count[0][wave] = sum;
   __syncthreads();
   for (int w = wave + 1; w < 4; ++w) sum += sh.count[0][w];
+  return sum;
+}
+// A key that at least kk of the workgroup's keys reach, hardly more if possible; where that takes a key that many have (`tie`), fewer than
+// kk reach the one after it.  At least kk keys reach lo, none passes top.  The keys' bins (256 from lo to top) mostly hold few enough
+// where the kk-th lies; otherwise its bin is halved until they do.  Every thread calls it, behind a barrier, with `hist` zero, as it
+// leaves it.
+template <int G>
+__device__ __forceinline__ uint32_t find_bound(const uint32_t* key, uint32_t lo, uint32_t top, int kk, bool* tie, TopkShared& sh) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int enough = kk + kk / 2 + 16;
+  const int shift = max(0, 24 - __clz(static_cast<int>(top - lo)));
+#pragma unroll
+  for (int g = 0; g < G; ++g)
+    if (key[g] >= lo) atomicAdd(&sh.hist[(key[g] - lo) >> shift], 1u);
+  __syncthreads();
+  const int mine = static_cast<int>(sh.hist[tid]);
+  sh.hist[tid] = 0;
+  const int from_here = sum_from_here(mine, sh);
+  if (from_here >= kk && from_here - mine < kk) {
+    sh.found[0] = tid;
+    sh.found[1] = from_here;
+  }
+  __syncthreads();
+  int reach = static_cast<int>(sh.found[1]);
+  lo += sh.found[0] << shift;
+  *tie = false;
+  if (reach <= enough) return lo;
+  uint32_t hi = lo + (1u << shift);
+  for (int turn = 0; hi - lo > 1 && reach > enough; turn ^= 1) {
+    const uint32_t mid = lo + ((hi - lo) >> 1);
+    int c = 0;
+#pragma unroll
+    for (int g = 0; g < G; ++g) c += __popcll(__ballot(key[g] >= mid));
+    if (lane == 0) sh.count[turn][8 + wave] = c;
+    __syncthreads();
+    c = (sh.count[turn][8] + sh.count[turn][9]) + (sh.count[turn][10] + sh.count[turn][11]);
+    if (c >= kk) lo = mid, reach = c;
+    else hi = mid;
+  }
+  *tie = reach > enough;
+  return lo;
+}
+// Candidates in order: the first kk to the output, the others' values to `spare`.  Their keys, lo to hi, fall into 256 bins; a candidate comes
+// behind those of higher bins, and behind the larger ones of its own, which it looks through.  (Looking through all of them took 4 us
+// for 147 candidates, 13 for 365.)  Every thread calls it, behind a barrier; `hist` is zero and `first` -1 then.
+static_assert(kTopkThreads == 256, "a bin a thread");
+template <int MODE>
+__device__ __forceinline__ void put_ranked(int cands, int kk, uint32_t lo, uint32_t hi, const TopkOut<MODE>& out, TopkShared& sh) {
+  const int tid = threadIdx.x;
+  const int shift = max(0, 24 - __clz(static_cast<int>(hi - lo)));
+  for (int c = tid; c < cands; c += kTopkThreads) {
+    const uint32_t bin = (static_cast<uint32_t>(sh.cand[c] >> 32) - lo) >> shift;
+    atomicAdd(&sh.hist[bin], 1u);
+    sh.next[c] = static_cast<int16_t>(atomicExch(&sh.first[bin], c));
+  }
+  __syncthreads();
+  // of every bin, how many are in higher ones
+  const int mine = static_cast<int>(sh.hist[tid]), sum = sum_from_here(mine, sh);
   sh.hist[tid] = static_cast<uint32_t>(sum - mine);
   __syncthreads();
   for (int c = tid; c < cands; c += kTopkThreads) {
@@ -452,10 +473,12 @@ __global__ __launch_bounds__(kTopkThreads) void topk_rows_kernel(const TopkArgs 
   }
   {
     const float most = quick_max(tm), least = -quick_max(tid < kk ? -tm : -INFINITY);
-    if (lane == 0) sh.count[1][wave] = __float_as_int(most), sh.count[1][4 + wave] = __float_as_int(least);
+    // (a sum is NaN where a logit is NaN or +infinity: maxima say nothing then)
+    const uint64_t odd = __ballot(!(all == all));
+    if (lane == 0) sh.count[1][wave] = __float_as_int(most), sh.count[1][4 + wave] = __float_as_int(least), sh.count[1][12 + wave] = odd != 0;
   }
-  // A sum is NaN where a logit is NaN or +infinity: maxima say nothing then.
-  const bool odd = __syncthreads_or(!(all == all));
+  __syncthreads();
+  const bool odd = (sh.count[1][12] | sh.count[1][13]) | (sh.count[1][14] | sh.count[1][15]);
   Sums<1> rest;
   bool done = false;
   if (!odd) {
@@ -465,7 +488,7 @@ __global__ __launch_bounds__(kTopkThreads) void topk_rows_kernel(const TopkArgs 
       least = fminf(least, __int_as_float(sh.count[1][4 + w]));
     }
     bool tie;
-    const uint32_t top = order_key(most), lo = find_bound<G>(key, order_key(least), top + 1, kk, &tie, sh);  // (the first kk threads' maxima reach `least`)
+    const uint32_t top = order_key(most), lo = find_bound<G>(key, order_key(least), top, kk, &tie, sh);  // (the first kk threads' maxima reach `least`)
     const uint32_t bound = tie ? lo + 1 : lo;
     // the streams that are read again, listed in a fixed order; the others' sums stay
     uint64_t votes[G];
@@ -593,7 +616,7 @@ __global__ __launch_bounds__(kTopkThreads) void topk_join_kernel(const TopkArgs 
   __syncthreads();
   for (int w = 0; w < 4; ++w) most = max(most, static_cast<uint32_t>(sh.count[1][w]));
   bool tie;
-  const uint32_t lo = find_bound<kJoin>(key, least, most + 1, a.k, &tie, sh);
+  const uint32_t lo = find_bound<kJoin>(key, least, most, a.k, &tie, sh);
   const uint32_t bound = tie ? lo + 1 : lo;
 #pragma unroll
   for (int g = 0; g < kJoin; ++g)
