@@ -42,8 +42,6 @@ __device__ __forceinline__ float quick_max(float x) {
   x = fmaxf(x, lane_move<0x140>(x));
   return fmaxf(fmaxf(from_lane(x, 0), from_lane(x, 16)), fmaxf(from_lane(x, 32), from_lane(x, 48)));
 }
-// exp(x) for x <= 0 with the hardware's exponential; `scale` = log2(e) / T.
-__device__ __forceinline__ float exp_scaled(float x, float scale) { return __builtin_amdgcn_exp2f(x * scale); }
 
 // A workgroup for each of N rows, row blockIdx.y * gridDim.x + blockIdx.x.
 static dim3 row_grid(int N) { return N <= 65536 ? dim3(N) : dim3(65536, static_cast<unsigned>(ceil_div(N, 65536))); }
@@ -165,6 +163,8 @@ __device__ __forceinline__ uint32_t order_key(float x) {
   if (u == 0x80000000u) u = 0;
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
+// The least logit whose key reaches `key` (no NaN's).
+__device__ __forceinline__ float logit_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key); }
 constexpr uint32_t kKeyOfNothing = 0x007fffffu;  // order_key(-infinity)
 
 struct TopkArgs {
@@ -182,7 +182,7 @@ struct TopkArgs {
   RowSums* part_sums;
 };
 enum { kTopkRows, kTopkSlices, kTopkJoin };  // whole rows; slices of rows; the slices' largest logits
-constexpr int kTopkThreads = 256, kTopkCand = 1024, kTopkStreams = 8;  // threads of a row, candidates, streams of a thread
+constexpr int kTopkThreads = 256, kTopkCand = 768, kTopkStreams = 8;  // threads of a row, candidates, streams of a thread
 
 struct TopkShared {
   __align__(16) unsigned long long cand[kTopkCand];  // (key, ~class) of the logits that may be among the largest: larger is in front
@@ -341,7 +341,7 @@ __device__ __forceinline__ float tail_of(const RowSums& sum, float temperature) 
 // Any row, NaN and infinities among it: the key of the k-th largest logit digit by digit (four of 8 bits, a histogram each over the logits
 // that share the digits in front).  The row is read seven times; only rows that the way below cannot take come here.
 template <typename T, int MODE>
-__device__ __noinline__ void topk_any(const T* row, int C, int kk, bool want_tail, const Scales& sc, const TopkOut<MODE>& out, TopkShared& sh, Sums<1>& rest) {
+__device__ __forceinline__ void topk_any(const T* row, int C, int kk, bool want_tail, const Scales& sc, const TopkOut<MODE>& out, TopkShared& sh, Sums<1>& rest) {
   const int tid = threadIdx.x;
   uint32_t prefix = 0;
   int need = kk;  // how many are still to be taken among the logits that share the prefix
@@ -390,14 +390,14 @@ __device__ __noinline__ void topk_any(const T* row, int C, int kk, bool want_tai
   if (want_tail) add_rest(row, C, prefix, last, sc, rest);
 }
 
-// One workgroup per row (or slice of one).  The row goes by once in 2048 streams, eight a thread, each with its largest logit and its sum
+// One workgroup per row (or slice of one), eight on a compute unit.  The row goes by once in 2048 streams, eight a thread, each with its largest logit and its sum
 // of exponentials.  A bound below which no logit of the row's k largest can lie is the k-th largest of the streams' maxima, or a little
 // less: streams whose maximum reaches it (little more than k) are read again, from the caches, for the logits that reach it (little
 // more than k again), and these are put in order by counting.  Their streams' sums are taken anew without them: nothing is subtracted.
 // Where many maxima are equal (masks, ties), the logits above their value are the candidates and the rest of the k is taken from the
 // equal ones in the order of the classes.
 template <typename T, int MODE>
-__global__ __launch_bounds__(kTopkThreads) void topk_rows_kernel(const TopkArgs a) {
+__global__ __launch_bounds__(kTopkThreads, 8) void topk_rows_kernel(const TopkArgs a) {
   constexpr int V = Elem<T>::VEC, NT = kTopkThreads, G = kTopkStreams, HALF = G / 2;
   __shared__ TopkShared sh;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -490,6 +490,7 @@ __global__ __launch_bounds__(kTopkThreads) void topk_rows_kernel(const TopkArgs 
     bool tie;
     const uint32_t top = order_key(most), lo = find_bound<G>(key, order_key(least), top, kk, &tie, sh);  // (the first kk threads' maxima reach `least`)
     const uint32_t bound = tie ? lo + 1 : lo;
+    const float from = logit_of(bound);
     // the streams that are read again, listed in a fixed order; the others' sums stay
     uint64_t votes[G];
 #pragma unroll
@@ -532,7 +533,7 @@ __global__ __launch_bounds__(kTopkThreads) void topk_rows_kernel(const TopkArgs 
           if (vec[u] < whole) x[u] = load16_any(row + vec[u] * V);
           if (g == 0 && r == 0 && t < left) {
             const float z = Elem<T>::load(row + whole * V + t);
-            if (order_key(z) >= bound) candidate(z, whole * V + t);
+            if (z >= from) candidate(z, whole * V + t);
             else rest.template add<1>(&z, sc);
           }
         }
@@ -544,7 +545,7 @@ __global__ __launch_bounds__(kTopkThreads) void topk_rows_kernel(const TopkArgs 
         Elem<T>::unpack(x[u], z);
 #pragma unroll
         for (int j = 0; j < V; ++j)
-          if (order_key(z[j]) >= bound) {
+          if (z[j] >= from) {
             candidate(z[j], vec[u] * V + j);
             z[j] = -INFINITY;
           }
