@@ -574,3 +574,11 @@ def test_the_interface_refuses_before_it_launches(rn):
     assert raw.distill_fwd_bwd(ctypes.byref(d), o, None, o, None, None, None, o, o, None, None, z, None) == -1
     torch.cuda.synchronize()
     assert bool((out == 3.0).all())
+
+
+def test_the_example_learns(rn):
+    from paper_1903_12650_amd import distill_example
+    losses = distill_example.run(steps=40)
+    assert torch.isfinite(losses).all()
+    first, last = float(losses[:4].mean()), float(losses[-4:].mean())
+    assert last < 0.8 * first, (first, last)
