@@ -519,7 +519,7 @@ __global__ __launch_bounds__(kTopkThreads, 8) void topk_rows_kernel(const TopkAr
       }
     };
     const int rounds = max(1, (whole + G * NT - 1) / (G * NT));
-    constexpr int AHEAD = 4;  // vectors whose loads go out together
+    constexpr int AHEAD = 2;  // vectors whose loads go out together
     for (int i0 = tid; i0 < owners * rounds; i0 += AHEAD * NT) {
       Vec16 x[AHEAD];
       int vec[AHEAD];
