@@ -182,12 +182,12 @@ struct TopkArgs {
   RowSums* part_sums;
 };
 enum { kTopkRows, kTopkSlices, kTopkJoin };  // whole rows; slices of rows; the slices' largest logits
-constexpr int kTopkThreads = 256, kTopkCand = 768, kTopkStreams = 8;  // threads of a row, candidates, streams of a thread
+constexpr int kTopkThreads = 256, kTopkCand = 768, kTopkStreams = 4, kTopkOwners = 512;  // threads of a row, candidates, streams of a thread, those read again (find_bound: 400)
 
 struct TopkShared {
   __align__(16) unsigned long long cand[kTopkCand];  // (key, ~class) of the logits that may be among the largest: larger is in front
   float value[kTopkCand], spare[kTopkCand];
-  uint16_t owner[512];  // (find_bound lets at most 400 streams through)
+  int owner[kTopkOwners];
   __align__(16) int count[2][4 * 16];
   int taken;
   int last;
@@ -390,15 +390,17 @@ __device__ __forceinline__ void topk_any(const T* row, int C, int kk, bool want_
   if (want_tail) add_rest(row, C, prefix, last, sc, rest);
 }
 
-// One workgroup per row (or slice of one), eight on a compute unit.  The row goes by once in 2048 streams, eight a thread, each with its largest logit and its sum
-// of exponentials.  A bound below which no logit of the row's k largest can lie is the k-th largest of the streams' maxima, or a little
-// less: streams whose maximum reaches it (little more than k) are read again, from the caches, for the logits that reach it (little
-// more than k again), and these are put in order by counting.  Their streams' sums are taken anew without them: nothing is subtracted.
+// One workgroup per row (or slice of one).  The row goes by once in 1024 streams of vectors, four a thread, each with its two largest
+// vector maxima, the sum of exponentials of the vector that has the largest, and that of the others.  A bound below which no logit of the
+// row's k largest can lie is the k-th largest of the streams' maxima, or a little less: of streams whose maximum reaches it (little
+// more than k) that vector is read again, of the few whose second does all vectors, for the logits that reach it (little more than k
+// again), and these are put in order by counting.  The sums of what is read again are taken anew without them: nothing is subtracted.
+// (With whole streams read again, 2048 x 131072 float, 16 vectors a stream, 256 us.)
 // Where many maxima are equal (masks, ties), the logits above their value are the candidates and the rest of the k is taken from the
 // equal ones in the order of the classes.
 template <typename T, int MODE>
 __global__ __launch_bounds__(kTopkThreads, 8) void topk_rows_kernel(const TopkArgs a) {
-  constexpr int V = Elem<T>::VEC, NT = kTopkThreads, G = kTopkStreams, HALF = G / 2;
+  constexpr int V = Elem<T>::VEC, NT = kTopkThreads, G = kTopkStreams;
   __shared__ TopkShared sh;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int slice = MODE == kTopkSlices ? blockIdx.x : 0, n = MODE == kTopkSlices ? blockIdx.y : blockIdx.y * gridDim.x + blockIdx.x;
@@ -410,56 +412,51 @@ __global__ __launch_bounds__(kTopkThreads, 8) void topk_rows_kernel(const TopkAr
   Scales sc;
   sc.t = sc.one = kLog2e / a.temperature;
   sc.slack = 20.f / sc.t;
-  float m[G], st[G], ref = -FLT_MAX, lim = -FLT_MAX;  // (one reference for a thread's streams, as in Sums)
+  float m[G], second[G], best[G], st[G], ref = -FLT_MAX, lim = -FLT_MAX;  // (one reference for a thread's streams, as in Sums)
+  int round[G];                                                           // where a stream's largest is
 #pragma unroll
-  for (int g = 0; g < G; ++g) m[g] = -INFINITY, st[g] = 0.f;
-  auto refer = [&](float top) __attribute__((always_inline)) {
-    if (top > lim) {
-      const float f = __builtin_amdgcn_exp2f((ref - top) * sc.t);
-#pragma unroll
-      for (int g = 0; g < G; ++g) st[g] *= f;
-      ref = top;
-      lim = top + sc.slack;
-    }
-  };
-  auto take = [&](const Vec16& x, int g) __attribute__((always_inline)) {
+  for (int g = 0; g < G; ++g) m[g] = second[g] = -INFINITY, best[g] = st[g] = 0.f, round[g] = 0;
+  auto take = [&](const Vec16& x, int g, int r) __attribute__((always_inline)) {
     float z[V];
     Elem<T>::unpack(x, z);
     float top = z[0];
 #pragma unroll
     for (int j = 1; j < V; ++j) top = fmaxf(top, z[j]);
-    m[g] = fmaxf(m[g], top);
-    refer(top);
+    if (top > lim) {
+      const float f = __builtin_amdgcn_exp2f((ref - top) * sc.t);
 #pragma unroll
-    for (int j = 0; j < V; ++j) st[g] += __builtin_amdgcn_exp2f((z[j] - ref) * sc.t);
-  };
-  int v = tid;
-  for (; v + (G - 1) * NT < whole; v += G * NT) {
-#pragma unroll
-    for (int h = 0; h < G; h += HALF) {
-      Vec16 x[HALF];
-#pragma unroll
-      for (int g = 0; g < HALF; ++g) x[g] = load16_any(row + (v + (h + g) * NT) * V);
-#pragma unroll
-      for (int g = 0; g < HALF; ++g) take(x[g], h + g);
+      for (int i = 0; i < G; ++i) st[i] *= f, best[i] *= f;
+      ref = top;
+      lim = top + sc.slack;
     }
-  }
+    float sum = 0.f;
 #pragma unroll
-  for (int h = 0; h < G; h += HALF) {
-    Vec16 x[HALF];
+    for (int j = 0; j < V; ++j) sum += __builtin_amdgcn_exp2f((z[j] - ref) * sc.t);
+    const bool up = top > m[g];
+    st[g] += up ? best[g] : sum;
+    best[g] = up ? sum : best[g];
+    second[g] = up ? m[g] : fmaxf(second[g], top);
+    m[g] = up ? top : m[g];
+    round[g] = up ? r : round[g];
+  };
+  int v = tid, r = 0;
+  for (; v + (G - 1) * NT < whole; v += G * NT, ++r) {
+    Vec16 x[G];
 #pragma unroll
-    for (int g = 0; g < HALF; ++g)
-      if (v + (h + g) * NT < whole) x[g] = load16_any(row + (v + (h + g) * NT) * V);
+    for (int g = 0; g < G; ++g) x[g] = load16_any(row + (v + g * NT) * V);
 #pragma unroll
-    for (int g = 0; g < HALF; ++g)
-      if (v + (h + g) * NT < whole) take(x[g], h + g);
+    for (int g = 0; g < G; ++g) take(x[g], g, r);
   }
-  if (tid < left) {  // (the classes behind the last vector: of the threads' first streams)
-    const float z = Elem<T>::load(row + whole * V + tid);
-    m[0] = fmaxf(m[0], z);
-    refer(z);
-    st[0] += __builtin_amdgcn_exp2f((z - ref) * sc.t);
+  {
+    Vec16 x[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+      if (v + g * NT < whole) x[g] = load16_any(row + (v + g * NT) * V);
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+      if (v + g * NT < whole) take(x[g], g, r);
   }
+  const float z_left = tid < left ? Elem<T>::load(row + whole * V + tid) : -INFINITY;  // (the classes behind the last vector)
   if (tid == 0) sh.taken = 0;
   sh.hist[tid] = 0;
   sh.first[tid] = -1;
@@ -468,13 +465,13 @@ __global__ __launch_bounds__(kTopkThreads, 8) void topk_rows_kernel(const TopkAr
 #pragma unroll
   for (int g = 0; g < G; ++g) {
     key[g] = order_key(m[g]);
-    all += st[g];
+    all += st[g] + best[g];
     tm = fmaxf(tm, m[g]);
   }
   {
     const float most = quick_max(tm), least = -quick_max(tid < kk ? -tm : -INFINITY);
     // (a sum is NaN where a logit is NaN or +infinity: maxima say nothing then)
-    const uint64_t odd = __ballot(!(all == all));
+    const uint64_t odd = __ballot(!(all == all) || !(z_left <= FLT_MAX));
     if (lane == 0) sh.count[1][wave] = __float_as_int(most), sh.count[1][4 + wave] = __float_as_int(least), sh.count[1][12 + wave] = odd != 0;
   }
   __syncthreads();
@@ -488,29 +485,37 @@ __global__ __launch_bounds__(kTopkThreads, 8) void topk_rows_kernel(const TopkAr
       least = fminf(least, __int_as_float(sh.count[1][4 + w]));
     }
     bool tie;
-    const uint32_t top = order_key(most), lo = find_bound<G>(key, order_key(least), top, kk, &tie, sh);  // (the first kk threads' maxima reach `least`)
+    const uint32_t lo = find_bound<G>(key, order_key(least), order_key(most), kk, &tie, sh);  // (the first kk threads' maxima reach `least`)
     const uint32_t bound = tie ? lo + 1 : lo;
     const float from = logit_of(bound);
-    // the streams that are read again, listed in a fixed order; the others' sums stay
-    uint64_t votes[G];
-#pragma unroll
-    for (int g = 0; g < G; ++g) {
-      votes[g] = __ballot(key[g] >= bound);
-      if (lane == 0) sh.count[0][16 + g * 4 + wave] = __popcll(votes[g]);
-    }
-    __syncthreads();
+    // what is read again, listed in a fixed order: single vectors from the front, streams from the end; the sums of everything else stay
     rest.ref = ref;
     rest.lim = lim;
-    int owners = 0;
+    uint64_t one[G], more[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      one[g] = __ballot(m[g] >= from && second[g] < from);
+      more[g] = __ballot(m[g] >= from && second[g] >= from);
+      if (lane == 0) sh.count[0][16 + g * 4 + wave] = __popcll(one[g]) | __popcll(more[g]) << 16;
+    }
+    __syncthreads();
+    int counts = 0;  // (single vectors, streams)
 #pragma unroll
     for (int g = 0; g < G; ++g) {
       const int4 c = *reinterpret_cast<const int4*>(&sh.count[0][16 + g * 4]);
-      const int at = owners + (wave > 0 ? c.x : 0) + (wave > 1 ? c.y : 0) + (wave > 2 ? c.z : 0);
-      owners += (c.x + c.y) + (c.z + c.w);
-      if (key[g] >= bound) sh.owner[at + __popcll(votes[g] & ((1ull << lane) - 1))] = static_cast<uint16_t>(tid * G + g);
-      else rest.st += st[g];
+      const int at = counts + (wave > 0 ? c.x : 0) + (wave > 1 ? c.y : 0) + (wave > 2 ? c.z : 0);
+      counts += (c.x + c.y) + (c.z + c.w);
+      const uint64_t below = (1ull << lane) - 1;
+      if (m[g] >= from) {
+        const bool single = second[g] < from;
+        if (single) sh.owner[(at & 0xffff) + __popcll(one[g] & below)] = tid + (round[g] * G + g) * NT;
+        else sh.owner[kTopkOwners - 1 - (at >> 16) - __popcll(more[g] & below)] = tid + g * NT;
+        rest.st += single ? st[g] : 0.f;
+      } else {
+        rest.st += st[g] + best[g];
+      }
     }
-    __syncthreads();
+    const int singles = counts & 0xffff, streams = counts >> 16;
     auto candidate = [&](float x, int i) __attribute__((always_inline)) {
       const int at = atomicAdd(&sh.taken, 1);
       if (at < kTopkCand) {
@@ -518,25 +523,28 @@ __global__ __launch_bounds__(kTopkThreads, 8) void topk_rows_kernel(const TopkAr
         sh.value[at] = x;
       }
     };
-    const int rounds = max(1, (whole + G * NT - 1) / (G * NT));
+    if (tid < left) {
+      if (z_left >= from) candidate(z_left, whole * V + tid);
+      else rest.template add<1>(&z_left, sc);
+    }
+    __syncthreads();
+    // (vector of item i: a listed one, or one of a listed stream's)
+    const int rounds = max(1, (whole + G * NT - 1) / (G * NT)), items = singles + streams * rounds;
     constexpr int AHEAD = 2;  // vectors whose loads go out together
-    for (int i0 = tid; i0 < owners * rounds; i0 += AHEAD * NT) {
+    for (int i0 = tid; i0 < items; i0 += AHEAD * NT) {
       Vec16 x[AHEAD];
       int vec[AHEAD];
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u) {
-        const int i = i0 + u * NT, o = i / rounds, r = i - o * rounds;
+        const int i = i0 + u * NT;
         vec[u] = whole;
-        if (i < owners * rounds) {
-          const int own = sh.owner[o], g = own & (G - 1), t = own / G;
-          vec[u] = t + (r * G + g) * NT;
-          if (vec[u] < whole) x[u] = load16_any(row + vec[u] * V);
-          if (g == 0 && r == 0 && t < left) {
-            const float z = Elem<T>::load(row + whole * V + t);
-            if (z >= from) candidate(z, whole * V + t);
-            else rest.template add<1>(&z, sc);
-          }
+        if (i < singles) {
+          vec[u] = sh.owner[i];
+        } else if (i < items) {
+          const int o = (i - singles) / rounds;
+          vec[u] = sh.owner[kTopkOwners - 1 - o] + (i - singles - o * rounds) * (G * NT);
         }
+        if (vec[u] < whole) x[u] = load16_any(row + vec[u] * V);
       }
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u) {
@@ -556,6 +564,9 @@ __global__ __launch_bounds__(kTopkThreads, 8) void topk_rows_kernel(const TopkAr
     const int cands = sh.taken;
     if (cands <= kTopkCand) {
       done = true;
+      // (the candidates' largest key: of the streams' or of the classes behind the last vector)
+      uint32_t top = order_key(most);
+      for (int i = 0; i < left; ++i) top = max(top, order_key(Elem<T>::load(row + whole * V + i)));
       put_ranked(cands, kk, bound, top, out, sh);
       for (int c = tid; c < cands - kk; c += NT) rest.template add<1>(&sh.spare[c], sc);
       if (cands < kk) {  // (many equal maxima)
