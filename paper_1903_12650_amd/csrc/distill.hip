@@ -111,7 +111,9 @@ struct Sums {
     float top = x[0];
 #pragma unroll
     for (int j = 1; j < V; ++j) top = fmaxf(top, x[j]);
-    if (top > lim) move(top, sc);
+    if (__any(top > lim)) {  // (one branch for the wave: without it the move is computed for every vector and selected)
+      if (top > lim) move(top, sc);
+    }
 #pragma unroll
     for (int j = 0; j < V; ++j) one(x[j], sc);
   }
@@ -422,12 +424,14 @@ __global__ __launch_bounds__(kTopkThreads, 8) void topk_rows_kernel(const TopkAr
     float top = z[0];
 #pragma unroll
     for (int j = 1; j < V; ++j) top = fmaxf(top, z[j]);
-    if (top > lim) {
-      const float f = __builtin_amdgcn_exp2f((ref - top) * sc.t);
+    if (__any(top > lim)) {
+      if (top > lim) {
+        const float f = __builtin_amdgcn_exp2f((ref - top) * sc.t);
 #pragma unroll
-      for (int i = 0; i < G; ++i) st[i] *= f, best[i] *= f;
-      ref = top;
-      lim = top + sc.slack;
+        for (int i = 0; i < G; ++i) st[i] *= f, best[i] *= f;
+        ref = top;
+        lim = top + sc.slack;
+      }
     }
     float sum = 0.f;
 #pragma unroll
@@ -897,15 +901,17 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(const DistillArgs a) {
   const bool want_sz = label >= 0 && a.smoothing > 0.f;
   Sums<EXPS> sums;
   double sz = 0;  // (in double: beside classes masked with the lowest float it still holds what the others add)
-  auto add = [&](const Vec16& x, int e) __attribute__((always_inline)) {  // e: the vector's first class, from the chunk's first
+  auto members = [&](int e) __attribute__((always_inline)) {  // e: a vector's first class, from the chunk's first
+    return member[static_cast<uint32_t>(e) >> 5] >> (e & 31) & ((1u << V) - 1);
+  };
+  auto add = [&](const Vec16& x, uint32_t bits) __attribute__((always_inline)) {
     float z[V];
     Elem<T>::unpack(x, z);
     if (want_sz) {
 #pragma unroll
       for (int j = 0; j < V; ++j) sz += static_cast<double>(z[j]);
     }
-    const uint32_t bits = member[e >> 5] >> (e & 31) & ((1u << V) - 1);
-    if (bits) {
+    if (__any(bits)) {
 #pragma unroll
       for (int j = 0; j < V; ++j) z[j] = bits >> j & 1 ? -INFINITY : z[j];
     }
@@ -923,7 +929,7 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(const DistillArgs a) {
 #pragma unroll
       for (int u = 0; u < U; ++u)
         if (u * NT + tid < whole) {
-          add(held[u], (u * NT + tid) * V);
+          add(held[u], members((u * NT + tid) * V));
           // the gradient unpacks them again: floats kept from here would be twice the registers
           asm volatile("" : "+v"(held[u].u.x), "+v"(held[u].u.y), "+v"(held[u].u.z), "+v"(held[u].u.w));
           __builtin_amdgcn_sched_barrier(0);
@@ -936,10 +942,13 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(const DistillArgs a) {
         Vec16 x[G];
 #pragma unroll
         for (int g = 0; g < G; ++g) x[g] = load16_any(from + (v + g * NT) * V);
+        uint32_t bits[G];
 #pragma unroll
-        for (int g = 0; g < G; ++g) add(x[g], (v + g * NT) * V);
+        for (int g = 0; g < G; ++g) bits[g] = members((v + g * NT) * V);
+#pragma unroll
+        for (int g = 0; g < G; ++g) add(x[g], bits[g]);
       }
-      for (; v < vecs; v += NT) add(load16_any(from + v * V), v * V);
+      for (; v < vecs; v += NT) add(load16_any(from + v * V), members(v * V));
     }
     if (tid < left && mine - c0 < chunk) {
       if (want_sz) sz += static_cast<double>(z_left);
@@ -1028,15 +1037,15 @@ __global__ __launch_bounds__(kSliceThreads) void distill_slice_sums_kernel(const
   const bool want_sz = label >= 0 && a.smoothing > 0.f;
   Sums<EXPS> sums;
   double sz = 0;
-  auto add = [&](const Vec16& x, int e) __attribute__((always_inline)) {
+  auto members = [&](int e) __attribute__((always_inline)) { return member[static_cast<uint32_t>(e) >> 5] >> (e & 31) & ((1u << V) - 1); };
+  auto add = [&](const Vec16& x, uint32_t bits) __attribute__((always_inline)) {
     float z[V];
     Elem<T>::unpack(x, z);
     if (want_sz) {
 #pragma unroll
       for (int j = 0; j < V; ++j) sz += static_cast<double>(z[j]);
     }
-    const uint32_t bits = member[e >> 5] >> (e & 31) & ((1u << V) - 1);
-    if (bits) {
+    if (__any(bits)) {
 #pragma unroll
       for (int j = 0; j < V; ++j) z[j] = bits >> j & 1 ? -INFINITY : z[j];
     }
@@ -1056,10 +1065,13 @@ __global__ __launch_bounds__(kSliceThreads) void distill_slice_sums_kernel(const
       Vec16 x[G];
 #pragma unroll
       for (int g = 0; g < G; ++g) x[g] = load16_any(from + (v + g * NT) * V);
+      uint32_t bits[G];
 #pragma unroll
-      for (int g = 0; g < G; ++g) add(x[g], (v + g * NT) * V);
+      for (int g = 0; g < G; ++g) bits[g] = members((v + g * NT) * V);
+#pragma unroll
+      for (int g = 0; g < G; ++g) add(x[g], bits[g]);
     }
-    for (; v < vecs; v += NT) add(load16_any(from + v * V), v * V);
+    for (; v < vecs; v += NT) add(load16_any(from + v * V), members(v * V));
     const int e = vecs * V + tid;
     if (e < chunk) {
       const float z = Elem<T>::load(from + e);
