@@ -43,6 +43,18 @@ __device__ __forceinline__ float quick_max(float x) {
   return fmaxf(fmaxf(from_lane(x, 0), from_lane(x, 16)), fmaxf(from_lane(x, 32), from_lane(x, 48)));
 }
 
+// Rows start at any element; their vectors start where 16 bytes do (vectors across that boundary took 228 us for loss and gradient of
+// 4096 x 50001 bf16, 98 for its largest logits; 50000 classes 184 and 89).  A row's classes count from the first vector on: place 0 is class
+// `head`, and the `head` classes in front of it follow the last class.
+struct Places {
+  int head, classes;
+  template <typename T>
+  __device__ __forceinline__ Places(const T* row, int C)
+      : head(min(C, static_cast<int>((0u - static_cast<uint32_t>(reinterpret_cast<uintptr_t>(row))) % 16u / sizeof(T)))), classes(C) {}
+  __device__ __forceinline__ int class_at(int place) const { return place + head < classes ? place + head : place + head - classes; }
+  __device__ __forceinline__ int of(int c) const { return c >= head ? c - head : c + classes - head; }  // (0 <= c < classes)
+};
+
 // A workgroup for each of N rows, row blockIdx.y * gridDim.x + blockIdx.x.
 static dim3 row_grid(int N) { return N <= 65536 ? dim3(N) : dim3(65536, static_cast<unsigned>(ceil_div(N, 65536))); }
 
@@ -409,7 +421,9 @@ __global__ __launch_bounds__(kTopkThreads, 8) void topk_rows_kernel(const TopkAr
   if (n >= a.N) return;
   const int C = MODE == kTopkSlices ? min(a.width, a.C - slice * a.width) : a.C;
   const T* row = static_cast<const T*>(a.logits) + n * a.ld + static_cast<int64_t>(slice) * a.width;
-  const int kk = min(a.k, C), whole = C / V, left = C - whole * V;
+  const Places places(row, C);
+  const T* vecs = row + places.head;
+  const int kk = min(a.k, C), whole = (C - places.head) / V, left = C - whole * V;
   const TopkOut<MODE> out{a, n, slice};
   Scales sc;
   sc.t = sc.one = kLog2e / a.temperature;
@@ -447,7 +461,7 @@ __global__ __launch_bounds__(kTopkThreads, 8) void topk_rows_kernel(const TopkAr
   for (; v + (G - 1) * NT < whole; v += G * NT, ++r) {
     Vec16 x[G];
 #pragma unroll
-    for (int g = 0; g < G; ++g) x[g] = load16_any(row + (v + g * NT) * V);
+    for (int g = 0; g < G; ++g) x[g] = load16(vecs + (v + g * NT) * V);
 #pragma unroll
     for (int g = 0; g < G; ++g) take(x[g], g, r);
   }
@@ -455,12 +469,13 @@ __global__ __launch_bounds__(kTopkThreads, 8) void topk_rows_kernel(const TopkAr
     Vec16 x[G];
 #pragma unroll
     for (int g = 0; g < G; ++g)
-      if (v + g * NT < whole) x[g] = load16_any(row + (v + g * NT) * V);
+      if (v + g * NT < whole) x[g] = load16(vecs + (v + g * NT) * V);
 #pragma unroll
     for (int g = 0; g < G; ++g)
       if (v + g * NT < whole) take(x[g], g, r);
   }
-  const float z_left = tid < left ? Elem<T>::load(row + whole * V + tid) : -INFINITY;  // (the classes behind the last vector)
+  const int c_left = places.class_at(whole * V + tid);
+  const float z_left = tid < left ? Elem<T>::load(row + c_left) : -INFINITY;  // (the classes of no vector)
   if (tid == 0) sh.taken = 0;
   sh.hist[tid] = 0;
   sh.first[tid] = -1;
@@ -528,7 +543,7 @@ __global__ __launch_bounds__(kTopkThreads, 8) void topk_rows_kernel(const TopkAr
       }
     };
     if (tid < left) {
-      if (z_left >= from) candidate(z_left, whole * V + tid);
+      if (z_left >= from) candidate(z_left, c_left);
       else rest.template add<1>(&z_left, sc);
     }
     __syncthreads();
@@ -548,7 +563,7 @@ __global__ __launch_bounds__(kTopkThreads, 8) void topk_rows_kernel(const TopkAr
           const int o = (i - singles) / rounds;
           vec[u] = sh.owner[kTopkOwners - 1 - o] + (i - singles - o * rounds) * (G * NT);
         }
-        if (vec[u] < whole) x[u] = load16_any(row + vec[u] * V);
+        if (vec[u] < whole) x[u] = load16(vecs + vec[u] * V);
       }
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u) {
@@ -558,7 +573,7 @@ __global__ __launch_bounds__(kTopkThreads, 8) void topk_rows_kernel(const TopkAr
 #pragma unroll
         for (int j = 0; j < V; ++j)
           if (z[j] >= from) {
-            candidate(z[j], vec[u] * V + j);
+            candidate(z[j], places.head + vec[u] * V + j);
             z[j] = -INFINITY;
           }
         rest.template add<V>(z, sc);
@@ -568,9 +583,9 @@ __global__ __launch_bounds__(kTopkThreads, 8) void topk_rows_kernel(const TopkAr
     const int cands = sh.taken;
     if (cands <= kTopkCand) {
       done = true;
-      // (the candidates' largest key: of the streams' or of the classes behind the last vector)
+      // (the candidates' largest key: of the streams' or of the classes of no vector)
       uint32_t top = order_key(most);
-      for (int i = 0; i < left; ++i) top = max(top, order_key(Elem<T>::load(row + whole * V + i)));
+      for (int i = 0; i < left; ++i) top = max(top, order_key(Elem<T>::load(row + places.class_at(whole * V + i))));
       put_ranked(cands, kk, bound, top, out, sh);
       for (int c = tid; c < cands - kk; c += NT) rest.template add<1>(&sh.spare[c], sc);
       if (cands < kk) {  // (many equal maxima)
@@ -699,12 +714,13 @@ struct RowShared {
   int first[1024], next[kTopMax + 1];  // the entries of every thread, as lists
   RowGrad g;
 };
-// Hands entry j, of class c, to the thread that writes class c's gradient: of whole vectors of V classes in turn, of the classes behind
-// them one each.  (c and C: from the first class of the workgroup's slice, and the slice's classes; a class outside is nobody's here.)
+// Hands entry j, of class c, to the thread that writes class c's gradient: of whole vectors of V classes in turn, of the classes of no
+// vector one each.  (c: from the first class of the workgroup's slice; a class outside is nobody's here.)
 template <int V, int NT>
-__device__ __forceinline__ void hand_over(RowShared& sh, int C, int j, int c) {
-  const int whole = C / V * V;
-  if (c >= 0 && c < C) sh.next[j] = atomicExch(&sh.first[c < whole ? c / V % NT : c - whole], j);
+__device__ __forceinline__ void hand_over(RowShared& sh, const Places& places, int j, int c) {
+  if (c < 0 || c >= places.classes) return;
+  const int whole = (places.classes - places.head) / V * V, at = places.of(c);
+  sh.next[j] = atomicExch(&sh.first[at < whole ? at / V % NT : at - whole], j);
 }
 
 // A row's gradient coefficients and loss, by one wave.  Everything is relative to the largest logit and the largest cell; the logarithms
@@ -716,13 +732,14 @@ struct RowEnd {
   const Scales& sc;
   const RowSums& r;
   RowShared& sh;
-  int label, k, first, classes;  // (the workgroup's slice of the row)
+  int label, k, first;  // (the first class of the workgroup's slice of the row)
+  const Places& places;
   float M, tau, AT, A1, S, pt;
   double Mt;
   bool empty, none;
 
-  __device__ __forceinline__ RowEnd(const DistillArgs& a_, const Scales& sc_, const RowSums& r_, RowShared& sh_, int label_, int k_, int first_, int classes_)
-      : a(a_), sc(sc_), r(r_), sh(sh_), label(label_), k(k_), first(first_), classes(classes_) {}
+  __device__ __forceinline__ RowEnd(const DistillArgs& a_, const Scales& sc_, const RowSums& r_, RowShared& sh_, int label_, int k_, int first_, const Places& places_)
+      : a(a_), sc(sc_), r(r_), sh(sh_), label(label_), k(k_), first(first_), places(places_) {}
   __device__ __forceinline__ float cell(double over) const { return __builtin_amdgcn_exp2f(static_cast<float>(over * static_cast<double>(kLog2e))); }
   __device__ __forceinline__ double teacher(int j) const { return sh.t[j] * (1.0 / static_cast<double>(a.temperature)) - Mt; }
 
@@ -787,7 +804,7 @@ struct RowEnd {
         float v = fmaf(c.coef_t, y, -c.offset);
         if constexpr (EXPS != 1) v += c.coef_1 * __builtin_amdgcn_exp2f(d * sc.one);
         sh.value[kTopMax] = v - g1 * (1.f - a.smoothing);
-        hand_over<V, NT>(sh, classes, kTopMax, label - first);
+        hand_over<V, NT>(sh, places, kTopMax, label - first);
       }
       sh.g = c;
     }
@@ -868,9 +885,11 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(const DistillArgs a) {
   const int n = blockIdx.y * gridDim.x + blockIdx.x;
   if (n >= a.N) return;
   const Scales sc = scales_of(a, EXPS);
-  const int k = a.alpha > 0.f ? a.k : 0, whole = a.C / V, left = a.C - whole * V;
   const T* row = static_cast<const T*>(a.logits) + n * a.ld;
   T* grad = a.grad ? static_cast<T*>(a.grad) + n * a.grad_ld : nullptr;
+  const Places places(row, a.C);
+  const T* vecs = row + places.head;
+  const int k = a.alpha > 0.f ? a.k : 0, whole = (a.C - places.head) / V, left = a.C - whole * V;
   // what the row's end needs goes out first: it is a chain of loads (entry, its logit)
   int at = -1;
   if (tid < k) {
@@ -885,10 +904,10 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(const DistillArgs a) {
   if constexpr (U > 0) {
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (u * NT + tid < whole) held[u] = load16_any(row + (u * NT + tid) * V);
+      if (u * NT + tid < whole) held[u] = load16(vecs + (u * NT + tid) * V);
   }
-  const int mine = whole * V + tid;  // (tid < left)
-  const float z_left = tid < left ? Elem<T>::load(row + mine) : -INFINITY;
+  const int mine = whole * V + tid, c_left = places.class_at(mine);  // (tid < left)
+  const float z_left = tid < left ? Elem<T>::load(row + c_left) : -INFINITY;
   if (w == 0.f) {  // (behind the loads: the weight is a load as well)
     for (int i = tid; grad && i < a.C; i += NT) Elem<T>::store(grad + i, 0.f);
     if (tid == 0) a.row_loss[n] = 0.f;
@@ -897,11 +916,12 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(const DistillArgs a) {
   if (at >= a.C || at < 0) at = -1;
   const float z_at = at >= 0 ? Elem<T>::load(row + at) : -INFINITY;
   if (tid == 0 && label >= 0) sh.z[kTopMax] = Elem<T>::load(row + label);
+  const int place = at >= 0 ? places.of(at) : -1;
 
   const bool want_sz = label >= 0 && a.smoothing > 0.f;
   Sums<EXPS> sums;
   double sz = 0;  // (in double: beside classes masked with the lowest float it still holds what the others add)
-  auto members = [&](int e) __attribute__((always_inline)) {  // e: a vector's first class, from the chunk's first
+  auto members = [&](int e) __attribute__((always_inline)) {  // e: a vector's first place, from the chunk's first
     return member[static_cast<uint32_t>(e) >> 5] >> (e & 31) & ((1u << V) - 1);
   };
   auto add = [&](const Vec16& x, uint32_t bits) __attribute__((always_inline)) {
@@ -923,7 +943,7 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(const DistillArgs a) {
     if (c0) __syncthreads();
     for (int i = tid; i < (chunk + 31) / 32; i += NT) member[i] = 0;
     __syncthreads();
-    if (at >= c0 && at - c0 < chunk) repeated = atomicOr(&member[(at - c0) >> 5], 1u << ((at - c0) & 31)) >> ((at - c0) & 31) & 1;
+    if (place >= c0 && place - c0 < chunk) repeated = atomicOr(&member[(place - c0) >> 5], 1u << ((place - c0) & 31)) >> ((place - c0) & 31) & 1;
     __syncthreads();
     if constexpr (U > 0) {
 #pragma unroll
@@ -935,22 +955,22 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(const DistillArgs a) {
           __builtin_amdgcn_sched_barrier(0);
         }
     } else {
-      const T* from = row + c0;
-      const int vecs = chunk / V;
+      const T* from = vecs + c0;
+      const int last = min(whole - c0 / V, CHUNK / V);
       int v = tid;
-      for (; v + (G - 1) * NT < vecs; v += G * NT) {
+      for (; v + (G - 1) * NT < last; v += G * NT) {
         Vec16 x[G];
 #pragma unroll
-        for (int g = 0; g < G; ++g) x[g] = load16_any(from + (v + g * NT) * V);
+        for (int g = 0; g < G; ++g) x[g] = load16(from + (v + g * NT) * V);
         uint32_t bits[G];
 #pragma unroll
         for (int g = 0; g < G; ++g) bits[g] = members((v + g * NT) * V);
 #pragma unroll
         for (int g = 0; g < G; ++g) add(x[g], bits[g]);
       }
-      for (; v < vecs; v += NT) add(load16_any(from + v * V), members(v * V));
+      for (; v < last; v += NT) add(load16(from + v * V), members(v * V));
     }
-    if (tid < left && mine - c0 < chunk) {
+    if (tid < left && mine >= c0 && mine - c0 < chunk) {
       if (want_sz) sz += static_cast<double>(z_left);
       if (!(member[(mine - c0) >> 5] >> ((mine - c0) & 31) & 1)) sums.template add<1>(&z_left, sc);
     }
@@ -966,9 +986,9 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(const DistillArgs a) {
     __syncthreads();
     if (drop) sh.at[tid] = at = -1;
   }
-  if (at >= 0) hand_over<V, NT>(sh, a.C, tid, at);
+  if (at >= 0) hand_over<V, NT>(sh, places, tid, at);
   const RowSums r = block_sums<EXPS, NT>(sums, sz, want_sz, sc, red);
-  RowEnd<EXPS, V, NT> end(a, sc, r, sh, label, k, 0, a.C);
+  RowEnd<EXPS, V, NT> end(a, sc, r, sh, label, k, 0, places);
   if (tid < 64) end.gradient(w, tail);
   __syncthreads();
   if (tid < 64) {
@@ -977,11 +997,12 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(const DistillArgs a) {
   }
   if (!grad) return;
   const RowGrad g = sh.g;
+  T* to = grad + places.head;
   if constexpr (U > 0) {
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (u * NT + tid < whole) {
-        store_gradient<T, EXPS, false>(grad + (u * NT + tid) * V, held[u], g, sc);
+        store_gradient<T, EXPS, false>(to + (u * NT + tid) * V, held[u], g, sc);
         __builtin_amdgcn_sched_barrier(0);
       }
   } else {
@@ -991,13 +1012,13 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(const DistillArgs a) {
     for (; v >= (G - 1) * NT; v -= G * NT) {
       Vec16 x[G];
 #pragma unroll
-      for (int i = 0; i < G; ++i) x[i] = load16_any(row + (v - i * NT) * V);
+      for (int i = 0; i < G; ++i) x[i] = load16(vecs + (v - i * NT) * V);
 #pragma unroll
-      for (int i = 0; i < G; ++i) store_gradient<T, EXPS, true>(grad + (v - i * NT) * V, x[i], g, sc);
+      for (int i = 0; i < G; ++i) store_gradient<T, EXPS, true>(to + (v - i * NT) * V, x[i], g, sc);
     }
-    for (; v >= 0; v -= NT) store_gradient<T, EXPS, true>(grad + v * V, load16_any(row + v * V), g, sc);
+    for (; v >= 0; v -= NT) store_gradient<T, EXPS, true>(to + v * V, load16(vecs + v * V), g, sc);
   }
-  if (tid < left) Elem<T>::store(grad + mine, gradient_of<EXPS>(z_left, g, sc));
+  if (tid < left) Elem<T>::store(grad + c_left, gradient_of<EXPS>(z_left, g, sc));
   // The entries' classes and the label's: written once more, each by the thread that wrote it first (whose stores to one address stay in
   // order: no barrier, which would wait for every store of the row).
   for (int j = sh.first[tid]; j >= 0; j = sh.next[j]) Elem<T>::store(grad + sh.at[j], sh.value[j]);
@@ -1025,12 +1046,16 @@ __global__ __launch_bounds__(kSliceThreads) void distill_slice_sums_kernel(const
   const Scales sc = scales_of(a, EXPS);
   const int k = a.alpha > 0.f ? a.k : 0;
   const T* row = static_cast<const T*>(a.logits) + n * a.ld + first;
+  const Places places(row, classes);
+  const T* vecs = row + places.head;
+  const int whole = (classes - places.head) / V, left = classes - whole * V, c_left = places.class_at(whole * V + tid);  // (tid < left)
   int at = tid < k ? a.t_indices[static_cast<int64_t>(n) * a.k + tid] : -1;
   if (a.row_weight && a.row_weight[n] == 0.f) return;
   int label = a.labels && a.alpha < 1.f ? a.labels[n] : -1;
   if (label >= a.C) label = -1;
   if (at >= a.C || at < 0) at = -1;
   const bool mine = at >= first && at - first < classes;
+  const int place = mine ? places.of(at - first) : -1;
   const float z_at = mine ? Elem<T>::load(row + (at - first)) : -INFINITY;
   if (tid == 0 && label >= first && label - first < classes) p.z[static_cast<int64_t>(n) * (kTopMax + 1) + kTopMax] = Elem<T>::load(row + (label - first));
   if (tid < k) at_s[tid] = at;
@@ -1053,28 +1078,28 @@ __global__ __launch_bounds__(kSliceThreads) void distill_slice_sums_kernel(const
   };
   bool repeated = false;
   for (int c0 = 0; c0 < classes; c0 += CHUNK) {
-    const int chunk = min(classes - c0, CHUNK), vecs = chunk / V, e_at = at - first - c0;
+    const int chunk = min(classes - c0, CHUNK), last = min(whole - c0 / V, CHUNK / V), e_at = place - c0;
     if (c0) __syncthreads();
     for (int i = tid; i < (chunk + 31) / 32; i += NT) member[i] = 0;
     __syncthreads();
     if (mine && e_at >= 0 && e_at < chunk) repeated = atomicOr(&member[e_at >> 5], 1u << (e_at & 31)) >> (e_at & 31) & 1;
     __syncthreads();
-    const T* from = row + c0;
+    const T* from = vecs + c0;
     int v = tid;
-    for (; v + (G - 1) * NT < vecs; v += G * NT) {
+    for (; v + (G - 1) * NT < last; v += G * NT) {
       Vec16 x[G];
 #pragma unroll
-      for (int g = 0; g < G; ++g) x[g] = load16_any(from + (v + g * NT) * V);
+      for (int g = 0; g < G; ++g) x[g] = load16(from + (v + g * NT) * V);
       uint32_t bits[G];
 #pragma unroll
       for (int g = 0; g < G; ++g) bits[g] = members((v + g * NT) * V);
 #pragma unroll
       for (int g = 0; g < G; ++g) add(x[g], bits[g]);
     }
-    for (; v < vecs; v += NT) add(load16_any(from + v * V), members(v * V));
-    const int e = vecs * V + tid;
-    if (e < chunk) {
-      const float z = Elem<T>::load(from + e);
+    for (; v < last; v += NT) add(load16(from + v * V), members(v * V));
+    const int e = whole * V + tid - c0;
+    if (tid < left && e >= 0 && e < chunk) {
+      const float z = Elem<T>::load(row + c_left);
       if (want_sz) sz += static_cast<double>(z);
       if (!(member[e >> 5] >> (e & 31) & 1)) sums.template add<1>(&z, sc);
     }
@@ -1097,12 +1122,15 @@ __global__ __launch_bounds__(kSliceThreads) void distill_slice_end_kernel(const 
   __shared__ RowShared sh;
   __shared__ RowSums red[NT / 64];
   const int tid = threadIdx.x, slice = blockIdx.x, n = blockIdx.y;
-  const int first = slice * p.width, classes = min(p.width, a.C - first), whole = classes / V, left = classes - whole * V;
+  const int first = slice * p.width, classes = min(p.width, a.C - first);
   const Scales sc = scales_of(a, EXPS);
   const int k = a.alpha > 0.f ? a.k : 0;
   const float w = a.row_weight ? a.row_weight[n] : 1.f / static_cast<float>(a.N);
   const T* row = static_cast<const T*>(a.logits) + n * a.ld + first;
   T* grad = a.grad ? static_cast<T*>(a.grad) + n * a.grad_ld + first : nullptr;
+  const Places places(row, classes);
+  const T* vecs = row + places.head;
+  const int whole = (classes - places.head) / V, left = classes - whole * V, c_left = places.class_at(whole * V + tid);  // (tid < left)
   if (w != 0.f) {
     const float tail = a.alpha > 0.f && a.t_tail ? a.t_tail[n] : -INFINITY;
     int label = a.labels && a.alpha < 1.f ? a.labels[n] : -1;
@@ -1124,9 +1152,9 @@ __global__ __launch_bounds__(kSliceThreads) void distill_slice_end_kernel(const 
       sz = part.sz;
     }
     __syncthreads();
-    if (at >= 0) hand_over<V, NT>(sh, classes, tid, at - first);
+    if (at >= 0) hand_over<V, NT>(sh, places, tid, at - first);
     const RowSums r = block_sums<EXPS, NT>(sums, sz, label >= 0 && a.smoothing > 0.f, sc, red);
-    RowEnd<EXPS, V, NT> end(a, sc, r, sh, label, k, first, classes);
+    RowEnd<EXPS, V, NT> end(a, sc, r, sh, label, k, first, places);
     if (tid < 64) end.gradient(w, tail);
     __syncthreads();
     if (slice == 0 && tid < 64) {
@@ -1136,16 +1164,17 @@ __global__ __launch_bounds__(kSliceThreads) void distill_slice_end_kernel(const 
     }
     if (grad) {
       const RowGrad g = sh.g;
+      T* to = grad + places.head;
       int v = tid;
       for (; v + (G - 1) * NT < whole; v += G * NT) {
         Vec16 x[G];
 #pragma unroll
-        for (int i = 0; i < G; ++i) x[i] = load16_any(row + (v + i * NT) * V);
+        for (int i = 0; i < G; ++i) x[i] = load16(vecs + (v + i * NT) * V);
 #pragma unroll
-        for (int i = 0; i < G; ++i) store_gradient<T, EXPS, false>(grad + (v + i * NT) * V, x[i], g, sc);
+        for (int i = 0; i < G; ++i) store_gradient<T, EXPS, false>(to + (v + i * NT) * V, x[i], g, sc);
       }
-      for (; v < whole; v += NT) store_gradient<T, EXPS, false>(grad + v * V, load16_any(row + v * V), g, sc);
-      if (tid < left) Elem<T>::store(grad + whole * V + tid, gradient_of<EXPS>(Elem<T>::load(row + whole * V + tid), g, sc));
+      for (; v < whole; v += NT) store_gradient<T, EXPS, false>(to + v * V, load16(vecs + v * V), g, sc);
+      if (tid < left) Elem<T>::store(grad + c_left, gradient_of<EXPS>(Elem<T>::load(row + c_left), g, sc));
       for (int j = sh.first[tid]; j >= 0; j = sh.next[j]) Elem<T>::store(grad + (sh.at[j] - first), sh.value[j]);
     }
   } else {

@@ -282,10 +282,12 @@ def test_distillation(rn, N, C, k, dtype, tail, alpha, ls, T, absent):
     for extra in (1, 8):
         zz = spread(z, extra)
         out = torch.full((N, C + 2 * extra), 5.0, dtype=dtype, device="cuda")
-        l2, r2, _ = rn.distill_fwd_bwd(zz, v, i, tl, labels, T, alpha, ls, w, 3.0, dlogits=out[:, :C])
-        assert torch.equal(l2, loss) and torch.equal(r2, rows) and torch.equal(out[:, :C], grad) and bool((out[:, C:] == 5.0).all())
-        l2, r2, _ = rn.distill_fwd_bwd(zz, v, i, tl, labels, T, alpha, ls, w, 3.0, dlogits=zz)
-        assert torch.equal(l2, loss) and torch.equal(r2, rows) and torch.equal(zz, grad)
+        l2, r2, _ = check_distill(rn, zz, v, i, tl, labels, T, alpha, ls, w, 3.0, dlogits=out[:, :C])
+        assert bool((out[:, C:] == 5.0).all())
+        if extra == 8:  # (the rows' 16-byte boundaries lie as before: the same sums)
+            assert torch.equal(l2, loss) and torch.equal(r2, rows) and torch.equal(out[:, :C], grad)
+        l3, r3, _ = rn.distill_fwd_bwd(zz, v, i, tl, labels, T, alpha, ls, w, 3.0, dlogits=zz)
+        assert torch.equal(l3, l2) and torch.equal(r3, r2) and torch.equal(zz, out[:, :C])
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
@@ -384,14 +386,12 @@ def test_rows_past_32_bits(rn, N, ld, used):
     x = base.view(N, ld)[:, :used]
     z, v, i, tl, labels = teacher(rn, N, used, 9, 1.0, 1)
     x.copy_(z.to(BF16))
-    z = x.contiguous()
-    for got, want in zip(rn.topk_rows(x, 9), rn.topk_rows(z, 9)):
+    check_topk(rn, x, 9, 1.0)
+    for got, want in zip(rn.quant_rows_i8(x), rn.quant_rows_i8(x.contiguous())):
         assert torch.equal(got, want)
-    for got, want in zip(rn.quant_rows_i8(x), rn.quant_rows_i8(z)):
-        assert torch.equal(got, want)
-    want = rn.distill_fwd_bwd(z, v, i, tl, labels, alpha=0.5)
-    got = rn.distill_fwd_bwd(x, v, i, tl, labels, alpha=0.5, dlogits=x)
-    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and torch.equal(x, want[2])
+    out = rn.distill_fwd_bwd(x, v, i, tl, labels, alpha=0.5)
+    check_distill(rn, x, v, i, tl, labels, alpha=0.5, dlogits=x)
+    assert torch.equal(x, out[2])
     w = rn.quant_rows_i8(torch.randn(used, 64, device="cuda"))
     a = torch.randn(N, 64, device="cuda")
     rn.fc_i8_fwd(a, *w, y=x)
@@ -433,14 +433,18 @@ def test_rows_that_start_anywhere(rn, dtype):
     z, v, i, tl, labels = teacher(rn, 9, 1001, 7, 2.0, 8)
     z = z.to(dtype).cuda()
     wide = spread(z, 5)
-    for r, c in ((1, 0), (2, 1), (3, 2), (0, 3), (5, 997)):
+    for r, c in ((1, 0), (2, 1), (3, 2), (0, 3), (4, 4), (1, 7), (5, 997)):
         part = wide[r:, c:1001]
         whole = part.contiguous()
-        for got, want in zip((*rn.topk_rows(part, 7), *rn.quant_rows_i8(part)), (*rn.topk_rows(whole, 7), *rn.quant_rows_i8(whole))):
+        check_topk(rn, part, 7, 2.0)
+        check_topk(rn, whole, 7, 0.5)
+        for got, want in zip(rn.quant_rows_i8(part), rn.quant_rows_i8(whole)):
             assert torch.equal(got, want)
         a = (v[r:], (i[r:] - c), tl[r:], labels[r:] - c, 2.0, 0.5, 0.1)  # (entries and labels in front of the part are absent)
-        for got, want in zip(rn.distill_fwd_bwd(part, *a), rn.distill_fwd_bwd(whole, *(t.clone() if torch.is_tensor(t) else t for t in a))):
-            assert torch.equal(got, want)
+        check_distill(rn, part, *a)
+        out = torch.full((9, 1009), 5.0, dtype=dtype, device="cuda")
+        check_distill(rn, part, *a, dlogits=out[:9 - r, 3:3 + 1001 - c])  # (its rows start elsewhere than the logits')
+        assert bool((out[:, :3] == 5.0).all()) and bool((out[:, 3 + 1001 - c:] == 5.0).all()) and bool((out[9 - r:] == 5.0).all())
         w = rn.quant_rows_i8(torch.randn(1001 - c, 70, device="cuda"))
         x = torch.randn(9 - r, 70, device="cuda")
         out = torch.full_like(wide, 5.0)
@@ -448,6 +452,26 @@ def test_rows_that_start_anywhere(rn, dtype):
         assert torch.equal(out[r:, c:1001], rn.fc_i8_fwd(x, *w, dtype=dtype))
         out[r:, c:1001] = 5.0
         assert bool((out == 5.0).all())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("C", [9000, 100003])
+def test_long_rows_that_start_anywhere(rn, C, dtype):
+    """Streamed rows and slices: entries and labels in front of the first vector, behind the last, and across chunks of classes."""
+    g = torch.Generator().manual_seed(C)
+    for start in (0, 1, 3, 5, 7):
+        wide = torch.randn(3, C + 8, generator=g).mul(3).to(dtype).cuda()
+        z = wide[:, start:start + C]
+        i = torch.tensor([[0, 1, 2, C - 1, C - 2, C // 2], [C - 1, 65535 % C, 65536 % C, 3, 4, 5], [6, 7, 8, 9, 7, 0]], dtype=torch.int32, device="cuda")
+        v = torch.randn(3, 6, generator=g).mul(2).cuda()
+        labels = torch.tensor([C - 3, 0, 6], dtype=torch.int32, device="cuda")
+        check_distill(rn, z, v, i, torch.tensor([1.0, -2.0, 0.5], device="cuda"), labels, 2.0, 0.5, 0.1)
+        check_topk(rn, z, 40, 1.0)
+        top = z.clone()
+        wide[:, start] = 50.0       # the largest at both ends
+        wide[:, start + C - 1] = 50.0
+        check_topk(rn, z, 3, 1.0)
+        z.copy_(top)
 
 
 @pytest.mark.parametrize("N, C", [(3, 70000), (200, 3000)])
