@@ -876,7 +876,7 @@ template <typename T, int EXPS, int NT, int U>
 __global__ __launch_bounds__(NT) void distill_rows_kernel(const DistillArgs a) {
   constexpr int V = Elem<T>::VEC;
   constexpr int CHUNK = U > 0 ? U * NT * V + 32 : 65536;  // classes whose membership bits are in LDS at a time
-  constexpr int G = 4;                                    // vectors whose loads go out together (U = 0)
+  constexpr int G = sizeof(T) == 2 ? 2 : 4, GG = 4;       // vectors whose loads go out together, for the sums and the gradient (U = 0)
   __shared__ uint32_t member[CHUNK / 32];
   __shared__ RowShared sh;
   __shared__ RowSums red[NT / 64];
@@ -1009,12 +1009,12 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(const DistillArgs a) {
     // from the end, where the caches still have the row
     int v = (whole - 1 - tid) / NT * NT + tid;  // (whole <= tid: below tid)
     if (whole <= tid) v = -1;
-    for (; v >= (G - 1) * NT; v -= G * NT) {
-      Vec16 x[G];
+    for (; v >= (GG - 1) * NT; v -= GG * NT) {
+      Vec16 x[GG];
 #pragma unroll
-      for (int i = 0; i < G; ++i) x[i] = load16(vecs + (v - i * NT) * V);
+      for (int i = 0; i < GG; ++i) x[i] = load16(vecs + (v - i * NT) * V);
 #pragma unroll
-      for (int i = 0; i < G; ++i) store_gradient<T, EXPS, true>(to + (v - i * NT) * V, x[i], g, sc);
+      for (int i = 0; i < GG; ++i) store_gradient<T, EXPS, true>(to + (v - i * NT) * V, x[i], g, sc);
     }
     for (; v >= 0; v -= NT) store_gradient<T, EXPS, true>(to + v * V, load16(vecs + v * V), g, sc);
   }
