@@ -244,7 +244,7 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_i8_kernel(const ProductAr
   }
 }
 
-// Few rows (M <= 16 * MB): the weights go by once, bound by memory; a workgroup owns 16 columns, its waves a part of K each.  A wave's lane reads
+// Few rows (M <= 16 * MB): the weights go by once, bound by memory; a workgroup owns 16 * CB columns, its waves a part of K each.  A wave's lane reads
 // 16 bytes of column lane % 16 at 16 * (lane / 16) of a step of 64, straight into the matrix cores (v_mfma_i32_16x16x64_i8), U steps'
 // loads in flight; the rows of activations are the second operand.  The waves' integer sums are added through LDS.
 // X: the activations are float or bfloat16 and quantized here (up to kFusedRows rows, into LDS), while the first weights are on their way:
@@ -256,21 +256,25 @@ struct FewArgs {
   int64_t ldx;
   int K;
 };
-template <typename T, int MB, typename X>
+template <typename T, int MB, int CB, typename X>
 __global__ __launch_bounds__(kFewThreads) void matmul_i8_few_kernel(const FewArgs a) {
   constexpr bool FUSED = !std::is_void<X>::value;
-  constexpr int U = 8;
+  constexpr int U = 8 / CB;
   extern __shared__ __align__(16) unsigned char smem[];
   __shared__ int red[kFewWaves][MB][256];
   __shared__ float scale_s[16 * MB];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  const int n0 = blockIdx.x * 16, M = a.p.M, N = a.p.N, Kp = a.p.Kp;
+  const int n0 = blockIdx.x * (16 * CB), M = a.p.M, N = a.p.N, Kp = a.p.Kp;
   const int steps = Kp >> 6, from = steps * wave / kFewWaves, to = steps * (wave + 1) / kFewWaves;
-  const int8_t* wp = a.p.w + static_cast<int64_t>(min(n0 + (lane & 15), N - 1)) * Kp + 16 * (lane >> 4);
-  i32x4 fw[U];
+  const int8_t* wp[CB];
+  i32x4 fw[U][CB];
 #pragma unroll
-  for (int u = 0; u < U; ++u)
-    if (from + u < to) fw[u] = *reinterpret_cast<const i32x4*>(wp + (from + u) * 64);
+  for (int c = 0; c < CB; ++c) {
+    wp[c] = a.p.w + static_cast<int64_t>(min(n0 + c * 16 + (lane & 15), N - 1)) * Kp + 16 * (lane >> 4);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (from + u < to) fw[u][c] = *reinterpret_cast<const i32x4*>(wp[c] + (from + u) * 64);
+  }
   const int8_t* xq[MB];  // this lane's rows
   if constexpr (FUSED) {
     constexpr int V = Elem<X>::VEC;
@@ -317,39 +321,50 @@ __global__ __launch_bounds__(kFewThreads) void matmul_i8_few_kernel(const FewArg
     const int m = min(b * 16 + (lane & 15), M - 1);
     xq[b] = (FUSED ? reinterpret_cast<const int8_t*>(smem) : a.p.q) + static_cast<int64_t>(m) * Kp + 16 * (lane >> 4);
   }
-  i32x4 acc[MB];
+  i32x4 acc[CB][MB];
 #pragma unroll
-  for (int b = 0; b < MB; ++b) acc[b] = i32x4{0, 0, 0, 0};
+  for (int c = 0; c < CB; ++c)
+#pragma unroll
+    for (int b = 0; b < MB; ++b) acc[c][b] = i32x4{0, 0, 0, 0};
   for (int s = from; s < to; s += U) {
-    i32x4 w[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) w[u] = fw[u];
+    i32x4 w[U][CB];
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (s + U + u < to) fw[u] = *reinterpret_cast<const i32x4*>(wp + (s + U + u) * 64);
+#pragma unroll
+      for (int c = 0; c < CB; ++c) {
+        w[u][c] = fw[u][c];
+        if (s + U + u < to) fw[u][c] = *reinterpret_cast<const i32x4*>(wp[c] + (s + U + u) * 64);
+      }
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (s + u < to) {
 #pragma unroll
-        for (int b = 0; b < MB; ++b)
-          acc[b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[u], *reinterpret_cast<const i32x4*>(xq[b] + (s + u) * 64), acc[b], 0, 0, 0);
+        for (int b = 0; b < MB; ++b) {
+          const i32x4 x = *reinterpret_cast<const i32x4*>(xq[b] + (s + u) * 64);
+#pragma unroll
+          for (int c = 0; c < CB; ++c) acc[c][b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[u][c], x, acc[c][b], 0, 0, 0);
+        }
       }
   }
   // column 4 * (lane / 16) + i of the 16, row lane % 16
 #pragma unroll
-  for (int b = 0; b < MB; ++b)
+  for (int c = 0; c < CB; ++c) {
+    if (FUSED || c) __syncthreads();  // (`red` has been read)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) red[wave][b][(lane & 15) * 16 + 4 * (lane >> 4) + i] = acc[b][i];
-  __syncthreads();
+    for (int b = 0; b < MB; ++b)
 #pragma unroll
-  for (int e = tid; e < MB * 256; e += kFewThreads) {
-    const int b = e >> 8, m = b * 16 + ((e >> 4) & 15), n = n0 + (e & 15);
-    if (m < M && n < N) {
-      int sum = 0;
+      for (int i = 0; i < 4; ++i) red[wave][b][(lane & 15) * 16 + 4 * (lane >> 4) + i] = acc[c][b][i];
+    __syncthreads();
 #pragma unroll
-      for (int w = 0; w < kFewWaves; ++w) sum += red[w][b][e & 255];
-      const float s = FUSED ? scale_s[m] : a.p.qs[m];
-      Elem<T>::store(static_cast<T*>(a.p.y) + m * a.p.ldy + n, fmaf(static_cast<float>(sum) * s, a.p.ws[n], a.p.bias ? a.p.bias[n] : 0.f));
+    for (int e = tid; e < MB * 256; e += kFewThreads) {
+      const int b = e >> 8, m = b * 16 + ((e >> 4) & 15), n = n0 + c * 16 + (e & 15);
+      if (m < M && n < N) {
+        int sum = 0;
+#pragma unroll
+        for (int w = 0; w < kFewWaves; ++w) sum += red[w][b][e & 255];
+        const float s = FUSED ? scale_s[m] : a.p.qs[m];
+        Elem<T>::store(static_cast<T*>(a.p.y) + m * a.p.ldy + n, fmaf(static_cast<float>(sum) * s, a.p.ws[n], a.p.bias ? a.p.bias[n] : 0.f));
+      }
     }
   }
 }
@@ -404,19 +419,28 @@ static void product_tile(ProductArgs a, hipStream_t s) {
   allow_big_lds(kernel, lds);
   RN50_LAUNCH("matmul_i8", kernel, dim3(static_cast<unsigned>(a.tiles_m) * a.tiles_n), dim3(64 * WM * WN), lds, s, a);
 }
-template <typename T, int MB, typename X>
+template <typename T, int MB, int CB, typename X>
 static void few_rows(const FewArgs& a, hipStream_t s) {
-  const auto kernel = matmul_i8_few_kernel<T, MB, X>;
+  const auto kernel = matmul_i8_few_kernel<T, MB, CB, X>;
   const int lds = std::is_void<X>::value ? 0 : static_cast<int>(align_up(static_cast<size_t>(a.p.M) * a.p.Kp, 16));
   if (lds) allow_big_lds(kernel, lds);
-  RN50_LAUNCH("matmul_i8", kernel, dim3(static_cast<unsigned>(ceil_div(a.p.N, 16))), dim3(kFewThreads), lds, s, a);
+  RN50_LAUNCH("matmul_i8", kernel, dim3(static_cast<unsigned>(ceil_div(a.p.N, 16 * CB))), dim3(kFewThreads), lds, s, a);
 }
 template <typename T>
 static void few_rows_quantized(const ProductArgs& p, hipStream_t s) {
   const FewArgs a{p, nullptr, 0, 0};
-  if (p.M <= 16) few_rows<T, 1, void>(a, s);
-  else if (p.M <= 32) few_rows<T, 2, void>(a, s);
-  else few_rows<T, 4, void>(a, s);
+  // 32 columns a workgroup, which reads the rows half as often, where enough workgroups are left: 64 x 8192 -> 8192 46 -> 36 us, 20 x 4096 -> 8192
+  // 17.3 -> 14.7, 48 x 2048 -> 16384 24.7 -> 18.2; 33 x 4096 -> 4096 13.6 -> 16.0, 64 x 8192 -> 2048 23 -> 28; with 16 rows 8192 -> 8192 23.8 -> 24.2.
+  const bool wide = p.N >= 8192;
+  if (p.M <= 16) {
+    few_rows<T, 1, 1, void>(a, s);
+  } else if (p.M <= 32) {
+    if (wide) few_rows<T, 2, 2, void>(a, s);
+    else few_rows<T, 2, 1, void>(a, s);
+  } else {
+    if (wide) few_rows<T, 4, 2, void>(a, s);
+    else few_rows<T, 4, 1, void>(a, s);
+  }
 }
 constexpr int kFewRows = 64;
 // Whether fc_i8_fwd takes its rows as they are.
@@ -503,10 +527,10 @@ extern "C" int fc_i8_fwd(int M, int N, int K, int x_dtype, const void* x, int64_
   float* qs = reinterpret_cast<float*>(q + align_up(static_cast<size_t>(M) * quant_i8_row_bytes(K), 256));
   if (few_fused(M, K)) {
     const FewArgs a{{nullptr, w, nullptr, w_scale, bias, y, ldy, M, N, static_cast<int>(quant_i8_row_bytes(K)), 0, 0}, x, ldx, K};
-    if (x_dtype == RN50_BF16 && y_dtype == RN50_BF16) few_rows<uint16_t, 1, uint16_t>(a, s);
-    else if (x_dtype == RN50_BF16) few_rows<float, 1, uint16_t>(a, s);
-    else if (y_dtype == RN50_BF16) few_rows<uint16_t, 1, float>(a, s);
-    else few_rows<float, 1, float>(a, s);
+    if (x_dtype == RN50_BF16 && y_dtype == RN50_BF16) few_rows<uint16_t, 1, 1, uint16_t>(a, s);
+    else if (x_dtype == RN50_BF16) few_rows<float, 1, 1, uint16_t>(a, s);
+    else if (y_dtype == RN50_BF16) few_rows<uint16_t, 1, 1, float>(a, s);
+    else few_rows<float, 1, 1, float>(a, s);
     return launch_status("fc_i8_fwd");
   }
   quant_run(M, K, x_dtype, x, ldx, q, qs, s);
