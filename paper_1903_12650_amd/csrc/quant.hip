@@ -247,7 +247,7 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_i8_kernel(const ProductAr
 // Few rows (M <= 16 * MB): the weights go by once, bound by memory; a workgroup owns 16 * CB columns, its waves a part of K each.  A wave's lane reads
 // 16 bytes of column lane % 16 at 16 * (lane / 16) of a step of 64, straight into the matrix cores (v_mfma_i32_16x16x64_i8), U steps'
 // loads in flight; the rows of activations are the second operand.  The waves' integer sums are added through LDS.
-// X: the activations are float or bfloat16 and quantized here (up to kFusedRows rows, into LDS), while the first weights are on their way:
+// X: the activations are float or bfloat16 and quantized here (up to 16 rows, into LDS: all threads each row, more than kFusedRows a wave a row), while the first weights are on their way:
 // no second launch; every workgroup does so for itself.
 constexpr int kFewThreads = 512, kFewWaves = kFewThreads / 64, kFusedRows = 4;
 struct FewArgs {
@@ -279,6 +279,23 @@ __global__ __launch_bounds__(kFewThreads) void matmul_i8_few_kernel(const FewArg
   if constexpr (FUSED) {
     constexpr int V = Elem<X>::VEC;
     const int whole = a.K / V, left = a.K - whole * V;
+    if (M > kFusedRows) {  // a wave a row
+      for (int m = wave; m < M; m += kFewWaves) {
+        const X* row = static_cast<const X*>(a.x) + m * a.ldx;
+        uint32_t top = 0;
+        for (int v = lane; v < whole; v += 64) top = top_of<X>(top, load16_any(row + v * V));
+        const float z_left = lane < left ? Elem<X>::load(row + whole * V + lane) : 0.f;
+        top = max(top_float_bits<X>(top), __float_as_uint(z_left) & 0x7fffffffu);
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), off, 64)));
+        float inv;
+        const float s = i8_scale(top, &inv);
+        int8_t* out = reinterpret_cast<int8_t*>(smem) + m * Kp;
+        for (int v = lane; v < whole; v += 64) store_quantized<X>(out + v * V, load16_any(row + v * V), inv);
+        for (int i = lane; i < Kp - whole * V; i += 64) out[whole * V + i] = static_cast<int8_t>(i < left && inv != 0.f ? i8_of(z_left, inv) : 0u);
+        if (lane == 0) scale_s[m] = s;
+      }
+    } else {  // all threads each of them
     uint32_t top[kFusedRows];
     float z_left[kFusedRows];
 #pragma unroll
@@ -314,6 +331,7 @@ __global__ __launch_bounds__(kFewThreads) void matmul_i8_few_kernel(const FewArg
         if (tid < Kp - whole * V) out[whole * V + tid] = static_cast<int8_t>(tid < left && inv != 0.f ? i8_of(z_left[m], inv) : 0u);
         if (tid == 0) scale_s[m] = s;
       }
+    }
     __syncthreads();
   }
 #pragma unroll
@@ -443,13 +461,14 @@ static void few_rows_quantized(const ProductArgs& p, hipStream_t s) {
   }
 }
 constexpr int kFewRows = 64;
-// Whether fc_i8_fwd takes its rows as they are.
+// Whether fc_i8_fwd takes its rows as they are.  Two launches -> one: 1 x 2048 -> 1000 7.6 -> 5.2 us, 1 x 8192 -> 8192 19 -> 16, 16 x 1024 -> 1000 8.3 -> 5.8;
+// 3 x 8192 -> 16384 34 -> 36 (every workgroup quantizes all rows), 64 x 256 -> 1000 8.3 -> 9.9 (eight rows a wave).
 static bool few_fused(int M, int K) {
   int64_t most = 16384;
 #ifdef RN50_TUNING  // tuning builds only: RN50_I8_FUSED=numbers
   if (const char* e = getenv("RN50_I8_FUSED")) most = atoi(e);
 #endif
-  return M <= kFusedRows && static_cast<int64_t>(M) * static_cast<int64_t>(quant_i8_row_bytes(K)) <= most;
+  return M <= 16 && static_cast<int64_t>(M) * static_cast<int64_t>(quant_i8_row_bytes(K)) <= most;
 }
 template <typename T>
 static void product_typed(const ProductArgs& a, hipStream_t s) {

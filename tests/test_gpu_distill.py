@@ -93,7 +93,7 @@ def test_quantized_rows_of_extreme_values(rn, dtype):
 PRODUCTS = [(1, 1, 1), (1, 1000, 2048), (1, 17, 64), (2, 33, 100), (3, 5, 4099), (7, 256, 512), (16, 129, 1000), (17, 1000, 2048), (40, 1000, 2048),
             (33, 96, 640), (64, 64, 64), (65, 130, 128), (127, 255, 192), (129, 257, 320), (256, 256, 256), (257, 300, 65), (300, 513, 1025),
             (515, 258, 2047), (1001, 777, 448), (20, 8193, 130), (64, 8200, 320), (49, 8192, 1000),
-            (4, 300, 4096), (5, 300, 4096), (2, 77, 8192), (3, 77, 8192)]
+            (4, 300, 4096), (5, 300, 4096), (2, 77, 8192), (3, 77, 8192), (16, 40, 1024), (16, 40, 1025), (9, 70, 1777), (13, 33, 5)]
 
 
 def product_bound(size, want, out):
