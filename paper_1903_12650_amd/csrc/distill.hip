@@ -614,43 +614,83 @@ __global__ __launch_bounds__(kTopkThreads, 8) void topk_rows_kernel(const TopkAr
   else a.tail[n] = tail_of(sum, a.temperature);
 }
 
-// The largest of a row's slices' largest logits: kJoin of them a thread at most, in registers (slices in their order, each in its own:
-// equal logits lie in the order of their classes).  One workgroup per row.
+// A row whose logits are PER a thread at most, in registers; they are their own streams, and nothing is read again.  The rows are short
+// ones, or the largest logits of a row's slices (slices in their order, each in its own: equal logits lie in the order of their classes).
+// One workgroup per row.
 constexpr int kJoin = 16;
-__global__ __launch_bounds__(kTopkThreads) void topk_join_kernel(const TopkArgs a) {
+template <typename T, int MODE, int PER>
+__global__ __launch_bounds__(kTopkThreads) void topk_short_kernel(const TopkArgs a) {
   constexpr int NT = kTopkThreads;
+  constexpr bool JOIN = MODE == kTopkJoin;
   __shared__ TopkShared sh;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = blockIdx.x;
-  const int total = a.slices * a.k;  // (at least k of them logits: every slice but the last has k)
-  const float* list = a.part_values + static_cast<int64_t>(n) * total;
-  const TopkOut<kTopkJoin> out{a, n, 0};
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = blockIdx.y * gridDim.x + blockIdx.x;
+  if (n >= a.N) return;
+  const int total = JOIN ? a.slices * a.k : a.C;  // (JOIN: at least k of them logits, every slice but the last has k)
+  const int kk = min(a.k, total);
+  const T* list = JOIN ? reinterpret_cast<const T*>(a.part_values) + static_cast<int64_t>(n) * total : static_cast<const T*>(a.logits) + n * a.ld;
+  const TopkOut<MODE> out{a, n, 0};
   Scales sc;
   sc.t = sc.one = kLog2e / a.temperature;
   sc.slack = 20.f / sc.t;
-  float z[kJoin];
-  uint32_t key[kJoin], most = 0;
+  float z[PER];
+  uint32_t key[PER], most = 0, least = 0xffffffffu;
 #pragma unroll
-  for (int g = 0; g < kJoin; ++g) {
+  for (int g = 0; g < PER; ++g) {
     const int i = g * NT + tid;
-    z[g] = i < total ? list[i] : -INFINITY;
-    key[g] = i < total ? order_key(z[g]) : 0;
+    z[g] = i < total ? Elem<T>::load(list + i) : -INFINITY;
+  }
+#pragma unroll
+  for (int g = 0; g < PER; ++g) {
+    const bool in = g * NT + tid < total;
+    key[g] = in ? order_key(z[g]) : 0;
     most = max(most, key[g]);
+    least = min(least, in ? key[g] : least);
   }
   if (tid == 0) sh.taken = 0;
   sh.hist[tid] = 0;
   sh.first[tid] = -1;
-  // of the first slice's k logits the last is one that k reach
-  const uint32_t least = order_key(list[a.k - 1]);
+  if (JOIN) least = order_key(Elem<T>::load(list + a.k - 1));  // of the first slice's k logits the last is one that k reach
 #pragma unroll
-  for (int off = 32; off > 0; off >>= 1) most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), off, 64)));
-  if (lane == 0) sh.count[1][wave] = static_cast<int>(most);
+  for (int off = 32; off > 0; off >>= 1) {
+    most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), off, 64)));
+    if (!JOIN) least = min(least, static_cast<uint32_t>(__shfl_xor(static_cast<int>(least), off, 64)));
+  }
+  if (lane == 0) sh.count[1][wave] = static_cast<int>(most), sh.count[1][4 + wave] = static_cast<int>(least);
   __syncthreads();
-  for (int w = 0; w < 4; ++w) most = max(most, static_cast<uint32_t>(sh.count[1][w]));
+  for (int w = 0; w < 4; ++w) {
+    most = max(most, static_cast<uint32_t>(sh.count[1][w]));
+    least = min(least, static_cast<uint32_t>(sh.count[1][4 + w]));
+  }
+  // (a row of masked logits and a few others: its bins are those of the others)
+  if (!JOIN && least == kKeyOfNothing) {
+    uint32_t above = most;
+    int c = 0;
+#pragma unroll
+    for (int g = 0; g < PER; ++g)
+      if (key[g] > kKeyOfNothing) {
+        above = min(above, key[g]);
+        ++c;
+      }
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) {
+      above = min(above, static_cast<uint32_t>(__shfl_xor(static_cast<int>(above), off, 64)));
+      c += __shfl_xor(c, off, 64);
+    }
+    __syncthreads();
+    if (lane == 0) sh.count[1][wave] = static_cast<int>(above), sh.count[1][4 + wave] = c;
+    __syncthreads();
+    c = 0;
+    for (int w = 0; w < 4; ++w) {
+      above = min(above, static_cast<uint32_t>(sh.count[1][w]));
+      c += sh.count[1][4 + w];
+    }
+    if (c >= kk) least = above;
+  }
   bool tie;
-  const uint32_t lo = find_bound<kJoin>(key, least, most, a.k, &tie, sh);
+  const uint32_t lo = find_bound<PER>(key, least, most, kk, &tie, sh);
   const uint32_t bound = tie ? lo + 1 : lo;
 #pragma unroll
-  for (int g = 0; g < kJoin; ++g)
+  for (int g = 0; g < PER; ++g)
     if (key[g] >= bound) {
       const int at = atomicAdd(&sh.taken, 1);
       if (at < kTopkCand) {
@@ -660,20 +700,20 @@ __global__ __launch_bounds__(kTopkThreads) void topk_join_kernel(const TopkArgs 
       z[g] = -INFINITY;
     }
   __syncthreads();
-  const int cands = min(sh.taken, kTopkCand);
-  put_ranked(cands, a.k, bound, most, out, sh);
-  if (cands < a.k) {  // the rest from the equal ones, in their order
-    const int need = a.k - cands;
-    uint64_t votes[kJoin];
+  const int cands = min(sh.taken, kTopkCand);  // (find_bound lets at most 400 through)
+  put_ranked(cands, kk, bound, most, out, sh);
+  if (cands < kk) {  // the rest from the equal ones, in their order
+    const int need = kk - cands;
+    uint64_t votes[PER];
 #pragma unroll
-    for (int g = 0; g < kJoin; ++g) {
+    for (int g = 0; g < PER; ++g) {
       votes[g] = __ballot(key[g] == lo);
       if (lane == 0) sh.count[0][g * 4 + wave] = __popcll(votes[g]);
     }
     __syncthreads();
     int before = 0;
 #pragma unroll
-    for (int g = 0; g < kJoin; ++g) {
+    for (int g = 0; g < PER; ++g) {
       int pos = before + __popcll(votes[g] & ((1ull << lane) - 1));
       for (int w = 0; w < 4; ++w) {
         const int c = sh.count[0][g * 4 + w];
@@ -686,11 +726,15 @@ __global__ __launch_bounds__(kTopkThreads) void topk_join_kernel(const TopkArgs 
       }
     }
   }
+  for (int r = kk + tid; r < a.k; r += NT) {
+    a.values[static_cast<int64_t>(n) * a.k + r] = -INFINITY;
+    a.indices[static_cast<int64_t>(n) * a.k + r] = -1;
+  }
   if (a.tail == nullptr) return;
   Sums<1> rest;
-  rest.template add<kJoin>(z, sc);
-  for (int c = tid; c < cands - a.k; c += NT) rest.template add<1>(&sh.spare[c], sc);
-  if (tid < a.slices) {
+  rest.template add<PER>(z, sc);
+  for (int c = tid; c < cands - kk; c += NT) rest.template add<1>(&sh.spare[c], sc);
+  if (JOIN && tid < a.slices) {
     const RowSums part = a.part_sums[static_cast<int64_t>(n) * a.slices + tid];
     Sums<1> p;
     p.ref = part.ref;
@@ -1237,11 +1281,19 @@ static void topk_slicing(int N, int C, int k, TopkArgs* a, void* workspace, size
 template <typename T>
 static void topk_run(TopkArgs a, hipStream_t s) {
   if (a.slices < 2) {
-    RN50_LAUNCH("topk_rows", (topk_rows_kernel<T, kTopkRows>), row_grid(a.N), dim3(kTopkThreads), 0, s, a);
+    // Short rows in registers (us, streams -> registers): 40 x 1000, 8 entries 6.6 -> 5.9, 64 x 1000, 256 entries float 51 -> 7.0 (fewer vectors than
+    // entries: no bound from their maxima), 86 x 306, 75 entries bf16 26 -> 6.0; with 16 logits a thread 64 x 2000, 200 entries bf16 28 -> 10.4, but
+    // 100 entries 8.2 -> 9.2, 64 x 4000, 256 entries 13.2 -> 14.2, 4096 x 2048, 16 entries 21 -> 42.
+    if (a.C <= kTopkThreads * 4)
+      RN50_LAUNCH("topk_rows", (topk_short_kernel<T, kTopkRows, 4>), row_grid(a.N), dim3(kTopkThreads), 0, s, a);
+    else if (a.C <= kTopkThreads * kJoin && a.C / Elem<T>::VEC * 2 < a.k * 3)
+      RN50_LAUNCH("topk_rows", (topk_short_kernel<T, kTopkRows, kJoin>), row_grid(a.N), dim3(kTopkThreads), 0, s, a);
+    else
+      RN50_LAUNCH("topk_rows", (topk_rows_kernel<T, kTopkRows>), row_grid(a.N), dim3(kTopkThreads), 0, s, a);
     return;
   }
   RN50_LAUNCH("topk_rows", (topk_rows_kernel<T, kTopkSlices>), dim3(a.slices, a.N), dim3(kTopkThreads), 0, s, a);
-  RN50_LAUNCH("topk_rows", topk_join_kernel, dim3(a.N), dim3(kTopkThreads), 0, s, a);
+  RN50_LAUNCH("topk_rows", (topk_short_kernel<float, kTopkJoin, kJoin>), row_grid(a.N), dim3(kTopkThreads), 0, s, a);
 }
 
 static int check_rows(const char* who, int N, int C, int dtype, const void* logits, int64_t ld) {

@@ -169,7 +169,7 @@ def check_topk(rn, x, k, temperature, tail=True):
 
 TOPK = [(1, 1, 1), (3, 5, 8), (40, 1000, 8), (2, 256, 256), (5, 257, 256), (9, 255, 1), (4, 1024, 100), (33, 4096, 32), (3, 8195, 64), (1, 50001, 100),
         (2, 65537, 17), (6, 40000, 256), (1, 131072, 64), (3, 300001, 128), (200, 2500, 10), (130, 33000, 50),
-        (1, 81933, 256), (7, 98304, 1), (241, 80001, 30)]
+        (1, 81933, 256), (7, 98304, 1), (241, 80001, 30), (9, 306, 75), (5, 1025, 200), (3, 2500, 256), (3, 1024, 256)]
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
@@ -183,7 +183,7 @@ def test_largest_logits(rn, N, C, k, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
-@pytest.mark.parametrize("C, k", [(1000, 7), (5000, 64), (70000, 100), (70000, 256), (100003, 100), (100003, 256)])
+@pytest.mark.parametrize("C, k", [(1000, 7), (1000, 256), (2100, 256), (5000, 64), (70000, 100), (70000, 256), (100003, 100), (100003, 256)])
 def test_largest_logits_of_awkward_rows(rn, C, k, dtype):
     g = torch.Generator().manual_seed(C + k)
     low = torch.finfo(dtype).min
