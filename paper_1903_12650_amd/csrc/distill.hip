@@ -1309,7 +1309,12 @@ template <typename T, int EXPS>
 static void distill_rows(const DistillArgs& a, dim3 grid, hipStream_t s) {
   constexpr int V = Elem<T>::VEC;
   const int64_t vecs = ceil_div(a.C, V);
-#define ROWS(NT, U) RN50_LAUNCH("distill", (distill_rows_kernel<T, EXPS, NT, U>), grid, dim3(NT), 0, s, a)
+  // Rows that are read twice are read from the last-level cache (256 MB) the second time while all that are in flight fit it: with four
+  // workgroups of rows of 256 KB on a compute unit they do not, so LDS that nobody uses keeps the fourth away (2048 x 131072 bf16 256 -> 250 us,
+  // 2048 x 180000 392 -> 369).
+  const int64_t fit = (int64_t{224} << 20) / (256 * static_cast<int64_t>(a.C) * static_cast<int64_t>(sizeof(T)));
+  const int pad = !a.grad || fit > 3 ? 0 : fit == 3 ? 24 * 1024 : 37 * 1024;
+#define ROWS(NT, U) RN50_LAUNCH("distill", (distill_rows_kernel<T, EXPS, NT, U>), grid, dim3(NT), U == 0 && NT == 512 ? pad : 0, s, a)
 #ifdef RN50_TUNING  // tuning builds only: RN50_DISTILL=threads,vectors held by a thread
   if constexpr (EXPS == 2) {
     int nt, u;
