@@ -51,7 +51,8 @@ int rn50_version(void);
 /* Measurement aid (not part of the method): while enabled, every launch whose kernel
  * tag begins with `kernel_tag` ("conv_fwd", "conv_dgrad", "conv_wgrad", "splitk_reduce"
  * (the second pass of a split weight gradient), "bn_stats", "bn_finalize", "bn_apply", "bn_bwd_reduce",
- * "bn_bwd_finalize", "bn_bwd_apply", "lars_norms", "lars_apply", "fc_bwd_da"; the empty
+ * "bn_bwd_finalize", "bn_bwd_apply", "lars_norms", "lars_apply", "fc_bwd_da", "quant_rows_i8", "matmul_i8", "topk_rows",
+ * "distill", "distill_loss"; the empty
  * string matches every tagged launch) is given a HIP event pair that receives the begin and end timestamps of that dispatch
  * on the launch stream, up to max_records launches.  rn50_profile_end waits for the
  * last recorded launch, writes the milliseconds each recorded kernel ran, in launch
@@ -500,8 +501,9 @@ int topk_rows(int N, int C, int k, int dtype, const void* logits, int64_t ld, fl
  *     alpha T (softmax(u)_i - p_j) for i = i_j,  alpha T softmax(u)_i (1 - p_r / q_r) for the others,
  *     + (1-alpha) (softmax(z)_i - (1-ls) [i == label] - ls / C)
  * An entry whose class is outside [0,C) is absent, and so is one whose class an entry in front of it has.  A row
- * without entries and tail has KL = 0; a label outside [0,C) (or labels NULL) leaves CE out.  A row of weight 0 is
- * not read, a row whose logits are all -infinity has no distribution: loss and gradient 0 for both.
+ * without entries and tail has KL = 0; a label outside [0,C) (or labels NULL) leaves CE out.  A row of weight 0 counts
+ * for nothing, whatever it holds, a row whose logits are all -infinity has no distribution: loss and gradient 0 for
+ * both.  With and without dlogits the losses are the same bits.
  * logits, dlogits: device dtype, rows of C elements ld >= C apart, grad_ld for the gradient; dlogits may be NULL (the
  * loss alone) or the logits' own memory (with grad_ld == ld), and must not overlap them otherwise.  t_values float
  * [N,k], t_indices int32 [N,k], t_tail float[N] or NULL; labels int32[N] or NULL; row_weight float[N] or NULL;

@@ -59,14 +59,15 @@ __device__ __forceinline__ void store_quantized(int8_t* to, const Vec16& x, floa
   else *reinterpret_cast<uint2*>(to) = inv != 0.f ? make_uint2(i8_four(f, inv), i8_four(f + 4, inv)) : make_uint2(0u, 0u);
 }
 
-// NT threads per row (a wave, or the workgroup), the row U vectors a thread at most: it is read once.  U = 0: it is read twice.
+// NT threads per row (a wave, or the workgroup), the row U vectors a thread at most: it is read once.  U = 0: it is read twice.  Bound by memory:
+// 8192 x 8192 bf16 (134 MB read, 67 written) 29 us, 50176 x 1024 26, 6 to 7 TB/s.
 template <typename T, int NT, int U>
 __global__ __launch_bounds__(256) void quant_rows_kernel(const T* __restrict__ x, int64_t ldx, int M, int K, int Kp, int8_t* __restrict__ q,
                                                          float* __restrict__ scale) {
   constexpr int V = Elem<T>::VEC;
   static_assert(NT == 64 || NT == 256, "a wave or a workgroup");
   __shared__ uint32_t red[4];
-  const int64_t m = static_cast<int64_t>(blockIdx.x) * (256 / NT) + threadIdx.x / NT;
+  const int64_t m = (static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x) * (256 / NT) + threadIdx.x / NT;
   if (m >= M) return;  // (a whole wave, or all of them)
   const int t = threadIdx.x % NT, whole = K / V, left = K - whole * V;
   const T* row = x + m * ldx;
@@ -123,6 +124,9 @@ struct ProductArgs {
 // straight into LDS (16 bytes a lane) into one of RING buffers while another is multiplied: one barrier a chunk.  Piece p (16 bytes) of
 // row r lies in slot p ^ ((r >> 1) & 7), which spreads the fragment reads (32 rows of one piece) over all banks.  Rows past the last and
 // the second half of a last chunk of 64 bytes are zeros.  The weights are the first operand, so that a lane has 4 consecutive columns of one row.
+// What bounds it: large products the power that the matrix cores may draw (8192^3 480 to 560 us, 2.0 to 2.3 POP/s, with whatever tile; the
+// same product of zeros 376 to 403), middle ones a workgroup's own chain: some 4 us of start, first loads and output stage around
+// 0.5 to 0.7 us a chunk, of which the matrix cores need 0.2 (128x128) to 0.85 (256x256).
 template <typename T, int BM, int BN, int WM, int WN, int RING>
 __global__ __launch_bounds__(64 * WM * WN) void matmul_i8_kernel(const ProductArgs a) {
   constexpr int NT = 64 * WM * WN, RPL = NT / 8, RA = BM / RPL, RB = BN / RPL, TM = BM / WM / 32, TN = BN / WN / 32;
@@ -424,7 +428,7 @@ static int check_product(const char* who, int M, int N, int K, const void* w, co
   RN50_REQUIRE(y_dtype == RN50_F32 || y_dtype == RN50_BF16, RN50_ERR_INVALID, "%s: dtype %d", who, y_dtype);
   RN50_REQUIRE(M > 0 && N > 0 && K > 0, RN50_ERR_INVALID, "%s: non-positive size", who);
   RN50_REQUIRE(K <= kI8MaxK, RN50_ERR_UNSUPPORTED, "%s: K=%d beyond %d, what a 32-bit sum holds", who, K, kI8MaxK);
-  RN50_REQUIRE(ceil_div(M, 64) * ceil_div(N, 64) <= (1 << 22), RN50_ERR_UNSUPPORTED, "%s: M=%d by N=%d beyond the launch grid", who, M, N);
+  RN50_REQUIRE(ceil_div(M, 64) * ceil_div(N, 64) <= (1 << 22) && N <= (1 << 26), RN50_ERR_UNSUPPORTED, "%s: M=%d by N=%d beyond the launch grid", who, M, N);
   RN50_REQUIRE(w && w_scale && y, RN50_ERR_INVALID, "%s: null pointer", who);
   RN50_REQUIRE(ldy >= N, RN50_ERR_INVALID, "%s: rows of %d elements %lld apart", who, N, static_cast<long long>(ldy));
   RN50_REQUIRE(aligned16(w), RN50_ERR_ALIGN, "%s: 8-bit rows not 16-byte aligned", who);
@@ -437,7 +441,11 @@ template <typename T>
 static void quant_typed(int M, int K, const T* x, int64_t ldx, int8_t* q, float* scale, hipStream_t s) {
   const int Kp = static_cast<int>(quant_i8_row_bytes(K));
   const int64_t vecs = K / Elem<T>::VEC;
-#define QUANT(NT, U) RN50_LAUNCH("quant_rows_i8", (quant_rows_kernel<T, NT, U>), dim3(static_cast<unsigned>(ceil_div(M, 256 / NT))), dim3(256), 0, s, x, ldx, M, K, Kp, q, scale)
+  const auto grid = [M](int rows) {  // of workgroups of so many rows
+    const int64_t n = ceil_div(M, rows);
+    return n <= 65536 ? dim3(static_cast<unsigned>(n)) : dim3(65536, static_cast<unsigned>(ceil_div(n, 65536)));
+  };
+#define QUANT(NT, U) RN50_LAUNCH("quant_rows_i8", (quant_rows_kernel<T, NT, U>), grid(256 / NT), dim3(256), 0, s, x, ldx, M, K, Kp, q, scale)
   if (vecs <= 64) QUANT(64, 1);
   else if (vecs <= 64 * 2) QUANT(64, 2);
   else if (vecs <= 64 * 4) QUANT(64, 4);

@@ -28,6 +28,8 @@ def test_refusals_come_before_anything_touches_the_device():
     assert raw.matmul_i8(2, 2, 8, one, None, one, one, None, 0, one, ld(2), None) == -1
     assert raw.matmul_i8(2, 2, 131072, one, one, one, one, None, 0, one, ld(2), None) == -2
     assert raw.matmul_i8(2, 2, 8, one, one, one, one, None, 5, one, ld(2), None) == -1
+    assert raw.matmul_i8(1 << 20, 1 << 20, 8, one, one, one, one, None, 0, one, ld(1 << 20), None) == -2
+    assert raw.matmul_i8(1, (1 << 26) + 1, 8, one, one, one, one, None, 0, one, ld(1 << 27), None) == -2
     assert raw.fc_i8_fwd(2, 2, 8, 0, one, ld(8), one, one, None, 0, one, ld(2), one, ctypes.c_size_t(8), None) == -3
     assert raw.topk_rows(2, 8, 257, 0, one, ld(8), f(1), one, one, None, None, z, None) == -2
     assert raw.topk_rows(2, 8, 3, 0, one, ld(8), f(float("inf")), one, one, None, None, z, None) == -1

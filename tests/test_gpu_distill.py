@@ -416,6 +416,13 @@ def test_more_rows_than_one_line_of_the_grid(rn):
     assert abs(total - float(loss)) < 1e-5 * total
 
 
+def test_quantized_rows_past_one_line_of_the_grid(rn):
+    x = torch.randn(4 * 65536 + 5, 9, device="cuda")
+    q, s = rn.quant_rows_i8(x)
+    for a, b in ((0, 200000), (200000, 262144), (262144, 262149)):
+        assert all(torch.equal(u, v[a:b]) for u, v in zip(rn.quant_rows_i8(x[a:b]), (q, s)))
+
+
 def test_one_long_row(rn):
     """More classes than 2^25, one row: the forms that share a row among workgroups."""
     C = 2 ** 25 + 37
