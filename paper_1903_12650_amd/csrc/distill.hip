@@ -227,6 +227,13 @@ struct TopkOut {
       a.indices[i] = MODE == kTopkJoin ? a.part_at[static_cast<int64_t>(n) * a.slices * a.k + at] : at;
     }
   }
+  __device__ __forceinline__ float value(int rank) const {
+    return MODE == kTopkSlices ? a.part_values[(static_cast<int64_t>(n) * a.slices + slice) * a.k + rank] : a.values[static_cast<int64_t>(n) * a.k + rank];
+  }
+  __device__ __forceinline__ int at(int rank) const {
+    return MODE == kTopkSlices ? a.part_at[(static_cast<int64_t>(n) * a.slices + slice) * a.k + rank] - slice * a.width
+                               : a.indices[static_cast<int64_t>(n) * a.k + rank];
+  }
 };
 
 // Of 256 bins, one a thread, with `mine` in this thread's: how many are in this and all higher ones.  Behind it the waves are past a barrier.
@@ -243,6 +250,33 @@ __device__ __forceinline__ int sum_from_here(int mine, TopkShared& sh) {
   for (int w = wave + 1; w < 4; ++w) sum += sh.count[0][w];
   return sum;
 }
+// Bins of keys, 256 from lo to top.  Keys go by exponents: between a logit below zero and one above lie more than a hundred powers of two in
+// which no logit is, and bins of equal width would put all logits into a few.  So magnitudes below 2^-8 of the larger end's count as one
+// there: of(.) leaves the order as it is, and a key reaches at(b) where its bin is b or a higher one.  (An end beyond 2^64 is a mask or no
+// number: the other end decides.)  4096 x 4000 bf16, 64 entries on
+// both sides of zero, 99 -> 39 us.
+struct KeyBins {
+  int flat, first, last, shift;
+  uint32_t end;
+  __device__ __forceinline__ KeyBins(uint32_t lo, uint32_t top) : end(top + 1u) {
+    const int a = static_cast<int>(lo ^ 0x80000000u), b = static_cast<int>(top ^ 0x80000000u);
+    const int below = ~a > 0x5f800000 ? 0 : ~a, above = b > 0x5f800000 ? 0 : b;
+    flat = a < 0 && b > 0 ? max(0, max(below, above) - (8 << 23)) : 0;
+    first = fold(a);
+    last = fold(b);
+    shift = max(0, 24 - __clz(static_cast<int>(static_cast<uint32_t>(last) - static_cast<uint32_t>(first))));
+  }
+  __device__ __forceinline__ int fold(int x) const { return x - min(max(x, -flat), flat); }
+  __device__ __forceinline__ uint32_t of(uint32_t key) const {
+    return (static_cast<uint32_t>(fold(static_cast<int>(key ^ 0x80000000u))) - static_cast<uint32_t>(first)) >> shift;
+  }
+  __device__ __forceinline__ uint32_t at(uint32_t bin) const {  // (bin 256: behind the last key)
+    const uint32_t step = bin << shift;
+    if (step > static_cast<uint32_t>(last) - static_cast<uint32_t>(first) || bin > 255) return end;
+    return unfold(static_cast<int>(static_cast<uint32_t>(first) + step));
+  }
+  __device__ __forceinline__ uint32_t unfold(int x) const { return static_cast<uint32_t>(x > 0 ? x + flat : x - flat) ^ 0x80000000u; }
+};
 // A key that at least kk of the workgroup's keys reach, hardly more if possible; where that takes a key that many have (`tie`), fewer than
 // kk reach the one after it.  At least kk keys reach lo, none passes top.  The keys' bins (256 from lo to top) mostly hold few enough
 // where the kk-th lies; otherwise its bin is halved until they do.  Every thread calls it, behind a barrier, with `hist` zero, as it
@@ -251,10 +285,10 @@ template <int G>
 __device__ __forceinline__ uint32_t find_bound(const uint32_t* key, uint32_t lo, uint32_t top, int kk, bool* tie, TopkShared& sh) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int enough = kk + kk / 2 + 16;
-  const int shift = max(0, 24 - __clz(static_cast<int>(top - lo)));
+  const KeyBins bins(lo, top);
 #pragma unroll
   for (int g = 0; g < G; ++g)
-    if (key[g] >= lo) atomicAdd(&sh.hist[(key[g] - lo) >> shift], 1u);
+    if (key[g] >= lo) atomicAdd(&sh.hist[bins.of(key[g])], 1u);
   __syncthreads();
   const int mine = static_cast<int>(sh.hist[tid]);
   sh.hist[tid] = 0;
@@ -265,10 +299,10 @@ __device__ __forceinline__ uint32_t find_bound(const uint32_t* key, uint32_t lo,
   }
   __syncthreads();
   int reach = static_cast<int>(sh.found[1]);
-  lo += sh.found[0] << shift;
+  lo = max(lo, bins.at(sh.found[0]));
   *tie = false;
   if (reach <= enough) return lo;
-  uint32_t hi = lo + (1u << shift);
+  uint32_t hi = bins.at(sh.found[0] + 1);
   for (int turn = 0; hi - lo > 1 && reach > enough; turn ^= 1) {
     const uint32_t mid = lo + ((hi - lo) >> 1);
     int c = 0;
@@ -290,9 +324,9 @@ static_assert(kTopkThreads == 256, "a bin a thread");
 template <int MODE>
 __device__ __forceinline__ void put_ranked(int cands, int kk, uint32_t lo, uint32_t hi, const TopkOut<MODE>& out, TopkShared& sh) {
   const int tid = threadIdx.x;
-  const int shift = max(0, 24 - __clz(static_cast<int>(hi - lo)));
+  const KeyBins bins(lo, hi);
   for (int c = tid; c < cands; c += kTopkThreads) {
-    const uint32_t bin = (static_cast<uint32_t>(sh.cand[c] >> 32) - lo) >> shift;
+    const uint32_t bin = bins.of(static_cast<uint32_t>(sh.cand[c] >> 32));
     atomicAdd(&sh.hist[bin], 1u);
     sh.next[c] = static_cast<int16_t>(atomicExch(&sh.first[bin], c));
   }
@@ -303,7 +337,7 @@ __device__ __forceinline__ void put_ranked(int cands, int kk, uint32_t lo, uint3
   __syncthreads();
   for (int c = tid; c < cands; c += kTopkThreads) {
     const unsigned long long me = sh.cand[c];
-    const uint32_t bin = (static_cast<uint32_t>(me >> 32) - lo) >> shift;
+    const uint32_t bin = bins.of(static_cast<uint32_t>(me >> 32));
     int rank = static_cast<int>(sh.hist[bin]);
     for (int j = sh.first[bin]; j >= 0; j = sh.next[j]) rank += sh.cand[j] > me;
     if (rank < kk) out.put(rank, sh.value[c], static_cast<int>(~static_cast<uint32_t>(me)));
@@ -496,7 +530,6 @@ __global__ __launch_bounds__(kTopkThreads, 8) void topk_rows_kernel(const TopkAr
   __syncthreads();
   const bool odd = (sh.count[1][12] | sh.count[1][13]) | (sh.count[1][14] | sh.count[1][15]);
   Sums<1> rest;
-  bool done = false;
   if (!odd) {
     float most = -INFINITY, least = INFINITY;
     for (int w = 0; w < 4; ++w) {
@@ -504,9 +537,9 @@ __global__ __launch_bounds__(kTopkThreads, 8) void topk_rows_kernel(const TopkAr
       least = fminf(least, __int_as_float(sh.count[1][4 + w]));
     }
     bool tie;
-    const uint32_t lo = find_bound<G>(key, order_key(least), order_key(most), kk, &tie, sh);  // (the first kk threads' maxima reach `least`)
-    const uint32_t bound = tie ? lo + 1 : lo;
-    const float from = logit_of(bound);
+    uint32_t lo = find_bound<G>(key, order_key(least), order_key(most), kk, &tie, sh);  // (the first kk threads' maxima reach `least`)
+    uint32_t bound = tie ? lo + 1 : lo;
+    float from = logit_of(bound);
     // what is read again, listed in a fixed order: single vectors from the front, streams from the end; the sums of everything else stay
     rest.ref = ref;
     rest.lim = lim;
@@ -535,6 +568,7 @@ __global__ __launch_bounds__(kTopkThreads, 8) void topk_rows_kernel(const TopkAr
       }
     }
     const int singles = counts & 0xffff, streams = counts >> 16;
+    sh.spare[tid] = rest.st;  // (a second look starts from it)
     auto candidate = [&](float x, int i) __attribute__((always_inline)) {
       const int at = atomicAdd(&sh.taken, 1);
       if (at < kTopkCand) {
@@ -542,62 +576,109 @@ __global__ __launch_bounds__(kTopkThreads, 8) void topk_rows_kernel(const TopkAr
         sh.value[at] = x;
       }
     };
-    if (tid < left) {
-      if (z_left >= from) candidate(z_left, c_left);
-      else rest.template add<1>(&z_left, sc);
-    }
     __syncthreads();
     // (vector of item i: a listed one, or one of a listed stream's)
     const int rounds = max(1, (whole + G * NT - 1) / (G * NT)), items = singles + streams * rounds;
-    constexpr int AHEAD = 2;  // vectors whose loads go out together
-    for (int i0 = tid; i0 < items; i0 += AHEAD * NT) {
-      Vec16 x[AHEAD];
-      int vec[AHEAD];
+    auto vector_of = [&](int i) __attribute__((always_inline)) {
+      if (i < singles) return sh.owner[i];
+      if (i >= items) return whole;
+      const int o = (i - singles) / rounds;
+      return sh.owner[kTopkOwners - 1 - o] + (i - singles - o * rounds) * (G * NT);
+    };
+    // (the candidates' largest key: of the streams' or of the classes of no vector)
+    uint32_t top = order_key(most);
+    for (int i = 0; i < left; ++i) top = max(top, order_key(Elem<T>::load(row + places.class_at(whole * V + i))));
+    int cands;
+#pragma unroll 1
+    for (;;) {
+      if (tid < left) {
+        if (z_left >= from) candidate(z_left, c_left);
+        else rest.template add<1>(&z_left, sc);
+      }
+      constexpr int AHEAD = 2;  // vectors whose loads go out together
+      for (int i0 = tid; i0 < items; i0 += AHEAD * NT) {
+        Vec16 x[AHEAD];
+        int vec[AHEAD];
 #pragma unroll
-      for (int u = 0; u < AHEAD; ++u) {
-        const int i = i0 + u * NT;
-        vec[u] = whole;
-        if (i < singles) {
-          vec[u] = sh.owner[i];
-        } else if (i < items) {
-          const int o = (i - singles) / rounds;
-          vec[u] = sh.owner[kTopkOwners - 1 - o] + (i - singles - o * rounds) * (G * NT);
+        for (int u = 0; u < AHEAD; ++u) {
+          vec[u] = vector_of(i0 + u * NT);
+          if (vec[u] < whole) x[u] = load16(vecs + vec[u] * V);
         }
-        if (vec[u] < whole) x[u] = load16(vecs + vec[u] * V);
-      }
 #pragma unroll
-      for (int u = 0; u < AHEAD; ++u) {
-        if (vec[u] >= whole) continue;
-        float z[V];
-        Elem<T>::unpack(x[u], z);
+        for (int u = 0; u < AHEAD; ++u) {
+          if (vec[u] >= whole) continue;
+          float z[V];
+          Elem<T>::unpack(x[u], z);
 #pragma unroll
-        for (int j = 0; j < V; ++j)
-          if (z[j] >= from) {
-            candidate(z[j], places.head + vec[u] * V + j);
-            z[j] = -INFINITY;
-          }
-        rest.template add<V>(z, sc);
-      }
-    }
-    __syncthreads();
-    const int cands = sh.taken;
-    if (cands <= kTopkCand) {
-      done = true;
-      // (the candidates' largest key: of the streams' or of the classes of no vector)
-      uint32_t top = order_key(most);
-      for (int i = 0; i < left; ++i) top = max(top, order_key(Elem<T>::load(row + places.class_at(whole * V + i))));
-      put_ranked(cands, kk, bound, top, out, sh);
-      for (int c = tid; c < cands - kk; c += NT) rest.template add<1>(&sh.spare[c], sc);
-      if (cands < kk) {  // (many equal maxima)
-        const int last = take_equal<T, MODE>(row, C, lo, kk - cands, cands, out, sh);
-        if (lo != kKeyOfNothing) {  // (the sums have all of the equal ones, and nothing is subtracted)
-          rest = Sums<1>();
-          add_rest(row, C, lo, last, sc, rest);
+          for (int j = 0; j < V; ++j)
+            if (z[j] >= from) {
+              candidate(z[j], places.head + vec[u] * V + j);
+              z[j] = -INFINITY;
+            }
+          rest.template add<V>(z, sc);
         }
       }
+      __syncthreads();
+      cands = sh.taken;
+      if (cands <= kTopkCand) break;
+      // Too many: large logits lie side by side (rows in the order of their classes' frequency).  A higher bound from bins of what is read
+      // again, the k-th largest's bin in bins of its own while it has too many: 4096 x 50001 bf16 in descending order 99 us (digit by digit,
+      // as topk_any does, 1490).
+      uint32_t hi = top;
+      int above = 0;
+      lo = bound;
+#pragma unroll 1
+      for (;;) {
+        const int shift = max(0, 24 - __clz(static_cast<int>(hi - lo)));
+        auto count = [&](float x) __attribute__((always_inline)) {
+          const uint32_t at = order_key(x);
+          if (at >= lo && at <= hi) atomicAdd(&sh.hist[(at - lo) >> shift], 1u);
+        };
+        if (tid < left) count(z_left);
+#pragma unroll 1
+        for (int i = tid; i < items; i += NT) {
+          const int vec = vector_of(i);
+          if (vec >= whole) continue;
+          float z[V];
+          Elem<T>::unpack(load16(vecs + vec * V), z);
+#pragma unroll
+          for (int j = 0; j < V; ++j) count(z[j]);
+        }
+        __syncthreads();
+        const int here = static_cast<int>(sh.hist[tid]), sum = above + sum_from_here(here, sh);
+        if (sum >= kk && sum - here < kk) {
+          sh.found[0] = tid;
+          sh.found[1] = sum;
+          sh.last = here;
+        }
+        sh.hist[tid] = 0;
+        if (tid == 0) sh.taken = 0;
+        __syncthreads();
+        const int reach = static_cast<int>(sh.found[1]);
+        lo += sh.found[0] << shift;
+        tie = shift == 0 && reach > kTopkCand;
+        if (tie || reach <= kTopkCand) break;
+        hi = min(hi, lo + ((1u << shift) - 1));
+        above = reach - sh.last;
+      }
+      bound = tie ? lo + 1 : lo;
+      from = logit_of(bound);
+      rest.ref = ref;
+      rest.lim = lim;
+      rest.st = sh.spare[tid];
     }
+    put_ranked(cands, kk, bound, top, out, sh);
+    for (int c = tid; c < cands - kk; c += NT) rest.template add<1>(&sh.spare[c], sc);
+    if (cands < kk) {  // (many equal maxima)
+      const int last = take_equal<T, MODE>(row, C, lo, kk - cands, cands, out, sh);
+      if (lo != kKeyOfNothing) {  // (the sums have all of the equal ones, and nothing is subtracted)
+        rest = Sums<1>();
+        add_rest(row, C, lo, last, sc, rest);
+      }
+    }
+  } else {
+    topk_any<T, MODE>(row, C, kk, true, sc, out, sh, rest);
   }
-  if (!done) topk_any<T, MODE>(row, C, kk, true, sc, out, sh, rest);
   for (int r = kk + tid; r < a.k; r += NT) {
     if (MODE == kTopkSlices) {
       out.put(r, -INFINITY, -1);
@@ -608,8 +689,17 @@ __global__ __launch_bounds__(kTopkThreads, 8) void topk_rows_kernel(const TopkAr
   }
   if (MODE == kTopkRows && a.tail == nullptr) return;
   __syncthreads();
-  const RowSums sum = block_sums<1, NT>(rest, 0.0, false, sc, sh.red);
+  RowSums sum = block_sums<1, NT>(rest, 0.0, false, sc, sh.red);
+  // The sums' references are those of all logits.  Where the others lie so far below the largest that terms may have been lost (each less than
+  // 2^-126 of a sum about it, fewer than 2^30 of them), they are taken anew.
+  if (sum.st < 0x1p-60f && kk < C && out.value(kk - 1) != -INFINITY) {
+    __syncthreads();
+    rest = Sums<1>();
+    add_rest(row, C, order_key(out.value(kk - 1)), out.at(kk - 1), sc, rest);
+    sum = block_sums<1, NT>(rest, 0.0, false, sc, sh.red);
+  }
   if (tid != 0) return;
+  if (sum.st == 0.f) sum.ref = -FLT_MAX;  // (a slice of nothing: its sum is joined with others)
   if (MODE == kTopkSlices) a.part_sums[static_cast<int64_t>(n) * a.slices + slice] = sum;
   else a.tail[n] = tail_of(sum, a.temperature);
 }

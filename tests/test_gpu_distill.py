@@ -214,6 +214,51 @@ def test_largest_logits_of_awkward_rows(rn, C, k, dtype):
 
 
 # ------------------------------------------------------- distillation loss
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("C, k", [(4001, 64), (9000, 256), (50001, 100), (50001, 256), (131072, 256)])
+def test_largest_logits_that_lie_side_by_side(rn, C, k, dtype):
+    """Rows in the order of their classes' frequency: the vectors that hold the largest logits hold more than are kept as candidates."""
+    g = torch.Generator().manual_seed(C * 3 + k)
+    x = torch.randn(14, C, generator=g)
+    rank = torch.log(torch.arange(1, C + 1).float())
+    x[0] = x[0].sort(descending=True)[0]
+    x[1] = x[1].sort()[0]
+    x[2] = x[2] - rank                                     # the largest on both sides of zero
+    x[3] = x[3] * 0.01 - rank * 0.1
+    x[4] = x[4] * 2 - rank * 2 + 9
+    x[5, 300:1400] = 5 + x[5, 300:1400] * 1e-3             # a hair apart
+    x[6, 300:1400] = 5 + torch.round(x[6, 300:1400] * 8) / 64  # and equal
+    x[7, 300:1400], x[7, 310] = 7.0, 1e30
+    x[8, C - 1200:] = -1e-3 * x[8, C - 1200:].abs() + 6
+    x[9] = torch.where(torch.arange(C) < 1500, x[9].abs() * 1e-20, float("-inf"))
+    x[10] = torch.where(torch.arange(C) < 1500, x[10] * 1e-20, -1.0)
+    x[11, 100:1200] = torch.linspace(-4, 40, 1100)
+    x[11, 1200:] = -5
+    x[12] = -3 - x[12].abs()
+    x[12, 64:1200] = torch.linspace(1e-9, 1e-6, 1136)
+    x[13] = torch.arange(C, 0, -1) * 1e30
+    check_topk(rn, x.to(dtype).cuda(), k, 1.0)
+    check_topk(rn, spread(x[:6].to(dtype).cuda(), 3), k, 3.0)
+    for n in (0, 2, 7):
+        check_topk(rn, x[n:n + 1].to(dtype).cuda(), k, 1.0)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("C, k", [(300, 3), (1001, 8), (4000, 256), (50001, 7), (131072, 64)])
+@pytest.mark.parametrize("temperature", [0.03, 1.0])
+def test_rests_far_below_the_largest_logits(rn, C, k, dtype, temperature):
+    g = torch.Generator().manual_seed(C + 5 * k)
+    x = torch.randn(12, C, generator=g)
+    for n, gap in enumerate((40, 90, 120, 1000, 1e30)):
+        x[n, torch.randperm(C, generator=g)[:k]] += gap    # as many as are taken
+        x[5 + n, torch.randperm(C, generator=g)[:max(1, k // 2)]] += gap
+    x[10, ::2], x[10, 7] = float("-inf"), 500.0
+    x[11, 3:] = float("-inf")                              # a few, or as many as are taken, and nothing else
+    check_topk(rn, x.to(dtype).cuda(), k, temperature)
+    for n in (1, 3, 10):
+        check_topk(rn, x[n:n + 1].to(dtype).cuda(), k, temperature)
+
+
 def teacher(rn, N, C, k, T, seed, tail=True, absent=False):
     g = torch.Generator().manual_seed(seed)
     t = torch.randn(N, C, generator=g) * 3
