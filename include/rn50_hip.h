@@ -484,7 +484,7 @@ int fc_i8_fwd(int M, int N, int K, int x_dtype, const void* x, int64_t ldx, cons
  * above every number.  values: device float [N,k]; indices: device int32 [N,k]; where a row has fewer
  * than k classes the rest is (-infinity, -1).  tail_lse (or NULL): device float[N], the logarithm of the
  * sum of exp(logit / temperature) over the classes that are not among them (-infinity if there are none).
- * logits: device dtype, rows of C elements ld >= C elements apart.  1 <= k <= 256. */
+ * logits: device dtype, rows of C elements ld >= C elements apart.  1 <= k <= 256; temperature 2^-126 or more. */
 size_t topk_rows_workspace_bytes(int N, int C, int k);
 int topk_rows(int N, int C, int k, int dtype, const void* logits, int64_t ld, float temperature, float* values,
               int32_t* indices, float* tail_lse, void* workspace, size_t workspace_bytes, void* stream);
@@ -507,7 +507,7 @@ int topk_rows(int N, int C, int k, int dtype, const void* logits, int64_t ld, fl
  * logits, dlogits: device dtype, rows of C elements ld >= C apart, grad_ld for the gradient; dlogits may be NULL (the
  * loss alone) or the logits' own memory (with grad_ld == ld), and must not overlap them otherwise.  t_values float
  * [N,k], t_indices int32 [N,k], t_tail float[N] or NULL; labels int32[N] or NULL; row_weight float[N] or NULL;
- * loss_out float[1]; row_loss_out float[N].  0 <= k <= 256 (k = 0: no entries), 0 <= alpha, ls <= 1, T > 0. */
+ * loss_out float[1]; row_loss_out float[N].  0 <= k <= 256 (k = 0: no entries), 0 <= alpha, ls <= 1, T 2^-126 or more. */
 typedef struct {
   int N, C, k;
   int dtype;

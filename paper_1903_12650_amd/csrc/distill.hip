@@ -443,7 +443,8 @@ __device__ __forceinline__ void topk_any(const T* row, int C, int kk, bool want_
 // row's k largest can lie is the k-th largest of the streams' maxima, or a little less: of streams whose maximum reaches it (little
 // more than k) that vector is read again, of the few whose second does all vectors, for the logits that reach it (little more than k
 // again), and these are put in order by counting.  The sums of what is read again are taken anew without them: nothing is subtracted.
-// (With whole streams read again, 2048 x 131072 float, 16 vectors a stream, 256 us.)
+// 4096 x 50001 bf16, 100 entries 88 us, 4.7 TB/s; bound by instructions: 39.7 million of a wave's, 3.2 million of them exponentials of four
+// issue slots, keep the vector ALUs busy in nine of ten cycles.  (With whole streams read again, 2048 x 131072 float, 16 vectors a stream, 256 us.)
 // Where many maxima are equal (masks, ties), the logits above their value are the candidates and the rest of the k is taken from the
 // equal ones in the order of the classes.
 template <typename T, int MODE>
@@ -706,7 +707,8 @@ __global__ __launch_bounds__(kTopkThreads, 8) void topk_rows_kernel(const TopkAr
 
 // A row whose logits are PER a thread at most, in registers; they are their own streams, and nothing is read again.  The rows are short
 // ones, or the largest logits of a row's slices (slices in their order, each in its own: equal logits lie in the order of their classes).
-// One workgroup per row.
+// One workgroup per row.  Bound by the chain from loads over bins and order to the output: 40 x 1000, 8 entries 6.1 us, of which a launch that does
+// nothing takes 2 to 4; the joining of 1 x 131072, 64 entries 6.6 behind the slices' 9.3.
 constexpr int kJoin = 16;
 template <typename T, int MODE, int PER>
 __global__ __launch_bounds__(kTopkThreads) void topk_short_kernel(const TopkArgs a) {
@@ -1001,11 +1003,12 @@ __device__ __forceinline__ void store_gradient(T* to, const Vec16& x, const RowG
 }
 
 // One workgroup per row, NT threads, at least as many as a row has entries: a thread has one at most.  Whole vectors of V classes go round the
-// threads, the C % V classes behind the last of them are one thread's each.
+// threads, the classes of no vector (in front of the first, behind the last) are one thread's each.
 // U > 0: the row is U vectors a thread at most and stays in registers between the sums and the gradient: it is read once.  U = 0: it is
-// read for the sums and again for the gradient, in chunks of classes whose membership bits fit LDS; the gradient is stored past the
+// read for the sums and again for the gradient (from its end), in chunks of classes whose membership bits fit LDS; the gradient is stored past the
 // caches, which keep the rows for their second reading (2048 x 131072 bf16 272 -> 246 us, float 500 -> 476).  A thread adds the same vectors in
-// the same order in both.
+// the same order in both.  Bound: the loss of 4096 x 50001 bf16, 87 us, by instructions (41.5 million of a wave's, one exponential a logit: the vector ALUs are never idle);
+// loss and gradient of 2048 x 131072, 250 us, by memory: one reading from it, one from the last-level cache and one writing, 6.4 TB/s together.
 template <typename T, int EXPS, int NT, int U>
 __global__ __launch_bounds__(NT) void distill_rows_kernel(const DistillArgs a) {
   constexpr int V = Elem<T>::VEC;
@@ -1160,7 +1163,8 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(const DistillArgs a) {
 
 // Few rows: slices of a row by workgroups of their own, in two launches.  The first leaves the sums of every slice and, from the slice that
 // has it, every entry's class and logit (a gradient in the logits' place overwrites them in the second); the second joins the
-// sums, every slice for itself, and writes the slice's gradient.
+// sums, every slice for itself, and writes the slice's gradient.  Bound by their chains: 7 x 131072 bf16, 32 entries 4.5 and 5.6 us and 3.4 for the loss,
+// of which a launch that does nothing takes 2 to 4 each.
 struct SliceArgs {
   RowSums* sums;  // [N][slices]
   int* at;        // [N][kTopMax]
@@ -1415,11 +1419,12 @@ static void distill_rows(const DistillArgs& a, dim3 grid, hipStream_t s) {
     }
   }
 #endif
-  // Small workgroups for short rows: a row is mostly its own end, which few waves share and barriers of few waves part (32768 rows of 1000
-  // bf16 106 us with 256 threads, 71 with 128; of 4096 164 -> 127; of 8192 134 streamed, 127 held).  From 1024 vectors on the row is
-  // streamed: held in registers it leaves too few workgroups to cover one another (4096 x 50001 bf16 228 us, held by 512 threads 309).
-  // 256 threads against 512: 8192 x 16384 bf16 120 us, 136; 4096 x 50001 239, 228; 2048 x 131072 284, 246; of 512 KB rows and more the rows in
-  // flight pass the last-level cache: 2048 x 131072 float 532 us with 512, 476 with 1024.
+  // Small workgroups for short rows: a row is mostly its own end, which few waves share and barriers of few waves part (bf16, 256 threads -> 128:
+  // 32768 x 1000 121 -> 90 us, 32768 x 4096 183 -> 161; 64 threads 82, but 40 x 1000 8.9 -> 9.5).  From 1024 vectors on the row is
+  // streamed: held in registers it leaves too few workgroups to cover one another (held, streamed: 16384 x 8192 150, 158, 16384 x 16384 262, 250,
+  // by 512 threads 4096 x 50001 342, 200).  256 threads against 512: 8192 x 20000 165, 186; 8192 x 24576 191, 187; 8192 x 32768 253, 240;
+  // 4096 x 50001 219, 200; 2048 x 131072 279, 253.  512 against 1024: 1024 x 262144 264, 274; float 2048 x 131072 492, 493, 2048 x 180000 771,
+  // 703 (fewer rows in flight for the last-level cache), 1024 x 262144 544, 511.
   const bool few = a.k <= 128;  // (an entry a thread)
   if (vecs <= 256) {
     if (few) ROWS(128, 2);
@@ -1429,9 +1434,9 @@ static void distill_rows(const DistillArgs& a, dim3 grid, hipStream_t s) {
     else ROWS(256, 2);
   } else if (vecs <= 1024) {
     ROWS(256, 4);
-  } else if (vecs <= 4096) {
+  } else if (vecs <= 3072) {
     ROWS(256, 0);
-  } else if (vecs <= 24576) {
+  } else if (vecs <= 32768) {
     ROWS(512, 0);
   } else {
     ROWS(1024, 0);
@@ -1512,7 +1517,7 @@ extern "C" int topk_rows(int N, int C, int k, int dtype, const void* logits, int
   clear_error();
   if (int rc = check_rows("topk_rows", N, C, dtype, logits, ld)) return rc;
   RN50_REQUIRE(k >= 1 && k <= kTopMax, RN50_ERR_UNSUPPORTED, "topk_rows: k=%d outside [1, %d]", k, kTopMax);
-  RN50_REQUIRE(temperature > 0.f && temperature <= FLT_MAX, RN50_ERR_INVALID, "topk_rows: temperature %g", temperature);
+  RN50_REQUIRE(temperature >= FLT_MIN && temperature <= FLT_MAX, RN50_ERR_INVALID, "topk_rows: temperature %g", temperature);
   RN50_REQUIRE(values && indices, RN50_ERR_INVALID, "topk_rows: null pointer");
   RN50_REQUIRE(aligned_to(values, 4) && aligned_to(indices, 4) && aligned_to(tail_lse, 4), RN50_ERR_ALIGN, "topk_rows: pointer not aligned to an element");
   RN50_REQUIRE(aligned16(workspace), RN50_ERR_ALIGN, "topk_rows: workspace not 16-byte aligned");
@@ -1541,7 +1546,7 @@ extern "C" int distill_fwd_bwd(const rn50_distill_desc* d, const void* logits, c
   RN50_REQUIRE(d, RN50_ERR_INVALID, "%s: null descriptor", who);
   if (int rc = check_rows(who, d->N, d->C, d->dtype, logits, d->ld)) return rc;
   RN50_REQUIRE(d->k >= 0 && d->k <= kTopMax, RN50_ERR_UNSUPPORTED, "%s: k=%d outside [0, %d]", who, d->k, kTopMax);
-  RN50_REQUIRE(d->temperature > 0.f && d->temperature <= FLT_MAX, RN50_ERR_INVALID, "%s: temperature %g", who, d->temperature);
+  RN50_REQUIRE(d->temperature >= FLT_MIN && d->temperature <= FLT_MAX, RN50_ERR_INVALID, "%s: temperature %g", who, d->temperature);
   RN50_REQUIRE(d->alpha >= 0.f && d->alpha <= 1.f, RN50_ERR_INVALID, "%s: alpha %g", who, d->alpha);
   RN50_REQUIRE(d->label_smoothing >= 0.f && d->label_smoothing <= 1.f, RN50_ERR_INVALID, "%s: label_smoothing %g", who, d->label_smoothing);
   RN50_REQUIRE(d->k == 0 || (t_values && t_indices), RN50_ERR_INVALID, "%s: null pointer", who);

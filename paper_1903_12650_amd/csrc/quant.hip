@@ -60,7 +60,7 @@ __device__ __forceinline__ void store_quantized(int8_t* to, const Vec16& x, floa
 }
 
 // NT threads per row (a wave, or the workgroup), the row U vectors a thread at most: it is read once.  U = 0: it is read twice.  Bound by memory:
-// 8192 x 8192 bf16 (134 MB read, 67 written) 29 us, 50176 x 1024 26, 6 to 7 TB/s.
+// 8192 x 8192 bf16 (134 MB read, 67 written) 36 us, 50176 x 1024 27, 5.7 TB/s.
 template <typename T, int NT, int U>
 __global__ __launch_bounds__(256) void quant_rows_kernel(const T* __restrict__ x, int64_t ldx, int M, int K, int Kp, int8_t* __restrict__ q,
                                                          float* __restrict__ scale) {
@@ -250,9 +250,10 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_i8_kernel(const ProductAr
 
 // Few rows (M <= 16 * MB): the weights go by once, bound by memory; a workgroup owns 16 * CB columns, its waves a part of K each.  A wave's lane reads
 // 16 bytes of column lane % 16 at 16 * (lane / 16) of a step of 64, straight into the matrix cores (v_mfma_i32_16x16x64_i8), U steps'
-// loads in flight; the rows of activations are the second operand.  The waves' integer sums are added through LDS.
-// X: the activations are float or bfloat16 and quantized here (up to 16 rows, into LDS: all threads each row, more than kFusedRows a wave a row), while the first weights are on their way:
-// no second launch; every workgroup does so for itself.
+// loads in flight; the rows of activations are the second operand.  The waves' integer sums are added through LDS.  1 x 8192 -> 8192 14.4 us with
+// the quantization (67 MB at 4.7 TB/s; a launch's start and end take some 4), 64 x 8192 -> 8192 31 (every workgroup reads the rows from its L2).
+// X: the activations are float or bfloat16 and quantized here (up to 16 rows, into LDS: all threads each row, more than kFusedRows a wave a
+// row), while the first weights are on their way: no second launch; every workgroup does so for itself.
 constexpr int kFewThreads = 512, kFewWaves = kFewThreads / 64, kFusedRows = 4;
 struct FewArgs {
   ProductArgs p;
@@ -300,41 +301,41 @@ __global__ __launch_bounds__(kFewThreads) void matmul_i8_few_kernel(const FewArg
         if (lane == 0) scale_s[m] = s;
       }
     } else {  // all threads each of them
-    uint32_t top[kFusedRows];
-    float z_left[kFusedRows];
+      uint32_t top[kFusedRows];
+      float z_left[kFusedRows];
 #pragma unroll
-    for (int m = 0; m < kFusedRows; ++m) {
-      top[m] = 0;
-      z_left[m] = 0.f;
-      if (m < M) {
-        const X* row = static_cast<const X*>(a.x) + m * a.ldx;
-        for (int v = tid; v < whole; v += kFewThreads) top[m] = top_of<X>(top[m], load16_any(row + v * V));
-        if (tid < left) z_left[m] = Elem<X>::load(row + whole * V + tid);
+      for (int m = 0; m < kFusedRows; ++m) {
+        top[m] = 0;
+        z_left[m] = 0.f;
+        if (m < M) {
+          const X* row = static_cast<const X*>(a.x) + m * a.ldx;
+          for (int v = tid; v < whole; v += kFewThreads) top[m] = top_of<X>(top[m], load16_any(row + v * V));
+          if (tid < left) z_left[m] = Elem<X>::load(row + whole * V + tid);
+        }
       }
-    }
 #pragma unroll
-    for (int m = 0; m < kFusedRows; ++m)
-      if (m < M) {
-        uint32_t t = max(top_float_bits<X>(top[m]), __float_as_uint(z_left[m]) & 0x7fffffffu);
+      for (int m = 0; m < kFusedRows; ++m)
+        if (m < M) {
+          uint32_t t = max(top_float_bits<X>(top[m]), __float_as_uint(z_left[m]) & 0x7fffffffu);
 #pragma unroll
-        for (int off = 32; off > 0; off >>= 1) t = max(t, static_cast<uint32_t>(__shfl_xor(static_cast<int>(t), off, 64)));
-        if (lane == 0) red[wave][0][m] = static_cast<int>(t);
-      }
-    __syncthreads();
+          for (int off = 32; off > 0; off >>= 1) t = max(t, static_cast<uint32_t>(__shfl_xor(static_cast<int>(t), off, 64)));
+          if (lane == 0) red[wave][0][m] = static_cast<int>(t);
+        }
+      __syncthreads();
 #pragma unroll
-    for (int m = 0; m < kFusedRows; ++m)
-      if (m < M) {
-        uint32_t t = 0;
+      for (int m = 0; m < kFusedRows; ++m)
+        if (m < M) {
+          uint32_t t = 0;
 #pragma unroll
-        for (int w = 0; w < kFewWaves; ++w) t = max(t, static_cast<uint32_t>(red[w][0][m]));
-        float inv;
-        const float s = i8_scale(t, &inv);
-        const X* row = static_cast<const X*>(a.x) + m * a.ldx;
-        int8_t* out = reinterpret_cast<int8_t*>(smem) + m * Kp;
-        for (int v = tid; v < whole; v += kFewThreads) store_quantized<X>(out + v * V, load16_any(row + v * V), inv);
-        if (tid < Kp - whole * V) out[whole * V + tid] = static_cast<int8_t>(tid < left && inv != 0.f ? i8_of(z_left[m], inv) : 0u);
-        if (tid == 0) scale_s[m] = s;
-      }
+          for (int w = 0; w < kFewWaves; ++w) t = max(t, static_cast<uint32_t>(red[w][0][m]));
+          float inv;
+          const float s = i8_scale(t, &inv);
+          const X* row = static_cast<const X*>(a.x) + m * a.ldx;
+          int8_t* out = reinterpret_cast<int8_t*>(smem) + m * Kp;
+          for (int v = tid; v < whole; v += kFewThreads) store_quantized<X>(out + v * V, load16_any(row + v * V), inv);
+          if (tid < Kp - whole * V) out[whole * V + tid] = static_cast<int8_t>(tid < left && inv != 0.f ? i8_of(z_left[m], inv) : 0u);
+          if (tid == 0) scale_s[m] = s;
+        }
     }
     __syncthreads();
   }
