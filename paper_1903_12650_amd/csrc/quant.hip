@@ -519,11 +519,13 @@ static void product_typed(const ProductArgs& a, hipStream_t s) {
   // The largest tile of which there are enough for the 256 compute units (256x256, 128x128, 128x64, 64x64 in us): 4096^3 65, 79, 90, 106;
   // 5000 x 5000 -> 1000 (80, 320, 640, 1264 tiles) 66, 40, 47, 54; 300 x 8192 -> 8192 (64, 192, 384, 640) 96, 42, 34, 39; 512 x 4096 -> 4096
   // (32, 128, 256, 512) 50, 23, 17, 18; 1000 x 2048 -> 1000 (16, 64, 128, 256) 29, 13, 9.4, 7.5.  The 256x256 one leaves a unit a single
-  // workgroup, so only where the last round is full enough.  Three or four buffers instead of two cost the workgroups that share a unit:
+  // workgroup, so only where its last round is full enough, 256x256 and 128x128: 1024 -> 256 by 130 tiles of 256 rows 23.4, 23.1, by 170 23.5, 25.8,
+  // by 196 24.2, 28.1, by 240 25.5, 30.9, by 300 40.8, 40.1, by 420 44.9, 52.5; 4096 -> 2048 by 136 tiles 54, 57, by 200 60, 69, by 264 108, 92,
+  // by 384 116, 113, by 424 115, 128.  Three or four buffers instead of two cost the workgroups that share a unit:
   // 4096^3 128x128 79 -> 99, 64x64 106 -> 110, 118.
   auto tiles = [&](int bm, int bn) { return ceil_div(a.M, bm) * ceil_div(a.N, bn); };
   const int64_t large = tiles(256, 256);
-  if (large >= 256 && large * 5 >= ceil_div(large, 256) * 256 * 4) product_tile<T, 256, 256, 2, 4, 2>(a, s);
+  if (large * 5 >= (large <= 256 ? 256 * 3 : ceil_div(large, 256) * 256 * 4)) product_tile<T, 256, 256, 2, 4, 2>(a, s);
   else if (tiles(128, 128) >= 256) product_tile<T, 128, 128, 2, 2, 2>(a, s);
   else if (tiles(128, 64) >= 256) product_tile<T, 128, 64, 2, 2, 3>(a, s);
   else product_tile<T, 64, 64, 2, 2, 2>(a, s);

@@ -122,6 +122,12 @@ def test_products(rn, M, N, K, x_type, y_type, bias):
         assert torch.equal(wide[:, :N], y) and bool((wide[:, N:] == 5.0).all())
 
 
+@pytest.mark.parametrize("x_type, y_type, bias", [(BF16, F32, True), (F32, BF16, False)])
+@pytest.mark.parametrize("M, N, K", [(2900, 3900, 70), (2817, 3841, 641), (4097, 4100, 130), (1500, 3900, 193), (1409, 3844, 1000), (1000, 2100, 193)])
+def test_products_of_many_tiles(rn, M, N, K, x_type, y_type, bias):
+    test_products(rn, M, N, K, x_type, y_type, bias)
+
+
 @pytest.mark.parametrize("M, N", [(1, 3), (5, 70), (70, 5), (200, 130)])
 def test_longest_sums_do_not_overflow(rn, M, N):
     K = 131071
