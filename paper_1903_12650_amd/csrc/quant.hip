@@ -124,13 +124,17 @@ struct ProductArgs {
 // straight into LDS (16 bytes a lane) into one of RING buffers while another is multiplied: one barrier a chunk.  Piece p (16 bytes) of
 // row r lies in slot p ^ ((r >> 1) & 7), which spreads the fragment reads (32 rows of one piece) over all banks.  Rows past the last and
 // the second half of a last chunk of 64 bytes are zeros.  The weights are the first operand, so that a lane has 4 consecutive columns of one row.
-// What bounds it: large products the power that the matrix cores may draw (8192^3 480 to 560 us, 2.0 to 2.3 POP/s, with whatever tile; the
-// same product of zeros 376 to 403), middle ones a workgroup's own chain: some 4 us of start, first loads and output stage around
-// 0.5 to 0.7 us a chunk, of which the matrix cores need 0.2 (128x128) to 0.85 (256x256).
+// What bounds it: large products the power that the matrix cores may draw beside LDS (8192^3 437 to 490 us, 2.2 to 2.5 POP/s; of zeros it is
+// faster), middle ones a workgroup's own chain: some 4 us of start, first loads and output stage around 0.6 (128x128) to 1.7 us (256x256)
+// a chunk, of which the matrix cores need 0.2 to 0.85.  Fragments are requested a step ahead (by the compiler's own order, where they are
+// needed: 8192^3 466 us, by 128x128 540 -> 513, 4096 x 1024 -> 4096 29.6 -> 25.4).
 template <typename T, int BM, int BN, int WM, int WN, int RING>
 __global__ __launch_bounds__(64 * WM * WN) void matmul_i8_kernel(const ProductArgs a) {
   constexpr int NT = 64 * WM * WN, RPL = NT / 8, RA = BM / RPL, RB = BN / RPL, TM = BM / WM / 32, TN = BN / WN / 32;
   constexpr int STAGE = (BM + BN) * 128;
+  // Requests of the next chunk: between the first steps where nothing else runs on the compute unit meanwhile (256x256: 8192^3 459 -> 437 us,
+  // 300 x 8192 -> 8192 88 -> 78), all at the front elsewhere (128x128: 8192^3 513, 532 spread).
+  constexpr bool SPREAD = NT == 512;
   static_assert(RA * RPL == BM && RB * RPL == BN && TM >= 1 && TN >= 1, "whole passes, whole blocks");
   extern __shared__ __align__(16) unsigned char smem[];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
@@ -153,13 +157,16 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_i8_kernel(const ProductAr
   typedef __attribute__((address_space(3))) unsigned char* lds_byte_ptr;
   const uint32_t dst = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_byte_ptr)smem)) + static_cast<uint32_t>(wave) * 1024u);
   const int chunks = (a.Kp + 127) >> 7;
-  auto load = [&](int c, int buffer) __attribute__((always_inline)) {
+  enum { ROWS = 1, COLUMNS = 2 };
+  auto load = [&](int c, int buffer, int what) __attribute__((always_inline)) {
     const uint32_t so = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(c) * 128u), to = dst + static_cast<uint32_t>(buffer) * STAGE;
     const bool in = c * 128 + piece * 16 < a.Kp;
 #pragma unroll
-    for (int i = 0; i < RA; ++i) buffer_load16_to_lds(rsA, to + i * (RPL * 128), in ? at_a[i] : kOob, so);
+    for (int i = 0; i < RA; ++i)
+      if (what & ROWS) buffer_load16_to_lds(rsA, to + i * (RPL * 128), in ? at_a[i] : kOob, so);
 #pragma unroll
-    for (int i = 0; i < RB; ++i) buffer_load16_to_lds(rsB, to + BM * 128 + i * (RPL * 128), in ? at_b[i] : kOob, so);
+    for (int i = 0; i < RB; ++i)
+      if (what & COLUMNS) buffer_load16_to_lds(rsB, to + BM * 128 + i * (RPL * 128), in ? at_b[i] : kOob, so);
   };
   i32x16 acc[TM][TN];
 #pragma unroll
@@ -173,11 +180,12 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_i8_kernel(const ProductAr
   for (int kk = 0; kk < 4; ++kk) frag[kk] = (lane & 31) * 128 + (((2 * kk + (lane >> 5)) ^ ((lane >> 1) & 7)) << 4);
 #pragma unroll
   for (int c = 0; c < RING - 1; ++c)
-    if (c < chunks) load(c, c);
+    if (c < chunks) load(c, c, ROWS | COLUMNS);
   int now = 0, next = RING - 1;  // buffers of this chunk and of the one that is requested
   for (int c = 0; c < chunks; ++c) {
     ring_wait<RING, RA + RB>(chunks - 1 - c);  // this chunk is there, and the buffer of the one before it has been read
-    if (c + RING - 1 < chunks) load(c + RING - 1, next);
+    const int ahead = c + RING - 1, into = next;
+    if (!SPREAD && ahead < chunks) load(ahead, into, ROWS | COLUMNS);
     const unsigned char* ta = smem + now * STAGE + wm * (BM / WM) * 128;
     const unsigned char* tb = smem + now * STAGE + BM * 128 + wn * (BN / WN) * 128;
     now = now + 1 == RING ? 0 : now + 1;
@@ -193,10 +201,13 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_i8_kernel(const ProductAr
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk) {
       if (kk < 3) read(kk + 1);
+      if (SPREAD && kk < 2 && ahead < chunks) load(ahead, into, kk == 0 ? ROWS : COLUMNS);
+      __builtin_amdgcn_sched_barrier(0);  // (the compiler would move every read to where its product waits for it)
 #pragma unroll
       for (int i = 0; i < TM; ++i)
 #pragma unroll
         for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fb[kk & 1][j], fa[kk & 1][i], acc[i][j], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
   // Output: a wave's 32 rows at a time through LDS (its own part of it), whole rows of the wave's columns from there.
@@ -516,16 +527,15 @@ static void product_typed(const ProductArgs& a, hipStream_t s) {
   }
 #endif
   if (a.M <= kFewRows) return few_rows_quantized<T>(a, s);
-  // The largest tile of which there are enough for the 256 compute units (256x256, 128x128, 128x64, 64x64 in us): 4096^3 65, 79, 90, 106;
-  // 5000 x 5000 -> 1000 (80, 320, 640, 1264 tiles) 66, 40, 47, 54; 300 x 8192 -> 8192 (64, 192, 384, 640) 96, 42, 34, 39; 512 x 4096 -> 4096
-  // (32, 128, 256, 512) 50, 23, 17, 18; 1000 x 2048 -> 1000 (16, 64, 128, 256) 29, 13, 9.4, 7.5.  The 256x256 one leaves a unit a single
-  // workgroup, so only where its last round is full enough, 256x256 and 128x128: 1024 -> 256 by 130 tiles of 256 rows 23.4, 23.1, by 170 23.5, 25.8,
-  // by 196 24.2, 28.1, by 240 25.5, 30.9, by 300 40.8, 40.1, by 420 44.9, 52.5; 4096 -> 2048 by 136 tiles 54, 57, by 200 60, 69, by 264 108, 92,
-  // by 384 116, 113, by 424 115, 128.  Three or four buffers instead of two cost the workgroups that share a unit:
-  // 4096^3 128x128 79 -> 99, 64x64 106 -> 110, 118.
+  // The largest tile of which there are enough for the 256 compute units (256x256, 128x128, 128x64, 64x64 in us): 4096^3 61, 72, 92, 109;
+  // 5000 x 5000 -> 1000 (80, 320, 640, 1264 tiles) 64, 42, 52, 58; 300 x 8192 -> 8192 (64, 192, 384, 640) 79, 42, 36, 40; 512 x 4096 -> 4096
+  // (32, 128, 256, 512) 44, 23, 16, 18; 1000 x 2048 -> 1000 (16, 64, 128, 256) 26, 13, 9.7, 7.6.  The 256x256 one leaves a unit a single
+  // workgroup, so only where its last round is full enough, 256x256 and 128x128: 1024 -> 256 by 130 tiles of 256 rows 21.7, 22.6, by 196 23.1, 24.6,
+  // by 240 25.0, 27.0, by 300 38.6, 35.5, by 380 43.6, 41.5, by 420 44.5, 47.5; 4096 -> 2048 by 136 tiles 51, 56, by 200 53, 60, by 264 100, 87,
+  // by 384 107, 106, by 424 110, 123.  Three or four buffers instead of two cost the workgroups that share a unit (4096^3 by 128x128 a quarter).
   auto tiles = [&](int bm, int bn) { return ceil_div(a.M, bm) * ceil_div(a.N, bn); };
   const int64_t large = tiles(256, 256);
-  if (large * 5 >= (large <= 256 ? 256 * 3 : ceil_div(large, 256) * 256 * 4)) product_tile<T, 256, 256, 2, 4, 2>(a, s);
+  if (large > 128 && (large <= 256 || large * 5 >= ceil_div(large, 256) * 256 * 4)) product_tile<T, 256, 256, 2, 4, 2>(a, s);
   else if (tiles(128, 128) >= 256) product_tile<T, 128, 128, 2, 2, 2>(a, s);
   else if (tiles(128, 64) >= 256) product_tile<T, 128, 64, 2, 2, 3>(a, s);
   else product_tile<T, 64, 64, 2, 2, 2>(a, s);
