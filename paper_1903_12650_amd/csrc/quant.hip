@@ -124,8 +124,8 @@ struct ProductArgs {
 // straight into LDS (16 bytes a lane) into one of RING buffers while another is multiplied: one barrier a chunk.  Piece p (16 bytes) of
 // row r lies in slot p ^ ((r >> 1) & 7), which spreads the fragment reads (32 rows of one piece) over all banks.  Rows past the last and
 // the second half of a last chunk of 64 bytes are zeros.  The weights are the first operand, so that a lane has 4 consecutive columns of one row.
-// What bounds it: large products the power that the matrix cores may draw beside LDS (8192^3 437 to 490 us, 2.2 to 2.5 POP/s; of zeros it is
-// faster), middle ones a workgroup's own chain: some 4 us of start, first loads and output stage around 0.6 (128x128) to 1.7 us (256x256)
+// What bounds it: large products the power that the matrix cores may draw beside LDS (8192^3 437 to 490 us, 2.2 to 2.5 POP/s; of zeros
+// 326), middle ones a workgroup's own chain: some 4 us of start, first loads and output stage around 0.6 (128x128) to 1.7 us (256x256)
 // a chunk, of which the matrix cores need 0.2 to 0.85.  Fragments are requested a step ahead (by the compiler's own order, where they are
 // needed: 8192^3 466 us, by 128x128 540 -> 513, 4096 x 1024 -> 4096 29.6 -> 25.4).
 template <typename T, int BM, int BN, int WM, int WN, int RING>
