@@ -483,7 +483,8 @@ int fc_i8_fwd(int M, int N, int K, int x_dtype, const void* x, int64_t ldx, cons
  * The k largest logits of every row, in descending order; equal ones in the order of their classes, a NaN
  * above every number.  values: device float [N,k]; indices: device int32 [N,k]; where a row has fewer
  * than k classes the rest is (-infinity, -1).  tail_lse (or NULL): device float[N], the logarithm of the
- * sum of exp(logit / temperature) over the classes that are not among them (-infinity if there are none).
+ * sum of exp(logit / temperature) over the classes that are not among them (-infinity if there are none, NaN where one of them
+ * is NaN, otherwise +infinity where one of them is).
  * logits: device dtype, rows of C elements ld >= C elements apart.  1 <= k <= 256; temperature 2^-126 or more. */
 size_t topk_rows_workspace_bytes(int N, int C, int k);
 int topk_rows(int N, int C, int k, int dtype, const void* logits, int64_t ld, float temperature, float* values,

@@ -33,10 +33,10 @@ def matmul_i8(q, q_scale, w, w_scale, bias=None):
 
 
 def lse(u, axis=1):
-    """log(sum(exp(u))) along an axis, -inf where there is nothing else."""
+    """log(sum(exp(u))) along an axis, -inf where there is nothing else, +inf where one is (and none is NaN)."""
     with np.errstate(all="ignore"):
         m = u.max(axis, keepdims=True) if u.shape[axis] else np.full([1 if i == axis % u.ndim else s for i, s in enumerate(u.shape)], -np.inf)
-        m = np.where(m == -np.inf, 0.0, m)
+        m = np.where(np.isinf(m), 0.0, m)
         return np.squeeze(np.log(np.exp(u - m).sum(axis, keepdims=True)) + m, axis)
 
 

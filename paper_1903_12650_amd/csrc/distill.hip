@@ -3,7 +3,7 @@
 //
 // Sums of exponentials run with their maximum: (m, s) stands for s * exp(m / T).  m starts at the lowest finite float, so that
 // nothing is ever subtracted from an infinity of its own sign: a logit of -infinity adds exp(-infinity) = 0, a row of nothing else
-// leaves s = 0, a logit of +infinity or NaN makes s NaN.
+// leaves s = 0, a NaN makes s NaN.  A logit of +infinity does so too, except among the classes that topk_rows did not take (Sums::infinite).
 #include <float.h>
 #include <stdlib.h>
 
@@ -118,6 +118,12 @@ struct Sums {
     st += other.st;
     s1 += other.s1;
   }
+  // A logit of +infinity makes the sum infinite and leaves the reference finite: nothing is subtracted from an infinity, here or where sums
+  // are joined (this one's reference is the largest there), and a NaN stays.
+  __device__ __forceinline__ void infinite(const Scales& sc) {
+    move(FLT_MAX, sc);
+    st += INFINITY;
+  }
   template <int V>
   __device__ __forceinline__ void add(const float* x, const Scales& sc) {
     float top = x[0];
@@ -179,7 +185,8 @@ __device__ __forceinline__ uint32_t order_key(float x) {
 }
 // The least logit whose key reaches `key` (no NaN's).
 __device__ __forceinline__ float logit_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key); }
-constexpr uint32_t kKeyOfNothing = 0x007fffffu;  // order_key(-infinity)
+constexpr uint32_t kKeyOfNothing = 0x007fffffu;   // order_key(-infinity)
+constexpr uint32_t kKeyOfInfinity = 0xff800000u;  // order_key(+infinity)
 
 struct TopkArgs {
   const void* logits;
@@ -371,6 +378,11 @@ __device__ __forceinline__ int take_equal(const T* row, int C, uint32_t key, int
   __syncthreads();
   return sh.last;
 }
+// One logit of the rest, +infinity among it (there are more of them than places).
+__device__ __forceinline__ void add_any(float x, const Scales& sc, Sums<1>& rest) {
+  if (x == INFINITY) rest.infinite(sc);
+  else rest.template add<1>(&x, sc);
+}
 // The sum over the classes that were not taken: keys below `key`, and equal to it behind class `last`.
 template <typename T>
 __device__ __forceinline__ void add_rest(const T* row, int C, uint32_t key, int last, const Scales& sc, Sums<1>& rest) {
@@ -378,7 +390,7 @@ __device__ __forceinline__ void add_rest(const T* row, int C, uint32_t key, int 
   for (int i = threadIdx.x; i < C; i += kTopkThreads) {
     const float x = Elem<T>::load(row + i);
     const uint32_t o = order_key(x);
-    if (o < key || (o == key && i > last)) rest.template add<1>(&x, sc);
+    if (o < key || (o == key && i > last)) add_any(x, sc, rest);
   }
 }
 
@@ -824,8 +836,16 @@ __global__ __launch_bounds__(kTopkThreads) void topk_short_kernel(const TopkArgs
   }
   if (a.tail == nullptr) return;
   Sums<1> rest;
+  if (most >= kKeyOfInfinity) {
+#pragma unroll
+    for (int g = 0; g < PER; ++g)
+      if (z[g] == INFINITY) {
+        rest.infinite(sc);
+        z[g] = -INFINITY;
+      }
+  }
   rest.template add<PER>(z, sc);
-  for (int c = tid; c < cands - kk; c += NT) rest.template add<1>(&sh.spare[c], sc);
+  for (int c = tid; c < cands - kk; c += NT) add_any(sh.spare[c], sc, rest);
   if (JOIN && tid < a.slices) {
     const RowSums part = a.part_sums[static_cast<int64_t>(n) * a.slices + tid];
     Sums<1> p;

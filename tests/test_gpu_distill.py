@@ -665,3 +665,33 @@ def test_the_example_learns(rn):
     assert torch.isfinite(losses).all()
     first, last = float(losses[:4].mean()), float(losses[-4:].mean())
     assert last < 0.8 * first, (first, last)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("C, k", [(300, 5), (1000, 40), (1000, 256), (2500, 256), (5000, 64), (50001, 100), (100003, 7), (100003, 256)])
+def test_more_infinities_than_places(rn, C, k, dtype):
+    """What is left then has an infinite sum, unless a NaN is left as well."""
+    g = torch.Generator().manual_seed(C + k)
+    x = torch.randn(12, C, generator=g)
+    inf, nan = float("inf"), float("nan")
+    some = lambda n: torch.randperm(C, generator=g)[:min(n, C)]
+    x[0, some(k + 1)] = inf
+    x[1, 5:5 + k + 30] = inf
+    x[2] = inf
+    x[3, some(k + 1)] = inf
+    x[3, C - 2] = nan                                      # one place goes to it
+    x[4, some(k + 5)] = nan
+    x[4, 3] = inf
+    x[5, some(k)] = inf                                    # as many as places: the rest is finite
+    x[6] = float("-inf")
+    x[6, some(k + 1)] = inf                                # and nothing else
+    x[7, C - k - 2:] = inf
+    x[8, torch.linspace(0, C - 1, k + 2).long().unique()] = inf  # spread over the row
+    x[9, :k + 3] = inf
+    x[9, :k - 1] = nan
+    x[10, 1], x[10, C - 1] = inf, inf
+    check_topk(rn, x.to(dtype).cuda(), k, 1.0)
+    check_topk(rn, spread(x.to(dtype).cuda(), 3), k, 0.25)
+    check_topk(rn, x.to(dtype).cuda(), 1, 1e30)
+    for n in (0, 3, 8):
+        check_topk(rn, x[n:n + 1].to(dtype).cuda(), k, 2.0)

@@ -119,3 +119,15 @@ def test_rows_that_have_nothing():
     # a teacher that is sure of a class the student rules out
     z[3, i[3, 0]] = -np.inf
     assert np.isposinf(od.distill(z, v, i, None, row_weight=w)[0])
+
+
+def test_the_rest_of_a_row_with_more_infinities_than_places():
+    x = np.random.default_rng(3).normal(size=(4, 9))
+    x[0, [1, 4, 6]] = np.inf             # one is left
+    x[1, [1, 4]] = np.inf                # none is
+    x[2, [1, 4, 6]], x[2, 8] = np.inf, np.nan  # a NaN takes a place
+    x[3, [0, 1, 2]], x[3, 5] = np.nan, np.inf  # and here one is left
+    v, i, tail = od.topk_rows(x, 2, 2.0)
+    assert i.tolist() == [[1, 4], [1, 4], [8, 1], [0, 1]]
+    assert np.isposinf(tail[0]) and np.isfinite(tail[1]) and np.isposinf(tail[2]) and np.isnan(tail[3])
+    np.testing.assert_allclose(tail[1], np.log(np.exp(np.delete(x[1], [1, 4]) / 2).sum()), rtol=1e-12)
