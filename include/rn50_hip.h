@@ -506,7 +506,7 @@ int topk_rows(int N, int C, int k, int dtype, const void* logits, int64_t ld, fl
  * for nothing, whatever it holds, a row whose logits are all -infinity has no distribution: loss and gradient 0 for
  * both.  With and without dlogits the losses are the same bits.
  * logits, dlogits: device dtype, rows of C elements ld >= C apart, grad_ld for the gradient; dlogits may be NULL (the
- * loss alone) or the logits' own memory (with grad_ld == ld), and must not overlap them otherwise.  t_values float
+ * loss alone) or the logits' own memory (with grad_ld == ld if there are several rows), and must not overlap them otherwise.  t_values float
  * [N,k], t_indices int32 [N,k], t_tail float[N] or NULL; labels int32[N] or NULL; row_weight float[N] or NULL;
  * loss_out float[1]; row_loss_out float[N].  0 <= k <= 256 (k = 0: no entries), 0 <= alpha, ls <= 1, T 2^-126 or more. */
 typedef struct {

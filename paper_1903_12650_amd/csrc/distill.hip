@@ -1573,7 +1573,7 @@ extern "C" int distill_fwd_bwd(const rn50_distill_desc* d, const void* logits, c
   RN50_REQUIRE(loss_out && row_loss_out, RN50_ERR_INVALID, "%s: null pointer", who);
   RN50_REQUIRE(!dlogits || d->grad_ld >= d->C, RN50_ERR_INVALID, "%s: gradient rows of %d elements %lld apart", who, d->C,
                static_cast<long long>(d->grad_ld));
-  RN50_REQUIRE(dlogits != logits || d->grad_ld == d->ld, RN50_ERR_INVALID, "%s: a gradient in the logits' place with rows of its own", who);
+  RN50_REQUIRE(dlogits != logits || d->grad_ld == d->ld || d->N == 1, RN50_ERR_INVALID, "%s: a gradient in the logits' place with rows of its own", who);
   RN50_REQUIRE(aligned_to(t_values, 4) && aligned_to(t_indices, 4) && aligned_to(t_tail, 4) && aligned_to(labels, 4) && aligned_to(row_weight, 4) &&
                    aligned_to(loss_out, 4) && aligned_to(row_loss_out, 4) && aligned_to(dlogits, d->dtype == RN50_BF16 ? 2 : 4),
                RN50_ERR_ALIGN, "%s: pointer not aligned to an element", who);

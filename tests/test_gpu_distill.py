@@ -695,3 +695,19 @@ def test_more_infinities_than_places(rn, C, k, dtype):
     check_topk(rn, x.to(dtype).cuda(), 1, 1e30)
     for n in (0, 3, 8):
         check_topk(rn, x[n:n + 1].to(dtype).cuda(), k, 2.0)
+
+
+@pytest.mark.parametrize("C", [1000, 40000])
+def test_one_row_in_place_whatever_its_strides_say(rn, C):
+    """A single row has no next one: its gradient may take its place through a view that names another distance."""
+    z, v, i, tl, labels = teacher(rn, 1, C, 7, 2.0, C)
+    want = rn.distill_fwd_bwd(z.cuda(), v, i, tl, labels, 2.0, 0.5)
+    wide = torch.full((1, C + 8), 5.0, device="cuda")
+    part = wide[:, :C]
+    part.copy_(z)
+    view = part[0].unsqueeze(0)
+    assert view.data_ptr() == part.data_ptr() and view.stride(0) != part.stride(0)
+    got = rn.distill_fwd_bwd(part, v, i, tl, labels, 2.0, 0.5, dlogits=view)
+    for a, b in zip(want, got):
+        assert torch.equal(a, b)
+    assert bool((wide[:, C:] == 5.0).all())
