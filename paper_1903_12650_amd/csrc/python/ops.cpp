@@ -74,6 +74,7 @@ int dtype_of(const at::Tensor& t) {
 int to_int(PyObject* o) {
   const long v = PyLong_AsLong(o);
   if (v == -1 && PyErr_Occurred()) throw PyError();
+  if (v != static_cast<int>(v)) raise(PyExc_OverflowError, "Python int too large to convert to C int");
   return static_cast<int>(v);
 }
 double to_double(PyObject* o) {

@@ -61,3 +61,15 @@ def test_native_calls_refuse_what_they_cannot_take(call, error):
     with pytest.raises(error) as e:
         call(rn, torch.zeros(4, 8))
     assert "frame #" not in str(e.value)
+
+
+@pytest.mark.parametrize("call", [
+    lambda rn, x: rn.topk_rows(x, 2 ** 32 + 3),
+    lambda rn, x: rn.topk_rows(x, -2 ** 32 + 3),
+    lambda rn, x: rn.matmul_i8(2 ** 32 + 8, x, x, x, x),
+    lambda rn, x: rn.conv_fwd(x[None, None], x[None, None], 2 ** 32 + 1, 0),
+])
+def test_numbers_past_32_bits_are_not_cut(call):
+    import paper_1903_12650_amd as rn
+    with pytest.raises(OverflowError):
+        call(rn, torch.zeros(4, 8))
