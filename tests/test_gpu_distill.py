@@ -711,3 +711,146 @@ def test_one_row_in_place_whatever_its_strides_say(rn, C):
     for a, b in zip(want, got):
         assert torch.equal(a, b)
     assert bool((wide[:, C:] == 5.0).all())
+
+
+# ----------------------------------------------- every form, every temperature
+# Bounds from what the kernels do, one after another (all in units of eps, of a sum's size):
+#  - additions: a thread's own terms (`chain`: its share of the row's vectors, and one more), 6 across a wave, at most 16 across a row's waves and
+#    14 more across slices;
+#  - a term's exponent has four roundings (the difference, log2(e), its division by T, their product), each of the exponent's own size.  A
+#    reference lies at most 20 ln 2 < 14 below the largest logit seen, and all moves of a term's reference together are no longer than the way from the
+#    term to the largest, and those 14: 2 * 4 * (way + 14); the way is on average at most the softmax's entropy, ln C;
+#  - the exponential 2, a move of the reference (its exponential, its product) 3, at most 10 of them.
+# Float losses at 131072 classes are held to some 5e-5 of a nat this way.
+def chain(C, dtype):
+    vec = 8 if dtype == BF16 else 4
+    vecs = -(-C // vec)
+    threads = 128 if vecs <= 512 else 256 if vecs <= 3072 else 512 if vecs <= 32768 else 1024  # (the fewest that such a row has)
+    return vec * -(-vecs // threads) + 1
+
+
+def sums_of(C, dtype):
+    return EPS * (chain(C, dtype) + 36 + 8 * (np.log(C) + 14) + 32)
+
+
+def row_spread(a):
+    """Largest minus smallest finite value of every row."""
+    fine = np.isfinite(a)
+    return np.where(fine, a, -np.inf).max(1, initial=-1e300) - np.where(fine, a, np.inf).min(1, initial=1e300)
+
+
+def check_sampled(rn, z, v, i, tl, labels, T, alpha, ls, w, picked, dlogits=None):
+    """The picked rows against the oracle; all others have weight 0, and their losses and gradients are zeros."""
+    N, C = z.shape
+    k = v.shape[1]
+    keep = z[picked].double().cpu().numpy()
+    dtype = z.dtype
+    loss, rows, grad = rn.distill_fwd_bwd(z, v, i, tl, labels, T, alpha, ls, w, 3.0, dlogits=dlogits)
+    others = torch.ones(N, dtype=torch.bool, device="cuda")
+    others[picked] = False
+    assert not rows[others].any() and not grad[others].any() and grad.dtype == dtype
+    vv = f64(v)[picked]
+    want_loss, want_rows, want, size = od.distill(keep, vv, i.cpu().numpy()[picked], None if tl is None else f64(tl)[picked],
+                                                  labels.cpu().numpy()[picked], T, alpha, ls, f64(w)[picked], 3.0)
+    e, zs = sums_of(C, dtype), row_spread(keep)
+    cells = EPS * (4 + 20 + 2 * (np.log(k + 1) + 1))  # the teacher's sum: four of a lane, the wave's; a rounding of each exponent
+    apart = (row_spread(vv) + zs) / T + np.log(k + 2) + np.log(C)  # log p - log q, at most
+    row_bound = alpha * T * T * (2 * e + cells + EPS * ((np.log(k + 1) + 3) * apart + 4 * (zs / T + np.log(C)))) \
+        + (1 - alpha) * (2 * e + 4 * EPS * (zs + np.log(C))) + 2 * EPS * np.abs(want_rows)
+    off = np.abs(f64(rows)[picked] - want_rows) / row_bound
+    assert (off <= 1).all(), (off.max(), row_bound.max())
+    assert abs(float(loss) - want_loss) <= float((np.abs(f64(w)[picked]) * row_bound).sum()) + 2 * EPS * abs(want_loss)
+    away = (keep.max(1)[:, None] - np.where(np.isfinite(keep), keep, keep.max(1)[:, None])) * max(1.0, 1.0 / T)
+    bound = size * (2 * e + cells + EPS * (8 * (np.minimum(away, 90) + 14) + 24)) + 1e-36
+    if dtype == BF16:
+        bound += 2.0 ** -8 * 1.01 * (np.abs(want) + bound) + 1e-38
+    got = f64(grad[picked])
+    off = np.abs(got - want) / bound
+    assert (off <= 1).all(), (np.unravel_index(off.argmax(), off.shape), off.max(), got.flat[off.argmax()], want.flat[off.argmax()])
+    return loss, rows, grad
+
+
+def sampled(rn, N, C, k, dtype, T, seed, rows=5):
+    """A few rows with weights; entries and labels at the ends, on both sides of a chunk of 65536 classes, some repeated and some absent."""
+    g = torch.Generator().manual_seed(seed)
+    picked = sorted({0, N - 1, *(int(j) for j in torch.randint(0, N, (max(1, rows - 2),), generator=g))})
+    z = (torch.randn(min(N, 9), C, generator=g) * 2).to(dtype).cuda().repeat(-(-N // 9), 1)[:N].contiguous()
+    i = torch.randint(0, C, (N, k), generator=g)
+    edges = [c for c in (65535, 65536, 0, C - 1, 65537, C - 2, 1, 65528, 65543, 131071, 131072) if c < C][:k]
+    i[:, :len(edges)] = torch.tensor(edges)
+    v = torch.randn(N, k, generator=g) * 2
+    if k > 2:
+        i[0, k - 1] = i[0, 0]            # again, with another value
+        i[picked[-1], k - 1] = i[picked[-1], 1]
+        i[picked[len(picked) // 2], k // 2] = -1
+    tl = torch.randn(N, generator=g) + np.log(C)
+    labels = torch.randint(0, C, (N,), generator=g)
+    for n, c in zip(picked, (65536 % C, C - 1, int(i[picked[2 % len(picked)], 0]))):
+        labels[n] = c
+    w = torch.zeros(N)
+    w[picked] = torch.linspace(0.5, 1.5, len(picked))
+    return z, v.cuda(), i.to(torch.int32).cuda(), (tl / T).cuda(), labels.to(torch.int32).cuda(), w.cuda(), picked
+
+
+# (rows, bfloat16 classes, float classes, entries): a workgroup's threads and what it holds of a row, or chunks of classes that it streams
+FORMS = [(7, 1001, 501, 9), (5, 2040, 1020, 200), (5, 3000, 1500, 20), (5, 3001, 1501, 200), (3, 5001, 2501, 130), (9, 9000, 4500, 64), (3, 25001, 13001, 100),
+         (129, 70001, 70001, 64), (130, 131072, 131072, 256), (129, 270001, 132001, 40), (1, 50001, 20001, 256), (6, 131073, 65537, 33), (2, 300007, 150001, 12)]
+
+
+@pytest.mark.parametrize("T, alpha, ls, tail", [(3.0, 0.6, 0.1, True), (0.3, 0.6, 0.1, True), (2.0, 0.7, 0.1, False), (4.0, 0.5, 0.0, True),
+                                               (1.0, 0.4, 0.1, True), (1.5, 1.0, 0.0, True)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("N, bf16_classes, float_classes, k", FORMS)
+def test_every_form_at_every_temperature(rn, N, bf16_classes, float_classes, k, dtype, T, alpha, ls, tail):
+    C = bf16_classes if dtype == BF16 else float_classes
+    z, v, i, tl, labels, w, picked = sampled(rn, N, C, k, dtype, T, N + C + k)
+    tl = tl if tail else None
+    loss, rows, grad = check_sampled(rn, z, v, i, tl, labels, T, alpha, ls, w, picked)
+    only = rn.distill_fwd_bwd(z, v, i, tl, labels, T, alpha, ls, w, 3.0, grad=False)
+    assert torch.equal(only[0], loss) and torch.equal(only[1], rows)
+    # from an odd element on, in place
+    wide = torch.full((N, C + 3), 5.0, dtype=dtype, device="cuda")
+    part = wide[:, 1:1 + C]
+    part.copy_(z)
+    check_sampled(rn, part, v, i, tl, labels, T, alpha, ls, w, picked, dlogits=part)
+    assert bool((wide[:, 0] == 5.0).all()) and bool((wide[:, 1 + C:] == 5.0).all())
+
+
+@pytest.mark.parametrize("T", [3.0, 0.7, 20.0])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("C", [700, 60000])
+def test_rows_where_something_is_missing_at_other_temperatures(rn, C, dtype, T):
+    N, k = 8, 6
+    z, v, i, tl, labels = teacher(rn, N, C, k, T, C)
+    w = torch.full((N,), 1.0 / N)
+    z[0] = float("-inf")
+    i[1], tl[1] = -1, float("-inf")
+    z[2], w[2] = float("nan"), 0.0
+    labels[3] = -100
+    i[4, 3] = i[4, 0]
+    keep = torch.zeros(C, dtype=torch.bool)
+    keep[i[5].cpu().long()] = True
+    keep[labels[5].item()] = True
+    z[5, ~keep] = float("-inf")
+    z[5, C // 2] = 0.5
+    z[6] = torch.finfo(dtype).min
+    z[7] *= 20
+    check_distill(rn, z.to(dtype).cuda(), v, i, tl, labels, T, 0.6, 0.0, w.cuda())
+
+
+@pytest.mark.parametrize("temperature", [0.5, 1.0, 3.0])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("N, C, k", [(7, 1000, 8), (5, 2500, 200), (6, 8195, 64), (5, 50001, 100), (1, 131072, 64), (7, 131073, 33), (241, 80001, 30)])
+def test_log_sum_exp_of_the_rest_holds_float(rn, N, C, k, dtype, temperature):
+    """The additions: at most C / 1024 vectors a stream and their own numbers, four streams, what is read again, a wave, the waves, slices;
+    exponents as above, from references that may be as high as the largest logit, which the rest does not have."""
+    g = torch.Generator().manual_seed(N + C + k)
+    x = (torch.randn(N, C, generator=g) * 2).to(dtype)
+    rows = range(N) if N < 10 else (0, 100, N - 1)
+    wv, wi, want = od.topk_rows(x[list(rows)].double().numpy(), k, temperature)
+    values, indices, tail = rn.topk_rows(x.cuda(), k, temperature)
+    assert np.array_equal(indices[list(rows)].cpu().numpy(), wi)
+    above = (wv[:, 0] - wv[:, -1]) / temperature
+    bound = EPS * (C / 512 + 64 + 8 * (np.log(C) + 14 + above) + 32 + 2 * np.abs(want))
+    off = np.abs(f64(tail)[list(rows)] - want) / bound
+    assert (off <= 1).all(), off.max()
