@@ -378,19 +378,18 @@ __device__ __forceinline__ int take_equal(const T* row, int C, uint32_t key, int
   __syncthreads();
   return sh.last;
 }
-// One logit of the rest, +infinity among it (there are more of them than places).
-__device__ __forceinline__ void add_any(float x, const Scales& sc, Sums<1>& rest) {
-  if (x == INFINITY) rest.infinite(sc);
-  else rest.template add<1>(&x, sc);
-}
-// The sum over the classes that were not taken: keys below `key`, and equal to it behind class `last`.
-template <typename T>
+// The sum over the classes that were not taken: keys below `key`, and equal to it behind class `last`.  INF: +infinity may be among them,
+// of which there are more than places then (looked for everywhere it costs rows of equal logits 4 %).
+template <bool INF, typename T>
 __device__ __forceinline__ void add_rest(const T* row, int C, uint32_t key, int last, const Scales& sc, Sums<1>& rest) {
 #pragma unroll 1
   for (int i = threadIdx.x; i < C; i += kTopkThreads) {
     const float x = Elem<T>::load(row + i);
     const uint32_t o = order_key(x);
-    if (o < key || (o == key && i > last)) add_any(x, sc, rest);
+    if (o < key || (o == key && i > last)) {
+      if (INF && x == INFINITY) rest.infinite(sc);
+      else rest.template add<1>(&x, sc);
+    }
   }
 }
 
@@ -447,7 +446,10 @@ __device__ __forceinline__ void topk_any(const T* row, int C, int kk, bool want_
   }
   const int last = take_equal<T, MODE>(row, C, prefix, need, above, out, sh);
   rest = Sums<1>();
-  if (want_tail) add_rest(row, C, prefix, last, sc, rest);
+  if (want_tail) {
+    if (prefix >= kKeyOfInfinity) add_rest<true>(row, C, prefix, last, sc, rest);
+    else add_rest<false>(row, C, prefix, last, sc, rest);
+  }
 }
 
 // One workgroup per row (or slice of one).  The row goes by once in 1024 streams of vectors, four a thread, each with its two largest
@@ -686,7 +688,7 @@ __global__ __launch_bounds__(kTopkThreads, 8) void topk_rows_kernel(const TopkAr
       const int last = take_equal<T, MODE>(row, C, lo, kk - cands, cands, out, sh);
       if (lo != kKeyOfNothing) {  // (the sums have all of the equal ones, and nothing is subtracted)
         rest = Sums<1>();
-        add_rest(row, C, lo, last, sc, rest);
+        add_rest<false>(row, C, lo, last, sc, rest);
       }
     }
   } else {
@@ -708,7 +710,7 @@ __global__ __launch_bounds__(kTopkThreads, 8) void topk_rows_kernel(const TopkAr
   if (sum.st < 0x1p-60f && kk < C && out.value(kk - 1) != -INFINITY) {
     __syncthreads();
     rest = Sums<1>();
-    add_rest(row, C, order_key(out.value(kk - 1)), out.at(kk - 1), sc, rest);
+    add_rest<false>(row, C, order_key(out.value(kk - 1)), out.at(kk - 1), sc, rest);  // (+infinity among them would have made it infinite)
     sum = block_sums<1, NT>(rest, 0.0, false, sc, sh.red);
   }
   if (tid != 0) return;
@@ -837,15 +839,18 @@ __global__ __launch_bounds__(kTopkThreads) void topk_short_kernel(const TopkArgs
   if (a.tail == nullptr) return;
   Sums<1> rest;
   if (most >= kKeyOfInfinity) {
+    bool left = false;  // of more infinities than places
 #pragma unroll
-    for (int g = 0; g < PER; ++g)
-      if (z[g] == INFINITY) {
-        rest.infinite(sc);
-        z[g] = -INFINITY;
-      }
+    for (int g = 0; g < PER; ++g) {
+      left |= z[g] == INFINITY;
+      z[g] = z[g] == INFINITY ? -INFINITY : z[g];
+    }
+    for (int c = tid; c < cands - kk; c += NT)
+      if (sh.spare[c] == INFINITY) left = true, sh.spare[c] = -INFINITY;
+    if (left) rest.infinite(sc);
   }
   rest.template add<PER>(z, sc);
-  for (int c = tid; c < cands - kk; c += NT) add_any(sh.spare[c], sc, rest);
+  for (int c = tid; c < cands - kk; c += NT) rest.template add<1>(&sh.spare[c], sc);
   if (JOIN && tid < a.slices) {
     const RowSums part = a.part_sums[static_cast<int64_t>(n) * a.slices + tid];
     Sums<1> p;
