@@ -400,7 +400,7 @@ __device__ __forceinline__ float tail_of(const RowSums& sum, float temperature) 
 // Any row, NaN and infinities among it: the key of the k-th largest logit digit by digit (four of 8 bits, a histogram each over the logits
 // that share the digits in front).  The row is read seven times; only rows that the way below cannot take come here.
 template <typename T, int MODE>
-__device__ __forceinline__ void topk_any(const T* row, int C, int kk, bool want_tail, const Scales& sc, const TopkOut<MODE>& out, TopkShared& sh, Sums<1>& rest) {
+__device__ __forceinline__ void topk_any(const T* row, int C, int kk, const Scales& sc, const TopkOut<MODE>& out, TopkShared& sh, Sums<1>& rest) {
   const int tid = threadIdx.x;
   uint32_t prefix = 0;
   int need = kk;  // how many are still to be taken among the logits that share the prefix
@@ -446,10 +446,8 @@ __device__ __forceinline__ void topk_any(const T* row, int C, int kk, bool want_
   }
   const int last = take_equal<T, MODE>(row, C, prefix, need, above, out, sh);
   rest = Sums<1>();
-  if (want_tail) {
-    if (prefix >= kKeyOfInfinity) add_rest<true>(row, C, prefix, last, sc, rest);
-    else add_rest<false>(row, C, prefix, last, sc, rest);
-  }
+  if (prefix >= kKeyOfInfinity) add_rest<true>(row, C, prefix, last, sc, rest);
+  else add_rest<false>(row, C, prefix, last, sc, rest);
 }
 
 // One workgroup per row (or slice of one).  The row goes by once in 1024 streams of vectors, four a thread, each with its two largest
@@ -692,7 +690,7 @@ __global__ __launch_bounds__(kTopkThreads, 8) void topk_rows_kernel(const TopkAr
       }
     }
   } else {
-    topk_any<T, MODE>(row, C, kk, true, sc, out, sh, rest);
+    topk_any<T, MODE>(row, C, kk, sc, out, sh, rest);
   }
   for (int r = kk + tid; r < a.k; r += NT) {
     if (MODE == kTopkSlices) {
