@@ -74,7 +74,8 @@ struct DistillArgs {
 
 // What a row's kernel has to know of the sums' exponentials.  The loss needs those of (z - m) / T and, with labels, of z - m.
 // EXPS = 1: one of the two (T = 1, or alpha = 0 or 1); 2, 4: T = 2 or 4, whose second exponential is a power of the first (a
-// multiplication or two in place of an exponential's four issue slots); 0: both.
+// multiplication or two in place of an exponential's four issue slots); 0: both.  T = 2 -> 3, bf16: the loss of 4096 x 50001 93 -> 100 us, loss
+// and gradient of 8192 x 8192 69.5 -> 75.5; of longer and of short rows the same.
 struct Scales {
   float t, one;  // log2(e) / T and log2(e) (EXPS = 1: the one that is needed, twice)
   float slack;   // the reference stays while logits pass it by less than this: 2^20 in either sum
