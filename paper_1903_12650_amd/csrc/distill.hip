@@ -992,7 +992,8 @@ struct RowEnd {
     if (!none) {
       if (!empty) loss += static_cast<double>(a.alpha) * a.temperature * a.temperature * kl;
       if (label >= 0) {
-        double ce = -(1.0 - a.smoothing) * ((static_cast<double>(sh.z[kTopMax]) - M) * to_1 - Z1);
+        double ce = 0;  // (a term of weight 0 is none, also where the label's logit is -infinity)
+        if (a.smoothing < 1.f) ce = -(1.0 - a.smoothing) * ((static_cast<double>(sh.z[kTopMax]) - M) * to_1 - Z1);
         if (a.smoothing > 0.f) ce -= static_cast<double>(a.smoothing) / a.C * ((r.sz - static_cast<double>(a.C) * M) - a.C * Z1);
         loss += (1.0 - a.alpha) * ce;
       }

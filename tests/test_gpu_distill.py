@@ -854,3 +854,20 @@ def test_log_sum_exp_of_the_rest_holds_float(rn, N, C, k, dtype, temperature):
     bound = EPS * (C / 512 + 64 + 8 * (np.log(C) + 14 + above) + 32 + 2 * np.abs(want))
     off = np.abs(f64(tail)[list(rows)] - want) / bound
     assert (off <= 1).all(), off.max()
+
+
+@pytest.mark.parametrize("alpha", [0.0, 0.5])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("N, C", [(4, 700), (4, 60000), (140, 40000)])
+def test_labels_that_smoothing_takes_all_weight_from(rn, N, C, dtype, alpha):
+    """label_smoothing = 1: every class has 1 / C, the label no more than the others.  A masked class makes the loss infinite, the label's too."""
+    z, v, i, tl, labels = teacher(rn, N, C, 5, 2.0, C)
+    z[0, labels[0].item()] = float("-inf")
+    z[1, (labels[1].item() + 1) % C] = float("-inf")
+    w = torch.zeros(N)
+    w[:4] = 0.25
+    z = z.to(dtype).cuda()
+    _, rows, grad = check_distill(rn, z, v, i, tl, labels, 2.0, alpha, 1.0, w.cuda())
+    assert torch.isposinf(rows[:2]).all() and torch.isfinite(rows[2:]).all()
+    again = rn.distill_fwd_bwd(z, v, i, tl, (labels + 1) % C, 2.0, alpha, 1.0, w.cuda())
+    assert torch.equal(again[1][2:], rows[2:])             # whatever the labels are
