@@ -87,9 +87,13 @@ def distill(z, t_values, t_indices, t_tail=None, labels=None, temperature=1.0, a
                     logq = np.append(u[at], lam) - Z
                     rows[n] += alpha * T * T * np.where(p == 0, 0.0, p * (logp - logq)).sum()
                     q, pr, qr = np.exp(u - Z), p[-1], np.exp(lam - Z)
-                    d = np.where(rest, np.where(np.isneginf(u), 0.0, np.exp(u - lam)) * (qr - pr), q)
+                    share = np.zeros(C)  # exp(u - lam), about the rest's own largest: beside a large one lam loses the logarithm of how many there are
+                    if rest.any() and u[rest].max() != -np.inf:
+                        share[rest] = np.exp(u[rest] - u[rest].max())
+                        share /= share.sum()
+                    d = np.where(rest, share * (qr - pr), q)
                     d[at] -= p[:-1]
-                    s = np.where(rest, np.where(np.isneginf(u), 0.0, np.exp(u - lam)) * (qr + pr), q)
+                    s = np.where(rest, share * (qr + pr), q)
                     s[at] += p[:-1]
                     grad[n] += alpha * T * d
                     size[n] += alpha * T * s

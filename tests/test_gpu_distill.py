@@ -871,3 +871,29 @@ def test_labels_that_smoothing_takes_all_weight_from(rn, N, C, dtype, alpha):
     assert torch.isposinf(rows[:2]).all() and torch.isfinite(rows[2:]).all()
     again = rn.distill_fwd_bwd(z, v, i, tl, (labels + 1) % C, 2.0, alpha, 1.0, w.cuda())
     assert torch.equal(again[1][2:], rows[2:])             # whatever the labels are
+
+
+@pytest.mark.parametrize("T", [1.0, 2.0, 0.7])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("C", [90, 700, 60000])
+def test_a_rest_masked_with_the_lowest_value_shares_the_tail(rn, C, dtype, T):
+    """Every class outside the entries is masked alike: they share the teacher's tail evenly.  The loss, T times the tail's probability times
+    3.4e38, passes the largest float or does not."""
+    z, v, i, tl, labels = teacher(rn, 3, C, 6, T, C)
+    z[1] = torch.finfo(dtype).min
+    z[1, i[1].cpu().long()] = torch.linspace(-1, 2, 6)
+    z[2, C // 2:] = torch.finfo(dtype).min
+    z = z.to(dtype).cuda()
+    _, rows, grad = rn.distill_fwd_bwd(z, v, i, tl, labels, T, 1.0)
+    _, want_rows, want, size = od.distill(f64(z), f64(v), i.cpu().numpy(), f64(tl), labels.cpu().numpy(), T, 1.0)
+    e = sum_error(C)
+    away = np.abs(f64(z).max(1)[:, None] - f64(z)) * max(1.0, 1.0 / T)
+    bound = size * (2 * e + EPS * (5 * np.minimum(away, 90) + 16)) + 1e-36
+    if dtype == BF16:
+        bound += 2.0 ** -8 * 1.01 * (np.abs(want) + bound) + 1e-38
+    assert (np.abs(f64(grad) - want) <= bound).all()
+    with np.errstate(over="ignore"):
+        np.testing.assert_allclose(rows.cpu().numpy(), want_rows.astype(np.float32), rtol=1e-4)
+    rest = torch.ones(C, dtype=torch.bool)
+    rest[i[1].cpu().long()] = False
+    assert bool((grad[1].cpu()[rest] == grad[1].cpu()[rest][0]).all()) and float(grad[1].cpu()[rest][0]) < 0

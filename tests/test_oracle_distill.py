@@ -131,3 +131,15 @@ def test_the_rest_of_a_row_with_more_infinities_than_places():
     assert i.tolist() == [[1, 4], [1, 4], [8, 1], [0, 1]]
     assert np.isposinf(tail[0]) and np.isfinite(tail[1]) and np.isposinf(tail[2]) and np.isnan(tail[3])
     np.testing.assert_allclose(tail[1], np.log(np.exp(np.delete(x[1], [1, 4]) / 2).sum()), rtol=1e-12)
+
+
+def test_a_rest_of_equal_logits_far_below_shares_the_tail():
+    low = float(np.finfo(np.float32).min)
+    z = np.full((2, 9), low)
+    z[0, 3], z[1, [2, 5]] = 1.0, 2.0
+    i, v, tail = np.array([[3, -1], [2, 5]]), np.ones((2, 2)), np.array([0.5, 0.25])
+    _, _, grad, _ = od.distill(z, v, i, tail, row_weight=np.ones(2))
+    for n, (inside, others) in enumerate((([3], 8), ([2, 5], 7))):
+        pr = np.exp(tail[n]) / (np.exp(tail[n]) + len(inside) * np.e)
+        np.testing.assert_allclose(np.delete(grad[n], inside), -pr / others, rtol=1e-12)
+        np.testing.assert_allclose(grad[n].sum(), 0, atol=1e-12)
