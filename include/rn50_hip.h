@@ -502,7 +502,7 @@ int topk_rows(int N, int C, int k, int dtype, const void* logits, int64_t ld, fl
  *     alpha T (softmax(u)_i - p_j) for i = i_j,  alpha T softmax(u)_i (1 - p_r / q_r) for the others,
  *     + (1-alpha) (softmax(z)_i - (1-ls) [i == label] - ls / C)
  * An entry whose class is outside [0,C) is absent, and so is one whose class an entry in front of it has.  A row
- * without entries and tail has KL = 0; a label outside [0,C) (or labels NULL) leaves CE out.  A row of weight 0 counts
+ * without entries and tail has KL = 0, and a cell of p below 2^-126 adds nothing to it; a label outside [0,C) (or labels NULL) leaves CE out.  A row of weight 0 counts
  * for nothing, whatever it holds, a row whose logits are all -infinity has no distribution: loss and gradient 0 for
  * both.  With and without dlogits the losses are the same bits.
  * logits, dlogits: device dtype, rows of C elements ld >= C apart, grad_ld for the gradient; dlogits may be NULL (the
