@@ -20,6 +20,8 @@ __all__ = ["F32", "BF16", "Rn50Error", "lib_path", "conv_fwd", "conv_dgrad", "co
            "LrSchedule", "TrainState", "resnet_train_step", "DECAY_NONE", "DECAY_STEP", "DECAY_POLY", "DECAY_LINEAR",
            "DECAY_TABLE", "resnet_init_params", "bn_relu_infer", "top1_accuracy", "resnet_eval",
            "quant_i8_row_bytes", "quant_rows_i8", "matmul_i8", "fc_i8_workspace_bytes", "fc_i8_fwd", "DistillDesc",
+           "Dropout", "dropout_fwd", "dropout_bwd", "quant_f8_row_bytes", "quant_f8_scale_bytes", "quant_blocks_f8",
+           "matmul_f8_workspace_bytes", "matmul_f8", "fc_f8_fwd_workspace_bytes", "fc_f8_fwd", "fc_f8_bwd_workspace_bytes", "fc_f8_bwd",
            "topk_rows_workspace_bytes", "topk_rows", "distill_workspace_bytes", "distill_fwd_bwd"]
 
 F32, BF16 = 0, 1
@@ -81,7 +83,8 @@ for _n in ("conv_fwd_workspace_bytes", "conv_dgrad_workspace_bytes", "conv_wgrad
            "bn_relu_fwd_workspace_bytes", "bn_relu_bwd_workspace_bytes", "lars_update_workspace_bytes",
            "resnet_plan_workspace_bytes", "conv_bn_sums_bytes", "resnet_train_state_bytes",
            "bn_relu_infer_workspace_bytes", "quant_i8_row_bytes", "fc_i8_workspace_bytes", "topk_rows_workspace_bytes",
-           "distill_workspace_bytes"):
+           "distill_workspace_bytes", "quant_f8_row_bytes", "quant_f8_scale_bytes", "matmul_f8_workspace_bytes",
+           "fc_f8_fwd_workspace_bytes", "fc_f8_bwd_workspace_bytes"):
     if hasattr(raw, _n):
         getattr(raw, _n).restype = ctypes.c_size_t
 for _n in ("resnet_plan_tensor_shape", "resnet_plan_tensor_offset", "resnet_plan_arena_elems", "resnet_plan_bn_channels",
@@ -381,6 +384,74 @@ def fc_i8_workspace_bytes(M, K):
 def fc_i8_fwd(x, w, w_scale, bias=None, dtype=torch.float32, y=None, workspace=None):
     """y [M, N] = x w^T + bias in 8-bit integers: x [M, K] is quantized by rows, w and w_scale are quant_rows_i8's of the weights."""
     return _ops.fc_i8_fwd(x, w, w_scale, bias, dtype, y, workspace)
+
+
+# -------------------------------------------------------------------- dropout
+class Dropout:
+    """rn50_dropout: probability p, seed and the call's number (0 to 2^64 - 1), which a counter in device memory (step, a tensor of one
+    64-bit integer, or None) moves on.  The mask is a function of these and of an element's place: the same object in the forward
+    and the backward call drops the same elements."""
+    __slots__ = ("p", "seed", "call", "step")
+
+    def __init__(self, p, seed, call=0, step=None):
+        self.p, self.seed, self.call, self.step = p, seed, call, step
+
+
+def dropout_fwd(x, dropout, residual=None, y=None):
+    """y = x kept and scaled, or 0 (+ residual).  x: a matrix with contiguous rows, or a contiguous tensor (rows: its last dimension);
+    y: optional tensor to fill, which may be x or residual themselves."""
+    return _ops.dropout_fwd(x, dropout, residual, y)
+
+
+def dropout_bwd(dy, dropout, dx=None):
+    """dx = dy kept and scaled, or 0, with the mask of dropout_fwd.  dx: optional tensor to fill, which may be dy itself."""
+    return _ops.dropout_bwd(dy, dropout, dx)
+
+
+# ----------------------------------------------- products in 8-bit floating point
+def quant_f8_row_bytes(K):
+    return raw.quant_f8_row_bytes(K)
+
+
+def quant_f8_scale_bytes(rows, K):
+    return raw.quant_f8_scale_bytes(rows, K)
+
+
+def quant_blocks_f8(x, format=torch.float8_e4m3fn, rows=True, columns=False, dropout=None):
+    """x [M, K] (float or bfloat16, rows contiguous; behind a dropout, if one is given) in 8-bit floating point with a power of two for
+    each 128 numbers.  Returns q [M, quant_f8_row_bytes(K)] and scale [ceil(K/512), M, 4] uint8, blocks along the rows, and
+    qt [K, quant_f8_row_bytes(M)] and scale_t [ceil(M/512), K, 4], blocks along the columns (None where not asked for)."""
+    return _ops.quant_blocks_f8(x, format, rows, columns, dropout)
+
+
+def matmul_f8_workspace_bytes(M, N, K):
+    return raw.matmul_f8_workspace_bytes(M, N, K)
+
+
+def matmul_f8(K, a, a_scale, w, w_scale, bias=None, dtype=torch.float32, y=None, workspace=None):
+    """y [M, N] = a w^T + bias of rows of K numbers, as quant_blocks_f8 leaves them (a in either format, w in e4m3)."""
+    return _ops.matmul_f8(K, a, a_scale, w, w_scale, bias, dtype, y, workspace)
+
+
+def fc_f8_fwd_workspace_bytes(M, N, K):
+    return raw.fc_f8_fwd_workspace_bytes(M, N, K)
+
+
+def fc_f8_fwd(x, w, w_scale, bias=None, dtype=torch.float32, dropout=None, save=False, y=None, workspace=None):
+    """y [M, N] = x w^T + bias: x [M, K] (behind the dropout) is quantized by rows; w and w_scale: quant_blocks_f8's q and scale of the
+    weights [N, K].  save: returns (y, xt, xt_scale) for fc_f8_bwd."""
+    return _ops.fc_f8_fwd(x, w, w_scale, bias, dtype, dropout, save, y, workspace)
+
+
+def fc_f8_bwd_workspace_bytes(M, N, K):
+    return raw.fc_f8_bwd_workspace_bytes(M, N, K)
+
+
+def fc_f8_bwd(dy, wt, wt_scale, xt, xt_scale, dtype=torch.float32, dropout=None, format=torch.float8_e4m3fn, need_dx=True, need_dw=True,
+              need_db=True, workspace=None):
+    """Returns dx [M, K] (dtype; behind the dropout's mask), dW [N, K] and db [N] (float), None where not needed.  dy [M, N] is quantized to
+    `format`; wt, wt_scale: quant_blocks_f8's qt and scale_t of the weights; xt, xt_scale: as fc_f8_fwd saved them."""
+    return _ops.fc_f8_bwd(dy, wt, wt_scale, xt, xt_scale, dtype, dropout, format, need_dx, need_dw, need_db, workspace)
 
 
 # --------------------------------------------------------------- distillation

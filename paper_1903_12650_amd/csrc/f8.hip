@@ -1,0 +1,624 @@
+// Products in 8-bit floating point with a power of two for every 128 numbers of the axis that is summed: matrices quantized along
+// their rows and, transposed, along their columns; the products; a linear layer's forward and backward pass.
+#include <stdlib.h>
+
+#include <algorithm>
+
+#include "conv_internal.h"
+#include "dropout.h"
+
+namespace rn50 {
+
+constexpr int kF8MaxK = 1 << 22;        // 256 rows of it stay inside a buffer descriptor's 32 bits
+constexpr uint32_t kF8Floor = 27u << 23;  // the bits of 2^-100: blocks below are quantized as if this were their largest magnitude
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+
+// Scale byte (e + 127) of a block from the bits of its largest magnitude, and 2^-e: with a = 1.m 2^(E - 127), the least e with
+// a <= 1.75 * 2^8 (e4m3; 2^15 e5m2) * 2^e.  An infinity's and a NaN's bits are above every number's: byte 127, `finite` false.
+template <bool E5>
+__device__ __forceinline__ uint32_t f8_scale(uint32_t amax_bits, float* inv, bool* finite) {
+  const uint32_t a = max(amax_bits, kF8Floor);
+  *finite = a < 0x7f800000u;
+  const uint32_t byte = *finite ? (a >> 23) - (E5 ? 15u : 8u) + ((a & 0x7fffffu) > 0x600000u ? 1u : 0u) : 127u;
+  *inv = __uint_as_float((254u - byte) << 23);
+  return byte;
+}
+// Four numbers as 8-bit ones, the first in the low byte.
+template <bool E5>
+__device__ __forceinline__ uint32_t f8_four(float a, float b, float c, float d, bool finite) {
+  int w;
+  if constexpr (E5) w = __builtin_amdgcn_cvt_pk_bf8_f32(c, d, __builtin_amdgcn_cvt_pk_bf8_f32(a, b, 0, false), true);
+  else w = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
+  return finite ? static_cast<uint32_t>(w) : 0x7f7f7f7fu;
+}
+// Largest of a row of 16 lanes, in all of them.
+__device__ __forceinline__ uint32_t max_of_16_lanes(uint32_t v) {
+  constexpr int ROR = 0x120;  // row_ror:n
+  v = max(v, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(v), ROR + 8, 0xf, 0xf, false)));
+  v = max(v, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(v), ROR + 4, 0xf, 0xf, false)));
+  v = max(v, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(v), ROR + 2, 0xf, 0xf, false)));
+  return max(v, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(v), ROR + 1, 0xf, 0xf, false)));
+}
+__device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+
+// ------------------------------------------------------------- quantization
+struct QuantArgs {
+  const void* x;
+  int64_t ldx;
+  int M, K, tiles_k;
+  uint8_t *q, *scale, *qt, *scale_t;
+  int Kp, Mp;
+  float* sums;  // float [row tiles][K]: the columns' sums of each tile of x as it is; or NULL
+  DropArgs drop;
+};
+// A tile of 16 * R rows by 128 columns in registers: thread t holds rows R * (t / 16) .. + R - 1 of the eight columns at 8 * (t % 16), the
+// elements of one Philox call a row.  A block along a row is 16 lanes' (DPP), a block along a column the workgroup's (LDS, R = 8).
+template <typename T, bool E5, int R, bool COLS, bool DROP>
+__global__ __launch_bounds__(256) void quant_blocks_kernel(const QuantArgs a) {
+  constexpr int V = Elem<T>::VEC;
+  static_assert(!COLS || R == 8, "a block of 128 rows");
+  const int tid = threadIdx.x, cg = tid & 15, rg = tid >> 4;
+  const int tm = blockIdx.x / a.tiles_k, tk = blockIdx.x - tm * a.tiles_k;
+  const int m0 = tm * 16 * R + rg * R, k0 = tk * 128 + cg * 8, cols = a.K - k0;
+  float f[R][8];
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const T* row = static_cast<const T*>(a.x) + static_cast<int64_t>(m0 + i) * a.ldx + k0;
+    if (m0 + i < a.M && cols >= 8) {
+#pragma unroll
+      for (int j = 0; j < 8; j += V) Elem<T>::unpack(load16_any(row + j), f[i] + j);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[i][j] = m0 + i < a.M && j < cols ? Elem<T>::load(row + j) : 0.f;
+    }
+  }
+  __shared__ uint32_t red[COLS ? 16 : 1][COLS ? 128 : 1];
+  __shared__ uint32_t col_scale[COLS ? 128 : 1];
+  __shared__ uint4 turned[COLS ? 1024 : 1];
+  if (COLS && a.sums) {
+    float (*part)[128] = reinterpret_cast<float (*)[128]>(red);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      float s = f[0][j];
+#pragma unroll
+      for (int i = 1; i < R; ++i) s += f[i][j];
+      part[rg][cg * 8 + j] = s;
+    }
+    __syncthreads();
+    if (tid < 128 && tk * 128 + tid < a.K) {
+      float s = 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s += part[i][tid];
+      a.sums[static_cast<int64_t>(tm) * a.K + tk * 128 + tid] = s;
+    }
+    __syncthreads();
+  }
+  if constexpr (DROP) {
+    const uint64_t call = drop_call(a.drop), per_row = static_cast<uint64_t>((a.K + 7) >> 3);
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const DropBits bits = drop_bits(a.drop, call, static_cast<uint64_t>(m0 + i) * per_row + static_cast<uint32_t>(k0 >> 3));
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[i][j] = drop_keeps(a.drop, bits, j) ? f[i][j] * a.drop.factor : 0.f;
+    }
+  }
+  if (a.q) {
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) top = max(top, magnitude(f[i][j]));
+      float inv;
+      bool finite;
+      const uint32_t byte = f8_scale<E5>(max_of_16_lanes(top), &inv, &finite);
+      if (m0 + i >= a.M) continue;  // (a row's 16 lanes together)
+      uint2 o = make_uint2(f8_four<E5>(f[i][0] * inv, f[i][1] * inv, f[i][2] * inv, f[i][3] * inv, finite),
+                           f8_four<E5>(f[i][4] * inv, f[i][5] * inv, f[i][6] * inv, f[i][7] * inv, finite));
+      if (cols < 8) {  // zeros past the last column, in NaN blocks too
+        const uint64_t keep = cols <= 0 ? 0 : (1ull << (8 * cols)) - 1;
+        o.x &= static_cast<uint32_t>(keep);
+        o.y &= static_cast<uint32_t>(keep >> 32);
+      }
+      *reinterpret_cast<uint2*>(a.q + static_cast<int64_t>(m0 + i) * a.Kp + k0) = o;
+      if (cg == 0) {
+        uint8_t* s = a.scale + (static_cast<int64_t>(tk >> 2) * a.M + m0 + i) * 4;
+        s[tk & 3] = static_cast<uint8_t>(byte);
+        if (tk == a.tiles_k - 1)
+          for (int j = (tk & 3) + 1; j < 4; ++j) s[j] = 0;
+      }
+    }
+  }
+  if constexpr (COLS) {
+    if (!a.qt) return;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < R; ++i) top = max(top, magnitude(f[i][j]));
+      red[rg][cg * 8 + j] = top;
+    }
+    __syncthreads();
+    if (tid < 128) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = max(top, red[i][tid]);
+      float inv;
+      bool finite;
+      const uint32_t byte = f8_scale<E5>(top, &inv, &finite);
+      col_scale[tid] = byte | (finite ? 0u : 256u);
+      const int k = tk * 128 + tid;
+      if (k < a.K) {
+        uint8_t* s = a.scale_t + (static_cast<int64_t>(tm >> 2) * a.K + k) * 4;
+        s[tm & 3] = static_cast<uint8_t>(byte);
+        if (tm == (a.Mp >> 7) - 1)
+          for (int j = (tm & 3) + 1; j < 4; ++j) s[j] = 0;
+      }
+    }
+    __syncthreads();
+    // Turned through LDS: column c has 16 pieces of 8 bytes, piece r of eight rows in place r ^ (c / 8), so that both sides touch all banks.
+    const int rows = a.M - m0;
+    const uint64_t keep = rows >= 8 ? ~0ull : rows <= 0 ? 0ull : (1ull << (8 * rows)) - 1;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t s = col_scale[cg * 8 + j];
+      const float inv = __uint_as_float((254u - (s & 255u)) << 23);
+      const bool finite = s < 256u;
+      uint2 o = make_uint2(f8_four<E5>(f[0][j] * inv, f[1][j] * inv, f[2][j] * inv, f[3][j] * inv, finite),
+                           f8_four<E5>(f[4][j] * inv, f[5][j] * inv, f[6][j] * inv, f[7][j] * inv, finite));
+      o.x &= static_cast<uint32_t>(keep);
+      o.y &= static_cast<uint32_t>(keep >> 32);
+      reinterpret_cast<uint2*>(turned)[(cg * 8 + j) * 16 + (rg ^ cg)] = o;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      const int c = p * 32 + (tid >> 3), piece = tid & 7, g = c >> 3, k = tk * 128 + c;
+      uint4 o = turned[c * 8 + (piece ^ (g >> 1))];
+      if (g & 1) o = make_uint4(o.z, o.w, o.x, o.y);
+      if (k < a.K) *reinterpret_cast<uint4*>(a.qt + static_cast<int64_t>(k) * a.Mp + tm * 128 + piece * 16) = o;
+    }
+  }
+}
+
+// db[n] = the sum of the row tiles' sums, in their order.
+__global__ __launch_bounds__(256) void f8_column_sums_kernel(const float* __restrict__ sums, int tiles, int N, float* __restrict__ db) {
+  const int n = blockIdx.x * 256 + threadIdx.x;
+  if (n >= N) return;
+  double s = 0.0;
+  for (int t = 0; t < tiles; ++t) s += sums[static_cast<int64_t>(t) * N + n];
+  db[n] = static_cast<float>(s);
+}
+
+// ------------------------------------------------------------------ products
+// 16 numbers of a row as bfloat16, times the row's power of two: exact.
+template <bool E5>
+__device__ __forceinline__ void f8_to_bf16(i32x4 v, float scale, bf16x8* out) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      bf16x2 two;
+      if constexpr (E5) two = h ? __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(v[i], scale, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(v[i], scale, false);
+      else two = h ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[i], scale, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[i], scale, false);
+      const int at = 4 * i + 2 * h;
+      out[at >> 3][at & 7] = two[0];
+      out[at >> 3][(at & 7) + 1] = two[1];
+    }
+}
+__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+struct F8Args {
+  const uint8_t *a, *w;
+  const uint32_t *as, *ws;  // dword [g][row]: four blocks' bytes
+  const float* bias;
+  void* y;
+  int64_t ldy;
+  int M, N, Kp, tiles_m, tiles_n;
+  DropArgs drop;  // of y's elements; threshold 0: none
+};
+
+// V consecutive columns of row m, from column n (a multiple of V; V divides 8).
+template <int V>
+__device__ __forceinline__ void drop_columns(const F8Args& a, uint64_t call, int m, int n, float* f) {
+  const DropBits bits = drop_bits(a.drop, call, static_cast<uint64_t>(m) * static_cast<uint32_t>((a.N + 7) >> 3) + static_cast<uint32_t>(n >> 3));
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    bool keep = drop_keeps(a.drop, bits, j);
+    if (V == 4 && (n & 4)) keep = drop_keeps(a.drop, bits, j + 4);
+    f[j] = keep ? f[j] * a.drop.factor : 0.f;
+  }
+}
+
+template <typename T, bool E5, bool EXACT, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) void matmul_f8_kernel(const F8Args a) {
+  constexpr int NT = 64 * WM * WN, RPL = NT / 8, RA = BM / RPL, RB = BN / RPL, TM = BM / WM / 32, TN = BN / WN / 32;
+  constexpr int STAGE = (BM + BN) * 128;
+  static_assert(RA * RPL == BM && RB * RPL == BN && TM >= 1 && TN >= 1, "whole passes, whole blocks");
+  extern __shared__ __align__(16) unsigned char smem[];
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const int wm = wave % WM, wn = wave / WM;
+  constexpr int GROUP = 4;
+  const int id = xcd_remap(blockIdx.x, gridDim.x);
+  const int per = GROUP * a.tiles_n, g = id / per, r = id - g * per, high = min(GROUP, a.tiles_m - g * GROUP);
+  const int m0 = (g * GROUP + r % high) * BM, n0 = r / high * BN;
+  const int rows = min(BM, a.M - m0), cols = min(BN, a.N - n0);
+  const rsrc_words rsA = make_rsrc_words(a.a + static_cast<int64_t>(m0) * a.Kp, static_cast<uint32_t>(rows) * a.Kp);
+  const rsrc_words rsB = make_rsrc_words(a.w + static_cast<int64_t>(n0) * a.Kp, static_cast<uint32_t>(cols) * a.Kp);
+  const int slot = tid & 7, lrow = tid >> 3, piece = slot ^ ((lrow >> 1) & 7);
+  uint32_t at_a[RA], at_b[RB];
+#pragma unroll
+  for (int i = 0; i < RA; ++i) at_a[i] = lrow + RPL * i < rows ? static_cast<uint32_t>(lrow + RPL * i) * a.Kp + piece * 16 : kOob;
+#pragma unroll
+  for (int i = 0; i < RB; ++i) at_b[i] = lrow + RPL * i < cols ? static_cast<uint32_t>(lrow + RPL * i) * a.Kp + piece * 16 : kOob;
+  typedef __attribute__((address_space(3))) unsigned char* lds_byte_ptr;
+  const uint32_t dst = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_byte_ptr)smem)) + static_cast<uint32_t>(wave) * 1024u);
+  const int chunks = a.Kp >> 7;
+  auto load = [&](int c, int buffer) __attribute__((always_inline)) {
+    const uint32_t so = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(c) * 128u), to = dst + static_cast<uint32_t>(buffer) * STAGE;
+#pragma unroll
+    for (int i = 0; i < RA; ++i) buffer_load16_to_lds(rsA, to + i * (RPL * 128), at_a[i], so);
+#pragma unroll
+    for (int i = 0; i < RB; ++i) buffer_load16_to_lds(rsB, to + BM * 128 + i * (RPL * 128), at_b[i], so);
+  };
+  // The scales of four chunks are a dword a row, read a group ahead; a chunk's byte is the low one.
+  uint32_t sa[TM], sb[TN], next_a[TM], next_b[TN];
+  auto load_scales = [&](int group) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i) next_a[i] = a.as[static_cast<int64_t>(group) * a.M + min(m0 + wm * (BM / WM) + i * 32 + (lane & 31), a.M - 1)];
+#pragma unroll
+    for (int j = 0; j < TN; ++j) next_b[j] = a.ws[static_cast<int64_t>(group) * a.N + min(n0 + wn * (BN / WN) + j * 32 + (lane & 31), a.N - 1)];
+  };
+  f32x16 acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+  int frag[4];
+#pragma unroll
+  for (int kk = 0; kk < 4; ++kk) frag[kk] = (lane & 31) * 128 + (((2 * kk + (lane >> 5)) ^ ((lane >> 1) & 7)) << 4);
+  load_scales(0);
+  load(0, 0);
+  for (int c = 0; c < chunks; ++c) {
+    ring_wait<2, RA + RB>(chunks - 1 - c);  // this chunk is there, and the buffer of the one before it has been read
+    if ((c & 3) == 0) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i) sa[i] = next_a[i];
+#pragma unroll
+      for (int j = 0; j < TN; ++j) sb[j] = next_b[j];
+      asm volatile("" ::: "memory");
+      if (c + 4 < chunks) load_scales((c >> 2) + 1);
+    } else {
+#pragma unroll
+      for (int i = 0; i < TM; ++i) sa[i] >>= 8;
+#pragma unroll
+      for (int j = 0; j < TN; ++j) sb[j] >>= 8;
+    }
+    if (c + 1 < chunks) load(c + 1, (c + 1) & 1);
+    const unsigned char* ta = smem + (c & 1) * STAGE + wm * (BM / WM) * 128;
+    const unsigned char* tb = smem + (c & 1) * STAGE + BM * 128 + wn * (BN / WN) * 128;
+    i32x4 fa[4][TM], fb[4][TN];
+    auto read = [&](int kk) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i) fa[kk][i] = *reinterpret_cast<const i32x4*>(ta + i * 32 * 128 + frag[kk]);
+#pragma unroll
+      for (int j = 0; j < TN; ++j) fb[kk][j] = *reinterpret_cast<const i32x4*>(tb + j * 32 * 128 + frag[kk]);
+    };
+    if constexpr (EXACT) {
+      read(0);
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) {
+        if (kk < 3) read(kk + 1);
+        bf16x8 xa[TM][2], xb[TN][2];
+#pragma unroll
+        for (int i = 0; i < TM; ++i) f8_to_bf16<E5>(fa[kk][i], scale_of(sa[i] & 255u), xa[i]);
+#pragma unroll
+        for (int j = 0; j < TN; ++j) f8_to_bf16<false>(fb[kk][j], scale_of(sb[j] & 255u), xb[j]);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xb[j][h], xa[i][h], acc[i][j], 0, 0, 0);
+      }
+    } else {
+      read(0);
+      read(1);
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        if (s == 0) {
+          read(2);
+          read(3);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int j = 0; j < TN; ++j) {
+            const i32x8 va = __builtin_shufflevector(fa[2 * s][i], fa[2 * s + 1][i], 0, 1, 2, 3, 4, 5, 6, 7);
+            const i32x8 vb = __builtin_shufflevector(fb[2 * s][j], fb[2 * s + 1][j], 0, 1, 2, 3, 4, 5, 6, 7);
+            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(vb, va, acc[i][j], 0, E5 ? 1 : 0, 0, static_cast<int>(sb[j]), 0, static_cast<int>(sa[i]));
+          }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  }
+  // Output: a wave's 32 rows at a time through LDS (its own part of it), whole rows of the wave's columns from there.
+  constexpr int WC = BN / WN, PITCH = WC + 4;  // floats (rows 16 bytes further along the banks)
+  static_assert(WM * WN * 32 * PITCH * 4 <= 2 * STAGE, "the output stage fits the buffers");
+  lds_reads_then_barrier();
+  float* mine = reinterpret_cast<float*>(smem) + wave * 32 * PITCH;
+  constexpr int V = Elem<T>::VEC, LPR = WC / V, RPP = 64 / LPR;  // lanes a row, rows a pass
+  const int col = n0 + wn * WC + lane % LPR * V;
+  const uint64_t call = a.drop.threshold ? drop_call(a.drop) : 0;
+  float b[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) b[j] = a.bias && col + j < a.N ? a.bias[col + j] : 0.f;
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int v = 0; v < 4; ++v)
+        *reinterpret_cast<float4*>(mine + (lane & 31) * PITCH + j * 32 + v * 8 + (lane >> 5) * 4) =
+            make_float4(acc[i][j][4 * v], acc[i][j][4 * v + 1], acc[i][j][4 * v + 2], acc[i][j][4 * v + 3]);
+    __builtin_amdgcn_wave_barrier();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int p = 0; p < 32 / RPP; ++p) {
+      const int row = p * RPP + lane / LPR, m = m0 + wm * (BM / WM) + i * 32 + row;
+      if (m < a.M && col < a.N) {
+        float f[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) f[j] = mine[row * PITCH + lane % LPR * V + j] + b[j];
+        if (a.drop.threshold) drop_columns<V>(a, call, m, col, f);
+        T* to = static_cast<T*>(a.y) + m * a.ldy + col;
+        if (col + V <= a.N) {
+          Vec16 o;
+          Elem<T>::pack(f, o);
+          store16_any(to, o);
+        } else {
+#pragma unroll
+          for (int j = 0; j < V; ++j)
+            if (col + j < a.N) Elem<T>::store(to + j, f[j]);
+        }
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  }
+}
+
+// ------------------------------------------------------------------- launches
+template <typename T, bool E5, bool EXACT, int BM, int BN, int WM, int WN>
+static void f8_tile(F8Args a, hipStream_t s) {
+  constexpr int lds = 2 * (BM + BN) * 128;
+  a.tiles_m = static_cast<int>(ceil_div(a.M, BM));
+  a.tiles_n = static_cast<int>(ceil_div(a.N, BN));
+  const auto kernel = matmul_f8_kernel<T, E5, EXACT, BM, BN, WM, WN>;
+  allow_big_lds(kernel, lds);
+  RN50_LAUNCH("matmul_f8", kernel, dim3(static_cast<unsigned>(a.tiles_m) * a.tiles_n), dim3(64 * WM * WN), lds, s, a);
+}
+template <typename T, bool E5, bool EXACT>
+static void f8_product(const F8Args& a, hipStream_t s) {
+  if (ceil_div(a.M, 128) * ceil_div(a.N, 128) >= 256) f8_tile<T, E5, EXACT, 128, 128, 2, 2>(a, s);
+  else f8_tile<T, E5, EXACT, 64, 64, 2, 2>(a, s);
+}
+static void f8_run(int a_format, int y_dtype, const F8Args& a, hipStream_t s) {
+  if (y_dtype == RN50_BF16 && a_format == RN50_E5M2) f8_product<uint16_t, true, false>(a, s);
+  else if (y_dtype == RN50_BF16) f8_product<uint16_t, false, false>(a, s);
+  else if (a_format == RN50_E5M2) f8_product<float, true, true>(a, s);
+  else f8_product<float, false, true>(a, s);
+}
+
+template <typename T, bool E5, bool DROP>
+static void quant_launch(QuantArgs a, hipStream_t s) {
+  const bool cols = a.qt || a.sums;
+  const unsigned grid = static_cast<unsigned>(ceil_div(a.M, cols ? 128 : 32) * a.tiles_k);
+  if (cols) RN50_LAUNCH("quant_blocks_f8", (quant_blocks_kernel<T, E5, 8, true, DROP>), dim3(grid), dim3(256), 0, s, a);
+  else RN50_LAUNCH("quant_blocks_f8", (quant_blocks_kernel<T, E5, 2, false, DROP>), dim3(grid), dim3(256), 0, s, a);
+}
+template <typename T>
+static void quant_typed(const QuantArgs& a, int format, hipStream_t s) {
+  if (format == RN50_E5M2) {
+    if (a.drop.threshold) quant_launch<T, true, true>(a, s);
+    else quant_launch<T, true, false>(a, s);
+  } else {
+    if (a.drop.threshold) quant_launch<T, false, true>(a, s);
+    else quant_launch<T, false, false>(a, s);
+  }
+}
+static void quant_run(int M, int K, int dtype, const void* x, int64_t ldx, const rn50_dropout* drop, int format, uint8_t* q, uint8_t* scale,
+                      uint8_t* qt, uint8_t* scale_t, float* sums, hipStream_t s) {
+  const QuantArgs a{x, ldx, M, K, static_cast<int>(ceil_div(K, 128)), q, scale, qt, scale_t, static_cast<int>(quant_f8_row_bytes(K)),
+                    static_cast<int>(quant_f8_row_bytes(M)), sums, drop_args(drop)};
+  if (dtype == RN50_BF16) quant_typed<uint16_t>(a, format, s);
+  else quant_typed<float>(a, format, s);
+}
+
+// --------------------------------------------------------------------- checks
+static int check_matrix(const char* who, int M, int K, int dtype, const void* x, int64_t ldx) {
+  RN50_REQUIRE(dtype == RN50_F32 || dtype == RN50_BF16, RN50_ERR_INVALID, "%s: dtype %d", who, dtype);
+  RN50_REQUIRE(M > 0 && K > 0, RN50_ERR_INVALID, "%s: non-positive size", who);
+  RN50_REQUIRE(x, RN50_ERR_INVALID, "%s: null pointer", who);
+  RN50_REQUIRE(ldx >= K, RN50_ERR_INVALID, "%s: rows of %d elements %lld apart", who, K, static_cast<long long>(ldx));
+  RN50_REQUIRE(aligned_to(x, dtype == RN50_BF16 ? 2 : 4), RN50_ERR_ALIGN, "%s: pointer not aligned to an element", who);
+  return RN50_OK;
+}
+static int check_quantized(const char* who, const void* q, const void* scale) {
+  RN50_REQUIRE(q && scale, RN50_ERR_INVALID, "%s: null pointer", who);
+  RN50_REQUIRE(aligned16(q) && aligned16(scale), RN50_ERR_ALIGN, "%s: 8-bit matrix or its scales not 16-byte aligned", who);
+  return RN50_OK;
+}
+static int check_format(const char* who, int format) {
+  RN50_REQUIRE(format == RN50_E4M3 || format == RN50_E5M2, RN50_ERR_INVALID, "%s: format %d", who, format);
+  return RN50_OK;
+}
+static int check_sum(const char* who, int K) {
+  RN50_REQUIRE(K <= kF8MaxK, RN50_ERR_UNSUPPORTED, "%s: sums of %d numbers, more than %d", who, K, kF8MaxK);
+  return RN50_OK;
+}
+static int check_tiles(const char* who, int M, int N, int rows, int cols) {
+  RN50_REQUIRE(ceil_div(M, rows) * ceil_div(N, cols) <= (1 << 22), RN50_ERR_UNSUPPORTED, "%s: %d by %d beyond the launch grid", who, M, N);
+  return RN50_OK;
+}
+static int check_workspace(const char* who, const void* workspace, size_t bytes, size_t need) {
+  if (need == 0) return RN50_OK;
+  RN50_REQUIRE(workspace && bytes >= need, RN50_ERR_WORKSPACE, "%s: workspace %zu < %zu bytes", who, bytes, need);
+  RN50_REQUIRE(aligned16(workspace), RN50_ERR_ALIGN, "%s: pointer not 16-byte aligned", who);
+  return RN50_OK;
+}
+
+// A workspace's parts, one behind the other.
+struct Parts {
+  uint8_t* p;
+  size_t used = 0;
+  template <typename T = uint8_t>
+  T* take(size_t bytes) {
+    uint8_t* at = p ? p + used : nullptr;
+    used += align_up(bytes, 256);
+    return reinterpret_cast<T*>(at);
+  }
+};
+static const uint32_t* words(const uint8_t* scale) { return reinterpret_cast<const uint32_t*>(scale); }
+static F8Args product_args(int M, int N, int K, const uint8_t* a, const uint8_t* as, const uint8_t* w, const uint8_t* ws, const float* bias, void* y,
+                           int64_t ldy, const rn50_dropout* drop) {
+  return F8Args{a, w, words(as), words(ws), bias, y, ldy, M, N, static_cast<int>(quant_f8_row_bytes(K)), 0, 0, drop_args(drop)};
+}
+
+}  // namespace rn50
+
+using namespace rn50;
+
+extern "C" size_t quant_f8_row_bytes(int K) { return K < 1 || K > kF8MaxK ? 0 : align_up(static_cast<size_t>(K), 128); }
+extern "C" size_t quant_f8_scale_bytes(int rows, int K) {
+  return rows < 1 || K < 1 || K > kF8MaxK ? 0 : static_cast<size_t>(ceil_div(K, 512)) * static_cast<size_t>(rows) * 4;
+}
+
+extern "C" int quant_blocks_f8(int M, int K, int dtype, const void* x, int64_t ldx, const rn50_dropout* dropout, int format, uint8_t* q,
+                               uint8_t* scale, uint8_t* qt, uint8_t* scale_t, void* stream) {
+  const char* who = "quant_blocks_f8";
+  clear_error();
+  if (int rc = check_matrix(who, M, K, dtype, x, ldx)) return rc;
+  if (int rc = check_format(who, format)) return rc;
+  if (int rc = check_dropout(who, dropout)) return rc;
+  RN50_REQUIRE(q || qt, RN50_ERR_INVALID, "%s: null pointer", who);
+  if (q || scale)
+    if (int rc = check_quantized(who, q, scale)) return rc;
+  if (qt || scale_t)
+    if (int rc = check_quantized(who, qt, scale_t)) return rc;
+  if (q)
+    if (int rc = check_sum(who, K)) return rc;
+  if (qt)
+    if (int rc = check_sum(who, M)) return rc;
+  if (int rc = check_tiles(who, M, K, qt ? 128 : 32, 128)) return rc;
+  quant_run(M, K, dtype, x, ldx, dropout, format, q, scale, qt, scale_t, nullptr, static_cast<hipStream_t>(stream));
+  return launch_status(who);
+}
+
+extern "C" size_t matmul_f8_workspace_bytes(int M, int N, int K) { return 0; }
+
+extern "C" int matmul_f8(int M, int N, int K, int a_format, const uint8_t* a, const uint8_t* a_scale, const uint8_t* w, const uint8_t* w_scale,
+                         const float* bias, int y_dtype, void* y, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream) {
+  const char* who = "matmul_f8";
+  clear_error();
+  RN50_REQUIRE(M > 0 && N > 0 && K > 0, RN50_ERR_INVALID, "%s: non-positive size", who);
+  if (int rc = check_format(who, a_format)) return rc;
+  if (int rc = check_sum(who, K)) return rc;
+  if (int rc = check_quantized(who, a, a_scale)) return rc;
+  if (int rc = check_quantized(who, w, w_scale)) return rc;
+  if (int rc = check_matrix(who, M, N, y_dtype, y, ldy)) return rc;
+  RN50_REQUIRE(aligned_to(bias, 4), RN50_ERR_ALIGN, "%s: pointer not aligned to an element", who);
+  if (int rc = check_tiles(who, M, N, 64, 64)) return rc;
+  if (int rc = check_workspace(who, workspace, workspace_bytes, matmul_f8_workspace_bytes(M, N, K))) return rc;
+  f8_run(a_format, y_dtype, product_args(M, N, K, a, a_scale, w, w_scale, bias, y, ldy, nullptr), static_cast<hipStream_t>(stream));
+  return launch_status(who);
+}
+
+extern "C" size_t fc_f8_fwd_workspace_bytes(int M, int N, int K) {
+  if (M < 1 || N < 1 || quant_f8_row_bytes(K) == 0) return 0;
+  Parts parts{nullptr};
+  parts.take(static_cast<size_t>(M) * quant_f8_row_bytes(K));
+  parts.take(quant_f8_scale_bytes(M, K));
+  return parts.used + matmul_f8_workspace_bytes(M, N, K);
+}
+
+extern "C" int fc_f8_fwd(int M, int N, int K, int x_dtype, const void* x, int64_t ldx, const rn50_dropout* dropout, const uint8_t* w,
+                         const uint8_t* w_scale, const float* bias, int y_dtype, void* y, int64_t ldy, uint8_t* xt, uint8_t* xt_scale,
+                         void* workspace, size_t workspace_bytes, void* stream) {
+  const char* who = "fc_f8_fwd";
+  clear_error();
+  if (int rc = check_matrix(who, M, K, x_dtype, x, ldx)) return rc;
+  RN50_REQUIRE(N > 0, RN50_ERR_INVALID, "%s: non-positive size", who);
+  if (int rc = check_dropout(who, dropout)) return rc;
+  if (int rc = check_sum(who, K)) return rc;
+  if (int rc = check_quantized(who, w, w_scale)) return rc;
+  if (int rc = check_matrix(who, M, N, y_dtype, y, ldy)) return rc;
+  RN50_REQUIRE(aligned_to(bias, 4), RN50_ERR_ALIGN, "%s: pointer not aligned to an element", who);
+  if (xt || xt_scale) {
+    if (int rc = check_quantized(who, xt, xt_scale)) return rc;
+    if (int rc = check_sum(who, M)) return rc;
+  }
+  if (int rc = check_tiles(who, M, N, 64, 64)) return rc;
+  if (int rc = check_tiles(who, M, K, xt ? 128 : 32, 128)) return rc;
+  if (int rc = check_workspace(who, workspace, workspace_bytes, fc_f8_fwd_workspace_bytes(M, N, K))) return rc;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  Parts parts{static_cast<uint8_t*>(workspace)};
+  uint8_t* q = parts.take(static_cast<size_t>(M) * quant_f8_row_bytes(K));
+  uint8_t* qs = parts.take(quant_f8_scale_bytes(M, K));
+  quant_run(M, K, x_dtype, x, ldx, dropout, RN50_E4M3, q, qs, xt, xt_scale, nullptr, s);
+  f8_run(RN50_E4M3, y_dtype, product_args(M, N, K, q, qs, w, w_scale, bias, y, ldy, nullptr), s);
+  return launch_status(who);
+}
+
+extern "C" size_t fc_f8_bwd_workspace_bytes(int M, int N, int K) {
+  if (quant_f8_row_bytes(M) == 0 || quant_f8_row_bytes(N) == 0 || K < 1) return 0;
+  Parts parts{nullptr};
+  parts.take(static_cast<size_t>(M) * quant_f8_row_bytes(N));
+  parts.take(quant_f8_scale_bytes(M, N));
+  parts.take(static_cast<size_t>(N) * quant_f8_row_bytes(M));
+  parts.take(quant_f8_scale_bytes(N, M));
+  parts.take(static_cast<size_t>(ceil_div(M, 128)) * N * 4);
+  return parts.used;
+}
+
+extern "C" int fc_f8_bwd(int M, int N, int K, int dy_dtype, const void* dy, int64_t ld_dy, int format, const uint8_t* wt, const uint8_t* wt_scale,
+                         const uint8_t* xt, const uint8_t* xt_scale, const rn50_dropout* dropout, int dx_dtype, void* dx, int64_t ld_dx,
+                         float* dW, float* db, void* workspace, size_t workspace_bytes, void* stream) {
+  const char* who = "fc_f8_bwd";
+  clear_error();
+  if (int rc = check_matrix(who, M, N, dy_dtype, dy, ld_dy)) return rc;
+  RN50_REQUIRE(K > 0, RN50_ERR_INVALID, "%s: non-positive size", who);
+  if (int rc = check_format(who, format)) return rc;
+  if (int rc = check_dropout(who, dropout)) return rc;
+  if (int rc = check_sum(who, M)) return rc;
+  if (int rc = check_sum(who, N)) return rc;
+  RN50_REQUIRE(dx || dW || db, RN50_ERR_INVALID, "%s: null pointer", who);
+  if (dx) {
+    if (int rc = check_quantized(who, wt, wt_scale)) return rc;
+    if (int rc = check_matrix(who, M, K, dx_dtype, dx, ld_dx)) return rc;
+  }
+  if (dW)
+    if (int rc = check_quantized(who, xt, xt_scale)) return rc;
+  RN50_REQUIRE(aligned_to(dW, 4) && aligned_to(db, 4), RN50_ERR_ALIGN, "%s: pointer not aligned to an element", who);
+  if (int rc = check_tiles(who, M, N, 32, 128)) return rc;
+  if (int rc = check_tiles(who, M, K, 64, 64)) return rc;
+  if (int rc = check_tiles(who, N, K, 64, 64)) return rc;
+  if (int rc = check_workspace(who, workspace, workspace_bytes, fc_f8_bwd_workspace_bytes(M, N, K))) return rc;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  Parts parts{static_cast<uint8_t*>(workspace)};
+  uint8_t* q = parts.take(static_cast<size_t>(M) * quant_f8_row_bytes(N));
+  uint8_t* qs = parts.take(quant_f8_scale_bytes(M, N));
+  uint8_t* qt = parts.take(static_cast<size_t>(N) * quant_f8_row_bytes(M));
+  uint8_t* qts = parts.take(quant_f8_scale_bytes(N, M));
+  const int tiles = static_cast<int>(ceil_div(M, 128));
+  float* sums = parts.take<float>(static_cast<size_t>(tiles) * N * 4);
+  quant_run(M, N, dy_dtype, dy, ld_dy, nullptr, format, dx ? q : nullptr, qs, dW ? qt : nullptr, qts, db ? sums : nullptr, s);
+  if (dx) f8_run(format, dx_dtype, product_args(M, K, N, q, qs, wt, wt_scale, nullptr, dx, ld_dx, dropout), s);
+  if (dW) f8_run(format, RN50_F32, product_args(N, K, M, qt, qts, xt, xt_scale, nullptr, dW, K, nullptr), s);
+  if (db) RN50_LAUNCH("quant_blocks_f8", f8_column_sums_kernel, dim3(static_cast<unsigned>(ceil_div(N, 256))), dim3(256), 0, s, sums, tiles, N, db);
+  return launch_status(who);
+}

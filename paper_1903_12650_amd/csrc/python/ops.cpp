@@ -419,6 +419,237 @@ PyObject* distill_fwd_bwd_py(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return Py_BuildValue("NNN", wrap(loss), wrap(row), out);
   });
 }
+// ------------------------------- dropout, products in 8-bit floating point
+int format_of(const at::Tensor& t) {
+  if (t.scalar_type() == at::kFloat8_e4m3fn) return RN50_E4M3;
+  if (t.scalar_type() == at::kFloat8_e5m2) return RN50_E5M2;
+  raise(PyExc_TypeError, (std::string("an 8-bit floating-point matrix is expected, got ") + c10::toString(t.scalar_type())).c_str());
+}
+at::ScalarType format_type(PyObject* o) {
+  if (!THPDtype_Check(o)) raise(PyExc_TypeError, "a torch.dtype is expected");
+  const at::ScalarType t = reinterpret_cast<THPDtype*>(o)->scalar_type;
+  if (t != at::kFloat8_e4m3fn && t != at::kFloat8_e5m2) raise(PyExc_TypeError, (std::string("unsupported format ") + c10::toString(t)).c_str());
+  return t;
+}
+int format_code(at::ScalarType t) { return t == at::kFloat8_e4m3fn ? RN50_E4M3 : RN50_E5M2; }
+struct Owned {  // (a new reference)
+  PyObject* o;
+  explicit Owned(PyObject* p) : o(p) { if (!p) throw PyError(); }
+  ~Owned() { Py_DECREF(o); }
+  Owned(const Owned&) = delete;
+};
+// What binding.py's Dropout holds (None: no dropout).
+struct DropArg {
+  rn50_dropout d{};
+  bool given = false;
+  DropArg(PyObject* o, const at::Tensor& like) {
+    if (o == Py_None) return;
+    given = true;
+    const Owned p(PyObject_GetAttrString(o, "p")), seed(PyObject_GetAttrString(o, "seed")), number(PyObject_GetAttrString(o, "call")), step(PyObject_GetAttrString(o, "step"));
+    d.p = static_cast<float>(to_double(p.o));
+    d.seed = word(seed.o);
+    d.call = word(number.o);
+    if (step.o == Py_None) return;
+    const at::Tensor& t = required(step.o);
+    if (t.scalar_type() != at::kLong && t.scalar_type() != at::kUInt64) raise(PyExc_TypeError, "step: a tensor of 64-bit integers is expected");
+    if (t.numel() != 1) raise(PyExc_ValueError, "step: one number is expected");
+    d.step = addr<const uint64_t>(t);
+    if (t.device() != like.device()) raise(PyExc_ValueError, "step: on another device");
+  }
+  static uint64_t word(PyObject* o) {
+    const unsigned long long v = PyLong_AsUnsignedLongLong(o);
+    if (v == static_cast<unsigned long long>(-1) && PyErr_Occurred()) throw PyError();
+    return v;
+  }
+  const rn50_dropout* get() const { return given ? &d : nullptr; }
+};
+// A matrix with contiguous rows, or a contiguous tensor of any shape as the rows of its last dimension.
+Rows any_rows(const at::Tensor& t) {
+  if (t.dim() == 2) return rows_of(t);
+  if (t.dim() == 0) raise(PyExc_ValueError, "a tensor of one dimension or more is expected");
+  if (!t.is_cuda() || !t.is_contiguous()) raise(PyExc_AssertionError, "device, contiguous tensors only");
+  const int64_t c = t.size(-1), n = c ? t.numel() / c : 0;
+  if (n > INT32_MAX || c > INT32_MAX) raise(PyExc_ValueError, "at most 2^31 - 1 rows and columns are expected");
+  return {t.data_ptr(), n, c, c};
+}
+// A tensor like `like`, given or made.
+at::Tensor output_like(PyObject* given, const at::Tensor& like, const char* what) {
+  const at::Tensor* t = tensor(given);
+  if (!t) return empty(like.sizes(), like.scalar_type(), like);
+  if (t->scalar_type() != like.scalar_type()) raise(PyExc_TypeError, (std::string(what) + ": the input's type is expected").c_str());
+  if (t->sizes() != like.sizes()) raise(PyExc_ValueError, (std::string(what) + ": the size does not fit").c_str());
+  if (t->device() != like.device()) raise(PyExc_ValueError, (std::string(what) + ": on another device").c_str());
+  return *t;
+}
+// dropout_fwd(x, dropout, residual, y)
+PyObject* dropout_fwd_py(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 4, [&]() -> PyObject* {
+    const at::Tensor& x = required(a[0]);
+    const int dt = dtype_of(x);
+    const Rows r = any_rows(x);
+    on_current_device(x);
+    const DropArg drop(a[1], x);
+    Rows res{nullptr, 0, 0, r.c};
+    if (a[2] != Py_None) res = any_rows(output_like(a[2], x, "residual"));
+    const at::Tensor y = output_like(a[3], x, "y");
+    const Rows out = any_rows(y);
+    void* const s = current_stream();
+    call([&] { return dropout_fwd(drop.get(), static_cast<int>(r.n), static_cast<int>(r.c), dt, r.p, r.ld, res.p, res.ld, out.p, out.ld, s); });
+    return wrap(y);
+  });
+}
+// dropout_bwd(dy, dropout, dx)
+PyObject* dropout_bwd_py(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 3, [&]() -> PyObject* {
+    const at::Tensor& dy = required(a[0]);
+    const int dt = dtype_of(dy);
+    const Rows r = any_rows(dy);
+    on_current_device(dy);
+    const DropArg drop(a[1], dy);
+    const at::Tensor dx = output_like(a[2], dy, "dx");
+    const Rows out = any_rows(dx);
+    void* const s = current_stream();
+    call([&] { return dropout_bwd(drop.get(), static_cast<int>(r.n), static_cast<int>(r.c), dt, r.p, r.ld, out.p, out.ld, s); });
+    return wrap(dx);
+  });
+}
+// An 8-bit matrix of `rows` rows of K numbers and its scales, made.
+struct Quantized {
+  at::Tensor q, scale;
+  uint8_t *pq = nullptr, *ps = nullptr;
+  Quantized() {}
+  Quantized(int64_t rows, int64_t K, at::ScalarType type, const at::Tensor& like) {
+    q = empty({rows, static_cast<int64_t>(quant_f8_row_bytes(static_cast<int>(K)))}, type, like);
+    scale = empty({(K + 511) / 512, rows, 4}, at::kByte, like);
+    pq = addr<uint8_t>(q);
+    ps = addr<uint8_t>(scale);
+  }
+  PyObject* first() const { return q.defined() ? wrap(q) : none(); }
+  PyObject* second() const { return q.defined() ? wrap(scale) : none(); }
+  static PyObject* none() { Py_INCREF(Py_None); return Py_None; }
+};
+// The same, given: q [rows, row bytes], scale [groups, rows, 4].
+struct GivenQuantized {
+  const uint8_t *q, *scale;
+  int64_t rows;
+  int format;
+  GivenQuantized(PyObject* oq, PyObject* os, int64_t K, const char* what, const at::Tensor& like) {
+    const at::Tensor& t = required(oq);
+    format = format_of(t);
+    if (t.dim() != 2) raise(PyExc_ValueError, (std::string(what) + ": a matrix is expected").c_str());
+    rows = t.size(0);
+    if (rows > INT32_MAX) raise(PyExc_ValueError, "a matrix of at most 2^31 - 1 rows is expected");
+    q = vec<uint8_t>(oq, t.scalar_type(), {rows, static_cast<int64_t>(quant_f8_row_bytes(static_cast<int>(K)))}, what, like);
+    scale = vec<uint8_t>(os, at::kByte, {(K + 511) / 512, rows, 4}, (std::string(what) + "_scale").c_str(), like);
+  }
+  void e4m3(const char* what) const {
+    if (format != RN50_E4M3) raise(PyExc_TypeError, (std::string(what) + ": torch.float8_e4m3fn is expected").c_str());
+  }
+};
+// quant_blocks_f8(x, format, rows, columns, dropout)
+PyObject* quant_blocks_f8_py(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 5, [&]() -> PyObject* {
+    const at::Tensor& x = required(a[0]);
+    const int dt = dtype_of(x), rows = PyObject_IsTrue(a[2]), columns = PyObject_IsTrue(a[3]);
+    if (rows < 0 || columns < 0) throw PyError();
+    const at::ScalarType type = format_type(a[1]);
+    const Rows r = rows_of(x);
+    on_current_device(x);
+    const DropArg drop(a[4], x);
+    const Quantized q = rows ? Quantized(r.n, r.c, type, x) : Quantized(), t = columns ? Quantized(r.c, r.n, type, x) : Quantized();
+    void* const s = current_stream();
+    call([&] { return quant_blocks_f8(static_cast<int>(r.n), static_cast<int>(r.c), dt, r.p, r.ld, drop.get(), format_code(type), q.pq, q.ps, t.pq, t.ps, s); });
+    return Py_BuildValue("NNNN", q.first(), q.second(), t.first(), t.second());
+  });
+}
+// matmul_f8(K, a, a_scale, w, w_scale, bias, dtype, y, workspace)
+PyObject* matmul_f8_py(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 9, [&]() -> PyObject* {
+    const int K = to_int(a[0]);
+    const at::Tensor& like = required(a[1]);
+    const GivenQuantized x(a[1], a[2], K, "a", like), w(a[3], a[4], K, "w", like);
+    w.e4m3("w");
+    const float* bias = vec<float>(a[5], at::kFloat, {w.rows}, "bias", like, true);
+    on_current_device(like);
+    const at::Tensor y = product_out(a[7], a[6], x.rows, w.rows, like);
+    const Rows r = rows_of(y);
+    const int dt = dtype_of(y), M = static_cast<int>(x.rows), N = static_cast<int>(w.rows);
+    const Workspace work(a[8], a[8] == Py_None ? matmul_f8_workspace_bytes(M, N, K) : 0, like);
+    void* const s = current_stream();
+    call([&] { return matmul_f8(M, N, K, x.format, x.q, x.scale, w.q, w.scale, bias, dt, r.p, r.ld, work.p, work.bytes, s); });
+    return wrap(y);
+  });
+}
+// fc_f8_fwd(x, w, w_scale, bias, dtype, dropout, save, y, workspace)
+PyObject* fc_f8_fwd_py(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 9, [&]() -> PyObject* {
+    const at::Tensor& x = required(a[0]);
+    const int xt = dtype_of(x);
+    const Rows rx = rows_of(x);
+    const GivenQuantized w(a[1], a[2], rx.c, "w", x);
+    w.e4m3("w");
+    const float* bias = vec<float>(a[3], at::kFloat, {w.rows}, "bias", x, true);
+    on_current_device(x);
+    const DropArg drop(a[5], x);
+    const int save = PyObject_IsTrue(a[6]);
+    if (save < 0) throw PyError();
+    const at::Tensor y = product_out(a[7], a[4], rx.n, w.rows, x);
+    const Rows ry = rows_of(y);
+    const int yt = dtype_of(y), M = static_cast<int>(rx.n), N = static_cast<int>(w.rows), K = static_cast<int>(rx.c);
+    const Quantized kept = save ? Quantized(rx.c, rx.n, at::kFloat8_e4m3fn, x) : Quantized();
+    const Workspace work(a[8], a[8] == Py_None ? fc_f8_fwd_workspace_bytes(M, N, K) : 0, x);
+    void* const s = current_stream();
+    call([&] {
+      return fc_f8_fwd(M, N, K, xt, rx.p, rx.ld, drop.get(), w.q, w.scale, bias, yt, ry.p, ry.ld, kept.pq, kept.ps, work.p, work.bytes, s);
+    });
+    if (!save) return wrap(y);
+    return Py_BuildValue("NNN", wrap(y), kept.first(), kept.second());
+  });
+}
+// fc_f8_bwd(dy, wt, wt_scale, xt, xt_scale, dtype, dropout, format, need_dx, need_dw, need_db, workspace)
+PyObject* fc_f8_bwd_py(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 12, [&]() -> PyObject* {
+    const at::Tensor& dy = required(a[0]);
+    const int dyt = dtype_of(dy);
+    const Rows r = rows_of(dy);
+    const int want[] = {PyObject_IsTrue(a[8]), PyObject_IsTrue(a[9]), PyObject_IsTrue(a[10])};
+    if (want[0] < 0 || want[1] < 0 || want[2] < 0) throw PyError();
+    const uint8_t *wq = nullptr, *ws = nullptr, *xq = nullptr, *xs = nullptr;
+    int64_t K = 1;
+    if (want[0]) {
+      const GivenQuantized w(a[1], a[2], r.c, "wt", dy);
+      w.e4m3("wt");
+      wq = w.q; ws = w.scale; K = w.rows;
+    }
+    if (want[1]) {
+      const GivenQuantized x(a[3], a[4], r.n, "xt", dy);
+      x.e4m3("xt");
+      if (want[0] && x.rows != K) raise(PyExc_ValueError, "xt: the size does not fit");
+      xq = x.q; xs = x.scale; K = x.rows;
+    }
+    const int format = format_code(format_type(a[7]));
+    on_current_device(dy);
+    const DropArg drop(a[6], dy);
+    at::Tensor dx, dw, db;
+    int dxt = RN50_F32;
+    if (want[0]) {
+      dx = empty({r.n, K}, float_type(a[5]), dy);
+      dxt = dtype_of(dx);
+    }
+    if (want[1]) dw = empty({r.c, K}, at::kFloat, dy);
+    if (want[2]) db = empty({r.c}, at::kFloat, dy);
+    const int M = static_cast<int>(r.n), N = static_cast<int>(r.c);
+    const Workspace work(a[11], a[11] == Py_None ? fc_f8_bwd_workspace_bytes(M, N, static_cast<int>(K)) : 0, dy);
+    void* const px = want[0] ? addr(dx) : nullptr;
+    float *const pw = want[1] ? addr<float>(dw) : nullptr, *const pb = want[2] ? addr<float>(db) : nullptr;
+    void* const s = current_stream();
+    call([&] {
+      return fc_f8_bwd(M, N, static_cast<int>(K), dyt, r.p, r.ld, format, wq, ws, xq, xs, drop.get(), dxt, px, K, pw, pb, work.p, work.bytes, s);
+    });
+    auto out = [](const at::Tensor& t) { return t.defined() ? wrap(t) : Quantized::none(); };
+    return Py_BuildValue("NNN", out(dx), out(dw), out(db));
+  });
+}
 // setup(Rn50Error, current raw stream of a device, current device)
 PyObject* setup_py(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 3, [&]() -> PyObject* {
@@ -435,6 +666,9 @@ PyObject* setup_py(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyMethodDef kMethods[] = {FAST("conv_fwd", conv_fwd_py), FAST("conv_dgrad", conv_dgrad_py), FAST("conv_wgrad", conv_wgrad_py),
                           FAST("bn_relu_fwd", bn_relu_fwd_py), FAST("bn_relu_bwd", bn_relu_bwd_py),
                           FAST("quant_rows_i8", quant_rows_i8_py), FAST("matmul_i8", matmul_i8_py), FAST("fc_i8_fwd", fc_i8_fwd_py),
+                          FAST("dropout_fwd", dropout_fwd_py), FAST("dropout_bwd", dropout_bwd_py),
+                          FAST("quant_blocks_f8", quant_blocks_f8_py), FAST("matmul_f8", matmul_f8_py),
+                          FAST("fc_f8_fwd", fc_f8_fwd_py), FAST("fc_f8_bwd", fc_f8_bwd_py),
                           FAST("topk_rows", topk_rows_py), FAST("distill_fwd_bwd", distill_fwd_bwd_py),
                           FAST("setup", setup_py), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_ops", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};

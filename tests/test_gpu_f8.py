@@ -1,0 +1,413 @@
+"""Dropout, matrices in 8-bit floating point, their products, and the linear layer made of them, against their 64-bit forms.
+
+Where the bounds come from (eps = 2^-24, half a unit in the last place of a float):
+ - masks and 8-bit numbers: whole numbers by definition, bit for bit;
+ - dropout: one product (or multiply-add) in float, one more rounding to bfloat16 (2^-8 of the result);
+ - float products: the factors are exact in bfloat16 and so are their products in float; a sum of K of them in any order is off by at
+   most 2 eps K (2: the matrix cores may cut instead of rounding) of the sum of their magnitudes; the bias's addition one more;
+ - bfloat16 products: the 8-bit matrix cores keep of eight products what lies above 2^-13 of the largest: each of seven loses less
+   than 2^-13 of it, 2^-10 of the eight's magnitudes together; then the sum's roundings as above and 2^-8 of the result;
+ - sums of a gradient's columns: float over 128 rows, in 64 bits behind that: 130 eps of the magnitudes."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import f8
+
+pytestmark = pytest.mark.gpu
+EPS = 2.0 ** -24
+BF16, F32 = torch.bfloat16, torch.float32
+FORMATS = {f8.E4M3: torch.float8_e4m3fn, f8.E5M2: torch.float8_e5m2}
+
+
+@pytest.fixture(scope="module")
+def rn():
+    import paper_1903_12650_amd as rn
+    return rn
+
+
+def spread(t, extra):
+    """The same matrix with rows `extra` elements further apart."""
+    wide = torch.full((t.shape[0], t.shape[1] + extra), float("nan"), dtype=t.dtype, device=t.device)
+    wide[:, :t.shape[1]] = t
+    return wide[:, :t.shape[1]]
+
+
+def offset(t, by):
+    """The same matrix, starting `by` elements behind an aligned address, its rows side by side."""
+    flat = torch.zeros(t.numel() + by, dtype=t.dtype, device=t.device)
+    flat[by:] = t.reshape(-1)
+    return flat[by:].view(t.shape)
+
+
+def f64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def bytes_of(t):
+    return t.view(torch.uint8).cpu().numpy()
+
+
+def values(M, K, seed, dtype=F32, size=1.0):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(M, K, generator=g) * torch.exp(torch.randn(M, 1, generator=g)) * torch.exp(torch.randn(1, K, generator=g)) * size
+    return x.to(dtype)
+
+
+def out_error(y_type, y):
+    return 2.0 ** -8 * np.abs(y) if y_type == BF16 else 0.0
+
+
+def product_error(y_type, K, y, size):
+    """Of a product without the bias's own rounding."""
+    e = 2 * EPS * (K + 1) * size
+    return e + 2.0 ** -10 * size + out_error(y_type, y) if y_type == BF16 else e
+
+
+def assert_within(got, want, bound, what=""):
+    got = f64(got) if isinstance(got, torch.Tensor) else got
+    assert got.shape == want.shape
+    excess = np.abs(got - want) - bound
+    worst = np.unravel_index(np.argmax(excess), excess.shape)
+    assert not np.isnan(got).any() and excess[worst] <= 0, (what, worst, got[worst], want[worst], np.broadcast_to(bound, want.shape)[worst])
+
+
+# -------------------------------------------------------------------- dropout
+DROP = [(1, 1), (3, 5), (7, 8), (2, 2047), (130, 9), (300, 1), (2, 5000), (40, 2048), (1, 70001), (257, 24)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("M, K", DROP)
+def test_dropout(rn, M, K, dtype):
+    x, r = values(M, K, M + K, dtype), values(M, K, M * K + 1, dtype)
+    for p, seed, call in ((0.0, 1, 0), (0.1, 2 ** 64 - 1, 5), (0.5, 12345678901234567, 2 ** 63 + 7), (1.0, 3, 0)):
+        d = rn.Dropout(p, seed, call)
+        want = f8.dropout(f64(x), p, seed, call)
+        for src in (x.cuda(), spread(x.cuda(), 3), offset(x.cuda(), 1)):
+            y = rn.dropout_fwd(src, d)
+            assert_within(y, want, EPS * np.abs(want) + out_error(dtype, want), (p, seed, call))
+            assert torch.equal(rn.dropout_bwd(src, d), y)
+            assert np.array_equal(f64(y) != 0, f8.kept(M, K, p, seed, call) & (f64(x) != 0))
+        want = f8.dropout(f64(x), p, seed, call, residual=f64(r))
+        y = rn.dropout_fwd(x.cuda(), d, r.cuda())
+        assert_within(y, want, EPS * np.abs(want) + out_error(dtype, want), (p, seed, call))
+        assert torch.equal(rn.dropout_fwd(offset(x.cuda(), 3), d, spread(r.cuda(), 5)), y)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_dropout_in_place_and_what_is_dropped(rn, dtype):
+    x = values(33, 77, 1, dtype)
+    x[:, 5], x[:, 6], x[:, 7] = float("inf"), float("nan"), float("-inf")
+    d = rn.Dropout(0.4, 9)
+    keep = torch.from_numpy(f8.kept(33, 77, 0.4, 9))
+    y = rn.dropout_fwd(x.cuda(), d)
+    assert (y.cpu()[~keep] == 0).all() and not torch.signbit(y.cpu()[~keep]).any()  # whatever was there
+    assert torch.equal(torch.isfinite(y.cpu()), torch.isfinite(x) | ~keep)
+    r = values(33, 77, 2, dtype).cuda()
+    want = rn.dropout_fwd(x.cuda(), d, r)
+    for place in ("x", "residual"):
+        a, b = x.cuda(), r.clone()
+        out = rn.dropout_fwd(a, d, b, y=a if place == "x" else b)
+        assert out.data_ptr() == (a if place == "x" else b).data_ptr()
+        assert torch.equal(out.view(torch.uint8), want.view(torch.uint8))
+    dy = r.clone()
+    assert torch.equal(rn.dropout_bwd(dy, d, dx=dy), rn.dropout_bwd(r, d))
+    wide = torch.full((33, 90), 7.0, dtype=dtype, device="cuda")
+    rn.dropout_fwd(x.cuda(), d, y=wide[:, :77])
+    assert (wide[:, 77:] == 7).all() and torch.equal(wide[:, :77].contiguous().view(torch.uint8), y.view(torch.uint8))
+
+
+def test_dropout_of_any_shape_goes_by_its_last_dimension(rn):
+    x = values(6, 20, 4).cuda()
+    d = rn.Dropout(0.3, 4)
+    y = rn.dropout_fwd(x, d)
+    assert torch.equal(rn.dropout_fwd(x.view(2, 3, 20), d).view(6, 20), y)
+    assert torch.equal(rn.dropout_fwd(x.view(1, 2, 3, 20), d, x.view(1, 2, 3, 20)).view(6, 20), rn.dropout_fwd(x, d, x))
+    assert torch.equal(rn.dropout_fwd(x[0].contiguous(), d), y[0])
+
+
+def test_dropout_step_counter_in_a_captured_graph(rn):
+    """The counter is read when the kernel runs: each replay has its own mask, forward and backward the same one."""
+    x, dy = values(50, 600, 1, BF16).cuda(), values(50, 600, 2, BF16).cuda()
+    step = torch.zeros(1, dtype=torch.int64, device="cuda")
+    one = torch.ones(1, dtype=torch.int64, device="cuda")
+    d = rn.Dropout(0.25, 77, 3 << 32, step)
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        rn.dropout_fwd(x, d, y=y)
+    torch.cuda.current_stream().wait_stream(s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        rn.dropout_fwd(x, d, y=y)
+        rn.dropout_bwd(dy, d, dx=dx)
+        step.add_(one)
+    step.zero_()
+    seen = []
+    for i in range(4):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert int(step.item()) == i + 1
+        keep = f8.kept(50, 600, 0.25, 77, 3 << 32, i)
+        fixed = rn.Dropout(0.25, 77, (3 << 32) + i)
+        assert torch.equal(y, rn.dropout_fwd(x, fixed)) and torch.equal(dx, rn.dropout_bwd(dy, fixed))
+        assert np.array_equal(f64(y) != 0, keep & (f64(x) != 0))
+        seen.append(keep)
+    assert not np.array_equal(seen[0], seen[1])
+
+
+def test_dropout_takes_the_training_state_s_step(rn):
+    plan = rn.ResnetPlan(4, rn.F32, 64, 10, (8, 12, 16, 24), (2, 1, 2, 1), 8, 4)
+    state = rn.TrainState(plan, first_step=41)
+    x = values(9, 40, 3).cuda()
+    y = rn.dropout_fwd(x, rn.Dropout(0.5, 8, 1 << 32, state.buf[:8].view(torch.int64)))
+    assert torch.equal(y, rn.dropout_fwd(x, rn.Dropout(0.5, 8, (1 << 32) + 41)))
+
+
+# -------------------------------------------------------------- 8-bit matrices
+QUANT = [(1, 1), (1, 128), (5, 7), (127, 129), (128, 128), (130, 513), (3, 2047), (257, 40), (600, 1100), (33, 8), (1025, 131)]
+
+
+def check_quantized(rn, x, fmt, src, dropout=None, xf=None):
+    """x: the numbers (float on the host); src: the tensor that is quantized."""
+    xf = x.float().numpy() if xf is None else xf
+    want = f8.quant(xf, fmt) + f8.quant(np.ascontiguousarray(xf.T), fmt)
+    for rows, columns in ((True, True), (True, False), (False, True)):
+        got = rn.quant_blocks_f8(src, FORMATS[fmt], rows=rows, columns=columns, dropout=dropout)
+        assert [g is None for g in got] == [not rows] * 2 + [not columns] * 2
+        for g, w, i in zip(got, want, range(4)):
+            if g is not None:
+                assert tuple(g.shape) == w.shape and np.array_equal(bytes_of(g), w), ("q scale qt scale_t".split()[i], rows, columns)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("M, K", QUANT)
+def test_quantized_blocks(rn, M, K, dtype, fmt):
+    x = values(M, K, M * 7 + K, dtype)
+    if M > 2:
+        x[1] = 0
+    for src in (x.cuda(), spread(x.cuda(), 1), offset(x.cuda(), 3)):
+        check_quantized(rn, x, fmt, src)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_quantized_blocks_at_the_edges(rn, dtype, fmt):
+    """Largest numbers at and one step beyond what a power holds, ties, numbers below the floor, the largest and smallest floats."""
+    F = torch.tensor(f8.LARGEST[fmt])
+    x = values(150, 300, 6, dtype)
+    for i, e in enumerate(range(-120, 112, 5)):
+        x[i] = (x[i].float().clamp(-1, 1) * F * 2.0 ** e).to(dtype)
+        x[i, 7] = (F * 2.0 ** e).to(dtype)
+        up = (F * 2.0 ** e * (1 + 2.0 ** -7 if dtype == BF16 else 1 + 2.0 ** -23))
+        x[i, 200] = up.to(dtype)
+    x[60, :] = torch.finfo(dtype).max
+    x[61, :] = torch.finfo(dtype).tiny
+    x[62, :] = torch.finfo(dtype).tiny / 4  # subnormal
+    x[63, :150] = 2.0 ** -100
+    x[64, :] = (torch.arange(300) * 0.125 - 18).to(dtype)
+    x[65, :], x[66, :] = 0.0, -0.0
+    check_quantized(rn, x, fmt, x.cuda())
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_quantized_blocks_with_infinities_and_nan(rn, dtype, fmt):
+    x = values(140, 270, 8, dtype)
+    x[3, 5], x[3, 260], x[130, 0], x[139, 269], x[7, 129] = float("inf"), float("nan"), float("-inf"), float("nan"), float("inf")
+    check_quantized(rn, x, fmt, x.cuda())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("M, K", [(1, 1), (40, 2047), (130, 300), (129, 8)])
+def test_quantized_blocks_behind_a_dropout(rn, M, K, dtype):
+    x = values(M, K, 12, dtype)
+    x[0, 0] = float("nan")
+    d = rn.Dropout(0.3, 5, 6)
+    keep = f8.kept(M, K, 0.3, 5, 6)
+    xf = np.where(keep, x.float().numpy() * f8.factor(0.3), np.float32(0))
+    check_quantized(rn, x, f8.E4M3, x.cuda(), d, xf)
+
+
+# ------------------------------------------------------------------- products
+MATMUL = [(1, 1, 1), (1, 1000, 2048), (3, 17, 127), (16, 40, 128), (17, 33, 300), (40, 1000, 2048), (64, 65, 513), (65, 70, 129),
+          (127, 255, 513), (128, 128, 128), (130, 20, 1100), (300, 200, 640), (257, 511, 2047), (5, 2900, 700), (2, 9, 20000), (1100, 1300, 260)]
+
+
+def quantized(x, fmt=f8.E4M3):
+    """(q, scale) on the device, (numbers) on the host."""
+    q, s = f8.quant(x.float().numpy(), fmt)
+    return torch.from_numpy(q).cuda().view(FORMATS[fmt]), torch.from_numpy(s).cuda(), f8.stands_for(q, s, fmt)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("M, N, K", MATMUL)
+def test_products(rn, M, N, K, fmt):
+    a, sa, na = quantized(values(M, K, 1), fmt)
+    w, sw, nw = quantized(values(N, K, 2, size=K ** -0.5))
+    bias = torch.randn(N, generator=torch.Generator().manual_seed(3))
+    for y_type in (F32, BF16):
+        for b in (None, bias):
+            want, size = f8.matmul(na, nw, None if b is None else b.double().numpy())
+            bound = product_error(y_type, K, want, size)
+            y = rn.matmul_f8(K, a, sa, w, sw, None if b is None else b.cuda(), dtype=y_type)
+            assert_within(y, want, bound, (y_type, b is not None))
+        wide = torch.full((M, N + 5), 3.0, dtype=y_type, device="cuda")
+        out = rn.matmul_f8(K, a, sa, w, sw, offset(bias.cuda()[None], 1)[0], y=wide[:, 1:N + 1])
+        assert torch.equal(out, y) and (wide[:, 0] == 3).all() and (wide[:, N + 1:] == 3).all()
+        assert torch.equal(rn.matmul_f8(K, a, sa, w, sw, bias.cuda(), dtype=y_type), y)  # the same bits every time
+
+
+def test_products_of_blocks_of_very_different_powers(rn):
+    """Largest and smallest powers side by side: each block's scale is its own, in every row of both factors."""
+    M, N, K = 70, 90, 1700
+    g = torch.Generator().manual_seed(1)
+    blocks = lambda rows: torch.exp2(torch.randint(-60, 56, (rows, 14), generator=g).float()).repeat_interleave(128, 1)[:, :K]  # noqa: E731
+    x, w = values(M, K, 1) * blocks(M), values(N, K, 2) * blocks(N)
+    a, sa, na = quantized(x)
+    b, sb, nb = quantized(w)
+    for y_type in (F32, BF16):
+        want, size = f8.matmul(na, nb)
+        fits = (size < 2.0 ** 125)
+        y = f64(rn.matmul_f8(K, a, sa, b, sb, dtype=y_type))
+        bound = product_error(y_type, K, want, size) + 2.0 ** -126
+        assert (np.abs(y - want) <= bound)[fits].all() and fits.mean() > 0.9
+    for e in (-108, -60, 0, 60):  # e4m3's whole range against its mirror image
+        x, w = torch.full((33, 256), 448.0 * 2.0 ** e), torch.full((20, 256), 448.0 * 2.0 ** min(-e, 100))
+        a, sa, na = quantized(x)
+        b, sb, nb = quantized(w)
+        for y_type in (F32, BF16):
+            want, size = f8.matmul(na, nb)
+            assert_within(rn.matmul_f8(256, a, sa, b, sb, dtype=y_type), want, product_error(y_type, 256, want, size))
+
+
+@pytest.mark.parametrize("M", [3, 40, 100])
+def test_nan_blocks_reach_their_row_and_column_only(rn, M):
+    x, w = values(M, 400, 1), values(70, 400, 2)
+    x[1, 300], w[5, 3], w[69, 399] = float("nan"), float("inf"), float("nan")
+    a, sa, _ = quantized(x)
+    b, sb, _ = quantized(w)
+    for y_type in (F32, BF16):
+        nan = torch.isnan(rn.matmul_f8(400, a, sa, b, sb, dtype=y_type)).cpu()
+        want = torch.zeros(M, 70, dtype=torch.bool)
+        want[1], want[:, 5], want[:, 69] = True, True, True
+        assert torch.equal(nan, want)
+
+
+# --------------------------------------------------------------- linear layer
+LAYER = [(1, 1, 1), (1, 1000, 2048), (2, 10, 131), (16, 33, 1000), (17, 40, 300), (40, 1000, 2048), (128, 130, 129), (200, 70, 513), (515, 300, 250)]
+
+
+@pytest.mark.parametrize("M, N, K", LAYER)
+def test_layer_forward(rn, M, N, K):
+    w = values(N, K, 2, size=K ** -0.5)
+    qw, sw = f8.quant(w.float().numpy())
+    dw, ds = torch.from_numpy(qw).cuda().view(torch.float8_e4m3fn), torch.from_numpy(sw).cuda()
+    bias = torch.randn(N, generator=torch.Generator().manual_seed(3))
+    for dtype, y_type, drop in ((BF16, F32, None), (F32, BF16, None), (BF16, BF16, (0.25, 9, 4)), (F32, F32, (0.5, 2 ** 40, 2 ** 50))):
+        x = values(M, K, 5, dtype)
+        d = None if drop is None else rn.Dropout(*drop)
+        want, size, xt, xts = f8.fc_fwd(x.float().numpy(), qw, sw, bias.double().numpy(), drop)
+        y, t, ts = rn.fc_f8_fwd(x.cuda(), dw, ds, bias.cuda(), dtype=y_type, dropout=d, save=True)
+        assert np.array_equal(bytes_of(t), xt) and np.array_equal(bytes_of(ts), xts)
+        assert_within(y, want, product_error(y_type, K, want, size), (dtype, y_type, drop))
+        alone = rn.fc_f8_fwd(spread(x.cuda(), 3), dw, ds, bias.cuda(), dtype=y_type, dropout=d)
+        assert_within(alone, want, product_error(y_type, K, want, size), ("not saved", dtype, y_type, drop))
+        wide = torch.full((M, N + 3), 3.0, dtype=y_type, device="cuda")
+        rn.fc_f8_fwd(offset(x.cuda(), 1), dw, ds, bias.cuda(), dropout=d, y=wide[:, 2:N + 2])
+        assert torch.equal(wide[:, 2:N + 2], alone) and (wide[:, :2] == 3).all() and (wide[:, N + 2:] == 3).all()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("M, N, K", LAYER + [(2950, 20, 40), (1, 300, 5000)])
+def test_layer_backward(rn, M, N, K, fmt):
+    wt, wts, _ = quantized(values(K, N, 2, size=K ** -0.5))
+    x = values(K, M, 4)
+    xt, xts, _ = quantized(x)
+    host = [bytes_of(t) for t in (wt, wts, xt, xts)]
+    for dtype, dx_type, drop in ((F32, BF16, None), (BF16, F32, (0.25, 9, 4)), (BF16, BF16, (0.5, 3, 0))):
+        dy = values(M, N, 6, dtype, size=1e-4)
+        d = None if drop is None else rn.Dropout(*drop)
+        (dx, sx), (dw, sw), (db, sb) = f8.fc_bwd(dy.float().numpy(), *host, fmt=fmt, drop=drop)
+        got = rn.fc_f8_bwd(dy.cuda(), wt, wts, xt, xts, dtype=dx_type, dropout=d, format=FORMATS[fmt])
+        assert [g.dtype for g in got] == [dx_type, F32, F32]
+        more = 4 * EPS if drop else 0  # (the factor's product)
+        bounds = (product_error(dx_type, N, dx, sx) + more * np.abs(dx), product_error(F32, M, dw, sw), 130 * EPS * sb)
+        for g, want, bound, what in zip(got, (dx, dw, db), bounds, ("dx", "dw", "db")):
+            assert_within(g, want, bound, (what, dtype, dx_type, drop))
+        for need in ((True, False, False), (False, True, False), (False, False, True), (True, False, True), (False, True, True)):
+            part = rn.fc_f8_bwd(spread(dy.cuda(), 7), wt if need[0] else None, wts if need[0] else None, xt if need[1] else None,
+                                xts if need[1] else None, dtype=dx_type, dropout=d, format=FORMATS[fmt], need_dx=need[0], need_dw=need[1],
+                                need_db=need[2])
+            for p, g, n in zip(part, got, need):
+                assert (p is None) == (not n) and (not n or torch.equal(p, g)), need
+
+
+def test_layer_gradients_by_differences(rn):
+    """Small whole numbers are quantized exactly and summed exactly: the layer is linear there, and its gradients are the differences."""
+    g = np.random.Generator(np.random.PCG64(5))
+    M, N, K = 70, 90, 200
+    x, w, dy = (torch.from_numpy(g.integers(-8, 9, s).astype(np.float32)).cuda() for s in ((M, K), (N, K), (M, N)))
+    bias = torch.arange(N, dtype=F32, device="cuda")
+    drop = rn.Dropout(0.5, 11, 3)  # (factor 2: exact)
+
+    def loss(x, w, b):
+        q, s, _, _ = rn.quant_blocks_f8(w)
+        return float((dy.double() * rn.fc_f8_fwd(x, q, s, b, dropout=drop).double()).sum())
+
+    q, s, t, ts = rn.quant_blocks_f8(w, rows=True, columns=True)
+    y, xt, xts = rn.fc_f8_fwd(x, q, s, bias, dropout=drop, save=True)
+    dx, dw, db = rn.fc_f8_bwd(dy, t, ts, xt, xts, dropout=drop)
+    for _ in range(12):
+        i, j, k = (int(g.integers(n)) for n in (M, N, K))
+        d = torch.zeros_like(x); d[i, k] = 1
+        assert float(dx[i, k]) == (loss(x + d, w, bias) - loss(x - d, w, bias)) / 2
+        d = torch.zeros_like(w); d[j, k] = 1
+        assert float(dw[j, k]) == (loss(x, w + d, bias) - loss(x, w - d, bias)) / 2
+        d = torch.zeros_like(bias); d[j] = 1
+        assert float(db[j]) == (loss(x, w, bias + d) - loss(x, w, bias - d)) / 2
+
+
+def test_layer_in_a_captured_graph(rn):
+    """Forward and backward of a layer behind a dropout whose counter moves on, as a training step runs them: every replay like the
+    eager calls with that counter, twice in a row with eager work between."""
+    M, N, K = 40, 100, 300
+    x, w, dy = values(M, K, 1, BF16).cuda(), values(N, K, 2, BF16).cuda(), values(M, N, 3, F32).cuda()
+    bias = torch.zeros(N, device="cuda")
+    step = torch.zeros(1, dtype=torch.int64, device="cuda")
+    one = torch.ones(1, dtype=torch.int64, device="cuda")
+
+    def layer(drop):
+        q, s, t, ts = rn.quant_blocks_f8(w, rows=True, columns=True)
+        y, xt, xts = rn.fc_f8_fwd(x, q, s, bias, dropout=drop, save=True)
+        return (y,) + rn.fc_f8_bwd(dy, t, ts, xt, xts, dropout=drop)
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        layer(rn.Dropout(0.2, 5, 0, step))
+    torch.cuda.current_stream().wait_stream(s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = layer(rn.Dropout(0.2, 5, 0, step))
+        step.add_(one)
+    step.zero_()
+    for i in range(4):
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(out, layer(rn.Dropout(0.2, 5, i))):
+            assert torch.equal(a, b), i
+
+
+def test_on_another_stream(rn):
+    x = values(300, 500, 1, BF16).cuda()
+    w, ws, _, _ = rn.quant_blocks_f8(values(400, 500, 2).cuda())
+    want = rn.fc_f8_fwd(x, w, ws, dtype=BF16)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        got = [rn.fc_f8_fwd(x, w, ws, dtype=BF16) for _ in range(3)]
+    s.synchronize()
+    assert all(torch.equal(g, want) for g in got)
