@@ -3,6 +3,7 @@
 #include <stdlib.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "conv_internal.h"
 #include "dropout.h"
@@ -231,12 +232,12 @@ __device__ __forceinline__ void drop_columns(const F8Args& a, uint64_t call, int
   }
 }
 
-template <typename T, bool E5, bool EXACT, int BM, int BN, int WM, int WN>
+template <typename T, bool E5, bool EXACT, int BM, int BN, int WM, int WN, int RING>
 __global__ __launch_bounds__(64 * WM * WN) void matmul_f8_kernel(const F8Args a) {
-  constexpr int NT = 64 * WM * WN, RPL = NT / 8, RA = BM / RPL, RB = BN / RPL, TM = BM / WM / 32, TN = BN / WN / 32;
-  constexpr int STAGE = (BM + BN) * 128;
-  static_assert(RA * RPL == BM && RB * RPL == BN && TM >= 1 && TN >= 1, "whole passes, whole blocks");
-  extern __shared__ __align__(16) unsigned char smem[];
+  constexpr int CB = 128, PPR = CB / 16, NT = 64 * WM * WN, RPL = NT / PPR, RA = BM / RPL, RB = BN / RPL, TM = BM / WM / 32, TN = BN / WN / 32;
+  constexpr int STAGE = (BM + BN) * CB, SCALES = (BM + BN) * 4;
+  static_assert(RA * RPL == BM && RB * RPL == BN && TM >= 1 && TN >= 1 && (RING & (RING - 1)) == 0, "whole passes, whole blocks");
+  extern __shared__ __align__(16) unsigned char smem[];  // RING stages, two groups' scales
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int wm = wave % WM, wn = wave / WM;
   constexpr int GROUP = 4;
@@ -246,29 +247,37 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_f8_kernel(const F8Args a)
   const int rows = min(BM, a.M - m0), cols = min(BN, a.N - n0);
   const rsrc_words rsA = make_rsrc_words(a.a + static_cast<int64_t>(m0) * a.Kp, static_cast<uint32_t>(rows) * a.Kp);
   const rsrc_words rsB = make_rsrc_words(a.w + static_cast<int64_t>(n0) * a.Kp, static_cast<uint32_t>(cols) * a.Kp);
-  const int slot = tid & 7, lrow = tid >> 3, piece = slot ^ ((lrow >> 1) & 7);
+  const int slot = tid % PPR, lrow = tid / PPR, piece = slot ^ ((lrow >> 1) & (PPR - 1));
   uint32_t at_a[RA], at_b[RB];
 #pragma unroll
   for (int i = 0; i < RA; ++i) at_a[i] = lrow + RPL * i < rows ? static_cast<uint32_t>(lrow + RPL * i) * a.Kp + piece * 16 : kOob;
 #pragma unroll
   for (int i = 0; i < RB; ++i) at_b[i] = lrow + RPL * i < cols ? static_cast<uint32_t>(lrow + RPL * i) * a.Kp + piece * 16 : kOob;
   typedef __attribute__((address_space(3))) unsigned char* lds_byte_ptr;
-  const uint32_t dst = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_byte_ptr)smem)) + static_cast<uint32_t>(wave) * 1024u);
-  const int chunks = a.Kp >> 7;
-  auto load = [&](int c, int buffer) __attribute__((always_inline)) {
-    const uint32_t so = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(c) * 128u), to = dst + static_cast<uint32_t>(buffer) * STAGE;
-#pragma unroll
-    for (int i = 0; i < RA; ++i) buffer_load16_to_lds(rsA, to + i * (RPL * 128), at_a[i], so);
-#pragma unroll
-    for (int i = 0; i < RB; ++i) buffer_load16_to_lds(rsB, to + BM * 128 + i * (RPL * 128), at_b[i], so);
+  const uint32_t base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_byte_ptr)smem));
+  const uint32_t dst = __builtin_amdgcn_readfirstlane(base + static_cast<uint32_t>(wave) * 1024u);
+  const int blocks = a.Kp >> 7, stages = a.Kp / CB;
+  constexpr int NL = RA + RB;
+  auto load_one = [&](int st, int l) __attribute__((always_inline)) {  // (l known when compiling; past the last stage: nothing is read, zeros arrive)
+    const uint32_t so = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(st) * CB), to = dst + static_cast<uint32_t>(st & (RING - 1)) * STAGE;
+    rsrc_words r = l < RA ? rsA : rsB;
+    r.z = st < stages ? r.z : 0;
+    if (l < RA) buffer_load16_to_lds(r, to + l * (RPL * CB), at_a[l < RA ? l : 0], so);
+    else buffer_load16_to_lds(r, to + BM * CB + (l - RA) * (RPL * CB), at_b[l < RA ? 0 : l - RA], so);
   };
-  // The scales of four chunks are a dword a row, read a group ahead; a chunk's byte is the low one.
-  uint32_t sa[TM], sb[TN], next_a[TM], next_b[TN];
+  // The scales of a group of four blocks are a dword a row, brought into LDS like the operands: 64 rows of the tile or of its columns a wave,
+  // a group ahead, again with every block (branches here would let the compiler move a step's products behind the next barrier).
+  constexpr int PARTS = (BM + BN) / 64;
   auto load_scales = [&](int group) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < TM; ++i) next_a[i] = a.as[static_cast<int64_t>(group) * a.M + min(m0 + wm * (BM / WM) + i * 32 + (lane & 31), a.M - 1)];
-#pragma unroll
-    for (int j = 0; j < TN; ++j) next_b[j] = a.ws[static_cast<int64_t>(group) * a.N + min(n0 + wn * (BN / WN) + j * 32 + (lane & 31), a.N - 1)];
+    for (int i = 0; i < (PARTS + WM * WN - 1) / (WM * WN); ++i) {
+      const int part = __builtin_amdgcn_readfirstlane((i * WM * WN + wave) % PARTS);
+      const bool of_a = part < BM / 64;
+      const uint32_t* from = of_a ? a.as + static_cast<int64_t>(group) * a.M + m0 : a.ws + static_cast<int64_t>(group) * a.N + n0;
+      const int there = group * 4 < blocks ? of_a ? rows : cols : 0;
+      buffer_load4_to_lds(make_rsrc_words(from, static_cast<uint32_t>(there) * 4u), base + RING * STAGE + static_cast<uint32_t>(group & 1) * SCALES + part * 256,
+                          static_cast<uint32_t>((of_a ? part : part - BM / 64) * 64 + lane) * 4u);
+    }
   };
   f32x16 acc[TM][TN];
 #pragma unroll
@@ -277,79 +286,105 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_f8_kernel(const F8Args a)
     for (int j = 0; j < TN; ++j)
 #pragma unroll
       for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
-  int frag[4];
+  int frag[CB / 32];
 #pragma unroll
-  for (int kk = 0; kk < 4; ++kk) frag[kk] = (lane & 31) * 128 + (((2 * kk + (lane >> 5)) ^ ((lane >> 1) & 7)) << 4);
-  load_scales(0);
-  load(0, 0);
-  for (int c = 0; c < chunks; ++c) {
-    ring_wait<2, RA + RB>(chunks - 1 - c);  // this chunk is there, and the buffer of the one before it has been read
-    if ((c & 3) == 0) {
+  for (int u = 0; u < CB / 32; ++u) frag[u] = (lane & 31) * CB + (((2 * u + (lane >> 5)) ^ ((lane >> 1) & (PPR - 1))) << 4);
+  // Fragments a step ahead (FAST: a stage, EXACT: half of one), across stages as well: the last step of a stage is multiplied behind the barrier that frees
+  // the stage's buffer, while the next stage's fragments and the loads of the one RING stages on are on their way.
+  constexpr int READS = EXACT ? 1 : 2;
+  i32x4 fa[2][READS][TM], fb[2][READS][TN];
+  uint32_t sa[TM], sb[TN], next_a[TM], next_b[TN];
+  constexpr int SB = 32 * READS, STEPS = 128 / SB;  // bytes of a row a step; steps a block
+  constexpr int READ = READS * (TM + TN);
+  auto read_one = [&](int block, int step, int n) __attribute__((always_inline)) {  // fragment n of a step, into set step & 1
+    const int st = block * (128 / CB) + step * SB / CB, u = n / (TM + TN), f = n % (TM + TN), at = frag[step * SB % CB / 32 + u];
+    const unsigned char* t = smem + (st & (RING - 1)) * STAGE + at;
+    if (f < TN) fb[step & 1][u][f] = *reinterpret_cast<const i32x4*>(t + (BM + wn * (BN / WN) + f * 32) * CB);
+    else fa[step & 1][u][f - TN] = *reinterpret_cast<const i32x4*>(t + (wm * (BM / WM) + (f - TN) * 32) * CB);
+  };
+  auto read = [&](int block, int step) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < TM; ++i) sa[i] = next_a[i];
+    for (int n = 0; n < READ; ++n) read_one(block, step, n);
+  };
+  auto read_scales = [&](int block) __attribute__((always_inline)) {
+    const unsigned char* t = smem + RING * STAGE + (block >> 2 & 1) * SCALES + (lane & 31) * 4;
 #pragma unroll
-      for (int j = 0; j < TN; ++j) sb[j] = next_b[j];
-      asm volatile("" ::: "memory");
-      if (c + 4 < chunks) load_scales((c >> 2) + 1);
-    } else {
+    for (int i = 0; i < TM; ++i) next_a[i] = *reinterpret_cast<const uint32_t*>(t + (wm * (BM / WM) + i * 32) * 4);
 #pragma unroll
-      for (int i = 0; i < TM; ++i) sa[i] >>= 8;
-#pragma unroll
-      for (int j = 0; j < TN; ++j) sb[j] >>= 8;
-    }
-    if (c + 1 < chunks) load(c + 1, (c + 1) & 1);
-    const unsigned char* ta = smem + (c & 1) * STAGE + wm * (BM / WM) * 128;
-    const unsigned char* tb = smem + (c & 1) * STAGE + BM * 128 + wn * (BN / WN) * 128;
-    i32x4 fa[4][TM], fb[4][TN];
-    auto read = [&](int kk) __attribute__((always_inline)) {
-#pragma unroll
-      for (int i = 0; i < TM; ++i) fa[kk][i] = *reinterpret_cast<const i32x4*>(ta + i * 32 * 128 + frag[kk]);
-#pragma unroll
-      for (int j = 0; j < TN; ++j) fb[kk][j] = *reinterpret_cast<const i32x4*>(tb + j * 32 * 128 + frag[kk]);
-    };
+    for (int j = 0; j < TN; ++j) next_b[j] = *reinterpret_cast<const uint32_t*>(t + (BM + wn * (BN / WN) + j * 32) * 4);
+  };
+  // A step's products; between them, one after the other, the next step's fragments are read and a stage's loads requested: in a bunch
+  // they hold the products up, four waves' 16 loads for as long as they take to go out.
+  auto multiply = [&](int set, int next_block, int next_step, bool loads, int st) __attribute__((always_inline)) {
+    constexpr int SLOTS = (EXACT ? 2 : 1) * TM * TN;
+    bf16x8 xa[EXACT ? TM : 1][2], xb[EXACT ? TN : 1][2];
     if constexpr (EXACT) {
-      read(0);
 #pragma unroll
-      for (int kk = 0; kk < 4; ++kk) {
-        if (kk < 3) read(kk + 1);
-        bf16x8 xa[TM][2], xb[TN][2];
+      for (int j = 0; j < TN; ++j) f8_to_bf16<false>(fb[set][0][j], scale_of(sb[j] & 255u), xb[j]);
 #pragma unroll
-        for (int i = 0; i < TM; ++i) f8_to_bf16<E5>(fa[kk][i], scale_of(sa[i] & 255u), xa[i]);
+      for (int i = 0; i < TM; ++i) f8_to_bf16<E5>(fa[set][0][i], scale_of(sa[i] & 255u), xa[i]);
+    }
 #pragma unroll
-        for (int j = 0; j < TN; ++j) f8_to_bf16<false>(fb[kk][j], scale_of(sb[j] & 255u), xb[j]);
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int i = 0; i < TM; ++i)
-#pragma unroll
-            for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xb[j][h], xa[i][h], acc[i][j], 0, 0, 0);
+    for (int n = 0; n < SLOTS; ++n) {
+      const int i = n % (TM * TN) / TN, j = n % TN;
+      if constexpr (EXACT) {
+        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xb[j][n / (TM * TN)], xa[i][n / (TM * TN)], acc[i][j], 0, 0, 0);
+      } else {
+        const i32x8 va = __builtin_shufflevector(fa[set][0][i], fa[set][READS - 1][i], 0, 1, 2, 3, 4, 5, 6, 7);
+        const i32x8 vb = __builtin_shufflevector(fb[set][0][j], fb[set][READS - 1][j], 0, 1, 2, 3, 4, 5, 6, 7);
+        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(vb, va, acc[i][j], 0, E5 ? 1 : 0, 0, static_cast<int>(sb[j]), 0, static_cast<int>(sa[i]));
       }
-    } else {
-      read(0);
-      read(1);
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        if (s == 0) {
-          read(2);
-          read(3);
+      for (int r = n * READ / SLOTS; r < (n + 1) * READ / SLOTS; ++r) read_one(next_block, next_step, r);
+      if (loads) {
+#pragma unroll
+        for (int l = n * NL / SLOTS; l < (n + 1) * NL / SLOTS; ++l) load_one(st, l);
+      }
+    }
+    // (the compiler would move every read to where its product waits for it)
+#pragma unroll
+    for (int n = 0; n < SLOTS; ++n) {
+      __builtin_amdgcn_sched_group_barrier(8, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(256, (READ + SLOTS - 1) / SLOTS, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  load_scales(0);
+  load_scales(1);
+#pragma unroll
+  for (int st = 0; st < RING; ++st)
+#pragma unroll
+    for (int l = 0; l < NL; ++l) load_one(st, l);
+  wait_loads_then_barrier<(RING - 1) * NL>();
+  read_scales(0);
+  read(0, 0);
+  for (int block = 0; block < blocks; ++block) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i) sa[i] = next_a[i] >> ((block & 3) * 8);
+#pragma unroll
+    for (int j = 0; j < TN; ++j) sb[j] = next_b[j] >> ((block & 3) * 8);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int step = 0; step < STEPS; ++step) {
+      const int done = (step + 1) * SB;  // bytes of this block whose fragments have been read
+      const int next = done < 128 ? block : block + 1, st = block * (128 / CB) + done / CB - 1;
+      if (done % CB == 0) {  // the next stage: it is there, and everyone has read this one, whose buffer is loaded anew
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        wait_loads_then_barrier<(RING - 2) * NL>();
+        if (done == 128) {
+          read_scales(block + 1);
+          load_scales(((block + 1) >> 2) + 1);
         }
         __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int i = 0; i < TM; ++i)
-#pragma unroll
-          for (int j = 0; j < TN; ++j) {
-            const i32x8 va = __builtin_shufflevector(fa[2 * s][i], fa[2 * s + 1][i], 0, 1, 2, 3, 4, 5, 6, 7);
-            const i32x8 vb = __builtin_shufflevector(fb[2 * s][j], fb[2 * s + 1][j], 0, 1, 2, 3, 4, 5, 6, 7);
-            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(vb, va, acc[i][j], 0, E5 ? 1 : 0, 0, static_cast<int>(sb[j]), 0, static_cast<int>(sa[i]));
-          }
-        __builtin_amdgcn_sched_barrier(0);
       }
+      multiply(step & 1, next, (step + 1) % STEPS, done % CB == 0, st + RING);  // (behind the last stage: zeros, not used)
     }
   }
   // Output: a wave's 32 rows at a time through LDS (its own part of it), whole rows of the wave's columns from there.
   constexpr int WC = BN / WN, PITCH = WC + 4;  // floats (rows 16 bytes further along the banks)
-  static_assert(WM * WN * 32 * PITCH * 4 <= 2 * STAGE, "the output stage fits the buffers");
-  lds_reads_then_barrier();
+  static_assert(WM * WN * 32 * PITCH * 4 <= RING * STAGE, "the output stage fits the buffers");
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  wait_loads_then_barrier<0>();
   float* mine = reinterpret_cast<float*>(smem) + wave * 32 * PITCH;
   constexpr int V = Elem<T>::VEC, LPR = WC / V, RPP = 64 / LPR;  // lanes a row, rows a pass
   const int col = n0 + wn * WC + lane % LPR * V;
@@ -393,19 +428,35 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_f8_kernel(const F8Args a)
 }
 
 // ------------------------------------------------------------------- launches
-template <typename T, bool E5, bool EXACT, int BM, int BN, int WM, int WN>
+template <typename T, bool E5, bool EXACT, int BM, int BN, int WM, int WN, int RING>
 static void f8_tile(F8Args a, hipStream_t s) {
-  constexpr int lds = 2 * (BM + BN) * 128;
+  constexpr int lds = RING * (BM + BN) * 128 + 2 * (BM + BN) * 4;
   a.tiles_m = static_cast<int>(ceil_div(a.M, BM));
   a.tiles_n = static_cast<int>(ceil_div(a.N, BN));
-  const auto kernel = matmul_f8_kernel<T, E5, EXACT, BM, BN, WM, WN>;
+  const auto kernel = matmul_f8_kernel<T, E5, EXACT, BM, BN, WM, WN, RING>;
   allow_big_lds(kernel, lds);
   RN50_LAUNCH("matmul_f8", kernel, dim3(static_cast<unsigned>(a.tiles_m) * a.tiles_n), dim3(64 * WM * WN), lds, s, a);
 }
 template <typename T, bool E5, bool EXACT>
 static void f8_product(const F8Args& a, hipStream_t s) {
-  if (ceil_div(a.M, 128) * ceil_div(a.N, 128) >= 256) f8_tile<T, E5, EXACT, 128, 128, 2, 2>(a, s);
-  else f8_tile<T, E5, EXACT, 64, 64, 2, 2>(a, s);
+#ifdef RN50_TUNING  // tuning builds only: RN50_F8_TILE=tile
+  if (const char* e = getenv("RN50_F8_TILE")) {
+    switch (atoi(e)) {
+      case 256: return f8_tile<T, E5, EXACT, 256, 256, 2, 4, 2>(a, s);
+      case 1288: return f8_tile<T, E5, EXACT, 128, 128, 2, 4, 2>(a, s);
+      case 1284: return f8_tile<T, E5, EXACT, 128, 128, 2, 2, 4>(a, s);
+      case 128644: return f8_tile<T, E5, EXACT, 128, 64, 2, 2, 4>(a, s);
+      case 644: return f8_tile<T, E5, EXACT, 64, 64, 2, 2, 4>(a, s);
+    }
+  }
+#endif
+  auto tiles = [&](int bm, int bn) { return ceil_div(a.M, bm) * ceil_div(a.N, bn); };
+  const int64_t large = tiles(256, 256);
+  if (large > 128 && (large <= 256 || large * 5 >= ceil_div(large, 256) * 256 * 4)) f8_tile<T, E5, EXACT, 256, 256, 2, 4, 2>(a, s);
+  else if (tiles(128, 128) > 256) f8_tile<T, E5, EXACT, 128, 128, 2, 4, 2>(a, s);
+  else if (tiles(128, 128) > 128) f8_tile<T, E5, EXACT, 128, 128, 2, 2, 4>(a, s);
+  else if (tiles(128, 64) > 128) f8_tile<T, E5, EXACT, 128, 64, 2, 2, 4>(a, s);
+  else f8_tile<T, E5, EXACT, 64, 64, 2, 2, 4>(a, s);
 }
 static void f8_run(int a_format, int y_dtype, const F8Args& a, hipStream_t s) {
   if (y_dtype == RN50_BF16 && a_format == RN50_E5M2) f8_product<uint16_t, true, false>(a, s);
