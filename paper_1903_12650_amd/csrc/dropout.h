@@ -42,5 +42,10 @@ __device__ __forceinline__ DropBits drop_bits(const DropArgs& d, uint64_t call, 
 __device__ __forceinline__ bool drop_keeps(const DropArgs& d, const DropBits& r, int j) {  // (j known when compiling)
   return (j & 1 ? r.w[j >> 1] >> 16 : r.w[j >> 1] & 0xffffu) >= d.threshold;
 }
+// The same for any j.
+__device__ __forceinline__ bool drop_keeps_at(const DropArgs& d, const DropBits& r, int j) {
+  const uint32_t lo = j & 2 ? r.w[1] : r.w[0], hi = j & 2 ? r.w[3] : r.w[2], w = j & 4 ? hi : lo;
+  return (j & 1 ? w >> 16 : w & 0xffffu) >= d.threshold;
+}
 
 }  // namespace rn50

@@ -217,6 +217,8 @@ struct F8Args {
   void* y;
   int64_t ldy;
   int M, N, Kp, tiles_m, tiles_n;
+  int part;       // blocks of the sum a workgroup takes (a multiple of 4; all of them: one part)
+  float* partial; // more than one part: float [part][M][N], summed by f8_join_kernel, which has bias, drop and y
   DropArgs drop;  // of y's elements; threshold 0: none
 };
 
@@ -241,12 +243,14 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_f8_kernel(const F8Args a)
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int wm = wave % WM, wn = wave / WM;
   constexpr int GROUP = 4;
-  const int id = xcd_remap(blockIdx.x, gridDim.x);
+  const int tiles = a.tiles_m * a.tiles_n, number = xcd_remap(blockIdx.x, gridDim.x), share = number / tiles, id = number - share * tiles;
   const int per = GROUP * a.tiles_n, g = id / per, r = id - g * per, high = min(GROUP, a.tiles_m - g * GROUP);
   const int m0 = (g * GROUP + r % high) * BM, n0 = r / high * BN;
   const int rows = min(BM, a.M - m0), cols = min(BN, a.N - n0);
-  const rsrc_words rsA = make_rsrc_words(a.a + static_cast<int64_t>(m0) * a.Kp, static_cast<uint32_t>(rows) * a.Kp);
-  const rsrc_words rsB = make_rsrc_words(a.w + static_cast<int64_t>(n0) * a.Kp, static_cast<uint32_t>(cols) * a.Kp);
+  const int first = share * a.part, blocks = min(a.part, (a.Kp >> 7) - first), stages = blocks * (128 / CB);
+  const uint32_t first_byte = static_cast<uint32_t>(first) * 128u;
+  const rsrc_words rsA = make_rsrc_words(a.a + static_cast<int64_t>(m0) * a.Kp + first_byte, static_cast<uint32_t>(rows) * a.Kp - first_byte);
+  const rsrc_words rsB = make_rsrc_words(a.w + static_cast<int64_t>(n0) * a.Kp + first_byte, static_cast<uint32_t>(cols) * a.Kp - first_byte);
   const int slot = tid % PPR, lrow = tid / PPR, piece = slot ^ ((lrow >> 1) & (PPR - 1));
   uint32_t at_a[RA], at_b[RB];
 #pragma unroll
@@ -256,7 +260,6 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_f8_kernel(const F8Args a)
   typedef __attribute__((address_space(3))) unsigned char* lds_byte_ptr;
   const uint32_t base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_byte_ptr)smem));
   const uint32_t dst = __builtin_amdgcn_readfirstlane(base + static_cast<uint32_t>(wave) * 1024u);
-  const int blocks = a.Kp >> 7, stages = a.Kp / CB;
   constexpr int NL = RA + RB;
   auto load_one = [&](int st, int l) __attribute__((always_inline)) {  // (l known when compiling; past the last stage: nothing is read, zeros arrive)
     const uint32_t so = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(st) * CB), to = dst + static_cast<uint32_t>(st & (RING - 1)) * STAGE;
@@ -273,7 +276,7 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_f8_kernel(const F8Args a)
     for (int i = 0; i < (PARTS + WM * WN - 1) / (WM * WN); ++i) {
       const int part = __builtin_amdgcn_readfirstlane((i * WM * WN + wave) % PARTS);
       const bool of_a = part < BM / 64;
-      const uint32_t* from = of_a ? a.as + static_cast<int64_t>(group) * a.M + m0 : a.ws + static_cast<int64_t>(group) * a.N + n0;
+      const uint32_t* from = of_a ? a.as + static_cast<int64_t>((first >> 2) + group) * a.M + m0 : a.ws + static_cast<int64_t>((first >> 2) + group) * a.N + n0;
       const int there = group * 4 < blocks ? of_a ? rows : cols : 0;
       buffer_load4_to_lds(make_rsrc_words(from, static_cast<uint32_t>(there) * 4u), base + RING * STAGE + static_cast<uint32_t>(group & 1) * SCALES + part * 256,
                           static_cast<uint32_t>((of_a ? part : part - BM / 64) * 64 + lane) * 4u);
@@ -356,6 +359,16 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_f8_kernel(const F8Args a)
 #pragma unroll
     for (int l = 0; l < NL; ++l) load_one(st, l);
   wait_loads_then_barrier<(RING - 1) * NL>();
+  if (wm * (BM / WM) >= rows || wn * (BN / WN) >= cols) {  // a wave without rows or columns of its own loads and waits as the others do
+    for (int block = 0; block < blocks; ++block) {
+      wait_loads_then_barrier<(RING - 2) * NL>();
+      load_scales(((block + 1) >> 2) + 1);
+#pragma unroll
+      for (int l = 0; l < NL; ++l) load_one(block + RING, l);
+    }
+    wait_loads_then_barrier<0>();
+    return;
+  }
   read_scales(0);
   read(0, 0);
   for (int block = 0; block < blocks; ++block) {
@@ -388,6 +401,7 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_f8_kernel(const F8Args a)
   float* mine = reinterpret_cast<float*>(smem) + wave * 32 * PITCH;
   constexpr int V = Elem<T>::VEC, LPR = WC / V, RPP = 64 / LPR;  // lanes a row, rows a pass
   const int col = n0 + wn * WC + lane % LPR * V;
+  T* const y = static_cast<T*>(a.y) + (a.partial ? static_cast<int64_t>(share) * a.M * a.N : 0);
   const uint64_t call = a.drop.threshold ? drop_call(a.drop) : 0;
   float b[V];
 #pragma unroll
@@ -410,7 +424,7 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_f8_kernel(const F8Args a)
 #pragma unroll
         for (int j = 0; j < V; ++j) f[j] = mine[row * PITCH + lane % LPR * V + j] + b[j];
         if (a.drop.threshold) drop_columns<V>(a, call, m, col, f);
-        T* to = static_cast<T*>(a.y) + m * a.ldy + col;
+        T* to = y + m * a.ldy + col;
         if (col + V <= a.N) {
           Vec16 o;
           Elem<T>::pack(f, o);
@@ -427,42 +441,266 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_f8_kernel(const F8Args a)
   }
 }
 
+// Few rows (M <= 16 * MB): the weights go by once, bound by memory; a workgroup owns 16 columns, its waves a part of K each.  A wave's lane has column
+// lane % 16 and 32 numbers at 32 * (lane / 16) of a block of 128, straight from memory, U blocks' loads in flight; as bfloat16, times their
+// power of two, they meet the rows' (the second operand) in v_mfma_f32_16x16x32_bf16.  The waves' sums are added through LDS, in order.
+// X: the rows are float or bfloat16 and quantized here, block by block as they are needed (a block's 128 numbers are four lanes'): no second launch.
+constexpr int kFewThreads = 512, kFewWaves = kFewThreads / 64;
+struct F8FewArgs {
+  F8Args p;
+  const void* x;
+  int64_t ldx;
+  int K;
+};
+__device__ __forceinline__ uint32_t scale_byte(const uint32_t* scales, int rows, int row, int block) {
+  return reinterpret_cast<const uint8_t*>(scales)[(static_cast<int64_t>(block >> 2) * rows + row) * 4 + (block & 3)];
+}
+template <typename T, bool E5, int MB, typename X>
+__global__ __launch_bounds__(kFewThreads) void matmul_f8_few_kernel(const F8FewArgs a) {
+  constexpr bool FUSED = !std::is_void<X>::value;
+  constexpr int U = FUSED ? 2 : 4;
+  __shared__ float red[kFewWaves][MB][256];
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, sub = lane >> 4;
+  const int n0 = blockIdx.x * 16, M = a.p.M, N = a.p.N, Kp = a.p.Kp;
+  const int blocks = Kp >> 7, from = blocks * wave / kFewWaves, to = blocks * (wave + 1) / kFewWaves;
+  const int col = min(n0 + (lane & 15), N - 1);
+  const uint8_t* wp = a.p.w + static_cast<int64_t>(col) * Kp + 32 * sub;
+  i32x4 fw[U][2];
+  uint32_t sw[U];
+  auto load_w = [&](int u, int b) __attribute__((always_inline)) {
+    fw[u][0] = *reinterpret_cast<const i32x4*>(wp + static_cast<int64_t>(b) * 128);
+    fw[u][1] = *reinterpret_cast<const i32x4*>(wp + static_cast<int64_t>(b) * 128 + 16);
+    sw[u] = scale_byte(a.p.ws, N, col, b);
+  };
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+    if (from + u < to) load_w(u, from + u);
+  int row[MB];
+#pragma unroll
+  for (int b = 0; b < MB; ++b) row[b] = min(b * 16 + (lane & 15), M - 1);
+  f32x4 acc[MB];
+#pragma unroll
+  for (int b = 0; b < MB; ++b) acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int s = from; s < to; s += U) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = s + u;
+      if (k >= to) break;
+      bf16x8 w[4];
+      f8_to_bf16<false>(fw[u][0], scale_of(sw[u]), w);
+      f8_to_bf16<false>(fw[u][1], scale_of(sw[u]), w + 2);
+      if (k + U < to) load_w(u, k + U);
+#pragma unroll
+      for (int b = 0; b < MB; ++b) {
+        i32x4 q[2];
+        uint32_t byte;
+        if constexpr (FUSED) {
+          constexpr int V = Elem<X>::VEC;
+          float f[32];
+          const int at = k * 128 + 32 * sub;
+          const X* x = static_cast<const X*>(a.x) + row[b] * a.ldx + at;
+          if (at + 32 <= a.K) {
+#pragma unroll
+            for (int j = 0; j < 32; j += V) Elem<X>::unpack(load16_any(x + j), f + j);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) f[j] = at + j < a.K ? Elem<X>::load(x + j) : 0.f;
+          }
+          uint32_t top = 0;
+#pragma unroll
+          for (int j = 0; j < 32; ++j) top = max(top, magnitude(f[j]));
+          top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 16, 64)));
+          top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 32, 64)));
+          float inv;
+          bool finite;
+          byte = f8_scale<E5>(top, &inv, &finite);
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            q[j >> 2][j & 3] = static_cast<int>(f8_four<E5>(f[4 * j] * inv, f[4 * j + 1] * inv, f[4 * j + 2] * inv, f[4 * j + 3] * inv, finite));
+        } else {
+          const uint8_t* x = a.p.a + static_cast<int64_t>(row[b]) * Kp + static_cast<int64_t>(k) * 128 + 32 * sub;
+          q[0] = *reinterpret_cast<const i32x4*>(x);
+          q[1] = *reinterpret_cast<const i32x4*>(x + 16);
+          byte = scale_byte(a.p.as, M, row[b], k);
+        }
+        bf16x8 v[4];
+        f8_to_bf16<E5>(q[0], scale_of(byte), v);
+        f8_to_bf16<E5>(q[1], scale_of(byte), v + 2);
+#pragma unroll
+        for (int h = 0; h < 4; ++h) acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[h], v[h], acc[b], 0, 0, 0);
+      }
+    }
+  }
+  // column 4 * (lane / 16) + i of the 16, row lane % 16
+#pragma unroll
+  for (int b = 0; b < MB; ++b) *reinterpret_cast<f32x4*>(&red[wave][b][(lane & 15) * 16 + 4 * sub]) = acc[b];
+  __syncthreads();
+  const uint64_t call = a.p.drop.threshold ? drop_call(a.p.drop) : 0;
+  for (int e = tid; e < MB * 256; e += kFewThreads) {
+    const int b = e >> 8, m = b * 16 + ((e >> 4) & 15), n = n0 + (e & 15);
+    if (m < M && n < N) {
+      float y = a.p.bias ? a.p.bias[n] : 0.f, sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < kFewWaves; ++w) sum += red[w][b][e & 255];
+      y += sum;
+      if (a.p.drop.threshold) {
+        const DropBits bits = drop_bits(a.p.drop, call, static_cast<uint64_t>(m) * static_cast<uint32_t>((N + 7) >> 3) + static_cast<uint32_t>(n >> 3));
+        y = drop_keeps_at(a.p.drop, bits, n & 7) ? y * a.p.drop.factor : 0.f;
+      }
+      Elem<T>::store(static_cast<T*>(a.p.y) + m * a.p.ldy + n, y);
+    }
+  }
+}
+
+// The parts of sums that were split, in order, with what the products' output stage has.
+template <typename T>
+__global__ __launch_bounds__(256) void f8_join_kernel(const F8Args a, int parts) {
+  constexpr int V = Elem<T>::VEC;
+  const uint64_t call = a.drop.threshold ? drop_call(a.drop) : 0;
+  const int per_row = (a.N + V - 1) / V;
+  const int64_t items = static_cast<int64_t>(a.M) * per_row, plane = static_cast<int64_t>(a.M) * a.N;
+  for (int64_t e = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; e < items; e += static_cast<int64_t>(gridDim.x) * 256) {
+    const int m = static_cast<int>(e / per_row), n = static_cast<int>(e - static_cast<int64_t>(m) * per_row) * V;
+    const float* p = a.partial + static_cast<int64_t>(m) * a.N + n;
+    float f[V];
+    T* to = static_cast<T*>(a.y) + m * a.ldy + n;
+    if (n + V <= a.N) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) f[j] = 0.f;
+#pragma unroll 4
+      for (int s = 0; s < parts; ++s) {
+        float g[V];
+#pragma unroll
+        for (int j = 0; j < V; j += 4) Elem<float>::unpack(load16_any(p + s * plane + j), g + j);
+#pragma unroll
+        for (int j = 0; j < V; ++j) f[j] += g[j];
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        f[j] = 0.f;
+        for (int s = 0; s < parts && n + j < a.N; ++s) f[j] += p[s * plane + j];
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j) f[j] += a.bias && n + j < a.N ? a.bias[n + j] : 0.f;
+    if (a.drop.threshold) drop_columns<V>(a, call, m, n, f);
+    if (n + V <= a.N) {
+      Vec16 o;
+      Elem<T>::pack(f, o);
+      store16_any(to, o);
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (n + j < a.N) Elem<T>::store(to + j, f[j]);
+    }
+  }
+}
+
 // ------------------------------------------------------------------- launches
 template <typename T, bool E5, bool EXACT, int BM, int BN, int WM, int WN, int RING>
-static void f8_tile(F8Args a, hipStream_t s) {
+static void f8_tile(F8Args a, int parts, hipStream_t s) {
   constexpr int lds = RING * (BM + BN) * 128 + 2 * (BM + BN) * 4;
   a.tiles_m = static_cast<int>(ceil_div(a.M, BM));
   a.tiles_n = static_cast<int>(ceil_div(a.N, BN));
   const auto kernel = matmul_f8_kernel<T, E5, EXACT, BM, BN, WM, WN, RING>;
   allow_big_lds(kernel, lds);
-  RN50_LAUNCH("matmul_f8", kernel, dim3(static_cast<unsigned>(a.tiles_m) * a.tiles_n), dim3(64 * WM * WN), lds, s, a);
+  RN50_LAUNCH("matmul_f8", kernel, dim3(static_cast<unsigned>(a.tiles_m) * a.tiles_n * parts), dim3(64 * WM * WN), lds, s, a);
+}
+// How a sum of K numbers is split over workgroups: `count` parts of `part` blocks each (the last may have fewer).
+struct F8Parts {
+  int count, part;
+};
+constexpr int kFewRows = 64;
+static F8Parts f8_parts(int M, int N, int K, bool exact) {
+  const int blocks = static_cast<int>(ceil_div(K, 128));
+  const int64_t tiles = ceil_div(M, 128) * ceil_div(N, 128);
+  int64_t n = 1;
+  if (M > kFewRows) {
+    if (tiles <= 128 && blocks >= 48) n = std::min<int64_t>(256 / tiles, blocks / 8);
+    if (exact) n = std::max(n, std::min<int64_t>(16, ceil_div(blocks, 128)));
+    if (tiles * n > (1 << 20)) n = 1;
+  }
+  const int part = static_cast<int>(align_up(static_cast<size_t>(ceil_div(blocks, n)), 4));
+  return F8Parts{static_cast<int>(ceil_div(blocks, part)), part};
+}
+static size_t f8_partial_bytes(int M, int N, int K) {  // (with exact sums there are as many parts or more)
+  const F8Parts p = f8_parts(M, N, K, true);
+  return p.count > 1 ? align_up(static_cast<size_t>(p.count) * M * N * 4, 256) : 0;
 }
 template <typename T, bool E5, bool EXACT>
-static void f8_product(const F8Args& a, hipStream_t s) {
+static void f8_tiles(const F8Args& a, int parts, hipStream_t s) {
 #ifdef RN50_TUNING  // tuning builds only: RN50_F8_TILE=tile
   if (const char* e = getenv("RN50_F8_TILE")) {
     switch (atoi(e)) {
-      case 256: return f8_tile<T, E5, EXACT, 256, 256, 2, 4, 2>(a, s);
-      case 1288: return f8_tile<T, E5, EXACT, 128, 128, 2, 4, 2>(a, s);
-      case 1284: return f8_tile<T, E5, EXACT, 128, 128, 2, 2, 4>(a, s);
-      case 128644: return f8_tile<T, E5, EXACT, 128, 64, 2, 2, 4>(a, s);
-      case 644: return f8_tile<T, E5, EXACT, 64, 64, 2, 2, 4>(a, s);
+      case 256: return f8_tile<T, E5, EXACT, 256, 256, 2, 4, 2>(a, parts, s);
+      case 1288: return f8_tile<T, E5, EXACT, 128, 128, 2, 4, 2>(a, parts, s);
+      case 1284: return f8_tile<T, E5, EXACT, 128, 128, 2, 2, 4>(a, parts, s);
+      case 128644: return f8_tile<T, E5, EXACT, 128, 64, 2, 2, 4>(a, parts, s);
+      case 644: return f8_tile<T, E5, EXACT, 64, 64, 2, 2, 4>(a, parts, s);
     }
   }
 #endif
-  auto tiles = [&](int bm, int bn) { return ceil_div(a.M, bm) * ceil_div(a.N, bn); };
+  auto tiles = [&](int bm, int bn) { return ceil_div(a.M, bm) * ceil_div(a.N, bn) * parts; };
   const int64_t large = tiles(256, 256);
-  if (large > 128 && (large <= 256 || large * 5 >= ceil_div(large, 256) * 256 * 4)) f8_tile<T, E5, EXACT, 256, 256, 2, 4, 2>(a, s);
-  else if (tiles(128, 128) > 256) f8_tile<T, E5, EXACT, 128, 128, 2, 4, 2>(a, s);
-  else if (tiles(128, 128) > 128) f8_tile<T, E5, EXACT, 128, 128, 2, 2, 4>(a, s);
-  else if (tiles(128, 64) > 128) f8_tile<T, E5, EXACT, 128, 64, 2, 2, 4>(a, s);
-  else f8_tile<T, E5, EXACT, 64, 64, 2, 2, 4>(a, s);
+  if (large > 128 && (large <= 256 || large * 5 >= ceil_div(large, 256) * 256 * 4)) f8_tile<T, E5, EXACT, 256, 256, 2, 4, 2>(a, parts, s);
+  else if (tiles(128, 128) > 256) f8_tile<T, E5, EXACT, 128, 128, 2, 4, 2>(a, parts, s);
+  else if (tiles(128, 128) > 128) f8_tile<T, E5, EXACT, 128, 128, 2, 2, 4>(a, parts, s);
+  else if (tiles(128, 64) > 128) f8_tile<T, E5, EXACT, 128, 64, 2, 2, 4>(a, parts, s);
+  else f8_tile<T, E5, EXACT, 64, 64, 2, 2, 4>(a, parts, s);
 }
-static void f8_run(int a_format, int y_dtype, const F8Args& a, hipStream_t s) {
-  if (y_dtype == RN50_BF16 && a_format == RN50_E5M2) f8_product<uint16_t, true, false>(a, s);
-  else if (y_dtype == RN50_BF16) f8_product<uint16_t, false, false>(a, s);
-  else if (a_format == RN50_E5M2) f8_product<float, true, true>(a, s);
-  else f8_product<float, false, true>(a, s);
+template <typename T, bool E5, int MB, typename X>
+static void f8_few(const F8FewArgs& a, hipStream_t s) {
+  RN50_LAUNCH("matmul_f8", (matmul_f8_few_kernel<T, E5, MB, X>), dim3(static_cast<unsigned>(ceil_div(a.p.N, 16))), dim3(kFewThreads), 0, s, a);
+}
+template <typename T, bool E5, bool EXACT>
+static void f8_product(F8Args a, int K, void* partial, hipStream_t s) {
+#ifdef RN50_TUNING
+  const bool few = a.M <= kFewRows && !getenv("RN50_F8_TILE");
+#else
+  const bool few = a.M <= kFewRows;
+#endif
+  if (few) {
+    const F8FewArgs f{a, nullptr, 0, 0};
+    if (a.M <= 16) f8_few<T, E5, 1, void>(f, s);
+    else if (a.M <= 32) f8_few<T, E5, 2, void>(f, s);
+    else if (a.M <= 48) f8_few<T, E5, 3, void>(f, s);
+    else f8_few<T, E5, 4, void>(f, s);
+    return;
+  }
+  F8Parts parts = f8_parts(a.M, a.N, K, EXACT);
+#ifdef RN50_TUNING
+  if (getenv("RN50_F8_TILE")) parts = F8Parts{1, a.Kp >> 7};
+#endif
+  if (parts.count == 1) {
+    a.part = a.Kp >> 7;
+    return f8_tiles<T, E5, EXACT>(a, 1, s);
+  }
+  F8Args p = a;  // the parts' sums, then all of them with the output stage's work
+  p.part = parts.part;
+  p.partial = static_cast<float*>(partial);
+  p.y = partial;
+  p.ldy = a.N;
+  p.bias = nullptr;
+  p.drop = drop_args(nullptr);
+  f8_tiles<float, E5, EXACT>(p, parts.count, s);
+  a.partial = p.partial;
+  const int64_t items = static_cast<int64_t>(a.M) * ceil_div(a.N, Elem<T>::VEC);
+  RN50_LAUNCH("matmul_f8", f8_join_kernel<T>, dim3(static_cast<unsigned>(std::min<int64_t>(ceil_div(items, 256), 1 << 16))), dim3(256), 0, s, a, parts.count);
+}
+static void f8_run(int a_format, int y_dtype, const F8Args& a, int K, void* partial, hipStream_t s) {
+  if (y_dtype == RN50_BF16 && a_format == RN50_E5M2) f8_product<uint16_t, true, false>(a, K, partial, s);
+  else if (y_dtype == RN50_BF16) f8_product<uint16_t, false, false>(a, K, partial, s);
+  else if (a_format == RN50_E5M2) f8_product<float, true, true>(a, K, partial, s);
+  else f8_product<float, false, true>(a, K, partial, s);
+}
+
+// Whether fc_f8_fwd takes its rows as they are.
+static bool f8_fused(int M, int K) {
+#ifdef RN50_TUNING  // tuning builds only: RN50_F8_FUSED=0
+  if (const char* e = getenv("RN50_F8_FUSED")) return atoi(e) && M <= 16;
+#endif
+  return M <= 16;
 }
 
 template <typename T, bool E5, bool DROP>
@@ -516,6 +754,11 @@ static int check_tiles(const char* who, int M, int N, int rows, int cols) {
   RN50_REQUIRE(ceil_div(M, rows) * ceil_div(N, cols) <= (1 << 22), RN50_ERR_UNSUPPORTED, "%s: %d by %d beyond the launch grid", who, M, N);
   return RN50_OK;
 }
+static int check_product_size(const char* who, int M, int N) {
+  if (int rc = check_tiles(who, M, N, 64, 64)) return rc;
+  RN50_REQUIRE(N <= (1 << 26), RN50_ERR_UNSUPPORTED, "%s: %d columns beyond the launch grid", who, N);
+  return RN50_OK;
+}
 static int check_workspace(const char* who, const void* workspace, size_t bytes, size_t need) {
   if (need == 0) return RN50_OK;
   RN50_REQUIRE(workspace && bytes >= need, RN50_ERR_WORKSPACE, "%s: workspace %zu < %zu bytes", who, bytes, need);
@@ -537,7 +780,7 @@ struct Parts {
 static const uint32_t* words(const uint8_t* scale) { return reinterpret_cast<const uint32_t*>(scale); }
 static F8Args product_args(int M, int N, int K, const uint8_t* a, const uint8_t* as, const uint8_t* w, const uint8_t* ws, const float* bias, void* y,
                            int64_t ldy, const rn50_dropout* drop) {
-  return F8Args{a, w, words(as), words(ws), bias, y, ldy, M, N, static_cast<int>(quant_f8_row_bytes(K)), 0, 0, drop_args(drop)};
+  return F8Args{a, w, words(as), words(ws), bias, y, ldy, M, N, static_cast<int>(quant_f8_row_bytes(K)), 0, 0, 0, nullptr, drop_args(drop)};
 }
 
 }  // namespace rn50
@@ -570,7 +813,9 @@ extern "C" int quant_blocks_f8(int M, int K, int dtype, const void* x, int64_t l
   return launch_status(who);
 }
 
-extern "C" size_t matmul_f8_workspace_bytes(int M, int N, int K) { return 0; }
+extern "C" size_t matmul_f8_workspace_bytes(int M, int N, int K) {
+  return M < 1 || N < 1 || quant_f8_row_bytes(K) == 0 ? 0 : f8_partial_bytes(M, N, K);
+}
 
 extern "C" int matmul_f8(int M, int N, int K, int a_format, const uint8_t* a, const uint8_t* a_scale, const uint8_t* w, const uint8_t* w_scale,
                          const float* bias, int y_dtype, void* y, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream) {
@@ -583,9 +828,9 @@ extern "C" int matmul_f8(int M, int N, int K, int a_format, const uint8_t* a, co
   if (int rc = check_quantized(who, w, w_scale)) return rc;
   if (int rc = check_matrix(who, M, N, y_dtype, y, ldy)) return rc;
   RN50_REQUIRE(aligned_to(bias, 4), RN50_ERR_ALIGN, "%s: pointer not aligned to an element", who);
-  if (int rc = check_tiles(who, M, N, 64, 64)) return rc;
+  if (int rc = check_product_size(who, M, N)) return rc;
   if (int rc = check_workspace(who, workspace, workspace_bytes, matmul_f8_workspace_bytes(M, N, K))) return rc;
-  f8_run(a_format, y_dtype, product_args(M, N, K, a, a_scale, w, w_scale, bias, y, ldy, nullptr), static_cast<hipStream_t>(stream));
+  f8_run(a_format, y_dtype, product_args(M, N, K, a, a_scale, w, w_scale, bias, y, ldy, nullptr), K, workspace, static_cast<hipStream_t>(stream));
   return launch_status(who);
 }
 
@@ -613,15 +858,23 @@ extern "C" int fc_f8_fwd(int M, int N, int K, int x_dtype, const void* x, int64_
     if (int rc = check_quantized(who, xt, xt_scale)) return rc;
     if (int rc = check_sum(who, M)) return rc;
   }
-  if (int rc = check_tiles(who, M, N, 64, 64)) return rc;
+  if (int rc = check_product_size(who, M, N)) return rc;
   if (int rc = check_tiles(who, M, K, xt ? 128 : 32, 128)) return rc;
   if (int rc = check_workspace(who, workspace, workspace_bytes, fc_f8_fwd_workspace_bytes(M, N, K))) return rc;
   hipStream_t s = static_cast<hipStream_t>(stream);
   Parts parts{static_cast<uint8_t*>(workspace)};
   uint8_t* q = parts.take(static_cast<size_t>(M) * quant_f8_row_bytes(K));
   uint8_t* qs = parts.take(quant_f8_scale_bytes(M, K));
+  if (f8_fused(M, K) && !xt && !dropout) {
+    const F8FewArgs a{product_args(M, N, K, nullptr, nullptr, w, w_scale, bias, y, ldy, nullptr), x, ldx, K};
+    if (x_dtype == RN50_BF16 && y_dtype == RN50_BF16) f8_few<uint16_t, false, 1, uint16_t>(a, s);
+    else if (x_dtype == RN50_BF16) f8_few<float, false, 1, uint16_t>(a, s);
+    else if (y_dtype == RN50_BF16) f8_few<uint16_t, false, 1, float>(a, s);
+    else f8_few<float, false, 1, float>(a, s);
+    return launch_status(who);
+  }
   quant_run(M, K, x_dtype, x, ldx, dropout, RN50_E4M3, q, qs, xt, xt_scale, nullptr, s);
-  f8_run(RN50_E4M3, y_dtype, product_args(M, N, K, q, qs, w, w_scale, bias, y, ldy, nullptr), s);
+  f8_run(RN50_E4M3, y_dtype, product_args(M, N, K, q, qs, w, w_scale, bias, y, ldy, nullptr), K, parts.take(0), s);
   return launch_status(who);
 }
 
@@ -633,7 +886,7 @@ extern "C" size_t fc_f8_bwd_workspace_bytes(int M, int N, int K) {
   parts.take(static_cast<size_t>(N) * quant_f8_row_bytes(M));
   parts.take(quant_f8_scale_bytes(N, M));
   parts.take(static_cast<size_t>(ceil_div(M, 128)) * N * 4);
-  return parts.used;
+  return parts.used + std::max(f8_partial_bytes(M, K, N), f8_partial_bytes(N, K, M));
 }
 
 extern "C" int fc_f8_bwd(int M, int N, int K, int dy_dtype, const void* dy, int64_t ld_dy, int format, const uint8_t* wt, const uint8_t* wt_scale,
@@ -656,8 +909,8 @@ extern "C" int fc_f8_bwd(int M, int N, int K, int dy_dtype, const void* dy, int6
     if (int rc = check_quantized(who, xt, xt_scale)) return rc;
   RN50_REQUIRE(aligned_to(dW, 4) && aligned_to(db, 4), RN50_ERR_ALIGN, "%s: pointer not aligned to an element", who);
   if (int rc = check_tiles(who, M, N, 32, 128)) return rc;
-  if (int rc = check_tiles(who, M, K, 64, 64)) return rc;
-  if (int rc = check_tiles(who, N, K, 64, 64)) return rc;
+  if (int rc = check_product_size(who, M, K)) return rc;
+  if (int rc = check_product_size(who, N, K)) return rc;
   if (int rc = check_workspace(who, workspace, workspace_bytes, fc_f8_bwd_workspace_bytes(M, N, K))) return rc;
   hipStream_t s = static_cast<hipStream_t>(stream);
   Parts parts{static_cast<uint8_t*>(workspace)};
@@ -668,8 +921,9 @@ extern "C" int fc_f8_bwd(int M, int N, int K, int dy_dtype, const void* dy, int6
   const int tiles = static_cast<int>(ceil_div(M, 128));
   float* sums = parts.take<float>(static_cast<size_t>(tiles) * N * 4);
   quant_run(M, N, dy_dtype, dy, ld_dy, nullptr, format, dx ? q : nullptr, qs, dW ? qt : nullptr, qts, db ? sums : nullptr, s);
-  if (dx) f8_run(format, dx_dtype, product_args(M, K, N, q, qs, wt, wt_scale, nullptr, dx, ld_dx, dropout), s);
-  if (dW) f8_run(format, RN50_F32, product_args(N, K, M, qt, qts, xt, xt_scale, nullptr, dW, K, nullptr), s);
+  void* partial = parts.take(0);
+  if (dx) f8_run(format, dx_dtype, product_args(M, K, N, q, qs, wt, wt_scale, nullptr, dx, ld_dx, dropout), N, partial, s);
+  if (dW) f8_run(format, RN50_F32, product_args(N, K, M, qt, qts, xt, xt_scale, nullptr, dW, K, nullptr), M, partial, s);
   if (db) RN50_LAUNCH("quant_blocks_f8", f8_column_sums_kernel, dim3(static_cast<unsigned>(ceil_div(N, 256))), dim3(256), 0, s, sums, tiles, N, db);
   return launch_status(who);
 }

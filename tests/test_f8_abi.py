@@ -55,6 +55,7 @@ def test_refusals_come_before_anything_touches_the_device():
     for bad in ({"M": 0}, {"N": 0}, {"K": 0}, {"fmt": 0}, {"a": None}, {"s": None}, {"w": None}, {"ws": None}, {"yt": 2}, {"y": None}, {"ldy": 1}):
         assert product(**bad) == -1, bad
     assert product(K=top) == -2 and product(M=1 << 20, N=1 << 20, ldy=1 << 20) == -2
+    assert product(N=(1 << 26) + 1, M=1, ldy=1 << 27) == -2
     assert product(a=odd) == -4 and product(ws=odd) == -4 and product(y=ctypes.c_void_p(6)) == -4 and product(b=ctypes.c_void_p(6)) == -4
 
     def forward(M=2, N=2, K=8, x=one, d=None, w=one, ws=one, b=None, y=one, xt=None, xs=None, work=one, n=big):
