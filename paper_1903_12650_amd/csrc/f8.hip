@@ -183,14 +183,30 @@ __global__ __launch_bounds__(256) void quant_blocks_kernel(const QuantArgs a) {
   }
 }
 
-// db[n] = the sum of the row tiles' sums, in their order.
-__global__ __launch_bounds__(256) void f8_column_sums_kernel(const float* __restrict__ sums, int tiles, int N, float* __restrict__ db) {
-  const int n = blockIdx.x * 256 + threadIdx.x;
-  if (n >= N) return;
-  double s = 0.0;
-  for (int t = 0; t < tiles; ++t) s += sums[static_cast<int64_t>(t) * N + n];
-  db[n] = static_cast<float>(s);
+// db[n] = the sum of the row tiles' sums: four threads a column, each every fourth tile in order, then the four; the same order whichever kernel
+// has it along (a launch of its own for these few bytes costs 4 us, and with one thread a column 90 us at 392 tiles of 256 columns).
+struct SumArgs {
+  const float* sums;
+  int tiles, N;
+  float* db;
+};
+constexpr int kSumColumns = 64;
+__device__ __forceinline__ void f8_column_sums(const SumArgs& a, int group) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  double* red = reinterpret_cast<double*>(smem);
+  const int tid = threadIdx.x, part = tid >> 6, n = group * kSumColumns + (tid & 63);
+  if (tid < 256) {
+    double s = 0.0;
+    if (n < a.N) {
+#pragma unroll 8
+      for (int t = part; t < a.tiles; t += 4) s += a.sums[static_cast<int64_t>(t) * a.N + n];
+    }
+    red[tid] = s;
+  }
+  __syncthreads();
+  if (tid < 64 && n < a.N) a.db[n] = static_cast<float>((red[tid] + red[64 + tid]) + (red[128 + tid] + red[192 + tid]));
 }
+__global__ __launch_bounds__(256) void f8_column_sums_kernel(const SumArgs a) { f8_column_sums(a, blockIdx.x); }
 
 // ------------------------------------------------------------------ products
 // 16 numbers of a row as bfloat16, times the row's power of two: exact.
@@ -220,6 +236,8 @@ struct F8Args {
   int part;       // blocks of the sum a workgroup takes (a multiple of 4; all of them: one part)
   float* partial; // more than one part: float [part][M][N], summed by f8_join_kernel, which has bias, drop and y
   DropArgs drop;  // of y's elements; threshold 0: none
+  int groups;     // workgroups of the product; those behind them add up `sum`
+  SumArgs sum;
 };
 
 // V consecutive columns of row m, from column n (a multiple of V; V divides 8).
@@ -235,7 +253,7 @@ __device__ __forceinline__ void drop_columns(const F8Args& a, uint64_t call, int
 }
 
 template <typename T, bool E5, bool EXACT, int BM, int BN, int WM, int WN, int RING>
-__global__ __launch_bounds__(64 * WM * WN) void matmul_f8_kernel(const F8Args a) {
+__device__ __forceinline__ void f8_tile_product(const F8Args& a, int group) {
   constexpr int CB = 128, PPR = CB / 16, NT = 64 * WM * WN, RPL = NT / PPR, RA = BM / RPL, RB = BN / RPL, TM = BM / WM / 32, TN = BN / WN / 32;
   constexpr int STAGE = (BM + BN) * CB, SCALES = (BM + BN) * 4;
   static_assert(RA * RPL == BM && RB * RPL == BN && TM >= 1 && TN >= 1 && (RING & (RING - 1)) == 0, "whole passes, whole blocks");
@@ -243,7 +261,7 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_f8_kernel(const F8Args a)
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int wm = wave % WM, wn = wave / WM;
   constexpr int GROUP = 4;
-  const int tiles = a.tiles_m * a.tiles_n, number = xcd_remap(blockIdx.x, gridDim.x), share = number / tiles, id = number - share * tiles;
+  const int tiles = a.tiles_m * a.tiles_n, number = xcd_remap(group, a.groups), share = number / tiles, id = number - share * tiles;
   const int per = GROUP * a.tiles_n, g = id / per, r = id - g * per, high = min(GROUP, a.tiles_m - g * GROUP);
   const int m0 = (g * GROUP + r % high) * BM, n0 = r / high * BN;
   const int rows = min(BM, a.M - m0), cols = min(BN, a.N - n0);
@@ -271,14 +289,14 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_f8_kernel(const F8Args a)
   // The scales of a group of four blocks are a dword a row, brought into LDS like the operands: 64 rows of the tile or of its columns a wave,
   // a group ahead, again with every block (branches here would let the compiler move a step's products behind the next barrier).
   constexpr int PARTS = (BM + BN) / 64;
-  auto load_scales = [&](int group) __attribute__((always_inline)) {
+  auto load_scales = [&](int four) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < (PARTS + WM * WN - 1) / (WM * WN); ++i) {
       const int part = __builtin_amdgcn_readfirstlane((i * WM * WN + wave) % PARTS);
       const bool of_a = part < BM / 64;
-      const uint32_t* from = of_a ? a.as + static_cast<int64_t>((first >> 2) + group) * a.M + m0 : a.ws + static_cast<int64_t>((first >> 2) + group) * a.N + n0;
-      const int there = group * 4 < blocks ? of_a ? rows : cols : 0;
-      buffer_load4_to_lds(make_rsrc_words(from, static_cast<uint32_t>(there) * 4u), base + RING * STAGE + static_cast<uint32_t>(group & 1) * SCALES + part * 256,
+      const uint32_t* from = of_a ? a.as + static_cast<int64_t>((first >> 2) + four) * a.M + m0 : a.ws + static_cast<int64_t>((first >> 2) + four) * a.N + n0;
+      const int there = four * 4 < blocks ? of_a ? rows : cols : 0;
+      buffer_load4_to_lds(make_rsrc_words(from, static_cast<uint32_t>(there) * 4u), base + RING * STAGE + static_cast<uint32_t>(four & 1) * SCALES + part * 256,
                           static_cast<uint32_t>((of_a ? part : part - BM / 64) * 64 + lane) * 4u);
     }
   };
@@ -294,6 +312,7 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_f8_kernel(const F8Args a)
   for (int u = 0; u < CB / 32; ++u) frag[u] = (lane & 31) * CB + (((2 * u + (lane >> 5)) ^ ((lane >> 1) & (PPR - 1))) << 4);
   // Fragments a step ahead (FAST: a stage, EXACT: half of one), across stages as well: the last step of a stage is multiplied behind the barrier that frees
   // the stage's buffer, while the next stage's fragments and the loads of the one RING stages on are on their way.
+  constexpr bool PIPED = EXACT && TM * TN <= 4;
   constexpr int READS = EXACT ? 1 : 2;
   i32x4 fa[2][READS][TM], fb[2][READS][TN];
   uint32_t sa[TM], sb[TN], next_a[TM], next_b[TN];
@@ -371,6 +390,59 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_f8_kernel(const F8Args a)
   }
   read_scales(0);
   read(0, 0);
+  if constexpr (PIPED) {
+    // Step t: its products, between them the conversion of step t + 1's fragments and the reads of step t + 2's.
+    bf16x8 xa[2][TM][2], xb[2][TN][2];
+    float fa_scale[TM], fb_scale[TN];
+    auto take_scales = [&](int block) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i) fa_scale[i] = scale_of(next_a[i] >> ((block & 3) * 8) & 255u);
+#pragma unroll
+      for (int j = 0; j < TN; ++j) fb_scale[j] = scale_of(next_b[j] >> ((block & 3) * 8) & 255u);
+    };
+    auto convert = [&](int set) __attribute__((always_inline)) {
+#pragma unroll
+      for (int j = 0; j < TN; ++j) f8_to_bf16<false>(fb[set][0][j], fb_scale[j], xb[set][j]);
+#pragma unroll
+      for (int i = 0; i < TM; ++i) f8_to_bf16<E5>(fa[set][0][i], fa_scale[i], xa[set][i]);
+    };
+    read(0, 1);
+    take_scales(0);
+    convert(0);
+    for (int block = 0; block < blocks; ++block) {
+#pragma unroll
+      for (int step = 0; step < 4; ++step) {
+        if (step == 2) {  // the next stage is there, and everyone has read this one
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          wait_loads_then_barrier<(RING - 2) * NL>();
+          read_scales(block + 1);
+          load_scales(((block + 1) >> 2) + 1);
+        }
+        if (step == 3) take_scales(block + 1);
+        __builtin_amdgcn_sched_barrier(0);
+        constexpr int SLOTS = 2 * TM * TN;
+#pragma unroll
+        for (int n = 0; n < SLOTS; ++n) {
+          const int i = n % (TM * TN) / TN, j = n % TN, h = n / (TM * TN);
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xb[step & 1][j][h], xa[step & 1][i][h], acc[i][j], 0, 0, 0);
+#pragma unroll
+          for (int r = n * READ / SLOTS; r < (n + 1) * READ / SLOTS; ++r) read_one(step < 2 ? block : block + 1, (step + 2) & 3, r);
+          if (step == 2) {
+#pragma unroll
+            for (int l = n * NL / SLOTS; l < (n + 1) * NL / SLOTS; ++l) load_one(block + RING, l);
+          }
+        }
+        convert((step + 1) & 1);
+#pragma unroll
+        for (int n = 0; n < SLOTS; ++n) {
+          __builtin_amdgcn_sched_group_barrier(8, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(256, (READ + SLOTS - 1) / SLOTS, 0);
+          __builtin_amdgcn_sched_group_barrier(2, 8 * READ / SLOTS, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  } else {
   for (int block = 0; block < blocks; ++block) {
 #pragma unroll
     for (int i = 0; i < TM; ++i) sa[i] = next_a[i] >> ((block & 3) * 8);
@@ -392,6 +464,7 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_f8_kernel(const F8Args a)
       }
       multiply(step & 1, next, (step + 1) % STEPS, done % CB == 0, st + RING);  // (behind the last stage: zeros, not used)
     }
+  }
   }
   // Output: a wave's 32 rows at a time through LDS (its own part of it), whole rows of the wave's columns from there.
   constexpr int WC = BN / WN, PITCH = WC + 4;  // floats (rows 16 bytes further along the banks)
@@ -440,6 +513,11 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_f8_kernel(const F8Args a)
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   }
 }
+template <typename T, bool E5, bool EXACT, int BM, int BN, int WM, int WN, int RING>
+__global__ __launch_bounds__(64 * WM * WN) void matmul_f8_kernel(const F8Args a) {
+  if (static_cast<int>(blockIdx.x) < a.groups) f8_tile_product<T, E5, EXACT, BM, BN, WM, WN, RING>(a, blockIdx.x);
+  else f8_column_sums(a.sum, blockIdx.x - a.groups);
+}
 
 // Few rows (M <= 16 * MB): the weights go by once, bound by memory; a workgroup owns 16 columns, its waves a part of K each.  A wave's lane has column
 // lane % 16 and 32 numbers at 32 * (lane / 16) of a block of 128, straight from memory, U blocks' loads in flight; as bfloat16, times their
@@ -456,12 +534,12 @@ __device__ __forceinline__ uint32_t scale_byte(const uint32_t* scales, int rows,
   return reinterpret_cast<const uint8_t*>(scales)[(static_cast<int64_t>(block >> 2) * rows + row) * 4 + (block & 3)];
 }
 template <typename T, bool E5, int MB, typename X>
-__global__ __launch_bounds__(kFewThreads) void matmul_f8_few_kernel(const F8FewArgs a) {
+__device__ __forceinline__ void f8_few_product(const F8FewArgs& a, int group) {
   constexpr bool FUSED = !std::is_void<X>::value;
   constexpr int U = FUSED ? 2 : 4;
   __shared__ float red[kFewWaves][MB][256];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, sub = lane >> 4;
-  const int n0 = blockIdx.x * 16, M = a.p.M, N = a.p.N, Kp = a.p.Kp;
+  const int n0 = group * 16, M = a.p.M, N = a.p.N, Kp = a.p.Kp;
   const int blocks = Kp >> 7, from = blocks * wave / kFewWaves, to = blocks * (wave + 1) / kFewWaves;
   const int col = min(n0 + (lane & 15), N - 1);
   const uint8_t* wp = a.p.w + static_cast<int64_t>(col) * Kp + 32 * sub;
@@ -551,6 +629,19 @@ __global__ __launch_bounds__(kFewThreads) void matmul_f8_few_kernel(const F8FewA
     }
   }
 }
+template <typename T, bool E5, int MB, typename X>
+__global__ __launch_bounds__(kFewThreads) void matmul_f8_few_kernel(const F8FewArgs a) {
+  f8_few_product<T, E5, MB, X>(a, blockIdx.x);
+}
+// The two products of a backward pass of few rows in one launch: the input's gradient by the first workgroups, the weights' (a sum of one
+// block) by tiles, and the bias's behind them.
+template <typename T, bool E5, int MB>
+__global__ __launch_bounds__(kFewThreads) void f8_few_backward_kernel(const F8FewArgs x, const F8Args w) {
+  const int group = static_cast<int>(blockIdx.x) - x.p.groups;
+  if (group < 0) f8_few_product<T, E5, MB, void>(x, blockIdx.x);
+  else if (group < w.groups) f8_tile_product<float, E5, true, 128, 128, 2, 4, 2>(w, group);
+  else f8_column_sums(w.sum, group - w.groups);
+}
 
 // The parts of sums that were split, in order, with what the products' output stage has.
 template <typename T>
@@ -598,6 +689,10 @@ __global__ __launch_bounds__(256) void f8_join_kernel(const F8Args a, int parts)
 }
 
 // ------------------------------------------------------------------- launches
+static int sum_groups(const SumArgs& a) { return a.db ? static_cast<int>(ceil_div(a.N, kSumColumns)) : 0; }
+static void sum_columns(const SumArgs& a, hipStream_t s) {
+  if (a.db) RN50_LAUNCH("quant_blocks_f8", f8_column_sums_kernel, dim3(static_cast<unsigned>(sum_groups(a))), dim3(256), 256 * sizeof(double), s, a);
+}
 template <typename T, bool E5, bool EXACT, int BM, int BN, int WM, int WN, int RING>
 static void f8_tile(F8Args a, int parts, hipStream_t s) {
   constexpr int lds = RING * (BM + BN) * 128 + 2 * (BM + BN) * 4;
@@ -605,7 +700,8 @@ static void f8_tile(F8Args a, int parts, hipStream_t s) {
   a.tiles_n = static_cast<int>(ceil_div(a.N, BN));
   const auto kernel = matmul_f8_kernel<T, E5, EXACT, BM, BN, WM, WN, RING>;
   allow_big_lds(kernel, lds);
-  RN50_LAUNCH("matmul_f8", kernel, dim3(static_cast<unsigned>(a.tiles_m) * a.tiles_n * parts), dim3(64 * WM * WN), lds, s, a);
+  a.groups = a.tiles_m * a.tiles_n * parts;
+  RN50_LAUNCH("matmul_f8", kernel, dim3(static_cast<unsigned>(a.groups + sum_groups(a.sum))), dim3(64 * WM * WN), lds, s, a);
 }
 // How a sum of K numbers is split over workgroups: `count` parts of `part` blocks each (the last may have fewer).
 struct F8Parts {
@@ -635,6 +731,7 @@ static void f8_tiles(const F8Args& a, int parts, hipStream_t s) {
     switch (atoi(e)) {
       case 256: return f8_tile<T, E5, EXACT, 256, 256, 2, 4, 2>(a, parts, s);
       case 1288: return f8_tile<T, E5, EXACT, 128, 128, 2, 4, 2>(a, parts, s);
+      case 12884: return f8_tile<T, E5, EXACT, 128, 128, 2, 4, 4>(a, parts, s);
       case 1284: return f8_tile<T, E5, EXACT, 128, 128, 2, 2, 4>(a, parts, s);
       case 128644: return f8_tile<T, E5, EXACT, 128, 64, 2, 2, 4>(a, parts, s);
       case 644: return f8_tile<T, E5, EXACT, 64, 64, 2, 2, 4>(a, parts, s);
@@ -666,7 +763,7 @@ static void f8_product(F8Args a, int K, void* partial, hipStream_t s) {
     else if (a.M <= 32) f8_few<T, E5, 2, void>(f, s);
     else if (a.M <= 48) f8_few<T, E5, 3, void>(f, s);
     else f8_few<T, E5, 4, void>(f, s);
-    return;
+    return sum_columns(a.sum, s);
   }
   F8Parts parts = f8_parts(a.M, a.N, K, EXACT);
 #ifdef RN50_TUNING
@@ -695,6 +792,28 @@ static void f8_run(int a_format, int y_dtype, const F8Args& a, int K, void* part
   else f8_product<float, false, true>(a, K, partial, s);
 }
 
+// Both products of a backward pass in one launch: few rows (whose sum into the weights is one block), more outputs than the few rows' kernel would take.
+static bool f8_few_backward_fits(int M, int N) { return M <= kFewRows && N > kFewRows; }
+template <typename T, bool E5>
+static void f8_few_backward(F8Args x, F8Args w, hipStream_t s) {
+  constexpr int lds = 2 * 256 * 128 + 2 * 256 * 4;
+  x.groups = static_cast<int>(ceil_div(x.N, 16));
+  w.tiles_m = static_cast<int>(ceil_div(w.M, 128));
+  w.tiles_n = static_cast<int>(ceil_div(w.N, 128));
+  w.groups = w.tiles_m * w.tiles_n;
+  w.part = w.Kp >> 7;
+  const F8FewArgs f{x, nullptr, 0, 0};
+  const dim3 grid(static_cast<unsigned>(x.groups + w.groups + sum_groups(w.sum)));
+#define FEW_BACKWARD(MB)                                                                                                  \
+  do {                                                                                                                    \
+    allow_big_lds(f8_few_backward_kernel<T, E5, MB>, lds);                                                                \
+    RN50_LAUNCH("matmul_f8", (f8_few_backward_kernel<T, E5, MB>), grid, dim3(kFewThreads), lds, s, f, w);                 \
+  } while (0)
+  if (x.M <= 16) FEW_BACKWARD(1);
+  else if (x.M <= 48) FEW_BACKWARD(3);
+  else FEW_BACKWARD(4);
+#undef FEW_BACKWARD
+}
 // Whether fc_f8_fwd takes its rows as they are.
 static bool f8_fused(int M, int K) {
 #ifdef RN50_TUNING  // tuning builds only: RN50_F8_FUSED=0
@@ -780,7 +899,7 @@ struct Parts {
 static const uint32_t* words(const uint8_t* scale) { return reinterpret_cast<const uint32_t*>(scale); }
 static F8Args product_args(int M, int N, int K, const uint8_t* a, const uint8_t* as, const uint8_t* w, const uint8_t* ws, const float* bias, void* y,
                            int64_t ldy, const rn50_dropout* drop) {
-  return F8Args{a, w, words(as), words(ws), bias, y, ldy, M, N, static_cast<int>(quant_f8_row_bytes(K)), 0, 0, 0, nullptr, drop_args(drop)};
+  return F8Args{a, w, words(as), words(ws), bias, y, ldy, M, N, static_cast<int>(quant_f8_row_bytes(K)), 0, 0, 0, nullptr, drop_args(drop), 0, {}};
 }
 
 }  // namespace rn50
@@ -922,8 +1041,18 @@ extern "C" int fc_f8_bwd(int M, int N, int K, int dy_dtype, const void* dy, int6
   float* sums = parts.take<float>(static_cast<size_t>(tiles) * N * 4);
   quant_run(M, N, dy_dtype, dy, ld_dy, nullptr, format, dx ? q : nullptr, qs, dW ? qt : nullptr, qts, db ? sums : nullptr, s);
   void* partial = parts.take(0);
-  if (dx) f8_run(format, dx_dtype, product_args(M, K, N, q, qs, wt, wt_scale, nullptr, dx, ld_dx, dropout), N, partial, s);
-  if (dW) f8_run(format, RN50_F32, product_args(N, K, M, qt, qts, xt, xt_scale, nullptr, dW, K, nullptr), M, partial, s);
-  if (db) RN50_LAUNCH("quant_blocks_f8", f8_column_sums_kernel, dim3(static_cast<unsigned>(ceil_div(N, 256))), dim3(256), 0, s, sums, tiles, N, db);
+  const SumArgs sum{sums, tiles, N, db};
+  F8Args px = product_args(M, K, N, q, qs, wt, wt_scale, nullptr, dx, ld_dx, dropout), pw = product_args(N, K, M, qt, qts, xt, xt_scale, nullptr, dW, K, nullptr);
+  if (dW) pw.sum = sum;
+  if (dx && dW && f8_few_backward_fits(M, N)) {
+    if (dx_dtype == RN50_BF16 && format == RN50_E5M2) f8_few_backward<uint16_t, true>(px, pw, s);
+    else if (dx_dtype == RN50_BF16) f8_few_backward<uint16_t, false>(px, pw, s);
+    else if (format == RN50_E5M2) f8_few_backward<float, true>(px, pw, s);
+    else f8_few_backward<float, false>(px, pw, s);
+    return launch_status(who);
+  }
+  if (dx) f8_run(format, dx_dtype, px, N, partial, s);
+  if (dW) f8_run(format, RN50_F32, pw, M, partial, s);
+  else sum_columns(sum, s);
   return launch_status(who);
 }
