@@ -12,6 +12,7 @@ namespace rn50 {
 
 constexpr int kF8MaxK = 1 << 22;        // 256 rows of it stay inside a buffer descriptor's 32 bits
 constexpr uint32_t kF8Floor = 27u << 23;  // the bits of 2^-100: blocks below are quantized as if this were their largest magnitude
+constexpr int64_t kPastBytes = 32 << 20;  // outputs that the L2s would not hold for the next kernel are stored past them
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef short s16x2 __attribute__((ext_vector_type(2)));
@@ -57,11 +58,11 @@ struct QuantArgs {
 // A tile of 16 * R rows by 128 columns in registers: thread t holds rows R * (t / 16) .. + R - 1 of the eight columns at 8 * (t % 16), the
 // elements of one Philox call a row.  A block along a row is 16 lanes' (DPP), a block along a column the workgroup's (LDS, R = 8).
 template <typename T, bool E5, int R, bool COLS, bool DROP>
-__global__ __launch_bounds__(256) void quant_blocks_kernel(const QuantArgs a) {
+__device__ __forceinline__ void quant_tile(const QuantArgs& a, int tile) {
   constexpr int V = Elem<T>::VEC;
   static_assert(!COLS || R == 8, "a block of 128 rows");
   const int tid = threadIdx.x, cg = tid & 15, rg = tid >> 4;
-  const int tm = blockIdx.x / a.tiles_k, tk = blockIdx.x - tm * a.tiles_k;
+  const int tm = tile / a.tiles_k, tk = tile - tm * a.tiles_k;
   const int m0 = tm * 16 * R + rg * R, k0 = tk * 128 + cg * 8, cols = a.K - k0;
   float f[R][8];
 #pragma unroll
@@ -181,6 +182,92 @@ __global__ __launch_bounds__(256) void quant_blocks_kernel(const QuantArgs a) {
       if (k < a.K) *reinterpret_cast<uint4*>(a.qt + static_cast<int64_t>(k) * a.Mp + tm * 128 + piece * 16) = o;
     }
   }
+}
+
+template <typename T, bool E5, int R, bool COLS, bool DROP>
+__global__ __launch_bounds__(256) void quant_blocks_kernel(const QuantArgs a) {
+  quant_tile<T, E5, R, COLS, DROP>(a, blockIdx.x);
+}
+// The columns' part of a tile alone, 32 columns of it: thread t holds rows 2 * (t / 4), + 1 of the eight columns at 8 * (t % 4).
+template <typename T, bool E5, bool DROP>
+__device__ __forceinline__ void quant_columns(const QuantArgs& a, int tile) {
+  constexpr int V = Elem<T>::VEC;
+  const int tiles = (a.K + 31) >> 5, tid = threadIdx.x, cg = tid & 3, rg = tid >> 2;
+  const int tm = tile / tiles, tk = tile - tm * tiles;
+  const int m0 = tm * 128 + rg * 2, k0 = tk * 32 + cg * 8, cols = a.K - k0;
+  float f[2][8];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const T* row = static_cast<const T*>(a.x) + static_cast<int64_t>(m0 + i) * a.ldx + k0;
+    if (m0 + i < a.M && cols >= 8) {
+#pragma unroll
+      for (int j = 0; j < 8; j += V) Elem<T>::unpack(load16_any(row + j), f[i] + j);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[i][j] = m0 + i < a.M && j < cols ? Elem<T>::load(row + j) : 0.f;
+    }
+  }
+  __shared__ float red[2][64][33];
+  __shared__ uint32_t col_scale[32];
+  __shared__ uint4 turned[256];
+  if (a.sums) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) red[0][rg][cg * 8 + j] = f[0][j] + f[1][j];
+  }
+  if constexpr (DROP) {
+    const uint64_t call = drop_call(a.drop), per_row = static_cast<uint64_t>((a.K + 7) >> 3);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const DropBits bits = drop_bits(a.drop, call, static_cast<uint64_t>(m0 + i) * per_row + static_cast<uint32_t>(k0 >> 3));
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[i][j] = drop_keeps(a.drop, bits, j) ? f[i][j] * a.drop.factor : 0.f;
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) red[1][rg][cg * 8 + j] = __uint_as_float(max(magnitude(f[0][j]), magnitude(f[1][j])));
+  __syncthreads();
+  if (tid < 64) {  // half a wave the largest magnitudes, the other half the sums
+    const int c = tid & 31, k = tk * 32 + c;
+    if (tid < 32) {
+      uint32_t top = 0;
+#pragma unroll 16
+      for (int i = 0; i < 64; ++i) top = max(top, __float_as_uint(red[1][i][c]));
+      float inv;
+      bool finite;
+      const uint32_t byte = f8_scale<E5>(top, &inv, &finite);
+      col_scale[c] = byte | (finite ? 0u : 256u);
+      if (a.qt && k < a.K) {
+        uint8_t* s = a.scale_t + (static_cast<int64_t>(tm >> 2) * a.K + k) * 4;
+        s[tm & 3] = static_cast<uint8_t>(byte);
+        if (tm == (a.Mp >> 7) - 1)
+          for (int j = (tm & 3) + 1; j < 4; ++j) s[j] = 0;
+      }
+    } else if (a.sums && k < a.K) {
+      float s = 0.f;
+#pragma unroll 16
+      for (int i = 0; i < 64; ++i) s += red[0][i][c];
+      a.sums[static_cast<int64_t>(tm) * a.K + k] = s;
+    }
+  }
+  if (!a.qt) return;
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const uint32_t s = col_scale[cg * 8 + j];
+    const float inv = __uint_as_float((254u - (s & 255u)) << 23);
+    uint32_t two = f8_four<E5>(f[0][j] * inv, f[1][j] * inv, 0.f, 0.f, s < 256u);
+    if (m0 + 1 >= a.M) two &= m0 < a.M ? 0xffu : 0u;  // zeros past the last row, in NaN blocks too
+    reinterpret_cast<uint16_t*>(turned)[(cg * 8 + j) * 64 + rg] = static_cast<uint16_t>(two);
+  }
+  __syncthreads();
+  const int k = tk * 32 + (tid >> 3);
+  if (k < a.K) *reinterpret_cast<uint4*>(a.qt + static_cast<int64_t>(k) * a.Mp + tm * 128 + (tid & 7) * 16) = turned[tid];
+}
+// Few tiles: rows and columns by workgroups of their own, 32 rows and 32 columns each, which read x twice but fill the card.
+template <typename T, bool E5, bool DROP>
+__global__ __launch_bounds__(256) void quant_small_kernel(const QuantArgs a, int row_tiles) {
+  if (static_cast<int>(blockIdx.x) < row_tiles) quant_tile<T, E5, 2, false, DROP>(a, blockIdx.x);
+  else quant_columns<T, E5, DROP>(a, blockIdx.x - row_tiles);
 }
 
 // db[n] = the sum of the row tiles' sums: four threads a column, each every fourth tile in order, then the four; the same order whichever kernel
@@ -479,40 +566,47 @@ __device__ __forceinline__ void f8_tile_product(const F8Args& a, int group) {
   float b[V];
 #pragma unroll
   for (int j = 0; j < V; ++j) b[j] = a.bias && col + j < a.N ? a.bias[col + j] : 0.f;
+  auto output = [&](auto past) __attribute__((always_inline)) {
 #pragma unroll
-  for (int i = 0; i < TM; ++i) {
+    for (int i = 0; i < TM; ++i) {
 #pragma unroll
-    for (int j = 0; j < TN; ++j)
+      for (int j = 0; j < TN; ++j)
 #pragma unroll
-      for (int v = 0; v < 4; ++v)
-        *reinterpret_cast<float4*>(mine + (lane & 31) * PITCH + j * 32 + v * 8 + (lane >> 5) * 4) =
-            make_float4(acc[i][j][4 * v], acc[i][j][4 * v + 1], acc[i][j][4 * v + 2], acc[i][j][4 * v + 3]);
-    __builtin_amdgcn_wave_barrier();
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        for (int v = 0; v < 4; ++v)
+          *reinterpret_cast<float4*>(mine + (lane & 31) * PITCH + j * 32 + v * 8 + (lane >> 5) * 4) =
+              make_float4(acc[i][j][4 * v], acc[i][j][4 * v + 1], acc[i][j][4 * v + 2], acc[i][j][4 * v + 3]);
+      __builtin_amdgcn_wave_barrier();
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
-    for (int p = 0; p < 32 / RPP; ++p) {
-      const int row = p * RPP + lane / LPR, m = m0 + wm * (BM / WM) + i * 32 + row;
-      if (m < a.M && col < a.N) {
-        float f[V];
+      for (int p = 0; p < 32 / RPP; ++p) {
+        const int row = p * RPP + lane / LPR, m = m0 + wm * (BM / WM) + i * 32 + row;
+        if (m < a.M && col < a.N) {
+          float f[V];
 #pragma unroll
-        for (int j = 0; j < V; ++j) f[j] = mine[row * PITCH + lane % LPR * V + j] + b[j];
-        if (a.drop.threshold) drop_columns<V>(a, call, m, col, f);
-        T* to = y + m * a.ldy + col;
-        if (col + V <= a.N) {
-          Vec16 o;
-          Elem<T>::pack(f, o);
-          store16_any(to, o);
-        } else {
+          for (int j = 0; j < V; ++j) f[j] = mine[row * PITCH + lane % LPR * V + j] + b[j];
+          if (a.drop.threshold) drop_columns<V>(a, call, m, col, f);
+          T* to = y + m * a.ldy + col;
+          if (col + V <= a.N) {
+            Vec16 o;
+            Elem<T>::pack(f, o);
+            if constexpr (decltype(past)::value) store16_any_stream(to, o);
+            else store16_any(to, o);
+          } else {
 #pragma unroll
-          for (int j = 0; j < V; ++j)
-            if (col + j < a.N) Elem<T>::store(to + j, f[j]);
+            for (int j = 0; j < V; ++j)
+              if (col + j < a.N) Elem<T>::store(to + j, f[j]);
+          }
         }
       }
+      __builtin_amdgcn_wave_barrier();
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
-    __builtin_amdgcn_wave_barrier();
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-  }
+  };
+  // (two whole copies: a choice at each store would be merged into one ordinary store)
+  if (!a.partial && static_cast<int64_t>(a.M) * a.N * static_cast<int64_t>(sizeof(T)) >= kPastBytes) output(std::true_type{});
+  else output(std::false_type{});
 }
+
 template <typename T, bool E5, bool EXACT, int BM, int BN, int WM, int WN, int RING>
 __global__ __launch_bounds__(64 * WM * WN) void matmul_f8_kernel(const F8Args a) {
   if (static_cast<int>(blockIdx.x) < a.groups) f8_tile_product<T, E5, EXACT, BM, BN, WM, WN, RING>(a, blockIdx.x);
@@ -768,6 +862,10 @@ static void f8_product(F8Args a, int K, void* partial, hipStream_t s) {
   F8Parts parts = f8_parts(a.M, a.N, K, EXACT);
 #ifdef RN50_TUNING
   if (getenv("RN50_F8_TILE")) parts = F8Parts{1, a.Kp >> 7};
+  if (const char* e = getenv("RN50_F8_PARTS")) {
+    parts.part = static_cast<int>(align_up(static_cast<size_t>(ceil_div(a.Kp >> 7, atoi(e))), 4));
+    parts.count = static_cast<int>(ceil_div(a.Kp >> 7, parts.part));
+  }
 #endif
   if (parts.count == 1) {
     a.part = a.Kp >> 7;
@@ -825,6 +923,16 @@ static bool f8_fused(int M, int K) {
 template <typename T, bool E5, bool DROP>
 static void quant_launch(QuantArgs a, hipStream_t s) {
   const bool cols = a.qt || a.sums;
+  int64_t few = 256;
+#ifdef RN50_TUNING  // tuning builds only: RN50_F8_QUANT=tiles
+  if (const char* e = getenv("RN50_F8_QUANT")) few = atoi(e);
+#endif
+  if (cols && ceil_div(a.M, 128) * a.tiles_k <= few) {
+    const int row_tiles = a.q ? static_cast<int>(ceil_div(a.M, 32) * a.tiles_k) : 0;
+    const unsigned small = static_cast<unsigned>(row_tiles + ceil_div(a.M, 128) * ceil_div(a.K, 32));
+    RN50_LAUNCH("quant_blocks_f8", (quant_small_kernel<T, E5, DROP>), dim3(small), dim3(256), 0, s, a, row_tiles);
+    return;
+  }
   const unsigned grid = static_cast<unsigned>(ceil_div(a.M, cols ? 128 : 32) * a.tiles_k);
   if (cols) RN50_LAUNCH("quant_blocks_f8", (quant_blocks_kernel<T, E5, 8, true, DROP>), dim3(grid), dim3(256), 0, s, a);
   else RN50_LAUNCH("quant_blocks_f8", (quant_blocks_kernel<T, E5, 2, false, DROP>), dim3(grid), dim3(256), 0, s, a);

@@ -166,7 +166,7 @@ def test_dropout_takes_the_training_state_s_step(rn):
 
 
 # -------------------------------------------------------------- 8-bit matrices
-QUANT = [(1, 1), (1, 128), (5, 7), (127, 129), (128, 128), (130, 513), (3, 2047), (257, 40), (600, 1100), (33, 8), (1025, 131)]
+QUANT = [(1, 1), (1, 128), (5, 7), (127, 129), (128, 128), (130, 513), (3, 2047), (257, 40), (600, 1100), (33, 8), (1025, 131), (4200, 1030), (130, 33001)]
 
 
 def check_quantized(rn, x, fmt, src, dropout=None, xf=None):
@@ -221,7 +221,7 @@ def test_quantized_blocks_with_infinities_and_nan(rn, dtype, fmt):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
-@pytest.mark.parametrize("M, K", [(1, 1), (40, 2047), (130, 300), (129, 8)])
+@pytest.mark.parametrize("M, K", [(1, 1), (40, 2047), (130, 300), (129, 8), (130, 16600)])
 def test_quantized_blocks_behind_a_dropout(rn, M, K, dtype):
     x = values(M, K, 12, dtype)
     x[0, 0] = float("nan")
@@ -322,7 +322,7 @@ def test_layer_forward(rn, M, N, K):
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
-@pytest.mark.parametrize("M, N, K", LAYER + [(2950, 20, 40), (1, 300, 5000), (7000, 20, 70), (100, 9000, 70)])
+@pytest.mark.parametrize("M, N, K", LAYER + [(2950, 20, 40), (1, 300, 5000), (7000, 20, 70), (100, 9000, 70), (4200, 1030, 20)])
 def test_layer_backward(rn, M, N, K, fmt):
     wt, wts, _ = quantized(values(K, N, 2, size=K ** -0.5))
     x = values(K, M, 4)
