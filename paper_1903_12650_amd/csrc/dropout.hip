@@ -99,15 +99,17 @@ static int dropout_run(const char* who, const rn50_dropout* d, int M, int K, int
   if (int rc = check_dropout(who, d)) return rc;
   DropoutArgs a{drop_args(d), x, residual, y, ldx, ldr, ldy, M, K, static_cast<int>(ceil_div(K, 8)), 1, {}};
   a.by_row = make_fastdiv(static_cast<uint32_t>(a.per_row));
+  // As many rows a workgroup as make whole rounds of its threads, as long as there are eight workgroups a compute unit: 50000 rows of 100 blocks two at
+  // a time 33 us, five 28 (otherwise one item a thread: 50176 x 1024 with a residual 55 us, four 58).
+  const int64_t one = a.per_row;
+  auto idle = [&](int64_t rows) { return static_cast<double>(align_up(static_cast<size_t>(rows * one), 256)) / static_cast<double>(rows * one); };
+  int64_t rows = std::max<int64_t>(1, 256 / one), most = std::min<int64_t>(8 * rows, M / 2048);
+  for (int64_t r = rows + 1; r <= most && one < 4096; ++r)
+    if (idle(r) < idle(rows) - 0.03) rows = r;
   constexpr int64_t kMostGroups = 1 << 20;  // (the rest of the rows by the same workgroups)
-  dim3 grid(static_cast<unsigned>(std::min<int64_t>(M, kMostGroups)), static_cast<unsigned>(std::min<int64_t>(ceil_div(a.per_row, 256), 16)));
-  // Four items a thread where there are enough for every compute unit several times over: 50176 x 1024 bf16 with a residual 51 -> 46 us, 4096 x 1024
-  // 4.8 -> 5.2, float 50176 x 1024 72 -> 78.
-  const int group = dtype == RN50_BF16 && static_cast<int64_t>(M) * a.per_row >= (1 << 21) ? 1024 : 256;
-  if (a.per_row < group) {
-    a.rows = group / a.per_row;
-    grid = dim3(static_cast<unsigned>(std::min(ceil_div(M, a.rows), kMostGroups)));
-  }
+  const int64_t parts = rows > 1 ? 1 : std::min<int64_t>(ceil_div(one, 256), 16);
+  a.rows = static_cast<int>(rows);
+  const dim3 grid(static_cast<unsigned>(std::min(ceil_div(M, rows), kMostGroups)), static_cast<unsigned>(parts));
   hipStream_t s = static_cast<hipStream_t>(stream);
   // (float: a lane's two stores are every other 16 bytes, half lines, which past the caches cost more: 50176 x 1024 72 -> 84 us)
   const bool past = dtype == RN50_BF16 && static_cast<int64_t>(M) * K * 2 >= kPastBytes;

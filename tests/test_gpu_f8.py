@@ -412,3 +412,41 @@ def test_on_another_stream(rn):
         got = [rn.fc_f8_fwd(x, w, ws, dtype=BF16) for _ in range(3)]
     s.synchronize()
     assert all(torch.equal(g, want) for g in got)
+
+
+def test_a_training_step_of_a_classifier(rn):
+    """The operators together, as a step uses them: weights quantized, features dropped out and multiplied, the loss and its gradient, the
+    layer's gradients, the update; each against its 64-bit form on what the step handed to it."""
+    M, N, K = 40, 100, 256
+    p, seed = 0.25, 2
+    a, w = values(M, K, 1, BF16).cuda(), values(N, K, 2, size=K ** -0.5).cuda()
+    labels = torch.arange(M, dtype=torch.int32).cuda() % N
+    master, grads, velocity = [w.clone(), torch.zeros(N, device="cuda")], [torch.empty_like(w), torch.empty(N, device="cuda")], [torch.zeros_like(w), torch.zeros(N, device="cuda")]
+    table = rn.LarsTable(master, grads, velocity, [5e-5, 0.0], [1, 0])
+    step = torch.zeros(1, dtype=torch.int64, device="cuda")
+    for i in range(3):
+        drop, told = rn.Dropout(p, seed, 1 << 32, step), (p, seed, 1 << 32, i)
+        q, s, t, ts = rn.quant_blocks_f8(master[0], columns=True)
+        assert np.array_equal(bytes_of(q), f8.quant(master[0].cpu().numpy())[0])
+        logits, xt, xts = rn.fc_f8_fwd(a, q, s, master[1], dropout=drop, save=True)
+        want, size, wxt, wxts = f8.fc_fwd(a.float().cpu().numpy(), bytes_of(q), bytes_of(s), f64(master[1]), told)
+        assert_within(logits, want, product_error(F32, K, want, size), "logits")
+        assert np.array_equal(bytes_of(xt), wxt) and np.array_equal(bytes_of(xts), wxts)
+        loss, _, dlogits = rn.distill_fwd_bwd(logits, None, None, None, labels, alpha=0.0, label_smoothing=0.1, dlogits=logits)
+        da, dw, db = rn.fc_f8_bwd(dlogits, t, ts, xt, xts, dtype=BF16, dropout=drop)
+        (wda, sda), (wdw, sdw), (wdb, sdb) = f8.fc_bwd(f64(dlogits), bytes_of(t), bytes_of(ts), wxt, wxts, drop=told)
+        assert_within(da, wda, product_error(BF16, N, wda, sda) + 4 * EPS * np.abs(wda), "da")
+        assert_within(dw, wdw, product_error(F32, M, wdw, sdw), "dW")
+        assert_within(db, wdb, 130 * EPS * sdb, "db")
+        grads[0].copy_(dw)
+        grads[1].copy_(db)
+        before = master[0].clone()
+        rn.lars_update(table, 0.001, 0.9, 1.0)
+        step.add_(1)
+        assert torch.isfinite(loss).all() and torch.isfinite(master[0]).all() and not torch.equal(before, master[0])
+
+
+def test_the_example_runs_in_8_bits(rn):
+    from paper_1903_12650_amd import distill_example
+    losses = distill_example.run(steps=6, batch=8, classes=50, k=4, f8=True, dropout=0.2)
+    assert losses.shape == (6,) and torch.isfinite(losses).all()
