@@ -81,6 +81,13 @@ __device__ __forceinline__ void buffer_load16_to_lds(rsrc_words r, uint32_t lds_
                : "s"(lds_addr), "v"(voffset), "s"(r), "s"(soffset)
                : "memory");  // (m0 is reserved: the compiler keeps nothing in it across statements)
 }
+// The same where `on` is not 0 (a uniform number), with the branch inside, so that the code around stays one piece for the scheduler.
+__device__ __forceinline__ void buffer_load16_to_lds_if(int on, rsrc_words r, uint32_t lds_addr, uint32_t voffset, uint32_t soffset) {
+  asm volatile("s_cmp_eq_u32 %4, 0\n\ts_cbranch_scc1 .Lskip%=\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds\n.Lskip%=:"
+               :
+               : "s"(lds_addr), "v"(voffset), "s"(r), "s"(soffset), "s"(on)
+               : "memory", "scc");
+}
 // The same by 4 bytes a lane: 256 bytes an instruction.
 __device__ __forceinline__ void buffer_load4_to_lds(rsrc_words r, uint32_t lds_addr, uint32_t voffset) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" : : "s"(lds_addr), "v"(voffset), "s"(r) : "memory");

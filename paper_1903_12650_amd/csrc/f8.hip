@@ -339,6 +339,12 @@ __device__ __forceinline__ void drop_columns(const F8Args& a, uint64_t call, int
   }
 }
 
+// LDS of a tile: RING stages and two groups' scales, where the output is staged afterwards.
+template <int BM, int BN, int WM, int WN, int RING>
+constexpr int f8_tile_lds() {
+  constexpr int loop = RING * (BM + BN) * 128 + 2 * (BM + BN) * 4, output = WM * WN * 32 * (BN / WN + 4) * 4;
+  return loop > output ? loop : output;
+}
 template <typename T, bool E5, bool EXACT, int BM, int BN, int WM, int WN, int RING>
 __device__ __forceinline__ void f8_tile_product(const F8Args& a, int group) {
   constexpr int CB = 128, PPR = CB / 16, NT = 64 * WM * WN, RPL = NT / PPR, RA = BM / RPL, RB = BN / RPL, TM = BM / WM / 32, TN = BN / WN / 32;
@@ -366,12 +372,16 @@ __device__ __forceinline__ void f8_tile_product(const F8Args& a, int group) {
   const uint32_t base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_byte_ptr)smem));
   const uint32_t dst = __builtin_amdgcn_readfirstlane(base + static_cast<uint32_t>(wave) * 1024u);
   constexpr int NL = RA + RB;
-  auto load_one = [&](int st, int l) __attribute__((always_inline)) {  // (l known when compiling; past the last stage: nothing is read, zeros arrive)
+  auto load_one = [&](int st, int l) __attribute__((always_inline)) {  // (l known when compiling)
     const uint32_t so = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(st) * CB), to = dst + static_cast<uint32_t>(st & (RING - 1)) * STAGE;
     rsrc_words r = l < RA ? rsA : rsB;
-    r.z = st < stages ? r.z : 0;
-    if (l < RA) buffer_load16_to_lds(r, to + l * (RPL * CB), at_a[l < RA ? l : 0], so);
-    else buffer_load16_to_lds(r, to + BM * CB + (l - RA) * (RPL * CB), at_b[l < RA ? 0 : l - RA], so);
+    const uint32_t at = l < RA ? at_a[l < RA ? l : 0] : at_b[l < RA ? 0 : l - RA], by = l < RA ? l * (RPL * CB) : BM * CB + (l - RA) * (RPL * CB);
+    if constexpr (RING == 2) {  // (nothing past the last stage: the waits are for all loads)
+      buffer_load16_to_lds_if(__builtin_amdgcn_readfirstlane(st < stages ? 1 : 0), r, to + by, at, so);
+    } else {  // (past the last stage zeros, so that the waits' counts hold)
+      r.z = st < stages ? r.z : 0;
+      buffer_load16_to_lds(r, to + by, at, so);
+    }
   };
   // The scales of a group of four blocks are a dword a row, brought into LDS like the operands: 64 rows of the tile or of its columns a wave,
   // a group ahead, again with every block (branches here would let the compiler move a step's products behind the next barrier).
@@ -464,7 +474,8 @@ __device__ __forceinline__ void f8_tile_product(const F8Args& a, int group) {
   for (int st = 0; st < RING; ++st)
 #pragma unroll
     for (int l = 0; l < NL; ++l) load_one(st, l);
-  wait_loads_then_barrier<(RING - 1) * NL>();
+  if (RING == 2 && stages == 1) wait_loads_then_barrier<0>();  // (there is no second stage whose loads may be on their way)
+  else wait_loads_then_barrier<(RING - 1) * NL>();
   if (wm * (BM / WM) >= rows || wn * (BN / WN) >= cols) {  // a wave without rows or columns of its own loads and waits as the others do
     for (int block = 0; block < blocks; ++block) {
       wait_loads_then_barrier<(RING - 2) * NL>();
@@ -555,7 +566,7 @@ __device__ __forceinline__ void f8_tile_product(const F8Args& a, int group) {
   }
   // Output: a wave's 32 rows at a time through LDS (its own part of it), whole rows of the wave's columns from there.
   constexpr int WC = BN / WN, PITCH = WC + 4;  // floats (rows 16 bytes further along the banks)
-  static_assert(WM * WN * 32 * PITCH * 4 <= RING * STAGE, "the output stage fits the buffers");
+  static_assert(WM * WN * 32 * PITCH * 4 <= f8_tile_lds<BM, BN, WM, WN, RING>(), "the output stage fits");
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   wait_loads_then_barrier<0>();
   float* mine = reinterpret_cast<float*>(smem) + wave * 32 * PITCH;
@@ -733,7 +744,7 @@ template <typename T, bool E5, int MB>
 __global__ __launch_bounds__(kFewThreads) void f8_few_backward_kernel(const F8FewArgs x, const F8Args w) {
   const int group = static_cast<int>(blockIdx.x) - x.p.groups;
   if (group < 0) f8_few_product<T, E5, MB, void>(x, blockIdx.x);
-  else if (group < w.groups) f8_tile_product<float, E5, true, 128, 128, 2, 4, 2>(w, group);
+  else if (group < w.groups) f8_tile_product<float, E5, true, 128, 128, 4, 2, 2>(w, group);
   else f8_column_sums(w.sum, group - w.groups);
 }
 
@@ -789,7 +800,7 @@ static void sum_columns(const SumArgs& a, hipStream_t s) {
 }
 template <typename T, bool E5, bool EXACT, int BM, int BN, int WM, int WN, int RING>
 static void f8_tile(F8Args a, int parts, hipStream_t s) {
-  constexpr int lds = RING * (BM + BN) * 128 + 2 * (BM + BN) * 4;
+  constexpr int lds = f8_tile_lds<BM, BN, WM, WN, RING>();
   a.tiles_m = static_cast<int>(ceil_div(a.M, BM));
   a.tiles_n = static_cast<int>(ceil_div(a.N, BN));
   const auto kernel = matmul_f8_kernel<T, E5, EXACT, BM, BN, WM, WN, RING>;
@@ -824,18 +835,24 @@ static void f8_tiles(const F8Args& a, int parts, hipStream_t s) {
   if (const char* e = getenv("RN50_F8_TILE")) {
     switch (atoi(e)) {
       case 256: return f8_tile<T, E5, EXACT, 256, 256, 2, 4, 2>(a, parts, s);
-      case 1288: return f8_tile<T, E5, EXACT, 128, 128, 2, 4, 2>(a, parts, s);
-      case 12884: return f8_tile<T, E5, EXACT, 128, 128, 2, 4, 4>(a, parts, s);
+      case 1288: return f8_tile<T, E5, EXACT, 128, 128, 4, 2, 2>(a, parts, s);
       case 1284: return f8_tile<T, E5, EXACT, 128, 128, 2, 2, 4>(a, parts, s);
       case 128644: return f8_tile<T, E5, EXACT, 128, 64, 2, 2, 4>(a, parts, s);
       case 644: return f8_tile<T, E5, EXACT, 64, 64, 2, 2, 4>(a, parts, s);
     }
   }
 #endif
+  // The largest tile of which there are enough for the 256 compute units, us (256x256, 128x128 by eight waves, by four with four buffers, 128x64, 64x64;
+  // bfloat16 / float): 4096^3 59, 70, -, -, - / 105, 124, 135, 181, 189; 1001 x 2047 -> 4099 (68, 264, 264, 520, 1040 tiles) 26, 19, 25, 27, 24 /
+  // 48, 31, 38, 41, 34; 4096 x 4096 -> 1024 (64, 256, 256, 512, 1024) 42, 25, 22, 30, 33 / 84, 37, 38, 47, 51; 512 x 4096 -> 4096 (32, 128, 128, 256, 512)
+  // 42, 24, 19, 16.5, 18 / 83, 32, 32, 25, 26; 1000 x 2048 -> 1000 (16, 64, 64, 128, 256) 25, 14, 12, 10, 8 / 46, 18, 20, 14, 12.
+  // The 256x256 one leaves a unit a single workgroup, so only where its last round is full enough, with short sums fuller (256x256, 128x128): 50176 ->
+  // 1024 by 784 tiles, sums of 256 39.5, 37.3 / 63, 55, of 768 60, 64 / 104, 98; 20000 -> 2000 by 632, 256 41, 37 / 52, 45.5, 1024 63, 64 / 95, 95;
+  // 8192 -> 4096 by 512, 256 21, 26 / 36, 37.
   auto tiles = [&](int bm, int bn) { return ceil_div(a.M, bm) * ceil_div(a.N, bn) * parts; };
-  const int64_t large = tiles(256, 256);
-  if (large > 128 && (large <= 256 || large * 5 >= ceil_div(large, 256) * 256 * 4)) f8_tile<T, E5, EXACT, 256, 256, 2, 4, 2>(a, parts, s);
-  else if (tiles(128, 128) > 256) f8_tile<T, E5, EXACT, 128, 128, 2, 4, 2>(a, parts, s);
+  const int64_t large = tiles(256, 256), places = ceil_div(large, 256) * 256;
+  if (large > 128 && (large <= 256 || large * 10 >= places * (a.Kp <= 1024 ? 9 : 8))) f8_tile<T, E5, EXACT, 256, 256, 2, 4, 2>(a, parts, s);
+  else if (tiles(128, 128) > 256) f8_tile<T, E5, EXACT, 128, 128, 4, 2, 2>(a, parts, s);
   else if (tiles(128, 128) > 128) f8_tile<T, E5, EXACT, 128, 128, 2, 2, 4>(a, parts, s);
   else if (tiles(128, 64) > 128) f8_tile<T, E5, EXACT, 128, 64, 2, 2, 4>(a, parts, s);
   else f8_tile<T, E5, EXACT, 64, 64, 2, 2, 4>(a, parts, s);
@@ -894,7 +911,7 @@ static void f8_run(int a_format, int y_dtype, const F8Args& a, int K, void* part
 static bool f8_few_backward_fits(int M, int N) { return M <= kFewRows && N > kFewRows; }
 template <typename T, bool E5>
 static void f8_few_backward(F8Args x, F8Args w, hipStream_t s) {
-  constexpr int lds = 2 * 256 * 128 + 2 * 256 * 4;
+  constexpr int lds = f8_tile_lds<128, 128, 4, 2, 2>();
   x.groups = static_cast<int>(ceil_div(x.N, 16));
   w.tiles_m = static_cast<int>(ceil_div(w.M, 128));
   w.tiles_n = static_cast<int>(ceil_div(w.N, 128));
