@@ -371,10 +371,10 @@ def test_layer_gradients_by_differences(rn):
         assert float(db[j]) == (loss(x, w, bias + d) - loss(x, w, bias - d)) / 2
 
 
-def test_layer_in_a_captured_graph(rn):
+@pytest.mark.parametrize("M, N, K", [(40, 100, 300), (12, 30, 300), (7000, 130, 70), (300, 700, 500)])
+def test_layer_in_a_captured_graph(rn, M, N, K):
     """Forward and backward of a layer behind a dropout whose counter moves on, as a training step runs them: every replay like the
-    eager calls with that counter, twice in a row with eager work between."""
-    M, N, K = 40, 100, 300
+    eager calls with that counter, with eager work between."""
     x, w, dy = values(M, K, 1, BF16).cuda(), values(N, K, 2, BF16).cuda(), values(M, N, 3, F32).cuda()
     bias = torch.zeros(N, device="cuda")
     step = torch.zeros(1, dtype=torch.int64, device="cuda")
@@ -400,6 +400,57 @@ def test_layer_in_a_captured_graph(rn):
         torch.cuda.synchronize()
         for a, b in zip(out, layer(rn.Dropout(0.2, 5, i))):
             assert torch.equal(a, b), i
+
+
+def test_a_dropout_of_everything_and_of_nothing(rn):
+    """p = 1: nothing gets through, forward or backward, whatever x holds; p = 0 (or below 2^-17): as without a dropout."""
+    M, N, K = 70, 40, 200
+    x, w, dy = values(M, K, 1).cuda(), values(N, K, 2).cuda(), values(M, N, 3).cuda()
+    q, s, t, ts = rn.quant_blocks_f8(w, columns=True)
+    bias = torch.arange(N, dtype=F32, device="cuda")
+    plain = rn.fc_f8_fwd(x, q, s, bias, save=True)
+    for p in (0.0, 2.0 ** -18):
+        for a, b in zip(rn.fc_f8_fwd(x, q, s, bias, dropout=rn.Dropout(p, 1), save=True), plain):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+    x[3, 5] = float("nan")
+    y, xt, xts = rn.fc_f8_fwd(x, q, s, bias, dropout=rn.Dropout(1.0, 1), save=True)
+    assert torch.equal(y, bias.expand(M, N)) and (xt.view(torch.uint8) == 0).all()
+    for dtype in (BF16, F32):
+        dx, dw, db = rn.fc_f8_bwd(dy, t, ts, xt, xts, dtype=dtype, dropout=rn.Dropout(1.0, 1))
+        assert (dx == 0).all() and (dw == 0).all() and (db != 0).any()
+
+
+def test_offsets_past_32_bits(rn):
+    """Matrices of more than 2^32 elements: what their last rows and columns come to is what the same rows give by themselves."""
+    if torch.cuda.get_device_properties(0).total_memory < 64 << 30:
+        pytest.skip("needs 40 GB")
+    M, K = 131072 + 256, 32768 + 128
+    x = torch.empty((M, K), dtype=BF16, device="cuda")
+    x.copy_(torch.randn(1, K, device="cuda"))
+    x[-300:] = torch.randn(300, K, device="cuda").bfloat16()
+    d = rn.Dropout(0.5, 3)
+    y = rn.dropout_fwd(x, d)
+    per = K // 8
+    b = np.uint64(M - 1) * np.uint64(per) + np.arange(per, dtype=np.uint64)
+    assert int(b[-1]) > 2 ** 29
+    ctr = np.zeros((per, 4), np.uint32)
+    ctr[:, 0], ctr[:, 1] = b & np.uint64(0xFFFFFFFF), (b >> np.uint64(32)) | np.uint64(1 << 31)
+    words = f8.philox4x32_10(ctr, (3, 0)).astype(np.uint32)
+    keep = np.stack([words & np.uint32(0xFFFF), words >> np.uint32(16)], -1).reshape(K) >= 32768
+    assert np.array_equal(f64(y[-1]) != 0, keep & (f64(x[-1]) != 0)) and torch.equal(y[-1][y[-1] != 0], (2 * x[-1])[y[-1] != 0])
+    del y
+    q, s, t, ts = rn.quant_blocks_f8(x, columns=True)
+    lq, ls, lt, lts = rn.quant_blocks_f8(x[-256:], columns=True)
+    assert torch.equal(q[-256:].view(torch.uint8), lq.view(torch.uint8)) and torch.equal(s[:, -256:], ls)
+    assert torch.equal(t.view(torch.uint8)[:, -256:], lt.view(torch.uint8))
+    del x, t, ts
+    N = 32768 + 70
+    w, ws, _, _ = rn.quant_blocks_f8(torch.randn(N, 128, device="cuda"))
+    a, sa = q[:, :128].contiguous(), s[:1, :, :].clone()
+    out = rn.matmul_f8(128, a, sa, w, ws, dtype=BF16)
+    assert out.numel() > 2 ** 32
+    assert torch.equal(out[-256:], rn.matmul_f8(128, a[-256:].contiguous(), sa[:, -256:].contiguous(), w, ws, dtype=BF16))
+    assert torch.equal(out[:256], rn.matmul_f8(128, a[:256].contiguous(), sa[:, :256].contiguous(), w, ws, dtype=BF16))
 
 
 def test_on_another_stream(rn):
