@@ -624,10 +624,12 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_f8_kernel(const F8Args a)
   else f8_column_sums(a.sum, blockIdx.x - a.groups);
 }
 
-// Few rows (M <= 16 * MB): the weights go by once, bound by memory; a workgroup owns 16 columns, its waves a part of K each.  A wave's lane has column
-// lane % 16 and 32 numbers at 32 * (lane / 16) of a block of 128, straight from memory, U blocks' loads in flight; as bfloat16, times their
-// power of two, they meet the rows' (the second operand) in v_mfma_f32_16x16x32_bf16.  The waves' sums are added through LDS, in order.
+// Few rows (M <= 16 * MB): the weights go by once, bound by memory; a workgroup owns 16 * CB columns, its waves a part of K each.  A wave's lane has column
+// lane % 16 and 32 numbers at 32 * (lane / 16) of a block of 128, straight from memory, U blocks' loads in flight; they meet the rows' (the second
+// operand) in v_mfma_scale_f32_16x16x128_f8f6f4, or (EXACT) as bfloat16, times their power of two, in v_mfma_f32_16x16x32_bf16.  The waves' sums
+// are added through LDS, in order.
 // X: the rows are float or bfloat16 and quantized here, block by block as they are needed (a block's 128 numbers are four lanes'): no second launch.
+// (The rows' loads beside the weights', U blocks ahead, change nothing: 40 x 2048 -> 1000 6.0 -> 6.4 us, 40 x 8192 -> 8192 34.0 -> 33.5.)
 constexpr int kFewThreads = 512, kFewWaves = kFewThreads / 64;
 struct F8FewArgs {
   F8Args p;
@@ -638,22 +640,27 @@ struct F8FewArgs {
 __device__ __forceinline__ uint32_t scale_byte(const uint32_t* scales, int rows, int row, int block) {
   return reinterpret_cast<const uint8_t*>(scales)[(static_cast<int64_t>(block >> 2) * rows + row) * 4 + (block & 3)];
 }
-template <typename T, bool E5, int MB, typename X>
+template <typename T, bool E5, bool EXACT, int MB, int CB, typename X>
 __device__ __forceinline__ void f8_few_product(const F8FewArgs& a, int group) {
   constexpr bool FUSED = !std::is_void<X>::value;
-  constexpr int U = FUSED ? 2 : 4;
+  constexpr int U = FUSED || CB > 1 ? 2 : 4;
   __shared__ float red[kFewWaves][MB][256];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, sub = lane >> 4;
-  const int n0 = group * 16, M = a.p.M, N = a.p.N, Kp = a.p.Kp;
+  const int n0 = group * (16 * CB), M = a.p.M, N = a.p.N, Kp = a.p.Kp;
   const int blocks = Kp >> 7, from = blocks * wave / kFewWaves, to = blocks * (wave + 1) / kFewWaves;
-  const int col = min(n0 + (lane & 15), N - 1);
-  const uint8_t* wp = a.p.w + static_cast<int64_t>(col) * Kp + 32 * sub;
-  i32x4 fw[U][2];
-  uint32_t sw[U];
-  auto load_w = [&](int u, int b) __attribute__((always_inline)) {
-    fw[u][0] = *reinterpret_cast<const i32x4*>(wp + static_cast<int64_t>(b) * 128);
-    fw[u][1] = *reinterpret_cast<const i32x4*>(wp + static_cast<int64_t>(b) * 128 + 16);
-    sw[u] = scale_byte(a.p.ws, N, col, b);
+  int col[CB];
+  i32x4 fw[U][CB][2];
+  uint32_t sw[U][CB];
+#pragma unroll
+  for (int c = 0; c < CB; ++c) col[c] = min(n0 + c * 16 + (lane & 15), N - 1);
+  auto load_w = [&](int u, int k) __attribute__((always_inline)) {
+#pragma unroll
+    for (int c = 0; c < CB; ++c) {
+      const uint8_t* w = a.p.w + static_cast<int64_t>(col[c]) * Kp + static_cast<int64_t>(k) * 128 + 32 * sub;
+      fw[u][c][0] = *reinterpret_cast<const i32x4*>(w);
+      fw[u][c][1] = *reinterpret_cast<const i32x4*>(w + 16);
+      sw[u][c] = scale_byte(a.p.ws, N, col[c], k);
+    }
   };
 #pragma unroll
   for (int u = 0; u < U; ++u)
@@ -661,17 +668,29 @@ __device__ __forceinline__ void f8_few_product(const F8FewArgs& a, int group) {
   int row[MB];
 #pragma unroll
   for (int b = 0; b < MB; ++b) row[b] = min(b * 16 + (lane & 15), M - 1);
-  f32x4 acc[MB];
+  f32x4 acc[CB][MB];
 #pragma unroll
-  for (int b = 0; b < MB; ++b) acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int c = 0; c < CB; ++c)
+#pragma unroll
+    for (int b = 0; b < MB; ++b) acc[c][b] = f32x4{0.f, 0.f, 0.f, 0.f};
   for (int s = from; s < to; s += U) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int k = s + u;
       if (k >= to) break;
-      bf16x8 w[4];
-      f8_to_bf16<false>(fw[u][0], scale_of(sw[u]), w);
-      f8_to_bf16<false>(fw[u][1], scale_of(sw[u]), w + 2);
+      bf16x8 w[EXACT ? CB : 1][4];
+      i32x8 w8[EXACT ? 1 : CB];
+      uint32_t scale_w[CB];
+#pragma unroll
+      for (int c = 0; c < CB; ++c) {
+        scale_w[c] = sw[u][c];
+        if constexpr (EXACT) {
+          f8_to_bf16<false>(fw[u][c][0], scale_of(sw[u][c]), w[c]);
+          f8_to_bf16<false>(fw[u][c][1], scale_of(sw[u][c]), w[c] + 2);
+        } else {
+          w8[c] = __builtin_shufflevector(fw[u][c][0], fw[u][c][1], 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+      }
       if (k + U < to) load_w(u, k + U);
 #pragma unroll
       for (int b = 0; b < MB; ++b) {
@@ -706,44 +725,58 @@ __device__ __forceinline__ void f8_few_product(const F8FewArgs& a, int group) {
           q[1] = *reinterpret_cast<const i32x4*>(x + 16);
           byte = scale_byte(a.p.as, M, row[b], k);
         }
-        bf16x8 v[4];
-        f8_to_bf16<E5>(q[0], scale_of(byte), v);
-        f8_to_bf16<E5>(q[1], scale_of(byte), v + 2);
+        if constexpr (EXACT) {
+          bf16x8 v[4];
+          f8_to_bf16<E5>(q[0], scale_of(byte), v);
+          f8_to_bf16<E5>(q[1], scale_of(byte), v + 2);
 #pragma unroll
-        for (int h = 0; h < 4; ++h) acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[h], v[h], acc[b], 0, 0, 0);
+          for (int c = 0; c < CB; ++c)
+#pragma unroll
+            for (int h = 0; h < 4; ++h) acc[c][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[c][h], v[h], acc[c][b], 0, 0, 0);
+        } else {
+          const i32x8 v = __builtin_shufflevector(q[0], q[1], 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+          for (int c = 0; c < CB; ++c)
+            acc[c][b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w8[c], v, acc[c][b], 0, E5 ? 1 : 0, 0, static_cast<int>(scale_w[c]), 0, static_cast<int>(byte));
+        }
       }
     }
   }
+  const uint64_t call = a.p.drop.threshold ? drop_call(a.p.drop) : 0;
   // column 4 * (lane / 16) + i of the 16, row lane % 16
 #pragma unroll
-  for (int b = 0; b < MB; ++b) *reinterpret_cast<f32x4*>(&red[wave][b][(lane & 15) * 16 + 4 * sub]) = acc[b];
-  __syncthreads();
-  const uint64_t call = a.p.drop.threshold ? drop_call(a.p.drop) : 0;
-  for (int e = tid; e < MB * 256; e += kFewThreads) {
-    const int b = e >> 8, m = b * 16 + ((e >> 4) & 15), n = n0 + (e & 15);
-    if (m < M && n < N) {
-      float y = a.p.bias ? a.p.bias[n] : 0.f, sum = 0.f;
+  for (int c = 0; c < CB; ++c) {
+    if (c) __syncthreads();  // (`red` has been read)
 #pragma unroll
-      for (int w = 0; w < kFewWaves; ++w) sum += red[w][b][e & 255];
-      y += sum;
-      if (a.p.drop.threshold) {
-        const DropBits bits = drop_bits(a.p.drop, call, static_cast<uint64_t>(m) * static_cast<uint32_t>((N + 7) >> 3) + static_cast<uint32_t>(n >> 3));
-        y = drop_keeps_at(a.p.drop, bits, n & 7) ? y * a.p.drop.factor : 0.f;
+    for (int b = 0; b < MB; ++b) *reinterpret_cast<f32x4*>(&red[wave][b][(lane & 15) * 16 + 4 * sub]) = acc[c][b];
+    __syncthreads();
+    for (int e = tid; e < MB * 256; e += kFewThreads) {
+      const int b = e >> 8, m = b * 16 + ((e >> 4) & 15), n = n0 + c * 16 + (e & 15);
+      if (m < M && n < N) {
+        float y = a.p.bias ? a.p.bias[n] : 0.f, sum = 0.f;
+#pragma unroll
+        for (int v = 0; v < kFewWaves; ++v) sum += red[v][b][e & 255];
+        y += sum;
+        if (a.p.drop.threshold) {
+          const DropBits bits = drop_bits(a.p.drop, call, static_cast<uint64_t>(m) * static_cast<uint32_t>((N + 7) >> 3) + static_cast<uint32_t>(n >> 3));
+          y = drop_keeps_at(a.p.drop, bits, n & 7) ? y * a.p.drop.factor : 0.f;
+        }
+        Elem<T>::store(static_cast<T*>(a.p.y) + m * a.p.ldy + n, y);
       }
-      Elem<T>::store(static_cast<T*>(a.p.y) + m * a.p.ldy + n, y);
     }
   }
 }
-template <typename T, bool E5, int MB, typename X>
+
+template <typename T, bool E5, int MB, int CB, typename X>
 __global__ __launch_bounds__(kFewThreads) void matmul_f8_few_kernel(const F8FewArgs a) {
-  f8_few_product<T, E5, MB, X>(a, blockIdx.x);
+  f8_few_product<T, E5, sizeof(T) == 4, MB, CB, X>(a, blockIdx.x);
 }
 // The two products of a backward pass of few rows in one launch: the input's gradient by the first workgroups, the weights' (a sum of one
 // block) by tiles, and the bias's behind them.
 template <typename T, bool E5, int MB>
 __global__ __launch_bounds__(kFewThreads) void f8_few_backward_kernel(const F8FewArgs x, const F8Args w) {
   const int group = static_cast<int>(blockIdx.x) - x.p.groups;
-  if (group < 0) f8_few_product<T, E5, MB, void>(x, blockIdx.x);
+  if (group < 0) f8_few_product<T, E5, sizeof(T) == 4, MB, 1, void>(x, blockIdx.x);
   else if (group < w.groups) f8_tile_product<float, E5, true, 128, 128, 4, 2, 2>(w, group);
   else f8_column_sums(w.sum, group - w.groups);
 }
@@ -848,18 +881,25 @@ static void f8_tiles(const F8Args& a, int parts, hipStream_t s) {
   // 42, 24, 19, 16.5, 18 / 83, 32, 32, 25, 26; 1000 x 2048 -> 1000 (16, 64, 64, 128, 256) 25, 14, 12, 10, 8 / 46, 18, 20, 14, 12.
   // The 256x256 one leaves a unit a single workgroup, so only where its last round is full enough, with short sums fuller (256x256, 128x128): 50176 ->
   // 1024 by 784 tiles, sums of 256 39.5, 37.3 / 63, 55, of 768 60, 64 / 104, 98; 20000 -> 2000 by 632, 256 41, 37 / 52, 45.5, 1024 63, 64 / 95, 95;
-  // 8192 -> 4096 by 512, 256 21, 26 / 36, 37.
+  // 8192 -> 4096 by 512, 256 21, 26 / 36, 37; 8192 -> 8192 by 1024, 128 - / 74, 47.
   auto tiles = [&](int bm, int bn) { return ceil_div(a.M, bm) * ceil_div(a.N, bn) * parts; };
   const int64_t large = tiles(256, 256), places = ceil_div(large, 256) * 256;
-  if (large > 128 && (large <= 256 || large * 10 >= places * (a.Kp <= 1024 ? 9 : 8))) f8_tile<T, E5, EXACT, 256, 256, 2, 4, 2>(a, parts, s);
+  if (large > 128 && !(EXACT && a.Kp <= 256) && (large <= 256 || large * 10 >= places * (a.Kp <= 1024 ? 9 : 8))) f8_tile<T, E5, EXACT, 256, 256, 2, 4, 2>(a, parts, s);
   else if (tiles(128, 128) > 256) f8_tile<T, E5, EXACT, 128, 128, 4, 2, 2>(a, parts, s);
   else if (tiles(128, 128) > 128) f8_tile<T, E5, EXACT, 128, 128, 2, 2, 4>(a, parts, s);
   else if (tiles(128, 64) > 128) f8_tile<T, E5, EXACT, 128, 64, 2, 2, 4>(a, parts, s);
   else f8_tile<T, E5, EXACT, 64, 64, 2, 2, 4>(a, parts, s);
 }
+template <typename T, bool E5, int MB, int CB, typename X>
+static void f8_few_columns(const F8FewArgs& a, hipStream_t s) {
+  RN50_LAUNCH("matmul_f8", (matmul_f8_few_kernel<T, E5, MB, CB, X>), dim3(static_cast<unsigned>(ceil_div(a.p.N, 16 * CB))), dim3(kFewThreads), 0, s, a);
+}
 template <typename T, bool E5, int MB, typename X>
 static void f8_few(const F8FewArgs& a, hipStream_t s) {
-  RN50_LAUNCH("matmul_f8", (matmul_f8_few_kernel<T, E5, MB, X>), dim3(static_cast<unsigned>(ceil_div(a.p.N, 16))), dim3(kFewThreads), 0, s, a);
+  // 32 columns a workgroup, which read and convert (or quantize) the rows half as often, where enough workgroups are left: 64 x 8192 -> 8192 44 -> 29 us,
+  // 64 x 1024 -> 16384 17 -> 12, 16 x 8192 -> 8192 with quantization 27 -> 21, 1 x 8192 -> 8192 20 -> 18; 40 x 4096 -> 4096 10.7 -> 13.
+  if (a.p.N >= 8192) f8_few_columns<T, E5, MB, 2, X>(a, s);
+  else f8_few_columns<T, E5, MB, 1, X>(a, s);
 }
 template <typename T, bool E5, bool EXACT>
 static void f8_product(F8Args a, int K, void* partial, hipStream_t s) {
@@ -907,8 +947,10 @@ static void f8_run(int a_format, int y_dtype, const F8Args& a, int K, void* part
   else f8_product<float, false, true>(a, K, partial, s);
 }
 
-// Both products of a backward pass in one launch: few rows (whose sum into the weights is one block), more outputs than the few rows' kernel would take.
-static bool f8_few_backward_fits(int M, int N) { return M <= kFewRows && N > kFewRows; }
+// Both products of a backward pass in one launch: few rows (whose sum into the weights is one block), more outputs than the few rows' kernel would take, and
+// an input's gradient that leaves room on the card beside the weights'.  One launch, two (M x K -> N, us): 40 x 2048 -> 1000 12.3, 15.8, 40 x 2048 ->
+// 2048 17.5, 21.0, 64 x 1024 -> 16384 48, 63, 8 x 4096 -> 8192 42, 45; 40 x 4096 -> 2048 22.9, 20.4, 40 x 4096 -> 4096 38, 31, 40 x 8192 -> 8192 122, 81.
+static bool f8_few_backward_fits(int M, int N, int K) { return M <= kFewRows && N > kFewRows && (M <= 16 || K <= 2048); }
 template <typename T, bool E5>
 static void f8_few_backward(F8Args x, F8Args w, hipStream_t s) {
   constexpr int lds = f8_tile_lds<128, 128, 4, 2, 2>();
@@ -929,13 +971,9 @@ static void f8_few_backward(F8Args x, F8Args w, hipStream_t s) {
   else FEW_BACKWARD(4);
 #undef FEW_BACKWARD
 }
-// Whether fc_f8_fwd takes its rows as they are.
-static bool f8_fused(int M, int K) {
-#ifdef RN50_TUNING  // tuning builds only: RN50_F8_FUSED=0
-  if (const char* e = getenv("RN50_F8_FUSED")) return atoi(e) && M <= 16;
-#endif
-  return M <= 16;
-}
+// Whether fc_f8_fwd takes its rows as they are.  Two launches -> one: 1 x 2048 -> 1000 7.8 -> 5.0 us, 8 x 4096 -> 4096 10.4 -> 8.2, 16 x 8192 -> 8192 20.6 -> 20.6
+// (every workgroup quantizes the rows).
+static bool f8_fused(int M) { return M <= 16; }
 
 template <typename T, bool E5, bool DROP>
 static void quant_launch(QuantArgs a, hipStream_t s) {
@@ -1109,7 +1147,7 @@ extern "C" int fc_f8_fwd(int M, int N, int K, int x_dtype, const void* x, int64_
   Parts parts{static_cast<uint8_t*>(workspace)};
   uint8_t* q = parts.take(static_cast<size_t>(M) * quant_f8_row_bytes(K));
   uint8_t* qs = parts.take(quant_f8_scale_bytes(M, K));
-  if (f8_fused(M, K) && !xt && !dropout) {
+  if (f8_fused(M) && !xt && !dropout) {
     const F8FewArgs a{product_args(M, N, K, nullptr, nullptr, w, w_scale, bias, y, ldy, nullptr), x, ldx, K};
     if (x_dtype == RN50_BF16 && y_dtype == RN50_BF16) f8_few<uint16_t, false, 1, uint16_t>(a, s);
     else if (x_dtype == RN50_BF16) f8_few<float, false, 1, uint16_t>(a, s);
@@ -1169,7 +1207,7 @@ extern "C" int fc_f8_bwd(int M, int N, int K, int dy_dtype, const void* dy, int6
   const SumArgs sum{sums, tiles, N, db};
   F8Args px = product_args(M, K, N, q, qs, wt, wt_scale, nullptr, dx, ld_dx, dropout), pw = product_args(N, K, M, qt, qts, xt, xt_scale, nullptr, dW, K, nullptr);
   if (dW) pw.sum = sum;
-  if (dx && dW && f8_few_backward_fits(M, N)) {
+  if (dx && dW && f8_few_backward_fits(M, N, K)) {
     if (dx_dtype == RN50_BF16 && format == RN50_E5M2) f8_few_backward<uint16_t, true>(px, pw, s);
     else if (dx_dtype == RN50_BF16) f8_few_backward<uint16_t, false>(px, pw, s);
     else if (format == RN50_E5M2) f8_few_backward<float, true>(px, pw, s);

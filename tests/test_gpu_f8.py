@@ -234,7 +234,8 @@ def test_quantized_blocks_behind_a_dropout(rn, M, K, dtype):
 # ------------------------------------------------------------------- products
 MATMUL = [(1, 1, 1), (1, 1000, 2048), (3, 17, 127), (16, 40, 128), (17, 33, 300), (40, 1000, 2048), (64, 65, 513), (65, 70, 129),
           (127, 255, 513), (128, 128, 128), (130, 20, 1100), (300, 200, 640), (257, 511, 2047), (5, 2900, 700), (2, 9, 20000), (1100, 1300, 260),
-          (130, 70, 7000), (65, 9, 20000), (1480, 1420, 260), (2100, 2200, 130), (2900, 2890, 130)]
+          (130, 70, 7000), (65, 9, 20000), (1480, 1420, 260), (2100, 2200, 130), (2900, 2890, 130),
+          (3, 8193, 700), (40, 8200, 300), (64, 8210, 129), (20, 9000, 1300)]
 
 
 def quantized(x, fmt=f8.E4M3):
@@ -298,7 +299,7 @@ def test_nan_blocks_reach_their_row_and_column_only(rn, M):
 
 
 # --------------------------------------------------------------- linear layer
-LAYER = [(1, 1, 1), (1, 1000, 2048), (2, 10, 131), (16, 33, 1000), (17, 40, 300), (40, 1000, 2048), (128, 130, 129), (200, 70, 513), (515, 300, 250)]
+LAYER = [(1, 1, 1), (1, 1000, 2048), (2, 10, 131), (16, 33, 1000), (17, 40, 300), (40, 1000, 2048), (128, 130, 129), (200, 70, 513), (515, 300, 250), (5, 8200, 300)]
 
 
 @pytest.mark.parametrize("M, N, K", LAYER)
@@ -322,7 +323,7 @@ def test_layer_forward(rn, M, N, K):
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
-@pytest.mark.parametrize("M, N, K", LAYER + [(2950, 20, 40), (1, 300, 5000), (7000, 20, 70), (100, 9000, 70), (4200, 1030, 20)])
+@pytest.mark.parametrize("M, N, K", LAYER + [(2950, 20, 40), (1, 300, 5000), (7000, 20, 70), (100, 9000, 70), (4200, 1030, 20), (17, 70, 8200), (40, 130, 2100), (9, 8200, 70)])
 def test_layer_backward(rn, M, N, K, fmt):
     wt, wts, _ = quantized(values(K, N, 2, size=K ** -0.5))
     x = values(K, M, 4)
