@@ -445,7 +445,9 @@ struct DropArg {
   DropArg(PyObject* o, const at::Tensor& like) {
     if (o == Py_None) return;
     given = true;
-    const Owned p(PyObject_GetAttrString(o, "p")), seed(PyObject_GetAttrString(o, "seed")), number(PyObject_GetAttrString(o, "call")), step(PyObject_GetAttrString(o, "step"));
+    static PyObject* const names[] = {PyUnicode_InternFromString("p"), PyUnicode_InternFromString("seed"), PyUnicode_InternFromString("call"),
+                                      PyUnicode_InternFromString("step")};
+    const Owned p(PyObject_GetAttr(o, names[0])), seed(PyObject_GetAttr(o, names[1])), number(PyObject_GetAttr(o, names[2])), step(PyObject_GetAttr(o, names[3]));
     d.p = static_cast<float>(to_double(p.o));
     d.seed = word(seed.o);
     d.call = word(number.o);
@@ -513,16 +515,26 @@ PyObject* dropout_bwd_py(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return wrap(dx);
   });
 }
-// An 8-bit matrix of `rows` rows of K numbers and its scales, made.
+// An 8-bit matrix of `rows` rows of K numbers and its scales, made: tensors of their own in one allocation (one after another they cost 1.3 us
+// each: 1001 x 2047 both ways 6.9 us, two allocations 5.2).
 struct Quantized {
   at::Tensor q, scale;
   uint8_t *pq = nullptr, *ps = nullptr;
   Quantized() {}
   Quantized(int64_t rows, int64_t K, at::ScalarType type, const at::Tensor& like) {
-    q = empty({rows, static_cast<int64_t>(quant_f8_row_bytes(static_cast<int>(K)))}, type, like);
-    scale = empty({(K + 511) / 512, rows, 4}, at::kByte, like);
+    const int64_t row = static_cast<int64_t>(quant_f8_row_bytes(static_cast<int>(K))), groups = (K + 511) / 512;
+    const int64_t bytes = (rows * row + 255) / 256 * 256;
+    const at::Tensor both = empty({bytes + groups * rows * 4}, at::kByte, like);
+    q = part(both, type, 0, {rows, row});
+    scale = part(both, at::kByte, bytes, {groups, rows, 4});
     pq = addr<uint8_t>(q);
     ps = addr<uint8_t>(scale);
+  }
+  static at::Tensor part(const at::Tensor& whole, at::ScalarType type, int64_t offset, at::IntArrayRef sizes) {
+    at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::TensorImpl::VIEW, c10::Storage(whole.storage()), whole.key_set(), c10::scalarTypeToTypeMeta(type));
+    t.unsafeGetTensorImpl()->set_storage_offset(offset);  // (types of one byte)
+    t.unsafeGetTensorImpl()->set_sizes_contiguous(sizes);
+    return t;
   }
   PyObject* first() const { return q.defined() ? wrap(q) : none(); }
   PyObject* second() const { return q.defined() ? wrap(scale) : none(); }
