@@ -12,7 +12,7 @@ namespace rn50 {
 
 constexpr int kF8MaxK = 1 << 22;        // 256 rows of it stay inside a buffer descriptor's 32 bits
 constexpr uint32_t kF8Floor = 27u << 23;  // the bits of 2^-100: blocks below are quantized as if this were their largest magnitude
-constexpr int64_t kPastBytes = 32 << 20;  // outputs that the L2s would not hold for the next kernel are stored past them
+constexpr int64_t kPastBytes = 32 << 20;  // outputs that the L2s would not hold for the next kernel are stored past the caches
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef short s16x2 __attribute__((ext_vector_type(2)));
@@ -57,7 +57,7 @@ struct QuantArgs {
 };
 // A tile of 16 * R rows by 128 columns in registers: thread t holds rows R * (t / 16) .. + R - 1 of the eight columns at 8 * (t % 16), the
 // elements of one Philox call a row.  A block along a row is 16 lanes' (DPP), a block along a column the workgroup's (LDS, R = 8).
-template <typename T, bool E5, int R, bool COLS, bool DROP>
+template <typename T, bool E5, int R, bool COLS, bool DROP, bool PAST>
 __device__ __forceinline__ void quant_tile(const QuantArgs& a, int tile) {
   constexpr int V = Elem<T>::VEC;
   static_assert(!COLS || R == 8, "a block of 128 rows");
@@ -123,7 +123,9 @@ __device__ __forceinline__ void quant_tile(const QuantArgs& a, int tile) {
         o.x &= static_cast<uint32_t>(keep);
         o.y &= static_cast<uint32_t>(keep >> 32);
       }
-      *reinterpret_cast<uint2*>(a.q + static_cast<int64_t>(m0 + i) * a.Kp + k0) = o;
+      uint64_t* to = reinterpret_cast<uint64_t*>(a.q + static_cast<int64_t>(m0 + i) * a.Kp + k0);
+      if constexpr (PAST) __builtin_nontemporal_store(__builtin_bit_cast(uint64_t, o), to);
+      else *to = __builtin_bit_cast(uint64_t, o);
       if (cg == 0) {
         uint8_t* s = a.scale + (static_cast<int64_t>(tk >> 2) * a.M + m0 + i) * 4;
         s[tk & 3] = static_cast<uint8_t>(byte);
@@ -177,16 +179,21 @@ __device__ __forceinline__ void quant_tile(const QuantArgs& a, int tile) {
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
       const int c = p * 32 + (tid >> 3), piece = tid & 7, g = c >> 3, k = tk * 128 + c;
-      uint4 o = turned[c * 8 + (piece ^ (g >> 1))];
-      if (g & 1) o = make_uint4(o.z, o.w, o.x, o.y);
-      if (k < a.K) *reinterpret_cast<uint4*>(a.qt + static_cast<int64_t>(k) * a.Mp + tm * 128 + piece * 16) = o;
+      Vec16 o;
+      o.u = turned[c * 8 + (piece ^ (g >> 1))];
+      if (g & 1) o.u = make_uint4(o.u.z, o.u.w, o.u.x, o.u.y);
+      uint8_t* to = a.qt + static_cast<int64_t>(k) * a.Mp + tm * 128 + piece * 16;
+      if (k < a.K) {
+        if constexpr (PAST) store16_any_stream(to, o);
+        else store16(to, o);
+      }
     }
   }
 }
 
-template <typename T, bool E5, int R, bool COLS, bool DROP>
+template <typename T, bool E5, int R, bool COLS, bool DROP, bool PAST>
 __global__ __launch_bounds__(256) void quant_blocks_kernel(const QuantArgs a) {
-  quant_tile<T, E5, R, COLS, DROP>(a, blockIdx.x);
+  quant_tile<T, E5, R, COLS, DROP, PAST>(a, blockIdx.x);
 }
 // The columns' part of a tile alone, 32 columns of it: thread t holds rows 2 * (t / 4), + 1 of the eight columns at 8 * (t % 4).
 template <typename T, bool E5, bool DROP>
@@ -266,7 +273,7 @@ __device__ __forceinline__ void quant_columns(const QuantArgs& a, int tile) {
 // Few tiles: rows and columns by workgroups of their own, 32 rows and 32 columns each, which read x twice but fill the card.
 template <typename T, bool E5, bool DROP>
 __global__ __launch_bounds__(256) void quant_small_kernel(const QuantArgs a, int row_tiles) {
-  if (static_cast<int>(blockIdx.x) < row_tiles) quant_tile<T, E5, 2, false, DROP>(a, blockIdx.x);
+  if (static_cast<int>(blockIdx.x) < row_tiles) quant_tile<T, E5, 2, false, DROP, false>(a, blockIdx.x);
   else quant_columns<T, E5, DROP>(a, blockIdx.x - row_tiles);
 }
 
@@ -976,38 +983,41 @@ static void f8_few_backward(F8Args x, F8Args w, hipStream_t s) {
 static bool f8_fused(int M) { return M <= 16; }
 
 template <typename T, bool E5, bool DROP>
-static void quant_launch(QuantArgs a, hipStream_t s) {
+static void quant_launch(QuantArgs a, bool past, hipStream_t s) {
   const bool cols = a.qt || a.sums;
-  int64_t few = 256;
-#ifdef RN50_TUNING  // tuning builds only: RN50_F8_QUANT=tiles
-  if (const char* e = getenv("RN50_F8_QUANT")) few = atoi(e);
-#endif
-  if (cols && ceil_div(a.M, 128) * a.tiles_k <= few) {
+  // (us, by tiles and by rows and columns apart: 40 x 1000 float 6.8, 4.5, 1001 x 2047 float 7.0, 5.0, 2048 x 2048 bf16 7.1, 5.9, 4096 x 2048 9.5, 12.8)
+  if (cols && ceil_div(a.M, 128) * a.tiles_k <= 256) {
     const int row_tiles = a.q ? static_cast<int>(ceil_div(a.M, 32) * a.tiles_k) : 0;
     const unsigned small = static_cast<unsigned>(row_tiles + ceil_div(a.M, 128) * ceil_div(a.K, 32));
     RN50_LAUNCH("quant_blocks_f8", (quant_small_kernel<T, E5, DROP>), dim3(small), dim3(256), 0, s, a, row_tiles);
     return;
   }
+  // Stored past the caches where no product follows at once: both ways of 8192 x 8192 bf16 62 -> 58 us, of 8192 x 4096 31 -> 24, 8192 x 8192 alone 37 -> 35; in front of a
+  // product they cost more than they save (50176 x 1024 -> 256 backward 89 -> 103).
   const unsigned grid = static_cast<unsigned>(ceil_div(a.M, cols ? 128 : 32) * a.tiles_k);
-  if (cols) RN50_LAUNCH("quant_blocks_f8", (quant_blocks_kernel<T, E5, 8, true, DROP>), dim3(grid), dim3(256), 0, s, a);
-  else RN50_LAUNCH("quant_blocks_f8", (quant_blocks_kernel<T, E5, 2, false, DROP>), dim3(grid), dim3(256), 0, s, a);
+#define QUANT(R, COLS, PAST) RN50_LAUNCH("quant_blocks_f8", (quant_blocks_kernel<T, E5, R, COLS, DROP, PAST>), dim3(grid), dim3(256), 0, s, a)
+  if (cols && past) QUANT(8, true, true);
+  else if (cols) QUANT(8, true, false);
+  else if (past) QUANT(2, false, true);
+  else QUANT(2, false, false);
+#undef QUANT
 }
 template <typename T>
-static void quant_typed(const QuantArgs& a, int format, hipStream_t s) {
+static void quant_typed(const QuantArgs& a, int format, bool past, hipStream_t s) {
   if (format == RN50_E5M2) {
-    if (a.drop.threshold) quant_launch<T, true, true>(a, s);
-    else quant_launch<T, true, false>(a, s);
+    if (a.drop.threshold) quant_launch<T, true, true>(a, past, s);
+    else quant_launch<T, true, false>(a, past, s);
   } else {
-    if (a.drop.threshold) quant_launch<T, false, true>(a, s);
-    else quant_launch<T, false, false>(a, s);
+    if (a.drop.threshold) quant_launch<T, false, true>(a, past, s);
+    else quant_launch<T, false, false>(a, past, s);
   }
 }
 static void quant_run(int M, int K, int dtype, const void* x, int64_t ldx, const rn50_dropout* drop, int format, uint8_t* q, uint8_t* scale,
-                      uint8_t* qt, uint8_t* scale_t, float* sums, hipStream_t s) {
+                      uint8_t* qt, uint8_t* scale_t, float* sums, bool past, hipStream_t s) {
   const QuantArgs a{x, ldx, M, K, static_cast<int>(ceil_div(K, 128)), q, scale, qt, scale_t, static_cast<int>(quant_f8_row_bytes(K)),
                     static_cast<int>(quant_f8_row_bytes(M)), sums, drop_args(drop)};
-  if (dtype == RN50_BF16) quant_typed<uint16_t>(a, format, s);
-  else quant_typed<float>(a, format, s);
+  if (dtype == RN50_BF16) quant_typed<uint16_t>(a, format, past, s);
+  else quant_typed<float>(a, format, past, s);
 }
 
 // --------------------------------------------------------------------- checks
@@ -1091,7 +1101,7 @@ extern "C" int quant_blocks_f8(int M, int K, int dtype, const void* x, int64_t l
   if (qt)
     if (int rc = check_sum(who, M)) return rc;
   if (int rc = check_tiles(who, M, K, qt ? 128 : 32, 128)) return rc;
-  quant_run(M, K, dtype, x, ldx, dropout, format, q, scale, qt, scale_t, nullptr, static_cast<hipStream_t>(stream));
+  quant_run(M, K, dtype, x, ldx, dropout, format, q, scale, qt, scale_t, nullptr, static_cast<int64_t>(M) * K >= kPastBytes, static_cast<hipStream_t>(stream));
   return launch_status(who);
 }
 
@@ -1155,7 +1165,7 @@ extern "C" int fc_f8_fwd(int M, int N, int K, int x_dtype, const void* x, int64_
     else f8_few<float, false, 1, float>(a, s);
     return launch_status(who);
   }
-  quant_run(M, K, x_dtype, x, ldx, dropout, RN50_E4M3, q, qs, xt, xt_scale, nullptr, s);
+  quant_run(M, K, x_dtype, x, ldx, dropout, RN50_E4M3, q, qs, xt, xt_scale, nullptr, false, s);
   f8_run(RN50_E4M3, y_dtype, product_args(M, N, K, q, qs, w, w_scale, bias, y, ldy, nullptr), K, parts.take(0), s);
   return launch_status(who);
 }
@@ -1202,7 +1212,7 @@ extern "C" int fc_f8_bwd(int M, int N, int K, int dy_dtype, const void* dy, int6
   uint8_t* qts = parts.take(quant_f8_scale_bytes(N, M));
   const int tiles = static_cast<int>(ceil_div(M, 128));
   float* sums = parts.take<float>(static_cast<size_t>(tiles) * N * 4);
-  quant_run(M, N, dy_dtype, dy, ld_dy, nullptr, format, dx ? q : nullptr, qs, dW ? qt : nullptr, qts, db ? sums : nullptr, s);
+  quant_run(M, N, dy_dtype, dy, ld_dy, nullptr, format, dx ? q : nullptr, qs, dW ? qt : nullptr, qts, db ? sums : nullptr, false, s);
   void* partial = parts.take(0);
   const SumArgs sum{sums, tiles, N, db};
   F8Args px = product_args(M, K, N, q, qs, wt, wt_scale, nullptr, dx, ld_dx, dropout), pw = product_args(N, K, M, qt, qts, xt, xt_scale, nullptr, dW, K, nullptr);
