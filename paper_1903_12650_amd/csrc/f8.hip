@@ -56,7 +56,9 @@ struct QuantArgs {
   DropArgs drop;
 };
 // A tile of 16 * R rows by 128 columns in registers: thread t holds rows R * (t / 16) .. + R - 1 of the eight columns at 8 * (t % 16), the
-// elements of one Philox call a row.  A block along a row is 16 lanes' (DPP), a block along a column the workgroup's (LDS, R = 8).
+// elements of one Philox call a row.  A block along a row is 16 lanes' (DPP), a block along a column the workgroup's (LDS, R = 8).  x is read once for
+// both, and for the columns' sums; bound by memory: 8192 x 8192 bf16 both ways 55 us (268 MB, 4.9 TB/s), behind a dropout as much arithmetic as memory
+// (8192 x 4096 32 to 37 us, Philox's multiplications 15 of them).
 template <typename T, bool E5, int R, bool COLS, bool DROP, bool PAST>
 __device__ __forceinline__ void quant_tile(const QuantArgs& a, int tile) {
   constexpr int V = Elem<T>::VEC;
@@ -346,7 +348,17 @@ __device__ __forceinline__ void drop_columns(const F8Args& a, uint64_t call, int
   }
 }
 
-// LDS of a tile: RING stages and two groups' scales, where the output is staged afterwards.
+// A tile of the product by WM x WN waves, each of 32x32 blocks of it.  FAST (bfloat16 results): two 8-bit fragments and their rows' scale bytes go into
+// v_mfma_scale_f32_32x32x64_f8f6f4 as they are, the scaling costs nothing; EXACT (float results): fragments become bfloat16, times their power of two
+// (exact: 4 of its 8 bits), for v_mfma_f32_32x32x16_bf16, since the 8-bit matrix cores drop bits that a float result has.
+// Operands go from memory into LDS past the registers, RING stages of 128 numbers a row, a row's 16-byte pieces exchanged so that a fragment's reads touch all
+// banks.  What bounds it: large tiles' matrix cores, at the clock that their power leaves (8192^3 bfloat16 397 to 437 us, 2500 to 2770 TFLOP/s, of
+// zeros 317; 8192 x 4096 x 4096 into floats 195 to 223, 1230 to 1410); middle ones' time per 128 numbers, 0.85 us a 128x128 float tile, 0.43 of
+// it matrix cores, beside conversions and LDS; with short sums starts and ends (50176 x 256 -> 1024 bfloat16 37 us: 25 without the sum, 32 without
+// the stores).  Four waves of 128x128 421 us where eight of 128x64 take 397; stages of 64 numbers, half lines of memory, 569.
+// Tiles go to the XCDs in runs, columns after columns of GROUP row tiles, so that an XCD's L2 sees both operands several times (GROUP 8: 495 us
+// to 492 at the time of its trial).
+// LDS: RING stages and two groups' scales, where the output is staged afterwards.
 template <int BM, int BN, int WM, int WN, int RING>
 constexpr int f8_tile_lds() {
   constexpr int loop = RING * (BM + BN) * 128 + 2 * (BM + BN) * 4, output = WM * WN * 32 * (BN / WN + 4) * 4;
@@ -548,28 +560,28 @@ __device__ __forceinline__ void f8_tile_product(const F8Args& a, int group) {
       }
     }
   } else {
-  for (int block = 0; block < blocks; ++block) {
+    for (int block = 0; block < blocks; ++block) {
 #pragma unroll
-    for (int i = 0; i < TM; ++i) sa[i] = next_a[i] >> ((block & 3) * 8);
+      for (int i = 0; i < TM; ++i) sa[i] = next_a[i] >> ((block & 3) * 8);
 #pragma unroll
-    for (int j = 0; j < TN; ++j) sb[j] = next_b[j] >> ((block & 3) * 8);
-    __builtin_amdgcn_sched_barrier(0);
+      for (int j = 0; j < TN; ++j) sb[j] = next_b[j] >> ((block & 3) * 8);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int step = 0; step < STEPS; ++step) {
-      const int done = (step + 1) * SB;  // bytes of this block whose fragments have been read
-      const int next = done < 128 ? block : block + 1, st = block * (128 / CB) + done / CB - 1;
-      if (done % CB == 0) {  // the next stage: it is there, and everyone has read this one, whose buffer is loaded anew
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        wait_loads_then_barrier<(RING - 2) * NL>();
-        if (done == 128) {
-          read_scales(block + 1);
-          load_scales(((block + 1) >> 2) + 1);
+      for (int step = 0; step < STEPS; ++step) {
+        const int done = (step + 1) * SB;  // bytes of this block whose fragments have been read
+        const int next = done < 128 ? block : block + 1, st = block * (128 / CB) + done / CB - 1;
+        if (done % CB == 0) {  // the next stage: it is there, and everyone has read this one, whose buffer is loaded anew
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          wait_loads_then_barrier<(RING - 2) * NL>();
+          if (done == 128) {
+            read_scales(block + 1);
+            load_scales(((block + 1) >> 2) + 1);
+          }
+          __builtin_amdgcn_sched_barrier(0);
         }
-        __builtin_amdgcn_sched_barrier(0);
+        multiply(step & 1, next, (step + 1) % STEPS, done % CB == 0, st + RING);  // (behind the last stage: zeros, not used)
       }
-      multiply(step & 1, next, (step + 1) % STEPS, done % CB == 0, st + RING);  // (behind the last stage: zeros, not used)
     }
-  }
   }
   // Output: a wave's 32 rows at a time through LDS (its own part of it), whole rows of the wave's columns from there.
   constexpr int WC = BN / WN, PITCH = WC + 4;  // floats (rows 16 bytes further along the banks)
@@ -788,7 +800,7 @@ __global__ __launch_bounds__(kFewThreads) void f8_few_backward_kernel(const F8Fe
   else f8_column_sums(w.sum, group - w.groups);
 }
 
-// The parts of sums that were split, in order, with what the products' output stage has.
+// The parts of sums that were split, in order, with what the products' output stage has: read once from the caches, 4 us for 16 parts of 256 x 1024.
 template <typename T>
 __global__ __launch_bounds__(256) void f8_join_kernel(const F8Args a, int parts) {
   constexpr int V = Elem<T>::VEC;
@@ -878,6 +890,7 @@ static void f8_tiles(const F8Args& a, int parts, hipStream_t s) {
       case 1288: return f8_tile<T, E5, EXACT, 128, 128, 4, 2, 2>(a, parts, s);
       case 1284: return f8_tile<T, E5, EXACT, 128, 128, 2, 2, 4>(a, parts, s);
       case 128644: return f8_tile<T, E5, EXACT, 128, 64, 2, 2, 4>(a, parts, s);
+      case 128642: return f8_tile<T, E5, EXACT, 128, 64, 2, 2, 2>(a, parts, s);
       case 644: return f8_tile<T, E5, EXACT, 64, 64, 2, 2, 4>(a, parts, s);
     }
   }
@@ -889,9 +902,13 @@ static void f8_tiles(const F8Args& a, int parts, hipStream_t s) {
   // The 256x256 one leaves a unit a single workgroup, so only where its last round is full enough, with short sums fuller (256x256, 128x128): 50176 ->
   // 1024 by 784 tiles, sums of 256 39.5, 37.3 / 63, 55, of 768 60, 64 / 104, 98; 20000 -> 2000 by 632, 256 41, 37 / 52, 45.5, 1024 63, 64 / 95, 95;
   // 8192 -> 4096 by 512, 256 21, 26 / 36, 37; 8192 -> 8192 by 1024, 128 - / 74, 47.
+  // With more than one and up to one and a half 128x128 tiles a unit units that have two end last: 128x64 ones with two buffers, three a unit, all in one round
+  // (128x128, 128x64; bfloat16 / float): 1001 x 2047 -> 4099 by 264, 520 20.2, 18.8 / 31.9, 29.0, x 512 10.3, 9.1 / 14.5, 13.0, x 8192 60, 57 / 103, 93;
+  // 2048 -> 2816 by 352, 704, x 512 10.5, 9.5 / 15.2, 14.2, x 8192 61.6, 62.1 / 109, 104; 2000 -> 4000 by 512, 1008, x 1000 15.9, 18.5 / 23.9, 26.0.
   auto tiles = [&](int bm, int bn) { return ceil_div(a.M, bm) * ceil_div(a.N, bn) * parts; };
   const int64_t large = tiles(256, 256), places = ceil_div(large, 256) * 256;
   if (large > 128 && !(EXACT && a.Kp <= 256) && (large <= 256 || large * 10 >= places * (a.Kp <= 1024 ? 9 : 8))) f8_tile<T, E5, EXACT, 256, 256, 2, 4, 2>(a, parts, s);
+  else if (tiles(128, 128) > 256 && tiles(128, 64) <= 768) f8_tile<T, E5, EXACT, 128, 64, 2, 2, 2>(a, parts, s);
   else if (tiles(128, 128) > 256) f8_tile<T, E5, EXACT, 128, 128, 4, 2, 2>(a, parts, s);
   else if (tiles(128, 128) > 128) f8_tile<T, E5, EXACT, 128, 128, 2, 2, 4>(a, parts, s);
   else if (tiles(128, 64) > 128) f8_tile<T, E5, EXACT, 128, 64, 2, 2, 4>(a, parts, s);
@@ -926,10 +943,6 @@ static void f8_product(F8Args a, int K, void* partial, hipStream_t s) {
   F8Parts parts = f8_parts(a.M, a.N, K, EXACT);
 #ifdef RN50_TUNING
   if (getenv("RN50_F8_TILE")) parts = F8Parts{1, a.Kp >> 7};
-  if (const char* e = getenv("RN50_F8_PARTS")) {
-    parts.part = static_cast<int>(align_up(static_cast<size_t>(ceil_div(a.Kp >> 7, atoi(e))), 4));
-    parts.count = static_cast<int>(ceil_div(a.Kp >> 7, parts.part));
-  }
 #endif
   if (parts.count == 1) {
     a.part = a.Kp >> 7;
