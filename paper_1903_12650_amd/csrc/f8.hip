@@ -891,11 +891,12 @@ static void f8_tiles(const F8Args& a, int parts, hipStream_t s) {
       case 1284: return f8_tile<T, E5, EXACT, 128, 128, 2, 2, 4>(a, parts, s);
       case 128644: return f8_tile<T, E5, EXACT, 128, 64, 2, 2, 4>(a, parts, s);
       case 128642: return f8_tile<T, E5, EXACT, 128, 64, 2, 2, 2>(a, parts, s);
+      case 642: return f8_tile<T, E5, EXACT, 64, 64, 2, 2, 2>(a, parts, s);
       case 644: return f8_tile<T, E5, EXACT, 64, 64, 2, 2, 4>(a, parts, s);
     }
   }
 #endif
-  // The largest tile of which there are enough for the 256 compute units, us (256x256, 128x128 by eight waves, by four with four buffers, 128x64, 64x64;
+  // The largest tile of which there are enough for the 256 compute units, us (256x256, 128x128 by eight waves, by four with four buffers, 128x64, 64x64 with four;
   // bfloat16 / float): 4096^3 59, 70, -, -, - / 105, 124, 135, 181, 189; 1001 x 2047 -> 4099 (68, 264, 264, 520, 1040 tiles) 26, 19, 25, 27, 24 /
   // 48, 31, 38, 41, 34; 4096 x 4096 -> 1024 (64, 256, 256, 512, 1024) 42, 25, 22, 30, 33 / 84, 37, 38, 47, 51; 512 x 4096 -> 4096 (32, 128, 128, 256, 512)
   // 42, 24, 19, 16.5, 18 / 83, 32, 32, 25, 26; 1000 x 2048 -> 1000 (16, 64, 64, 128, 256) 25, 14, 12, 10, 8 / 46, 18, 20, 14, 12.
@@ -905,12 +906,18 @@ static void f8_tiles(const F8Args& a, int parts, hipStream_t s) {
   // With more than one and up to one and a half 128x128 tiles a unit units that have two end last: 128x64 ones with two buffers, three a unit, all in one round
   // (128x128, 128x64; bfloat16 / float): 1001 x 2047 -> 4099 by 264, 520 20.2, 18.8 / 31.9, 29.0, x 512 10.3, 9.1 / 14.5, 13.0, x 8192 60, 57 / 103, 93;
   // 2048 -> 2816 by 352, 704, x 512 10.5, 9.5 / 15.2, 14.2, x 8192 61.6, 62.1 / 109, 104; 2000 -> 4000 by 512, 1008, x 1000 15.9, 18.5 / 23.9, 26.0.
+  // Four buffers pay with long sums a workgroup only.  256 tiles, 128x128 by eight waves and two buffers, by four and four, sums of 256, 1024, 4096, 8192:
+  // 6.6, 10.7, 26.6, 47.7 and 7.7, 10.7, 22.3, 37.3 / 9.2, 15.2, 37.1, 67 and 10.7, 16.1, 36.9, 64.  1024 -> 2000 by 512 64x64 with two buffers, by 256
+  // 128x64 with four, sums of 256, 512, 1024: 5.3, 6.0, 8.1 and 5.8, 6.5, 7.9 / 6.7, 7.9, 10.7 and 7.5, 8.4, 10.9; 300 -> 500 64x64, two and
+  // four: 4.4, 4.8, 6.1 and 4.6, 5.0, 6.2 / 4.9, 5.8, 7.7 and 5.0, 5.9, 7.7.
   auto tiles = [&](int bm, int bn) { return ceil_div(a.M, bm) * ceil_div(a.N, bn) * parts; };
   const int64_t large = tiles(256, 256), places = ceil_div(large, 256) * 256;
   if (large > 128 && !(EXACT && a.Kp <= 256) && (large <= 256 || large * 10 >= places * (a.Kp <= 1024 ? 9 : 8))) f8_tile<T, E5, EXACT, 256, 256, 2, 4, 2>(a, parts, s);
   else if (tiles(128, 128) > 256 && tiles(128, 64) <= 768) f8_tile<T, E5, EXACT, 128, 64, 2, 2, 2>(a, parts, s);
   else if (tiles(128, 128) > 256) f8_tile<T, E5, EXACT, 128, 128, 4, 2, 2>(a, parts, s);
+  else if (tiles(128, 128) > 128 && a.part <= (EXACT ? 32 : 8)) f8_tile<T, E5, EXACT, 128, 128, 4, 2, 2>(a, parts, s);
   else if (tiles(128, 128) > 128) f8_tile<T, E5, EXACT, 128, 128, 2, 2, 4>(a, parts, s);
+  else if (a.part <= 4) f8_tile<T, E5, EXACT, 64, 64, 2, 2, 2>(a, parts, s);
   else if (tiles(128, 64) > 128) f8_tile<T, E5, EXACT, 128, 64, 2, 2, 4>(a, parts, s);
   else f8_tile<T, E5, EXACT, 64, 64, 2, 2, 4>(a, parts, s);
 }
