@@ -305,7 +305,7 @@ __device__ __forceinline__ void f8_column_sums(const SumArgs& a, int group) {
 __global__ __launch_bounds__(256) void f8_column_sums_kernel(const SumArgs a) { f8_column_sums(a, blockIdx.x); }
 
 // ------------------------------------------------------------------ products
-// 16 numbers of a row as bfloat16, times the row's power of two: exact.
+// 16 numbers of a row as bfloat16, times a power of two: exact.
 template <bool E5>
 __device__ __forceinline__ void f8_to_bf16(i32x4 v, float scale, bf16x8* out) {
 #pragma unroll
@@ -320,7 +320,9 @@ __device__ __forceinline__ void f8_to_bf16(i32x4 v, float scale, bf16x8* out) {
       out[at >> 3][(at & 7) + 1] = two[1];
     }
 }
-__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
+// Half of a block's power: at the end of float's range q 2^e may be 2^128, past bfloat16's.  Sums of products of both halves are a quarter: kBack puts them right.
+__device__ __forceinline__ float half_scale(uint32_t byte) { return __uint_as_float(byte << 23) * 0.5f; }
+constexpr float kBack = 4.f;
 
 struct F8Args {
   const uint8_t *a, *w;
@@ -353,8 +355,8 @@ __device__ __forceinline__ void drop_columns(const F8Args& a, uint64_t call, int
 // (exact: 4 of its 8 bits), for v_mfma_f32_32x32x16_bf16, since the 8-bit matrix cores drop bits that a float result has.
 // Operands go from memory into LDS past the registers, RING stages of 128 numbers a row, a row's 16-byte pieces exchanged so that a fragment's reads touch all
 // banks.  What bounds it: large tiles' matrix cores, at the clock that their power leaves (8192^3 bfloat16 397 to 437 us, 2500 to 2770 TFLOP/s, of
-// zeros 317; 8192 x 4096 x 4096 into floats 195 to 223, 1230 to 1410); middle ones' time per 128 numbers, 0.85 us a 128x128 float tile, 0.43 of
-// it matrix cores, beside conversions and LDS; with short sums starts and ends (50176 x 256 -> 1024 bfloat16 37 us: 25 without the sum, 32 without
+// zeros 317; 8192 x 4096 x 4096 into floats 195 to 223, 1230 to 1410); middle ones' conversions and LDS reads beside the matrix cores (1001 x 2047 ->
+// 4099 into floats 27 to 29 us, matrix cores busy 35 %); with short sums starts and ends (50176 x 256 -> 1024 bfloat16 37 us: 25 without the sum, 32 without
 // the stores).  Four waves of 128x128 421 us where eight of 128x64 take 397; stages of 64 numbers, half lines of memory, 569.
 // Tiles go to the XCDs in runs, columns after columns of GROUP row tiles, so that an XCD's L2 sees both operands several times (GROUP 8: 495 us
 // to 492 at the time of its trial).
@@ -458,9 +460,9 @@ __device__ __forceinline__ void f8_tile_product(const F8Args& a, int group) {
     bf16x8 xa[EXACT ? TM : 1][2], xb[EXACT ? TN : 1][2];
     if constexpr (EXACT) {
 #pragma unroll
-      for (int j = 0; j < TN; ++j) f8_to_bf16<false>(fb[set][0][j], scale_of(sb[j] & 255u), xb[j]);
+      for (int j = 0; j < TN; ++j) f8_to_bf16<false>(fb[set][0][j], half_scale(sb[j] & 255u), xb[j]);
 #pragma unroll
-      for (int i = 0; i < TM; ++i) f8_to_bf16<E5>(fa[set][0][i], scale_of(sa[i] & 255u), xa[i]);
+      for (int i = 0; i < TM; ++i) f8_to_bf16<E5>(fa[set][0][i], half_scale(sa[i] & 255u), xa[i]);
     }
 #pragma unroll
     for (int n = 0; n < SLOTS; ++n) {
@@ -513,9 +515,9 @@ __device__ __forceinline__ void f8_tile_product(const F8Args& a, int group) {
     float fa_scale[TM], fb_scale[TN];
     auto take_scales = [&](int block) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < TM; ++i) fa_scale[i] = scale_of(next_a[i] >> ((block & 3) * 8) & 255u);
+      for (int i = 0; i < TM; ++i) fa_scale[i] = half_scale(next_a[i] >> ((block & 3) * 8) & 255u);
 #pragma unroll
-      for (int j = 0; j < TN; ++j) fb_scale[j] = scale_of(next_b[j] >> ((block & 3) * 8) & 255u);
+      for (int j = 0; j < TN; ++j) fb_scale[j] = half_scale(next_b[j] >> ((block & 3) * 8) & 255u);
     };
     auto convert = [&](int set) __attribute__((always_inline)) {
 #pragma unroll
@@ -613,7 +615,7 @@ __device__ __forceinline__ void f8_tile_product(const F8Args& a, int group) {
         if (m < a.M && col < a.N) {
           float f[V];
 #pragma unroll
-          for (int j = 0; j < V; ++j) f[j] = mine[row * PITCH + lane % LPR * V + j] + b[j];
+          for (int j = 0; j < V; ++j) f[j] = fmaf(mine[row * PITCH + lane % LPR * V + j], EXACT ? kBack : 1.f, b[j]);
           if (a.drop.threshold) drop_columns<V>(a, call, m, col, f);
           T* to = y + m * a.ldy + col;
           if (col + V <= a.N) {
@@ -646,7 +648,7 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_f8_kernel(const F8Args a)
 // Few rows (M <= 16 * MB): the weights go by once, bound by memory; a workgroup owns 16 * CB columns, its waves a part of K each.  A wave's lane has column
 // lane % 16 and 32 numbers at 32 * (lane / 16) of a block of 128, straight from memory, U blocks' loads in flight; they meet the rows' (the second
 // operand) in v_mfma_scale_f32_16x16x128_f8f6f4, or (EXACT) as bfloat16, times their power of two, in v_mfma_f32_16x16x32_bf16.  The waves' sums
-// are added through LDS, in order.
+// are added through LDS, in order.  1 x 2048 -> 1000 with the quantization 5.4 us, 40 x 2048 -> 1000 5.9, of them 2 to 3 the launch; 1 x 8192 -> 8192 18, 3.7 TB/s.
 // X: the rows are float or bfloat16 and quantized here, block by block as they are needed (a block's 128 numbers are four lanes'): no second launch.
 // (The rows' loads beside the weights', U blocks ahead, change nothing: 40 x 2048 -> 1000 6.0 -> 6.4 us, 40 x 8192 -> 8192 34.0 -> 33.5.)
 constexpr int kFewThreads = 512, kFewWaves = kFewThreads / 64;
@@ -704,8 +706,8 @@ __device__ __forceinline__ void f8_few_product(const F8FewArgs& a, int group) {
       for (int c = 0; c < CB; ++c) {
         scale_w[c] = sw[u][c];
         if constexpr (EXACT) {
-          f8_to_bf16<false>(fw[u][c][0], scale_of(sw[u][c]), w[c]);
-          f8_to_bf16<false>(fw[u][c][1], scale_of(sw[u][c]), w[c] + 2);
+          f8_to_bf16<false>(fw[u][c][0], half_scale(sw[u][c]), w[c]);
+          f8_to_bf16<false>(fw[u][c][1], half_scale(sw[u][c]), w[c] + 2);
         } else {
           w8[c] = __builtin_shufflevector(fw[u][c][0], fw[u][c][1], 0, 1, 2, 3, 4, 5, 6, 7);
         }
@@ -746,8 +748,8 @@ __device__ __forceinline__ void f8_few_product(const F8FewArgs& a, int group) {
         }
         if constexpr (EXACT) {
           bf16x8 v[4];
-          f8_to_bf16<E5>(q[0], scale_of(byte), v);
-          f8_to_bf16<E5>(q[1], scale_of(byte), v + 2);
+          f8_to_bf16<E5>(q[0], half_scale(byte), v);
+          f8_to_bf16<E5>(q[1], half_scale(byte), v + 2);
 #pragma unroll
           for (int c = 0; c < CB; ++c)
 #pragma unroll
@@ -775,7 +777,7 @@ __device__ __forceinline__ void f8_few_product(const F8FewArgs& a, int group) {
         float y = a.p.bias ? a.p.bias[n] : 0.f, sum = 0.f;
 #pragma unroll
         for (int v = 0; v < kFewWaves; ++v) sum += red[v][b][e & 255];
-        y += sum;
+        y = fmaf(sum, EXACT ? kBack : 1.f, y);
         if (a.p.drop.threshold) {
           const DropBits bits = drop_bits(a.p.drop, call, static_cast<uint64_t>(m) * static_cast<uint32_t>((N + 7) >> 3) + static_cast<uint32_t>(n >> 3));
           y = drop_keeps_at(a.p.drop, bits, n & 7) ? y * a.p.drop.factor : 0.f;
@@ -800,7 +802,7 @@ __global__ __launch_bounds__(kFewThreads) void f8_few_backward_kernel(const F8Fe
   else f8_column_sums(w.sum, group - w.groups);
 }
 
-// The parts of sums that were split, in order, with what the products' output stage has: read once from the caches, 4 us for 16 parts of 256 x 1024.
+// The parts of sums that were split, in order, with what the products' output stage has: read once from the caches, 4.5 us for 14 parts of 256 x 1024.
 template <typename T>
 __global__ __launch_bounds__(256) void f8_join_kernel(const F8Args a, int parts) {
   constexpr int V = Elem<T>::VEC;

@@ -285,6 +285,30 @@ def test_products_of_blocks_of_very_different_powers(rn):
             assert_within(rn.matmul_f8(256, a, sa, b, sb, dtype=y_type), want, product_error(y_type, 256, want, size))
 
 
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("M", [1, 3, 40, 70, 300, 1100])
+def test_products_at_the_end_of_the_range(rn, M, fmt):
+    """The types' largest and lowest numbers round to +-2^128, which is past float's range: what they are multiplied with brings them back, and zeros stay zeros."""
+    N, K = 90, 300
+    x, w = values(M, K, 1), values(N, K, 2, size=2.0 ** -30)
+    x[0, 5] = torch.finfo(F32).max
+    x[-1] = torch.finfo(BF16).min
+    x[:, 7] = 0
+    w[1], w[2] = 0, 0
+    w[2, 7] = torch.finfo(F32).max
+    a, sa, na = quantized(x, fmt)
+    b, sb, nb = quantized(w)
+    want, size = f8.matmul(na, nb)
+    assert np.abs(na).max() == 2.0 ** 128 and size.max() < 2.0 ** 120
+    for y_type in (F32, BF16):
+        bound = product_error(y_type, K, want, size)
+        y = rn.matmul_f8(K, a, sa, b, sb, dtype=y_type)
+        assert_within(y, want, bound, y_type)
+        assert (y[:, 1:3] == 0).all()
+        if fmt == f8.E4M3:
+            assert torch.equal(rn.fc_f8_fwd(x.cuda(), b, sb, dtype=y_type), y)
+
+
 @pytest.mark.parametrize("M", [3, 40, 100])
 def test_nan_blocks_reach_their_row_and_column_only(rn, M):
     x, w = values(M, 400, 1), values(70, 400, 2)
