@@ -309,6 +309,20 @@ def test_products_at_the_end_of_the_range(rn, M, fmt):
             assert torch.equal(rn.fc_f8_fwd(x.cuda(), b, sb, dtype=y_type), y)
 
 
+def test_products_of_the_smallest_numbers(rn):
+    """e5m2 numbers under the floor's power, down to 2^-131, below bfloat16's normal ones when they are converted: their products are exact."""
+    for M in (16, 70, 300):
+        x, w = torch.zeros(M, 128), torch.full((20, 128), 2.0 ** 60)
+        for i in range(12):
+            x[i, i] = 2.0 ** (-120 - i)
+        a, sa, na = quantized(x, f8.E5M2)
+        b, sb, nb = quantized(w)
+        want = f8.matmul(na, nb)[0]
+        assert (want[:12] == 2.0 ** (-60.0 - np.arange(12))[:, None]).all()
+        for y_type in (F32, BF16):
+            assert np.array_equal(f64(rn.matmul_f8(128, a, sa, b, sb, dtype=y_type)), want)
+
+
 @pytest.mark.parametrize("M", [3, 40, 100])
 def test_nan_blocks_reach_their_row_and_column_only(rn, M):
     x, w = values(M, 400, 1), values(70, 400, 2)
