@@ -354,7 +354,7 @@ __device__ __forceinline__ void drop_columns(const F8Args& a, uint64_t call, int
 // v_mfma_scale_f32_32x32x64_f8f6f4 as they are, the scaling costs nothing; EXACT (float results): fragments become bfloat16, times their power of two
 // (exact: 4 of its 8 bits), for v_mfma_f32_32x32x16_bf16, since the 8-bit matrix cores drop bits that a float result has.
 // Operands go from memory into LDS past the registers, RING stages of 128 numbers a row, a row's 16-byte pieces exchanged so that a fragment's reads touch all
-// banks.  What bounds it: large tiles' matrix cores, at the clock that their power leaves (8192^3 bfloat16 397 to 437 us, 2500 to 2770 TFLOP/s, of
+// banks.  What bounds it: large tiles' matrix cores, at the clock that their power leaves (8192^3 bfloat16 397 to 447 us, 2460 to 2770 TFLOP/s, of
 // zeros 317; 8192 x 4096 x 4096 into floats 195 to 223, 1230 to 1410); middle ones' conversions and LDS reads beside the matrix cores (1001 x 2047 ->
 // 4099 into floats 27 to 29 us, matrix cores busy 35 %); with short sums starts and ends (50176 x 256 -> 1024 bfloat16 37 us: 25 without the sum, 32 without
 // the stores).  Four waves of 128x128 421 us where eight of 128x64 take 397; stages of 64 numbers, half lines of memory, 569.
@@ -872,14 +872,21 @@ static F8Parts f8_parts(int M, int N, int K, bool exact) {
   const int64_t tiles = ceil_div(M, 128) * ceil_div(N, 128);
   int64_t n = 1;
   if (M > kFewRows) {
-    if (tiles <= 128 && blocks >= 48) n = std::min<int64_t>(256 / tiles, blocks / 8);
+    // Where tiles are few and sums long, so that both cover the card; the parts cost a second launch (parts, one 64x64 or 128x64 tile a sum; us by sums of 2048,
+    // 4096, 6200, 8192, 11000): float 300 -> 500 (12 tiles) 11.4, 11.9, 13.9, 15.4, 17.8 and 11.1, 18.4, 26.0, 32.7, 42.6, 500 -> 1000 (32) 13.0, 17.0,
+    // 22.6, 23.8, 26.1 and 11.3, 18.6, 26.2, 33.0, 42.8, 1000 -> 1000 (64) 17.2, 24.0, 28.8, 28.4, 34.5 and 11.7, 18.9, 27.0, 33.3, 43.3, 1024 -> 2000
+    // (128) 25.1, 29.6, 39.3, 43.1, 53.1 and 15.9, 25.6, 35.8, 44.9, 58.6; bfloat16 12 tiles 11.2, 12.0, 13.7, 16.0, 17.0 and 8.2, 12.5, 17.3, 21.3, 27.3,
+    // 32 11.7, 14.9, 19.7, 21.3, 22.3 and 8.3, 12.5, 17.2, 21.3, 27.2, 128 21.5, 23.2, 26.9, 29.1, 34.6 and 10.6, 16.4, 22.1, 27.7, 34.9.
+    const int least = exact ? (tiles <= 32 ? 32 : 64) : (tiles <= 16 ? 32 : 80);
+    if (tiles <= 128 && blocks >= least) n = std::min<int64_t>(256 / tiles, blocks / 8);
+    // (more than 16384 numbers into one float: its roundings)
     if (exact) n = std::max(n, std::min<int64_t>(16, ceil_div(blocks, 128)));
     if (tiles * n > (1 << 20)) n = 1;
   }
   const int part = static_cast<int>(align_up(static_cast<size_t>(ceil_div(blocks, n)), 4));
   return F8Parts{static_cast<int>(ceil_div(blocks, part)), part};
 }
-static size_t f8_partial_bytes(int M, int N, int K) {  // (with exact sums there are as many parts or more)
+static size_t f8_partial_bytes(int M, int N, int K) {  // (with exact sums there are as many parts or more, whatever the tiles)
   const F8Parts p = f8_parts(M, N, K, true);
   return p.count > 1 ? align_up(static_cast<size_t>(p.count) * M * N * 4, 256) : 0;
 }

@@ -234,7 +234,7 @@ def test_quantized_blocks_behind_a_dropout(rn, M, K, dtype):
 # ------------------------------------------------------------------- products
 MATMUL = [(1, 1, 1), (1, 1000, 2048), (3, 17, 127), (16, 40, 128), (17, 33, 300), (40, 1000, 2048), (64, 65, 513), (65, 70, 129),
           (127, 255, 513), (128, 128, 128), (130, 20, 1100), (300, 200, 640), (257, 511, 2047), (5, 2900, 700), (2, 9, 20000), (1100, 1300, 260),
-          (130, 70, 7000), (65, 9, 20000), (1480, 1420, 260), (2100, 2200, 130), (2900, 2890, 130),
+          (130, 70, 7000), (300, 500, 4100), (500, 600, 8200), (65, 9, 20000), (1480, 1420, 260), (2100, 2200, 130), (2900, 2890, 130),
           (2090, 2130, 700), (1000, 1100, 700), (1480, 1420, 4200), (3, 8193, 700), (40, 8200, 300), (64, 8210, 129), (20, 9000, 1300)]
 
 
