@@ -360,6 +360,25 @@ __device__ __forceinline__ void drop_columns(const F8Args& a, uint64_t call, int
 // the stores).  Four waves of 128x128 421 us where eight of 128x64 take 397; stages of 64 numbers, half lines of memory, 569.
 // Tiles go to the XCDs in runs, columns after columns of GROUP row tiles, so that an XCD's L2 sees both operands several times (GROUP 8: 495 us
 // to 492 at the time of its trial).
+// What a stage's loads are asked for: past the last stage nothing, from the beginning.  A lane's offset is checked against the length less the scalar
+// offset, a difference that must not go below 0 (no length behind an offset would leave the answer to how the hardware subtracts).
+struct StageRange {
+  uint32_t bytes, offset;
+};
+__host__ __device__ constexpr StageRange stage_range(uint32_t bytes, int st, int stages) {
+  return st < stages ? StageRange{bytes, static_cast<uint32_t>(st) * 128u} : StageRange{0, 0};
+}
+// Lanes ask for `at` of a row, 112 at most, of as many stages as a single row has.
+constexpr bool stages_stay_inside(int stages) {
+  for (int st = 0; st < stages + 8; ++st) {
+    const StageRange r = stage_range(static_cast<uint32_t>(stages) * 128u, st, stages);
+    if (r.offset > r.bytes) return false;
+    if ((112u + 16u <= r.bytes - r.offset) != (st < stages)) return false;
+  }
+  return true;
+}
+static_assert(stages_stay_inside(1) && stages_stay_inside(2) && stages_stay_inside(5) && stages_stay_inside(64), "stages past the sum ask for nothing");
+
 // LDS: RING stages and two groups' scales, where the output is staged afterwards.
 template <int BM, int BN, int WM, int WN, int RING>
 constexpr int f8_tile_lds() {
@@ -394,14 +413,16 @@ __device__ __forceinline__ void f8_tile_product(const F8Args& a, int group) {
   const uint32_t dst = __builtin_amdgcn_readfirstlane(base + static_cast<uint32_t>(wave) * 1024u);
   constexpr int NL = RA + RB;
   auto load_one = [&](int st, int l) __attribute__((always_inline)) {  // (l known when compiling)
-    const uint32_t so = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(st) * CB), to = dst + static_cast<uint32_t>(st & (RING - 1)) * STAGE;
+    const uint32_t to = dst + static_cast<uint32_t>(st & (RING - 1)) * STAGE;
     rsrc_words r = l < RA ? rsA : rsB;
     const uint32_t at = l < RA ? at_a[l < RA ? l : 0] : at_b[l < RA ? 0 : l - RA], by = l < RA ? l * (RPL * CB) : BM * CB + (l - RA) * (RPL * CB);
     if constexpr (RING == 2) {  // (nothing past the last stage: the waits are for all loads)
+      const uint32_t so = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(st) * CB);
       buffer_load16_to_lds_if(__builtin_amdgcn_readfirstlane(st < stages ? 1 : 0), r, to + by, at, so);
     } else {  // (past the last stage zeros, so that the waits' counts hold)
-      r.z = st < stages ? r.z : 0;
-      buffer_load16_to_lds(r, to + by, at, so);
+      const StageRange range = stage_range(static_cast<uint32_t>(r.z), st, stages);
+      r.z = static_cast<int>(range.bytes);
+      buffer_load16_to_lds(r, to + by, at, __builtin_amdgcn_readfirstlane(range.offset));
     }
   };
   // The scales of a group of four blocks are a dword a row, brought into LDS like the operands: 64 rows of the tile or of its columns a wave,
