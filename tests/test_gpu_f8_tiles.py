@@ -1,4 +1,4 @@
-"""Products in 8-bit floating point bit for bit.
+"""Products in 8-bit floating point by every tile, ring and split, bit for bit.
 
 The factors are small whole numbers times a power of two that differs from block to block and row to row: a, w in {-2, .., 2} * 2^{-1, 0, 1}.
 Products are multiples of 1/4 up to 16, all eight products that the 8-bit matrix cores add at once share a power (so the smallest is a quarter of
@@ -55,11 +55,55 @@ def check_product(rn, M, N, K, fmt, seed=1):
         assert (wide[:, N:] == 5).all()
 
 
+# Few rows: 16 to 64 of them, 16 or 32 columns a workgroup, a wave with no block, one, several.
+FEW = [(1, 40, 128), (1, 1000, 2048), (16, 33, 1100), (17, 70, 700), (33, 1000, 2048), (40, 8200, 1300), (48, 17, 20000), (64, 8201, 1500), (64, 64, 50176)]
 # 64x64 tiles by sums of one to four blocks and of more (past the last block their rings ask for nothing), single rows and columns in the last tile.
 SMALL = [(65, 65, k) for k in (1, 128, 256, 384, 512, 513, 640, 769, 1000, 1100, 1300, 2000)] + [(300, 200, 500), (193, 257, 2100)]
+# 128x64 tiles with four buffers; 128x128 ones by eight waves with two, by four with four; 128x64 with two, three a unit; 128x128 in many rounds.
+MIDDLE = [(1100, 1300, 700), (1025, 1281, 1500), (2000, 1500, 130), (2000, 1500, 1000), (1921, 1409, 1500), (2000, 1500, 4300), (2200, 2100, 130), (2177, 2113, 1500),
+          (2200, 2100, 4300), (6100, 4090, 600), (6017, 4097, 1500)]
+# 256x256 tiles: sums across groups of scales, ragged, outputs past the caches in float (32 MiB and more) and in both types.
+LARGE = [(2900, 2890, 1300), (2900, 2900, 260), (3329, 3073, 1100), (4090, 4000, 520), (7900, 4000, 1100), (8191, 4090, 2047)]
+# Sums in parts: few tiles and long sums, and sums of more than 16384 numbers whatever the tiles.
+PARTS = [(130, 70, 7000), (300, 500, 4100), (500, 600, 11000), (1024, 2000, 11000), (1000, 1030, 11000), (256, 1024, 50176), (2000, 1500, 20000), (4090, 4090, 16500),
+         (65, 9, 100000)]
 
 
 @pytest.mark.parametrize("fmt", [E4M3, E5M2])
-@pytest.mark.parametrize("M, N, K", SMALL)
+@pytest.mark.parametrize("M, N, K", FEW + SMALL + MIDDLE + LARGE + PARTS)
 def test_whole_numbers(rn, M, N, K, fmt):
     check_product(rn, M, N, K, fmt)
+
+
+@pytest.mark.parametrize("fmt", [E4M3, E5M2])
+@pytest.mark.parametrize("M, N, K", [(40, 1000, 700), (40, 2900, 300), (12, 300, 5000), (1300, 300, 700), (1100, 2900, 2900), (1024, 4090, 4000), (20000, 256, 1024), (50176, 256, 1000),
+                                     (20000, 64, 200)])
+def test_layer_of_whole_numbers(rn, M, N, K, fmt):
+    """Gradients of a layer of small whole numbers: they are quantized exactly, in either format, and a dropout of one half doubles what it keeps."""
+    g = torch.Generator(device="cuda").manual_seed(M + N)
+    x, w, dy = (torch.randint(-2, 3, s, device="cuda", generator=g).float() for s in ((M, K), (N, K), (M, N)))
+    drop = rn.Dropout(0.5, 7, 1)
+    kept = rn.dropout_fwd(torch.ones_like(x), drop)
+    _, _, wt, wts = rn.quant_blocks_f8(w, rows=False, columns=True)
+    _, _, xt, xts = rn.quant_blocks_f8(x, rows=False, columns=True, dropout=drop)
+    want_dx, want_dw, want_db = torch.matmul(dy, w) * kept, torch.matmul(dy.t().contiguous(), x * kept), dy.sum(0)
+    for dtype in (F32, BF16):
+        dx, dw, db = rn.fc_f8_bwd(dy.to(dtype), wt, wts, xt, xts, dtype=dtype, dropout=drop, format=fmt)
+        assert torch.equal(dx, want_dx.to(dtype)) and torch.equal(dw, want_dw) and torch.equal(db, want_db)
+        assert torch.equal(rn.fc_f8_bwd(dy.to(dtype), None, None, xt, xts, format=fmt, need_dx=False)[1], want_dw)
+
+
+@pytest.mark.parametrize("fmt", [E4M3, E5M2])
+@pytest.mark.parametrize("M, N, K", [(3, 70, 400), (40, 70, 400), (100, 70, 1000), (300, 90, 400), (1100, 1300, 1000), (2000, 1500, 1500), (2900, 2900, 700)])
+def test_nan_blocks(rn, M, N, K, fmt):
+    """A block of NaN on either side reaches its row or column and no other, in both formats."""
+    x, w = torch.ones((M, K), device="cuda"), torch.ones((N, K), device="cuda")
+    x[1, K - 1], x[M - 1, 0], w[5, 3], w[N - 1, 200] = float("nan"), float("inf"), float("-inf"), float("nan")
+    a, sa, _, _ = rn.quant_blocks_f8(x, fmt)
+    b, sb, _, _ = rn.quant_blocks_f8(w)
+    want = torch.full((M, N), float(K), device="cuda")
+    want[1], want[M - 1], want[:, 5], want[:, N - 1] = (float("nan"),) * 4
+    for y_type in (F32, BF16):
+        y = rn.matmul_f8(K, a, sa, b, sb, dtype=y_type)
+        assert torch.equal(torch.isnan(y), torch.isnan(want))
+        assert torch.equal(torch.nan_to_num(y), torch.nan_to_num(want.to(y_type)))
