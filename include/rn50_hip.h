@@ -540,7 +540,7 @@ int fc_f8_fwd(int M, int N, int K, int x_dtype, const void* x, int64_t ldx, cons
               void* workspace, size_t workspace_bytes, void* stream);
 /* Its backward pass.  dy [M,N] (device dy_dtype, rows ld_dy apart) is quantized to `format` along its rows and along its columns:
  *   dx[m,k] = drop(sum_n dy[m,n] w[n,k])   (drop: as dropout_bwd; dx_dtype, rows ld_dx apart)
- *   dW[n,k] = sum_m dy[m,n] x[m,k] (float [N,K]),   db[n] = sum_m dy[m,n] of dy as it is (float)
+ *   dW[n,k] = sum_m dy[m,n] x[m,k] (float [N,K]),   db[n] = sum_m dy[m,n] of dy as it is (summed in 64 bits; float)
  * wt [K, quant_f8_row_bytes(N)] and wt_scale: quant_blocks_f8's qt, scale_t of the weights [N,K]; xt, xt_scale: as fc_f8_fwd left
  * them.  Sums as in matmul_f8, by the result's type.  Each of dx, dW, db may be NULL and is left out then (wt with dx, xt with dW).  M, N <= 2^22. */
 size_t fc_f8_bwd_workspace_bytes(int M, int N, int K);

@@ -52,7 +52,7 @@ struct QuantArgs {
   int M, K, tiles_k;
   uint8_t *q, *scale, *qt, *scale_t;
   int Kp, Mp;
-  float* sums;  // float [row tiles][K]: the columns' sums of each tile of x as it is; or NULL
+  double* sums;  // [row tiles][K]: the columns' sums of each tile of x as it is; or NULL
   DropArgs drop;
 };
 // A tile of 16 * R rows by 128 columns in registers: thread t holds rows R * (t / 16) .. + R - 1 of the eight columns at 8 * (t % 16), the
@@ -82,19 +82,24 @@ __device__ __forceinline__ void quant_tile(const QuantArgs& a, int tile) {
   __shared__ uint32_t col_scale[COLS ? 128 : 1];
   __shared__ uint4 turned[COLS ? 1024 : 1];
   if (COLS && a.sums) {
-    float (*part)[128] = reinterpret_cast<float (*)[128]>(red);
+    // two columns' sums of a row group are 16 bytes, pair p of thread cg's four in place p ^ (cg / 4): 16 lanes' stores touch all banks
+    double2 (*part)[64] = reinterpret_cast<double2 (*)[64]>(turned);
+    static_assert(!COLS || sizeof(turned) >= 16 * 64 * sizeof(double2), "the row groups' sums fit");
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      float s = f[0][j];
+    for (int p = 0; p < 4; ++p) {
+      double2 s = make_double2(f[0][2 * p], f[0][2 * p + 1]);
 #pragma unroll
-      for (int i = 1; i < R; ++i) s += f[i][j];
-      part[rg][cg * 8 + j] = s;
+      for (int i = 1; i < R; ++i) {
+        s.x += f[i][2 * p];
+        s.y += f[i][2 * p + 1];
+      }
+      part[rg][cg * 4 + (p ^ (cg >> 2))] = s;
     }
     __syncthreads();
     if (tid < 128 && tk * 128 + tid < a.K) {
-      float s = 0.f;
+      double s = 0.0;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s += part[i][tid];
+      for (int i = 0; i < 16; ++i) s += reinterpret_cast<const double*>(part[i])[(tid >> 1 ^ tid >> 5) * 2 + (tid & 1)];
       a.sums[static_cast<int64_t>(tm) * a.K + tk * 128 + tid] = s;
     }
     __syncthreads();
@@ -216,12 +221,13 @@ __device__ __forceinline__ void quant_columns(const QuantArgs& a, int tile) {
       for (int j = 0; j < 8; ++j) f[i][j] = m0 + i < a.M && j < cols ? Elem<T>::load(row + j) : 0.f;
     }
   }
-  __shared__ float red[2][64][33];
+  __shared__ uint32_t red[64][33];
+  __shared__ __align__(16) double part[64][33];
   __shared__ uint32_t col_scale[32];
-  __shared__ uint4 turned[256];
+  uint4* turned = reinterpret_cast<uint4*>(part);  // (behind the sums)
   if (a.sums) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) red[0][rg][cg * 8 + j] = f[0][j] + f[1][j];
+    for (int j = 0; j < 8; ++j) part[rg][cg * 8 + j] = static_cast<double>(f[0][j]) + f[1][j];
   }
   if constexpr (DROP) {
     const uint64_t call = drop_call(a.drop), per_row = static_cast<uint64_t>((a.K + 7) >> 3);
@@ -233,14 +239,14 @@ __device__ __forceinline__ void quant_columns(const QuantArgs& a, int tile) {
     }
   }
 #pragma unroll
-  for (int j = 0; j < 8; ++j) red[1][rg][cg * 8 + j] = __uint_as_float(max(magnitude(f[0][j]), magnitude(f[1][j])));
+  for (int j = 0; j < 8; ++j) red[rg][cg * 8 + j] = max(magnitude(f[0][j]), magnitude(f[1][j]));
   __syncthreads();
-  if (tid < 64) {  // half a wave the largest magnitudes, the other half the sums
+  if ((tid & 63) < 32 && tid < 128) {  // half a wave the largest magnitudes, half of another the sums
     const int c = tid & 31, k = tk * 32 + c;
     if (tid < 32) {
       uint32_t top = 0;
 #pragma unroll 16
-      for (int i = 0; i < 64; ++i) top = max(top, __float_as_uint(red[1][i][c]));
+      for (int i = 0; i < 64; ++i) top = max(top, red[i][c]);
       float inv;
       bool finite;
       const uint32_t byte = f8_scale<E5>(top, &inv, &finite);
@@ -252,9 +258,9 @@ __device__ __forceinline__ void quant_columns(const QuantArgs& a, int tile) {
           for (int j = (tm & 3) + 1; j < 4; ++j) s[j] = 0;
       }
     } else if (a.sums && k < a.K) {
-      float s = 0.f;
+      double s = 0.0;
 #pragma unroll 16
-      for (int i = 0; i < 64; ++i) s += red[0][i][c];
+      for (int i = 0; i < 64; ++i) s += part[i][c];
       a.sums[static_cast<int64_t>(tm) * a.K + k] = s;
     }
   }
@@ -279,10 +285,12 @@ __global__ __launch_bounds__(256) void quant_small_kernel(const QuantArgs a, int
   else quant_columns<T, E5, DROP>(a, blockIdx.x - row_tiles);
 }
 
-// db[n] = the sum of the row tiles' sums: four threads a column, each every fourth tile in order, then the four; the same order whichever kernel
-// has it along (a launch of its own for these few bytes costs 4 us, and with one thread a column 90 us at 392 tiles of 256 columns).
+// db[n] = the sum of the row tiles' sums, all of it in 64 bits: a gradient's columns all but cancel, and floats over a tile's 128 rows cost three times the
+// error (backward pass of 50176 x 1024 -> 256 85.4 -> 86.3 us, of 8192 x 4096 -> 4096 329.6 -> 331.2).  Four threads a column, each every fourth tile in
+// order, then the four; the same order whichever kernel has it along (a launch of its own for these few bytes costs 4 us, and with one thread a column 90 us
+// at 392 tiles of 256 columns).
 struct SumArgs {
-  const float* sums;
+  const double* sums;
   int tiles, N;
   float* db;
 };
@@ -1063,7 +1071,7 @@ static void quant_typed(const QuantArgs& a, int format, bool past, hipStream_t s
   }
 }
 static void quant_run(int M, int K, int dtype, const void* x, int64_t ldx, const rn50_dropout* drop, int format, uint8_t* q, uint8_t* scale,
-                      uint8_t* qt, uint8_t* scale_t, float* sums, bool past, hipStream_t s) {
+                      uint8_t* qt, uint8_t* scale_t, double* sums, bool past, hipStream_t s) {
   const QuantArgs a{x, ldx, M, K, static_cast<int>(ceil_div(K, 128)), q, scale, qt, scale_t, static_cast<int>(quant_f8_row_bytes(K)),
                     static_cast<int>(quant_f8_row_bytes(M)), sums, drop_args(drop)};
   if (dtype == RN50_BF16) quant_typed<uint16_t>(a, format, past, s);
@@ -1227,7 +1235,7 @@ extern "C" size_t fc_f8_bwd_workspace_bytes(int M, int N, int K) {
   parts.take(quant_f8_scale_bytes(M, N));
   parts.take(static_cast<size_t>(N) * quant_f8_row_bytes(M));
   parts.take(quant_f8_scale_bytes(N, M));
-  parts.take(static_cast<size_t>(ceil_div(M, 128)) * N * 4);
+  parts.take(static_cast<size_t>(ceil_div(M, 128)) * N * sizeof(double));
   return parts.used + std::max(f8_partial_bytes(M, K, N), f8_partial_bytes(N, K, M));
 }
 
@@ -1261,7 +1269,7 @@ extern "C" int fc_f8_bwd(int M, int N, int K, int dy_dtype, const void* dy, int6
   uint8_t* qt = parts.take(static_cast<size_t>(N) * quant_f8_row_bytes(M));
   uint8_t* qts = parts.take(quant_f8_scale_bytes(N, M));
   const int tiles = static_cast<int>(ceil_div(M, 128));
-  float* sums = parts.take<float>(static_cast<size_t>(tiles) * N * 4);
+  double* sums = parts.take<double>(static_cast<size_t>(tiles) * N * sizeof(double));
   quant_run(M, N, dy_dtype, dy, ld_dy, nullptr, format, dx ? q : nullptr, qs, dW ? qt : nullptr, qts, db ? sums : nullptr, false, s);
   void* partial = parts.take(0);
   const SumArgs sum{sums, tiles, N, db};
