@@ -12,6 +12,7 @@ namespace rn50 {
 
 constexpr int kF8MaxK = 1 << 22;        // 256 rows of it stay inside a buffer descriptor's 32 bits
 constexpr uint32_t kF8Floor = 27u << 23;  // the bits of 2^-100: blocks below are quantized as if this were their largest magnitude
+constexpr int kFloatBlocks = 128;         // blocks of 128 numbers that one float of an exact sum takes: its roundings
 constexpr int64_t kPastBytes = 32 << 20;  // outputs that the L2s would not hold for the next kernel are stored past the caches
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
@@ -680,7 +681,10 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_f8_kernel(const F8Args a)
 // are added through LDS, in order.  1 x 2048 -> 1000 with the quantization 5.4 us, 40 x 2048 -> 1000 5.9, of them 2 to 3 the launch; 1 x 8192 -> 8192 18, 3.7 TB/s.
 // X: the rows are float or bfloat16 and quantized here, block by block as they are needed (a block's 128 numbers are four lanes'): no second launch.
 // (The rows' loads beside the weights', U blocks ahead, change nothing: 40 x 2048 -> 1000 6.0 -> 6.4 us, 40 x 8192 -> 8192 34.0 -> 33.5.)
+// FOLD (EXACT, sums of which a wave has more than kFloatBlocks blocks): a register takes that many before it is added to the others, in registers that the
+// other kernels do without (32 rows' ones have just enough for two workgroups a unit: 24 x 4096 -> 7000 14.1 us, with them 14.4).
 constexpr int kFewThreads = 512, kFewWaves = kFewThreads / 64;
+constexpr int kFewLong = kFewWaves * kFloatBlocks * 128;
 struct F8FewArgs {
   F8Args p;
   const void* x;
@@ -690,7 +694,7 @@ struct F8FewArgs {
 __device__ __forceinline__ uint32_t scale_byte(const uint32_t* scales, int rows, int row, int block) {
   return reinterpret_cast<const uint8_t*>(scales)[(static_cast<int64_t>(block >> 2) * rows + row) * 4 + (block & 3)];
 }
-template <typename T, bool E5, bool EXACT, int MB, int CB, typename X>
+template <typename T, bool E5, bool EXACT, int MB, int CB, typename X, bool FOLD = false>
 __device__ __forceinline__ void f8_few_product(const F8FewArgs& a, int group) {
   constexpr bool FUSED = !std::is_void<X>::value;
   constexpr int U = FUSED || CB > 1 ? 2 : 4;
@@ -723,7 +727,26 @@ __device__ __forceinline__ void f8_few_product(const F8FewArgs& a, int group) {
   for (int c = 0; c < CB; ++c)
 #pragma unroll
     for (int b = 0; b < MB; ++b) acc[c][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+  f32x4 folded[FOLD ? CB : 1][MB];
+  if constexpr (FOLD) {
+#pragma unroll
+    for (int c = 0; c < CB; ++c)
+#pragma unroll
+      for (int b = 0; b < MB; ++b) folded[c][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  auto fold = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int c = 0; c < CB; ++c)
+#pragma unroll
+      for (int b = 0; b < MB; ++b) {
+        folded[c][b] += acc[c][b];
+        acc[c][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+  };
   for (int s = from; s < to; s += U) {
+    if constexpr (FOLD) {
+      if (((s - from) & (kFloatBlocks - 1)) == 0) fold();
+    }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int k = s + u;
@@ -792,6 +815,13 @@ __device__ __forceinline__ void f8_few_product(const F8FewArgs& a, int group) {
       }
     }
   }
+  if constexpr (FOLD) {
+    fold();
+#pragma unroll
+    for (int c = 0; c < CB; ++c)
+#pragma unroll
+      for (int b = 0; b < MB; ++b) acc[c][b] = folded[c][b];
+  }
   const uint64_t call = a.p.drop.threshold ? drop_call(a.p.drop) : 0;
   // column 4 * (lane / 16) + i of the 16, row lane % 16
 #pragma unroll
@@ -817,9 +847,9 @@ __device__ __forceinline__ void f8_few_product(const F8FewArgs& a, int group) {
   }
 }
 
-template <typename T, bool E5, int MB, int CB, typename X>
+template <typename T, bool E5, int MB, int CB, typename X, bool FOLD>
 __global__ __launch_bounds__(kFewThreads) void matmul_f8_few_kernel(const F8FewArgs a) {
-  f8_few_product<T, E5, sizeof(T) == 4, MB, CB, X>(a, blockIdx.x);
+  f8_few_product<T, E5, sizeof(T) == 4, MB, CB, X, FOLD>(a, blockIdx.x);
 }
 // The two products of a backward pass of few rows in one launch: the input's gradient by the first workgroups, the weights' (a sum of one
 // block) by tiles, and the bias's behind them.
@@ -908,8 +938,8 @@ static F8Parts f8_parts(int M, int N, int K, bool exact) {
     // 32 11.7, 14.9, 19.7, 21.3, 22.3 and 8.3, 12.5, 17.2, 21.3, 27.2, 128 21.5, 23.2, 26.9, 29.1, 34.6 and 10.6, 16.4, 22.1, 27.7, 34.9.
     const int least = exact ? (tiles <= 32 ? 32 : 64) : (tiles <= 16 ? 32 : 80);
     if (tiles <= 128 && blocks >= least) n = std::min<int64_t>(256 / tiles, blocks / 8);
-    // (more than 16384 numbers into one float: its roundings)
-    if (exact) n = std::max(n, std::min<int64_t>(16, ceil_div(blocks, 128)));
+    // (for the floats' roundings; up to 16 parts, since each is a matrix of its own)
+    if (exact) n = std::max(n, std::min<int64_t>(16, ceil_div(blocks, kFloatBlocks)));
     if (tiles * n > (1 << 20)) n = 1;
   }
   const int part = static_cast<int>(align_up(static_cast<size_t>(ceil_div(blocks, n)), 4));
@@ -961,7 +991,9 @@ static void f8_tiles(const F8Args& a, int parts, hipStream_t s) {
 }
 template <typename T, bool E5, int MB, int CB, typename X>
 static void f8_few_columns(const F8FewArgs& a, hipStream_t s) {
-  RN50_LAUNCH("matmul_f8", (matmul_f8_few_kernel<T, E5, MB, CB, X>), dim3(static_cast<unsigned>(ceil_div(a.p.N, 16 * CB))), dim3(kFewThreads), 0, s, a);
+  const dim3 grid(static_cast<unsigned>(ceil_div(a.p.N, 16 * CB)));
+  if (sizeof(T) == 4 && a.p.Kp > kFewLong) RN50_LAUNCH("matmul_f8", (matmul_f8_few_kernel<T, E5, MB, CB, X, sizeof(T) == 4>), grid, dim3(kFewThreads), 0, s, a);
+  else RN50_LAUNCH("matmul_f8", (matmul_f8_few_kernel<T, E5, MB, CB, X, false>), grid, dim3(kFewThreads), 0, s, a);
 }
 template <typename T, bool E5, int MB, typename X>
 static void f8_few(const F8FewArgs& a, hipStream_t s) {
@@ -1015,7 +1047,7 @@ static void f8_run(int a_format, int y_dtype, const F8Args& a, int K, void* part
 // Both products of a backward pass in one launch: few rows (whose sum into the weights is one block), more outputs than the few rows' kernel would take, and
 // an input's gradient that leaves room on the card beside the weights'.  One launch, two (M x K -> N, us): 40 x 2048 -> 1000 12.3, 15.8, 40 x 2048 ->
 // 2048 17.5, 21.0, 64 x 1024 -> 16384 48, 63, 8 x 4096 -> 8192 42, 45; 40 x 4096 -> 2048 22.9, 20.4, 40 x 4096 -> 4096 38, 31, 40 x 8192 -> 8192 122, 81.
-static bool f8_few_backward_fits(int M, int N, int K) { return M <= kFewRows && N > kFewRows && (M <= 16 || K <= 2048); }
+static bool f8_few_backward_fits(int M, int N, int K) { return M <= kFewRows && N > kFewRows && N <= kFewLong && (M <= 16 || K <= 2048); }
 template <typename T, bool E5>
 static void f8_few_backward(F8Args x, F8Args w, hipStream_t s) {
   constexpr int lds = f8_tile_lds<128, 128, 4, 2, 2>();
