@@ -525,16 +525,19 @@ int quant_blocks_f8(int M, int K, int dtype, const void* x, int64_t ldx, const r
                     uint8_t* scale, uint8_t* qt, uint8_t* scale_t, void* stream);
 /* y[m,n] = sum_k a[m,k] * w[n,k] + bias[n] of the numbers that a (a_format) and w (RN50_E4M3) stand for, rounded to y's type.
  * a [M,row bytes], w [N,row bytes], their scales: device, as quant_blocks_f8 leaves them; bias float[N] or NULL; y: device
- * y_dtype, rows of N elements ldy >= N elements apart.  With y_dtype RN50_F32 products and sums are float.  With RN50_BF16 they are
+ * y_dtype, rows of N elements ldy >= N elements apart.  workspace: *_workspace_bytes_for() with what the call is given; *_workspace_bytes()
+ * is enough for every call of that size, here and below.  With y_dtype RN50_F32 products and sums are float.  With RN50_BF16 they are
  * those of the 8-bit matrix cores, which keep of every eight products the bits down to 2^-13 of the largest one's: the sum is off by
  * at most 2^-10 of the sum of the products' magnitudes (2e-5 of the result's size with normally distributed numbers, a hundredth of y's rounding). */
 size_t matmul_f8_workspace_bytes(int M, int N, int K);
+size_t matmul_f8_workspace_bytes_for(int M, int N, int K, int y_dtype);
 int matmul_f8(int M, int N, int K, int a_format, const uint8_t* a, const uint8_t* a_scale, const uint8_t* w, const uint8_t* w_scale,
               const float* bias, int y_dtype, void* y, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream);
 /* A linear layer's forward pass: x (behind dropout, or NULL) is quantized by rows to RN50_E4M3 and multiplied with w [N,row bytes].
  * xt, xt_scale (both or neither): the same numbers quantized along the batch, as quant_blocks_f8's qt, scale_t: what fc_f8_bwd
  * takes (M <= 2^22). */
 size_t fc_f8_fwd_workspace_bytes(int M, int N, int K);
+size_t fc_f8_fwd_workspace_bytes_for(int M, int N, int K, int y_dtype);
 int fc_f8_fwd(int M, int N, int K, int x_dtype, const void* x, int64_t ldx, const rn50_dropout* dropout, const uint8_t* w,
               const uint8_t* w_scale, const float* bias, int y_dtype, void* y, int64_t ldy, uint8_t* xt, uint8_t* xt_scale,
               void* workspace, size_t workspace_bytes, void* stream);
@@ -544,6 +547,7 @@ int fc_f8_fwd(int M, int N, int K, int x_dtype, const void* x, int64_t ldx, cons
  * wt [K, quant_f8_row_bytes(N)] and wt_scale: quant_blocks_f8's qt, scale_t of the weights [N,K]; xt, xt_scale: as fc_f8_fwd left
  * them.  Sums as in matmul_f8, by the result's type.  Each of dx, dW, db may be NULL and is left out then (wt with dx, xt with dW).  M, N <= 2^22. */
 size_t fc_f8_bwd_workspace_bytes(int M, int N, int K);
+size_t fc_f8_bwd_workspace_bytes_for(int M, int N, int K, int dx_dtype, int dx, int dW, int db); /* (dx, dW, db: 0 where it will be NULL) */
 int fc_f8_bwd(int M, int N, int K, int dy_dtype, const void* dy, int64_t ld_dy, int format, const uint8_t* wt, const uint8_t* wt_scale,
               const uint8_t* xt, const uint8_t* xt_scale, const rn50_dropout* dropout, int dx_dtype, void* dx, int64_t ld_dx,
               float* dW, float* db, void* workspace, size_t workspace_bytes, void* stream);

@@ -84,7 +84,8 @@ for _n in ("conv_fwd_workspace_bytes", "conv_dgrad_workspace_bytes", "conv_wgrad
            "resnet_plan_workspace_bytes", "conv_bn_sums_bytes", "resnet_train_state_bytes",
            "bn_relu_infer_workspace_bytes", "quant_i8_row_bytes", "fc_i8_workspace_bytes", "topk_rows_workspace_bytes",
            "distill_workspace_bytes", "quant_f8_row_bytes", "quant_f8_scale_bytes", "matmul_f8_workspace_bytes",
-           "fc_f8_fwd_workspace_bytes", "fc_f8_bwd_workspace_bytes"):
+           "fc_f8_fwd_workspace_bytes", "fc_f8_bwd_workspace_bytes", "matmul_f8_workspace_bytes_for", "fc_f8_fwd_workspace_bytes_for",
+           "fc_f8_bwd_workspace_bytes_for"):
     if hasattr(raw, _n):
         getattr(raw, _n).restype = ctypes.c_size_t
 for _n in ("resnet_plan_tensor_shape", "resnet_plan_tensor_offset", "resnet_plan_arena_elems", "resnet_plan_bn_channels",
@@ -133,12 +134,16 @@ def _stream():
     return ctypes.c_void_p(_raw_stream())
 
 
-def _dt(t):
-    if t.dtype == torch.float32:
+def _dtype(dtype):
+    if dtype == torch.float32:
         return F32
-    if t.dtype == torch.bfloat16:
+    if dtype == torch.bfloat16:
         return BF16
-    raise TypeError(f"unsupported dtype {t.dtype}")
+    raise TypeError(f"unsupported dtype {dtype}")
+
+
+def _dt(t):
+    return _dtype(t.dtype)
 
 
 def _ws(nbytes, device):
@@ -424,8 +429,9 @@ def quant_blocks_f8(x, format=torch.float8_e4m3fn, rows=True, columns=False, dro
     return _ops.quant_blocks_f8(x, format, rows, columns, dropout)
 
 
-def matmul_f8_workspace_bytes(M, N, K):
-    return raw.matmul_f8_workspace_bytes(M, N, K)
+def matmul_f8_workspace_bytes(M, N, K, dtype=torch.float32):
+    """Of a result of that type (float: enough for either)."""
+    return raw.matmul_f8_workspace_bytes_for(M, N, K, _dtype(dtype))
 
 
 def matmul_f8(K, a, a_scale, w, w_scale, bias=None, dtype=torch.float32, y=None, workspace=None):
@@ -433,8 +439,9 @@ def matmul_f8(K, a, a_scale, w, w_scale, bias=None, dtype=torch.float32, y=None,
     return _ops.matmul_f8(K, a, a_scale, w, w_scale, bias, dtype, y, workspace)
 
 
-def fc_f8_fwd_workspace_bytes(M, N, K):
-    return raw.fc_f8_fwd_workspace_bytes(M, N, K)
+def fc_f8_fwd_workspace_bytes(M, N, K, dtype=torch.float32):
+    """Of a result of that type (float: enough for either)."""
+    return raw.fc_f8_fwd_workspace_bytes_for(M, N, K, _dtype(dtype))
 
 
 def fc_f8_fwd(x, w, w_scale, bias=None, dtype=torch.float32, dropout=None, save=False, y=None, workspace=None):
@@ -443,8 +450,9 @@ def fc_f8_fwd(x, w, w_scale, bias=None, dtype=torch.float32, dropout=None, save=
     return _ops.fc_f8_fwd(x, w, w_scale, bias, dtype, dropout, save, y, workspace)
 
 
-def fc_f8_bwd_workspace_bytes(M, N, K):
-    return raw.fc_f8_bwd_workspace_bytes(M, N, K)
+def fc_f8_bwd_workspace_bytes(M, N, K, dtype=torch.float32, need_dx=True, need_dw=True, need_db=True):
+    """Of the gradients that are needed, dx of that type (the defaults: enough for every call)."""
+    return raw.fc_f8_bwd_workspace_bytes_for(M, N, K, _dtype(dtype), int(need_dx), int(need_dw), int(need_db))
 
 
 def fc_f8_bwd(dy, wt, wt_scale, xt, xt_scale, dtype=torch.float32, dropout=None, format=torch.float8_e4m3fn, need_dx=True, need_dw=True,

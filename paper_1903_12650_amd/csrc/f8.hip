@@ -945,8 +945,8 @@ static F8Parts f8_parts(int M, int N, int K, bool exact) {
   const int part = static_cast<int>(align_up(static_cast<size_t>(ceil_div(blocks, n)), 4));
   return F8Parts{static_cast<int>(ceil_div(blocks, part)), part};
 }
-static size_t f8_partial_bytes(int M, int N, int K) {  // (with exact sums there are as many parts or more, whatever the tiles)
-  const F8Parts p = f8_parts(M, N, K, true);
+static size_t f8_partial_bytes(int M, int N, int K, int y_dtype) {  // (float results: as many parts as others or more, whatever the tiles)
+  const F8Parts p = f8_parts(M, N, K, y_dtype != RN50_BF16);
   return p.count > 1 ? align_up(static_cast<size_t>(p.count) * M * N * 4, 256) : 0;
 }
 template <typename T, bool E5, bool EXACT>
@@ -1195,9 +1195,10 @@ extern "C" int quant_blocks_f8(int M, int K, int dtype, const void* x, int64_t l
   return launch_status(who);
 }
 
-extern "C" size_t matmul_f8_workspace_bytes(int M, int N, int K) {
-  return M < 1 || N < 1 || quant_f8_row_bytes(K) == 0 ? 0 : f8_partial_bytes(M, N, K);
+extern "C" size_t matmul_f8_workspace_bytes_for(int M, int N, int K, int y_dtype) {
+  return M < 1 || N < 1 || quant_f8_row_bytes(K) == 0 ? 0 : f8_partial_bytes(M, N, K, y_dtype);
 }
+extern "C" size_t matmul_f8_workspace_bytes(int M, int N, int K) { return matmul_f8_workspace_bytes_for(M, N, K, RN50_F32); }
 
 extern "C" int matmul_f8(int M, int N, int K, int a_format, const uint8_t* a, const uint8_t* a_scale, const uint8_t* w, const uint8_t* w_scale,
                          const float* bias, int y_dtype, void* y, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream) {
@@ -1211,18 +1212,19 @@ extern "C" int matmul_f8(int M, int N, int K, int a_format, const uint8_t* a, co
   if (int rc = check_matrix(who, M, N, y_dtype, y, ldy)) return rc;
   RN50_REQUIRE(aligned_to(bias, 4), RN50_ERR_ALIGN, "%s: pointer not aligned to an element", who);
   if (int rc = check_product_size(who, M, N)) return rc;
-  if (int rc = check_workspace(who, workspace, workspace_bytes, matmul_f8_workspace_bytes(M, N, K))) return rc;
+  if (int rc = check_workspace(who, workspace, workspace_bytes, matmul_f8_workspace_bytes_for(M, N, K, y_dtype))) return rc;
   f8_run(a_format, y_dtype, product_args(M, N, K, a, a_scale, w, w_scale, bias, y, ldy, nullptr), K, workspace, static_cast<hipStream_t>(stream));
   return launch_status(who);
 }
 
-extern "C" size_t fc_f8_fwd_workspace_bytes(int M, int N, int K) {
+extern "C" size_t fc_f8_fwd_workspace_bytes_for(int M, int N, int K, int y_dtype) {
   if (M < 1 || N < 1 || quant_f8_row_bytes(K) == 0) return 0;
   Parts parts{nullptr};
   parts.take(static_cast<size_t>(M) * quant_f8_row_bytes(K));
   parts.take(quant_f8_scale_bytes(M, K));
-  return parts.used + matmul_f8_workspace_bytes(M, N, K);
+  return parts.used + matmul_f8_workspace_bytes_for(M, N, K, y_dtype);
 }
+extern "C" size_t fc_f8_fwd_workspace_bytes(int M, int N, int K) { return fc_f8_fwd_workspace_bytes_for(M, N, K, RN50_F32); }
 
 extern "C" int fc_f8_fwd(int M, int N, int K, int x_dtype, const void* x, int64_t ldx, const rn50_dropout* dropout, const uint8_t* w,
                          const uint8_t* w_scale, const float* bias, int y_dtype, void* y, int64_t ldy, uint8_t* xt, uint8_t* xt_scale,
@@ -1242,7 +1244,7 @@ extern "C" int fc_f8_fwd(int M, int N, int K, int x_dtype, const void* x, int64_
   }
   if (int rc = check_product_size(who, M, N)) return rc;
   if (int rc = check_tiles(who, M, K, xt ? 128 : 32, 128)) return rc;
-  if (int rc = check_workspace(who, workspace, workspace_bytes, fc_f8_fwd_workspace_bytes(M, N, K))) return rc;
+  if (int rc = check_workspace(who, workspace, workspace_bytes, fc_f8_fwd_workspace_bytes_for(M, N, K, y_dtype))) return rc;
   hipStream_t s = static_cast<hipStream_t>(stream);
   Parts parts{static_cast<uint8_t*>(workspace)};
   uint8_t* q = parts.take(static_cast<size_t>(M) * quant_f8_row_bytes(K));
@@ -1260,16 +1262,31 @@ extern "C" int fc_f8_fwd(int M, int N, int K, int x_dtype, const void* x, int64_
   return launch_status(who);
 }
 
-extern "C" size_t fc_f8_bwd_workspace_bytes(int M, int N, int K) {
-  if (quant_f8_row_bytes(M) == 0 || quant_f8_row_bytes(N) == 0 || K < 1) return 0;
-  Parts parts{nullptr};
-  parts.take(static_cast<size_t>(M) * quant_f8_row_bytes(N));
-  parts.take(quant_f8_scale_bytes(M, N));
-  parts.take(static_cast<size_t>(N) * quant_f8_row_bytes(M));
-  parts.take(quant_f8_scale_bytes(N, M));
-  parts.take(static_cast<size_t>(ceil_div(M, 128)) * N * sizeof(double));
-  return parts.used + std::max(f8_partial_bytes(M, K, N), f8_partial_bytes(N, K, M));
+// The parts of a backward pass's workspace: what is not asked for has none.
+struct BackwardParts {
+  uint8_t *q, *qs, *qt, *qts;
+  double* sums;
+  void* partial;
+  size_t bytes;
+};
+static BackwardParts backward_parts(void* workspace, int M, int N, int K, int dx_dtype, bool dx, bool dW, bool db) {
+  Parts parts{static_cast<uint8_t*>(workspace)};
+  BackwardParts b;
+  b.q = parts.take(dx ? static_cast<size_t>(M) * quant_f8_row_bytes(N) : 0);
+  b.qs = parts.take(dx ? quant_f8_scale_bytes(M, N) : 0);
+  b.qt = parts.take(dW ? static_cast<size_t>(N) * quant_f8_row_bytes(M) : 0);
+  b.qts = parts.take(dW ? quant_f8_scale_bytes(N, M) : 0);
+  b.sums = parts.take<double>(db ? static_cast<size_t>(ceil_div(M, 128)) * N * sizeof(double) : 0);
+  b.partial = parts.take(0);
+  b.bytes = parts.used + std::max(dx ? f8_partial_bytes(M, K, N, dx_dtype) : 0, dW ? f8_partial_bytes(N, K, M, RN50_F32) : 0);
+  return b;
 }
+
+extern "C" size_t fc_f8_bwd_workspace_bytes_for(int M, int N, int K, int dx_dtype, int dx, int dW, int db) {
+  if (quant_f8_row_bytes(M) == 0 || quant_f8_row_bytes(N) == 0 || K < 1) return 0;
+  return backward_parts(nullptr, M, N, K, dx_dtype, dx != 0, dW != 0, db != 0).bytes;
+}
+extern "C" size_t fc_f8_bwd_workspace_bytes(int M, int N, int K) { return fc_f8_bwd_workspace_bytes_for(M, N, K, RN50_F32, 1, 1, 1); }
 
 extern "C" int fc_f8_bwd(int M, int N, int K, int dy_dtype, const void* dy, int64_t ld_dy, int format, const uint8_t* wt, const uint8_t* wt_scale,
                          const uint8_t* xt, const uint8_t* xt_scale, const rn50_dropout* dropout, int dx_dtype, void* dx, int64_t ld_dx,
@@ -1293,19 +1310,12 @@ extern "C" int fc_f8_bwd(int M, int N, int K, int dy_dtype, const void* dy, int6
   if (int rc = check_tiles(who, M, N, 32, 128)) return rc;
   if (int rc = check_product_size(who, M, K)) return rc;
   if (int rc = check_product_size(who, N, K)) return rc;
-  if (int rc = check_workspace(who, workspace, workspace_bytes, fc_f8_bwd_workspace_bytes(M, N, K))) return rc;
+  const BackwardParts at = backward_parts(workspace, M, N, K, dx_dtype, dx, dW, db);
+  if (int rc = check_workspace(who, workspace, workspace_bytes, at.bytes)) return rc;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  Parts parts{static_cast<uint8_t*>(workspace)};
-  uint8_t* q = parts.take(static_cast<size_t>(M) * quant_f8_row_bytes(N));
-  uint8_t* qs = parts.take(quant_f8_scale_bytes(M, N));
-  uint8_t* qt = parts.take(static_cast<size_t>(N) * quant_f8_row_bytes(M));
-  uint8_t* qts = parts.take(quant_f8_scale_bytes(N, M));
-  const int tiles = static_cast<int>(ceil_div(M, 128));
-  double* sums = parts.take<double>(static_cast<size_t>(tiles) * N * sizeof(double));
-  quant_run(M, N, dy_dtype, dy, ld_dy, nullptr, format, dx ? q : nullptr, qs, dW ? qt : nullptr, qts, db ? sums : nullptr, false, s);
-  void* partial = parts.take(0);
-  const SumArgs sum{sums, tiles, N, db};
-  F8Args px = product_args(M, K, N, q, qs, wt, wt_scale, nullptr, dx, ld_dx, dropout), pw = product_args(N, K, M, qt, qts, xt, xt_scale, nullptr, dW, K, nullptr);
+  quant_run(M, N, dy_dtype, dy, ld_dy, nullptr, format, dx ? at.q : nullptr, at.qs, dW ? at.qt : nullptr, at.qts, db ? at.sums : nullptr, false, s);
+  const SumArgs sum{at.sums, static_cast<int>(ceil_div(M, 128)), N, db};
+  F8Args px = product_args(M, K, N, at.q, at.qs, wt, wt_scale, nullptr, dx, ld_dx, dropout), pw = product_args(N, K, M, at.qt, at.qts, xt, xt_scale, nullptr, dW, K, nullptr);
   if (dW) pw.sum = sum;
   if (dx && dW && f8_few_backward_fits(M, N, K)) {
     if (dx_dtype == RN50_BF16 && format == RN50_E5M2) f8_few_backward<uint16_t, true>(px, pw, s);
@@ -1314,8 +1324,8 @@ extern "C" int fc_f8_bwd(int M, int N, int K, int dy_dtype, const void* dy, int6
     else f8_few_backward<float, false>(px, pw, s);
     return launch_status(who);
   }
-  if (dx) f8_run(format, dx_dtype, px, N, partial, s);
-  if (dW) f8_run(format, RN50_F32, pw, M, partial, s);
+  if (dx) f8_run(format, dx_dtype, px, N, at.partial, s);
+  if (dW) f8_run(format, RN50_F32, pw, M, at.partial, s);
   else sum_columns(sum, s);
   return launch_status(who);
 }

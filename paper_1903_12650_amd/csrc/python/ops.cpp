@@ -586,7 +586,7 @@ PyObject* matmul_f8_py(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::Tensor y = product_out(a[7], a[6], x.rows, w.rows, like);
     const Rows r = rows_of(y);
     const int dt = dtype_of(y), M = static_cast<int>(x.rows), N = static_cast<int>(w.rows);
-    const Workspace work(a[8], a[8] == Py_None ? matmul_f8_workspace_bytes(M, N, K) : 0, like);
+    const Workspace work(a[8], a[8] == Py_None ? matmul_f8_workspace_bytes_for(M, N, K, dt) : 0, like);
     void* const s = current_stream();
     call([&] { return matmul_f8(M, N, K, x.format, x.q, x.scale, w.q, w.scale, bias, dt, r.p, r.ld, work.p, work.bytes, s); });
     return wrap(y);
@@ -609,7 +609,7 @@ PyObject* fc_f8_fwd_py(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Rows ry = rows_of(y);
     const int yt = dtype_of(y), M = static_cast<int>(rx.n), N = static_cast<int>(w.rows), K = static_cast<int>(rx.c);
     const Quantized kept = save ? Quantized(rx.c, rx.n, at::kFloat8_e4m3fn, x) : Quantized();
-    const Workspace work(a[8], a[8] == Py_None ? fc_f8_fwd_workspace_bytes(M, N, K) : 0, x);
+    const Workspace work(a[8], a[8] == Py_None ? fc_f8_fwd_workspace_bytes_for(M, N, K, yt) : 0, x);
     void* const s = current_stream();
     call([&] {
       return fc_f8_fwd(M, N, K, xt, rx.p, rx.ld, drop.get(), w.q, w.scale, bias, yt, ry.p, ry.ld, kept.pq, kept.ps, work.p, work.bytes, s);
@@ -651,7 +651,7 @@ PyObject* fc_f8_bwd_py(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (want[1]) dw = empty({r.c, K}, at::kFloat, dy);
     if (want[2]) db = empty({r.c}, at::kFloat, dy);
     const int M = static_cast<int>(r.n), N = static_cast<int>(r.c);
-    const Workspace work(a[11], a[11] == Py_None ? fc_f8_bwd_workspace_bytes(M, N, static_cast<int>(K)) : 0, dy);
+    const Workspace work(a[11], a[11] == Py_None ? fc_f8_bwd_workspace_bytes_for(M, N, static_cast<int>(K), dxt, want[0], want[1], want[2]) : 0, dy);
     void* const px = want[0] ? addr(dx) : nullptr;
     float *const pw = want[1] ? addr<float>(dw) : nullptr, *const pb = want[2] ? addr<float>(db) : nullptr;
     void* const s = current_stream();

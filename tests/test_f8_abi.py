@@ -103,3 +103,38 @@ def test_numbers_past_32_bits_are_not_cut(call):
     import paper_1903_12650_amd as rn
     with pytest.raises(OverflowError):
         call(rn, torch.zeros(4, 8))
+
+
+def test_workspaces_are_what_a_call_uses():
+    """A bfloat16 product of many tiles is not split however long its sum: it needs none, and none is asked for.  What is smaller than needed is refused."""
+    import paper_1903_12650_amd as rn
+    F, B = torch.float32, torch.bfloat16
+    sizes = [(M, N, K) for M in (1, 64, 65, 300, 1000, 8192) for N in (9, 500, 2000, 8192) for K in (100, 4200, 8192, 11000, 28672, 100000)]
+    for s in sizes:
+        assert rn.matmul_f8_workspace_bytes(*s, B) <= rn.matmul_f8_workspace_bytes(*s, F) == rn.matmul_f8_workspace_bytes(*s) == rn.raw.matmul_f8_workspace_bytes(*s)
+        assert rn.fc_f8_fwd_workspace_bytes(*s, B) <= rn.fc_f8_fwd_workspace_bytes(*s) == rn.raw.fc_f8_fwd_workspace_bytes(*s)
+        most = rn.raw.fc_f8_bwd_workspace_bytes(*s)
+        for dtype in (F, B):
+            both = rn.fc_f8_bwd_workspace_bytes(*s, dtype)
+            assert both <= most
+            for need in ((True, False, False), (False, True, False), (False, False, True), (True, False, True)):
+                assert rn.fc_f8_bwd_workspace_bytes(*s, dtype, *need) <= both
+    assert rn.matmul_f8_workspace_bytes(8192, 8192, 28672, B) == 0 and rn.matmul_f8_workspace_bytes(8192, 8192, 28672) == 2 * 8192 * 8192 * 4
+    assert rn.matmul_f8_workspace_bytes(300, 500, 11000, B) > 0  # (few tiles: split in either type)
+    assert rn.fc_f8_fwd_workspace_bytes(8192, 8192, 28672, B) < 8192 * 28672 * 1.1
+    assert rn.fc_f8_bwd_workspace_bytes(8192, 28672, 8192, B, need_dw=False) < 8192 * 28672 * 1.1
+    assert rn.fc_f8_bwd_workspace_bytes(65536, 8192, 8192, need_dx=False, need_dw=False) == 512 * 8192 * 8
+    assert rn.matmul_f8_workspace_bytes(0, 8, 8, B) == rn.fc_f8_fwd_workspace_bytes(8, 8, 0, B) == rn.fc_f8_bwd_workspace_bytes(8, 8, 0, B) == 0
+    with pytest.raises(TypeError):
+        rn.matmul_f8_workspace_bytes(8, 8, 8, torch.float16)
+
+    raw, one, ld = rn.raw, ctypes.c_void_p(256), ctypes.c_int64
+    for s, dtype, code in (((300, 500, 11000), B, 1), ((2000, 1500, 20000), F, 0)):
+        M, N, K = s
+        less = ctypes.c_size_t(rn.matmul_f8_workspace_bytes(*s, dtype) - 1)
+        assert raw.matmul_f8(M, N, K, E4M3, one, one, one, one, None, code, one, ld(N), one, less, None) == -3
+        less = ctypes.c_size_t(rn.fc_f8_fwd_workspace_bytes(*s, dtype) - 1)
+        assert raw.fc_f8_fwd(M, N, K, 0, one, ld(K), None, one, one, None, code, one, ld(N), None, None, one, less, None) == -3
+        for dx, dw, db in ((one, one, one), (one, None, None), (None, one, None), (None, None, one)):
+            less = ctypes.c_size_t(rn.fc_f8_bwd_workspace_bytes(*s, dtype, dx is not None, dw is not None, db is not None) - 1)
+            assert raw.fc_f8_bwd(M, N, K, 0, one, ld(N), E4M3, one, one, one, one, None, code, dx, ld(K), dw, db, one, less, None) == -3

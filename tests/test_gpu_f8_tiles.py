@@ -107,3 +107,31 @@ def test_nan_blocks(rn, M, N, K, fmt):
         y = rn.matmul_f8(K, a, sa, b, sb, dtype=y_type)
         assert torch.equal(torch.isnan(y), torch.isnan(want))
         assert torch.equal(torch.nan_to_num(y), torch.nan_to_num(want.to(y_type)))
+
+
+@pytest.mark.parametrize("M, N, K", [(40, 300, 700), (300, 500, 11000), (1100, 1000, 17000), (2000, 1500, 17000), (17000, 300, 200), (20000, 60, 70)])
+def test_workspaces_of_just_what_is_asked_for(rn, M, N, K):
+    """Workspaces as large as the sizes say for a call's types and gradients: nothing behind them is touched, and the results are those of the largest."""
+    def workspace(size):
+        flat = torch.full((size + 4096,), 0xA5, dtype=torch.uint8, device="cuda")
+        return flat[:size], flat[size:]
+
+    def untouched(tail):
+        return bool((tail == 0xA5).all())
+
+    x, w, dy = (torch.randint(-2, 3, s, device="cuda").float() for s in ((M, K), (N, K), (M, N)))
+    q, s, t, ts = rn.quant_blocks_f8(w, columns=True)
+    a, sa, at, ats = rn.quant_blocks_f8(x, columns=True)
+    for dtype in (F32, BF16):
+        want = torch.matmul(x, w.t()).to(dtype)
+        some, tail = workspace(rn.matmul_f8_workspace_bytes(M, N, K, dtype))
+        assert torch.equal(rn.matmul_f8(K, a, sa, q, s, dtype=dtype, workspace=some if len(some) else None), want) and untouched(tail)
+        some, tail = workspace(rn.fc_f8_fwd_workspace_bytes(M, N, K, dtype))
+        assert torch.equal(rn.fc_f8_fwd(x, q, s, dtype=dtype, workspace=some), want) and untouched(tail)
+        want = (torch.matmul(dy, w).to(dtype), torch.matmul(dy.t().contiguous(), x), dy.sum(0))
+        for need in ((True, True, True), (True, False, False), (False, True, False), (False, False, True), (True, False, True), (True, True, False), (False, True, True)):
+            some, tail = workspace(rn.fc_f8_bwd_workspace_bytes(M, N, K, dtype, *need))
+            got = rn.fc_f8_bwd(dy, t, ts, at, ats, dtype=dtype, need_dx=need[0], need_dw=need[1], need_db=need[2], workspace=some)
+            for g, v, n in zip(got, want, need):
+                assert (g is None) != n and (not n or torch.equal(g, v)), (dtype, need)
+            assert untouched(tail), (dtype, need)
