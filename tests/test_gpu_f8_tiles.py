@@ -2,7 +2,7 @@
 
 The factors are small whole numbers times a power of two that differs from block to block and row to row: a, w in {-2, .., 2} * 2^{-1, 0, 1}.
 Products are multiples of 1/4 up to 16, all eight products that the 8-bit matrix cores add at once share a power (so the smallest is a quarter of
-the largest, far above 2^-13 of it), and sums of K <= 2^17 of them are multiples of 1/4 below 2^21: floats hold each of them
+the largest, far above 2^-13 of it), and sums of K < 2^18 of them are multiples of 1/4 below 2^22: floats hold each of them
 in any order.  So a float result is equal to the sum, a bfloat16 one to its rounding, and a product that is lost, doubled or scaled by another
 block's power shows."""
 import pytest
@@ -42,7 +42,7 @@ def whole_numbers(rows, K, fmt, seed):
 
 
 def check_product(rn, M, N, K, fmt, seed=1):
-    assert K <= 1 << 17
+    assert K < 1 << 18
     a, sa, na = whole_numbers(M, K, fmt, seed)
     w, sw, nw = whole_numbers(N, K, E4M3, seed + 1)
     bias = (torch.arange(N, device="cuda") % 7).float()
@@ -53,10 +53,16 @@ def check_product(rn, M, N, K, fmt, seed=1):
         differ = (y != want.to(y_type)).nonzero()
         assert len(differ) == 0, (y_type, len(differ), differ[0].tolist(), float(y[tuple(differ[0])]), float(want[tuple(differ[0])]))
         assert (wide[:, N:] == 5).all()
+        if fmt == E4M3:  # rows that are quantized on the way: the same numbers
+            for x in (na[:, :K], na[:, :K].to(BF16)):
+                assert torch.equal(rn.fc_f8_fwd(x, w, sw, bias, dtype=y_type), want.to(y_type))
 
 
 # Few rows: 16 to 64 of them, 16 or 32 columns a workgroup, a wave with no block, one, several.
-FEW = [(1, 40, 128), (1, 1000, 2048), (16, 33, 1100), (17, 70, 700), (33, 1000, 2048), (40, 8200, 1300), (48, 17, 20000), (64, 8201, 1500), (64, 64, 50176)]
+FEW = [(1, 40, 128), (1, 1000, 2048), (16, 33, 1100), (17, 70, 700), (33, 1000, 2048), (40, 8200, 1300), (48, 17, 20000), (64, 8201, 1500), (64, 64, 50176),
+       (1, 8200, 700), (20, 9000, 1300)]
+# Few rows and sums that are folded (more than 131072 numbers), 16 and 32 columns a workgroup.
+LONG = [(M, N, 140000) for M in (1, 20, 40, 64) for N in (33, 8200)]
 # 64x64 tiles by sums of one to four blocks and of more (past the last block their rings ask for nothing), single rows and columns in the last tile.
 SMALL = [(65, 65, k) for k in (1, 128, 256, 384, 512, 513, 640, 769, 1000, 1100, 1300, 2000)] + [(300, 200, 500), (193, 257, 2100)]
 # 128x64 tiles with four buffers; 128x128 ones by eight waves with two, by four with four; 128x64 with two, three a unit; 128x128 in many rounds.
@@ -64,19 +70,19 @@ MIDDLE = [(1100, 1300, 700), (1025, 1281, 1500), (2000, 1500, 130), (2000, 1500,
           (2200, 2100, 4300), (6100, 4090, 600), (6017, 4097, 1500)]
 # 256x256 tiles: sums across groups of scales, ragged, outputs past the caches in float (32 MiB and more) and in both types.
 LARGE = [(2900, 2890, 1300), (2900, 2900, 260), (3329, 3073, 1100), (4090, 4000, 520), (7900, 4000, 1100), (8191, 4090, 2047)]
-# Sums in parts: few tiles and long sums, and sums of more than 16384 numbers whatever the tiles.
-PARTS = [(130, 70, 7000), (300, 500, 4100), (500, 600, 11000), (1024, 2000, 11000), (1000, 1030, 11000), (256, 1024, 50176), (2000, 1500, 20000), (4090, 4090, 16500),
+# Sums in parts: few tiles and long sums (512 x 9216 -> 512 in parts of eight blocks), and sums of more than 16384 numbers whatever the tiles.
+PARTS = [(130, 70, 7000), (300, 500, 4100), (300, 500, 7168), (500, 510, 9216), (500, 600, 11000), (1024, 2000, 11000), (1000, 1030, 11000), (256, 1024, 50176), (2000, 1500, 20000), (4090, 4090, 16500),
          (65, 9, 100000)]
 
 
 @pytest.mark.parametrize("fmt", [E4M3, E5M2])
-@pytest.mark.parametrize("M, N, K", FEW + SMALL + MIDDLE + LARGE + PARTS)
+@pytest.mark.parametrize("M, N, K", FEW + LONG + SMALL + MIDDLE + LARGE + PARTS)
 def test_whole_numbers(rn, M, N, K, fmt):
     check_product(rn, M, N, K, fmt)
 
 
 @pytest.mark.parametrize("fmt", [E4M3, E5M2])
-@pytest.mark.parametrize("M, N, K", [(40, 1000, 700), (40, 2900, 300), (12, 300, 5000), (1300, 300, 700), (1100, 2900, 2900), (1024, 4090, 4000), (20000, 256, 1024), (50176, 256, 1000),
+@pytest.mark.parametrize("M, N, K", [(40, 1000, 700), (60, 1000, 700), (40, 2900, 300), (12, 300, 5000), (1300, 300, 700), (1100, 2900, 2900), (1024, 4090, 4000), (20000, 256, 1024), (50176, 256, 1000),
                                      (20000, 64, 200)])
 def test_layer_of_whole_numbers(rn, M, N, K, fmt):
     """Gradients of a layer of small whole numbers: they are quantized exactly, in either format, and a dropout of one half doubles what it keeps."""
