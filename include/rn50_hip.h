@@ -526,9 +526,11 @@ int quant_blocks_f8(int M, int K, int dtype, const void* x, int64_t ldx, const r
 /* y[m,n] = sum_k a[m,k] * w[n,k] + bias[n] of the numbers that a (a_format) and w (RN50_E4M3) stand for, rounded to y's type.
  * a [M,row bytes], w [N,row bytes], their scales: device, as quant_blocks_f8 leaves them; bias float[N] or NULL; y: device
  * y_dtype, rows of N elements ldy >= N elements apart.  workspace: *_workspace_bytes_for() with what the call is given; *_workspace_bytes()
- * is enough for every call of that size, here and below.  With y_dtype RN50_F32 products and sums are float.  With RN50_BF16 they are
- * those of the 8-bit matrix cores, which keep of every eight products the bits down to 2^-13 of the largest one's: the sum is off by
- * at most 2^-10 of the sum of the products' magnitudes (2e-5 of the result's size with normally distributed numbers, a hundredth of y's rounding). */
+ * is enough for every call of that size, here and below.  With y_dtype RN50_F32 products and sums are float: off by at
+ * most 2^-23 K of the sum of the products' magnitudes (one float takes at most 16384 numbers up to M = 64; above, sums of more are cut into
+ * up to 16 parts where y has up to 2^30 elements).  With RN50_BF16 they are those of the 8-bit matrix cores, which keep of every eight products the bits down
+ * to 2^-13 of the largest one's: off by at most 2^-10 + 2^-23 K of the sum of the products' magnitudes (2e-5 of the result's size with normally
+ * distributed numbers, a hundredth of y's rounding).  Where sums all but cancel and that matters, ask for float. */
 size_t matmul_f8_workspace_bytes(int M, int N, int K);
 size_t matmul_f8_workspace_bytes_for(int M, int N, int K, int y_dtype);
 int matmul_f8(int M, int N, int K, int a_format, const uint8_t* a, const uint8_t* a_scale, const uint8_t* w, const uint8_t* w_scale,
