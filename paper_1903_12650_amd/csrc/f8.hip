@@ -361,9 +361,10 @@ __device__ __forceinline__ void drop_columns(const F8Args& a, uint64_t call, int
 
 // A tile of the product by WM x WN waves, each of 32x32 blocks of it.  FAST (bfloat16 results): two 8-bit fragments and their rows' scale bytes go into
 // v_mfma_scale_f32_32x32x64_f8f6f4 as they are, the scaling costs nothing.  Of every eight products these matrix cores drop what lies below 2^-13 of the
-// largest, 1.2e-5 to 1.6e-5 of a sum, three hundred times less than a step of bfloat16: one result in 300 is rounded to the other side (2.7e-4 of y's size
-// between the two), the error against 64 bits is 1.6593e-3 instead of 1.6592e-3 with float sums, which take twice as long (8192^3).  EXACT (float results): fragments become bfloat16, times their power of two
-// (exact: 4 of its 8 bits), for v_mfma_f32_32x32x16_bf16, since the 8-bit matrix cores drop bits that a float result has.
+// largest, 1.2e-5 to 1.6e-5 of a sum's usual size, a hundredth of its rounding to bfloat16: one result in 45 to 80 is rounded to the other side (2.7e-4 of y's
+// size between the two), the error against 64 bits is 1.6593e-3 instead of 1.6592e-3 with float sums, which take twice as long (8192^3).  EXACT (float
+// results): fragments become bfloat16, times their power of two (exact: 4 of its 8 bits), for v_mfma_f32_32x32x16_bf16, since the 8-bit matrix cores drop bits
+// that a float result has.
 // Operands go from memory into LDS past the registers, RING stages of 128 numbers a row, a row's 16-byte pieces exchanged so that a fragment's reads touch all
 // banks.  What bounds it: large tiles' matrix cores, at the clock that their power leaves (8192^3 bfloat16 397 to 447 us, 2460 to 2770 TFLOP/s, of
 // zeros 317; 8192 x 4096 x 4096 into floats 195 to 223, 1230 to 1410); middle ones' conversions and LDS reads beside the matrix cores (1001 x 2047 ->
@@ -678,13 +679,15 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_f8_kernel(const F8Args a)
 }
 
 // Few rows (M <= 16 * MB): the weights go by once, bound by memory; a workgroup owns 16 * CB columns, its waves a part of K each.  A wave's lane has column
-// lane % 16 and 32 numbers at 32 * (lane / 16) of a block of 128, straight from memory, U blocks' loads in flight; they meet the rows' (the second
-// operand) in v_mfma_scale_f32_16x16x128_f8f6f4, or (EXACT) as bfloat16, times their power of two, in v_mfma_f32_16x16x32_bf16.  The waves' sums
-// are added through LDS, in order.  1 x 2048 -> 1000 with the quantization 5.4 us, 40 x 2048 -> 1000 5.9, of them 2 to 3 the launch; 1 x 8192 -> 8192 18, 3.7 TB/s.
+// lane % 16 and 32 numbers at 32 * (lane / 16) of a block of 128, straight from memory, U blocks' loads in flight; they meet the rows' (the second operand) in
+// v_mfma_scale_f32_16x16x128_f8f6f4, or (EXACT) as bfloat16, times their power of two, in v_mfma_f32_16x16x32_bf16.  The waves' sums are added through LDS, in
+// order.  (bfloat16 results from float sums: 64 x 4096 -> 7000 23.4 -> 25.2 us, 8 x 1024 -> 16384 with the quantization 6.2 -> 7.7.)  1 x 2048 -> 1000 with the
+// quantization 5.4 us, 40 x 2048 -> 1000 5.9, of them 2 to 3 the launch; 1 x 8192 -> 8192 18, 3.7 TB/s.
 // X: the rows are float or bfloat16 and quantized here, block by block as they are needed (a block's 128 numbers are four lanes'): no second launch.
 // (The rows' loads beside the weights', U blocks ahead, change nothing: 40 x 2048 -> 1000 6.0 -> 6.4 us, 40 x 8192 -> 8192 34.0 -> 33.5.)
 // FOLD (EXACT, sums of which a wave has more than kFloatBlocks blocks): a register takes that many before it is added to the others, in registers that the
-// other kernels do without (32 rows' ones have just enough for two workgroups a unit: 24 x 4096 -> 7000 14.1 us, with them 14.4).
+// other kernels do without (32 rows' ones have 127 of the 128 that leave a unit two workgroups; with the sums kept in LDS and 128 registers 24 x 4096 -> 7000
+// took 14.4 us instead of 14.1).
 constexpr int kFewThreads = 512, kFewWaves = kFewThreads / 64;
 constexpr int kFewLong = kFewWaves * kFloatBlocks * 128;
 struct F8FewArgs {
