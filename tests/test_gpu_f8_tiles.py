@@ -69,7 +69,7 @@ SMALL = [(65, 65, k) for k in (1, 128, 256, 384, 512, 513, 640, 769, 1000, 1100,
 MIDDLE = [(1100, 1300, 700), (1025, 1281, 1500), (2000, 1500, 130), (2000, 1500, 1000), (1921, 1409, 1500), (2000, 1500, 4300), (2200, 2100, 130), (2177, 2113, 1500),
           (2200, 2100, 4300), (6100, 4090, 600), (6017, 4097, 1500)]
 # 256x256 tiles: sums across groups of scales, ragged, outputs past the caches in float (32 MiB and more) and in both types.
-LARGE = [(2900, 2890, 1300), (2900, 2900, 260), (3329, 3073, 1100), (4090, 4000, 520), (7900, 4000, 1100), (8191, 4090, 2047)]
+LARGE = [(2900, 2890, 1300), (2900, 2900, 260), (3329, 3085, 1100), (4090, 4000, 520), (7900, 4000, 1100), (8191, 4090, 2047)]
 # Sums in parts: few tiles and long sums (512 x 9216 -> 512 in parts of eight blocks), and sums of more than 16384 numbers whatever the tiles.
 PARTS = [(130, 70, 7000), (300, 500, 4100), (300, 500, 7168), (500, 510, 9216), (500, 600, 11000), (1024, 2000, 11000), (1000, 1030, 11000), (256, 1024, 50176), (2000, 1500, 20000), (4090, 4090, 16500),
          (65, 9, 100000)]
